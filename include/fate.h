@@ -550,6 +550,120 @@ fate_status_t fate_place_baseline_device(const fate_dags_t *dags, const fate_sta
                                          float kappa_prefix, uint64_t *d_devices, int64_t *d_order,
                                          int32_t *d_status, void *d_ws, size_t ws_bytes, void *stream);
 
+/* Attention of a planned wave: what a device runs for the stages that a plan
+ * gave it.  The prefix groups that scoring tracks per device (kappa, grp(v),
+ * L(v)) stand for keys and values kept in a paged cache; the calls below fill
+ * that cache, attend over it, and attend whole prompts that have none:
+ *   fate_kv_append    stores new keys and values, rotated to their positions
+ *   fate_attn_paged   new tokens (chunks, a few, one) over their sequences' pages
+ *   fate_attn_prompt  whole prompts, packed, causal, without a cache
+ * Forward only.  All arrays are device memory unless said otherwise; every
+ * call is enqueued on `stream`, never synchronises and can be captured.  The
+ * host checks what it can see (sizes, types, strides, alignment); errors in
+ * the device arrays (`off`, `kv_len`, `pages`) are found by the kernels, which
+ * then read and write nothing outside the arrays, store FATE_EINVAL in
+ * d_status[b] of the sequence (when d_status is not null; nothing else is
+ * written there, so clear it first) and leave that sequence's results
+ * unspecified. */
+
+/* Element types of queries, keys, values and outputs. */
+enum { FATE_BF16 = 0, FATE_F16 = 1 };
+
+#define FATE_MAX_HEAD_DIM 256
+#define FATE_MAX_HEADS 256
+
+/* Heads: heads_q a multiple of heads_kv (query head h reads key head
+ * h / (heads_q / heads_kv)), head_dim a multiple of 8 up to
+ * FATE_MAX_HEAD_DIM. */
+typedef struct {
+    int32_t dtype, heads_q, heads_kv, head_dim;
+} fate_heads_t;
+
+/* Packed token rows: element i of head h of token t is data[t * token +
+ * h * head + i].  Strides are in elements, multiples of 8, not negative; data
+ * is aligned to 16 bytes.  Written rows must not overlap (both strides at
+ * least head_dim). */
+typedef struct {
+    void *data;
+    int64_t token, head;
+} fate_rows_t;
+
+/* Paged cache: element i of head h in slot s of page p is k[p * page +
+ * h * head + s * token + i], values likewise in v.  Strides and alignment as
+ * for rows; page_size a power of two up to 1024. */
+typedef struct {
+    void *k, *v;
+    int64_t page, head, token;
+    int32_t n_pages, page_size;
+} fate_kv_cache_t;
+
+/* The sequences of a call: B of them over T packed token rows.
+ *   off[B+1]     sequence b's rows are off[b] .. off[b+1] (ascending); rows
+ *                outside every sequence are neither read nor written
+ *   kv_len[B]    keys of sequence b in the cache, the call's own tokens
+ *                included: row i of n stands at position kv_len[b] - n + i
+ *   pages        sequence b's page for positions [j * page_size,
+ *                (j + 1) * page_size) is pages[b * pages_stride + j],
+ *                j < max_pages; entries past its last key are not read
+ * fate_attn_prompt reads off alone. */
+typedef struct {
+    int32_t B, max_pages;
+    int64_t T, pages_stride;
+    const int32_t *off, *kv_len, *pages;
+} fate_seqs_t;
+
+/* fate_kv_append: rotate the new keys to their positions and store them and
+ * the values in the cache; rotate the queries into q_out.
+ *   table[table_rows][rot]  float32: row p holds the rot/2 cosines, then the
+ *     rot/2 sines of position p.  rot (even, 0 .. head_dim) dimensions are
+ *     rotated, the rest pass; pairs are (j, j + rot/2), or (2j, 2j + 1) with
+ *     interleaved = 1: (x, y) -> (x cos - y sin, y cos + x sin), in float32,
+ *     rounded once.  rot = 0: no rotation, table may be null.
+ *   q, q_out  both null for no queries; q_out may be q itself (same strides).
+ * A row at a negative position (more new tokens than keys) has no place: its
+ * key and value are not stored, its query comes out zero.  A position at or
+ * past table_rows or max_pages * page_size, or a page outside 0 .. n_pages - 1,
+ * is an error of its sequence.  No page that is written may be another
+ * sequence's in the same call.
+ * Errors: EINVAL (null pointers, types, strides, alignment, rot, heads),
+ * ERANGE (heads, head_dim, page_size, T * heads at 2^31), EHIP. */
+fate_status_t fate_kv_append(const fate_heads_t *heads, const fate_seqs_t *seqs, const fate_rows_t *q,
+                             const fate_rows_t *k, const fate_rows_t *v, const float *table, int64_t table_rows,
+                             int32_t rot, int32_t interleaved, const fate_kv_cache_t *cache,
+                             const fate_rows_t *q_out, int32_t *d_status, void *stream);
+
+/* fate_attn_paged_ws_size: device workspace bytes fate_attn_paged needs for
+ * these heads, sequences (B, T, max_pages) and max_new.  Errors: EINVAL,
+ * ERANGE. */
+fate_status_t fate_attn_paged_ws_size(const fate_heads_t *heads, const fate_seqs_t *seqs,
+                                      const fate_kv_cache_t *cache, int64_t max_new, size_t *bytes);
+
+/* fate_attn_paged: causal attention of the call's tokens over their
+ * sequences' keys in the cache (which fate_attn_paged only reads: append
+ * first).  The row at position p sees the keys 0 .. p:
+ *   out = sum_j softmax_j(scale q.k_j) v_j,  d_lse = log sum_j exp(scale q.k_j)
+ * with the products of 16-bit operands summed in float32, the statistics in
+ * float32 and the weights rounded to the operands' type for the second
+ * product.  A row that sees no key (p < 0) gets zeros and -infinity.  Keys and
+ * values that a row does not see never reach it, whatever they hold (a page's
+ * slots past the last key may hold anything).
+ *   max_new   an upper bound of the tokens per sequence (1 .. T), which picks
+ *             the kernels; a larger sequence is still computed, slower
+ *   scale     positive and finite
+ *   d_lse     [T][heads_q] float32, or null
+ *   d_ws      fate_attn_paged_ws_size bytes, aligned to 16, contents irrelevant
+ * Errors: EINVAL, ERANGE, ESIZE (workspace), EHIP. */
+fate_status_t fate_attn_paged(const fate_heads_t *heads, const fate_seqs_t *seqs, const fate_rows_t *q,
+                              const fate_kv_cache_t *cache, int64_t max_new, float scale, const fate_rows_t *out,
+                              float *d_lse, int32_t *d_status, void *d_ws, size_t ws_bytes, void *stream);
+
+/* fate_attn_prompt: causal attention of whole prompts: row i of a sequence
+ * sees the sequence's rows 0 .. i of k and v.  Otherwise as fate_attn_paged.
+ * Errors: EINVAL, ERANGE, EHIP. */
+fate_status_t fate_attn_prompt(const fate_heads_t *heads, const fate_seqs_t *seqs, const fate_rows_t *q,
+                               const fate_rows_t *k, const fate_rows_t *v, float scale, const fate_rows_t *out,
+                               float *d_lse, int32_t *d_status, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -19,7 +19,12 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libfate.so")
 SOURCES = [os.path.join(CSRC, "fate_host.cpp"), os.path.join(CSRC, "fate_kernels.hip"),
            os.path.join(CSRC, "fate_commit.hip"), os.path.join(CSRC, "fate_plan.hip"),
-           os.path.join(CSRC, "fate_sim.cpp"), os.path.join(CSRC, "fate_simdev.hip")]
+           os.path.join(CSRC, "fate_sim.cpp"), os.path.join(CSRC, "fate_simdev.hip"),
+           os.path.join(CSRC, "fate_attn_api.cpp"), os.path.join(CSRC, "fate_attn_tile.hip"),
+           os.path.join(CSRC, "fate_attn_few.hip"), os.path.join(CSRC, "fate_kv.hip")]
+# The attention kernels take what the caller's tensors hold: NaN and infinities
+# keep their meaning there, so they are compiled without KERNEL_FLAGS.
+NAN_SOURCES = ("fate_attn_tile.hip", "fate_attn_few.hip", "fate_kv.hip")
 ARCH = os.environ.get("FATE_OFFLOAD_ARCH", "gfx950")
 
 
@@ -46,6 +51,7 @@ def commands(out: str = LIB, objdir: str = None) -> list:
     plan_o = os.path.join(objdir, "fate_plan.o")
     sim_o = os.path.join(objdir, "fate_sim.o")
     simdev_o = os.path.join(objdir, "fate_simdev.o")
+    attn_o = [os.path.join(objdir, os.path.splitext(os.path.basename(src))[0] + ".o") for src in SOURCES[6:]]
     inc = ["-I", INCLUDE, "-I", CSRC]
     return [
         [hipcc(), *COMMON, *inc, "-c", SOURCES[0], "-o", host_o],
@@ -54,8 +60,9 @@ def commands(out: str = LIB, objdir: str = None) -> list:
         [hipcc(), *COMMON, *KERNEL_FLAGS, *inc, "-c", SOURCES[3], "-o", plan_o],
         [hipcc(), *COMMON, *inc, "-c", SOURCES[4], "-o", sim_o],
         [hipcc(), *COMMON, *KERNEL_FLAGS, *inc, "-c", SOURCES[5], "-o", simdev_o],
+        *[[hipcc(), *COMMON, *inc, "-c", src, "-o", obj] for src, obj in zip(SOURCES[6:], attn_o)],
         [hipcc(), "--offload-arch=" + ARCH, "-shared", "-fPIC", host_o, kern_o, commit_o, plan_o, sim_o, simdev_o,
-         "-o", out, "-lpthread"],
+         *attn_o, "-o", out, "-lpthread"],
     ]
 
 
@@ -88,7 +95,8 @@ def build_sanitized(verbose: bool = False) -> str:
     for src in SOURCES:
         obj = os.path.join(SAN_DIR, os.path.basename(src) + ".o")
         host_only = src.endswith(".cpp")
-        cmd = [hipcc(), *COMMON, *([] if host_only else KERNEL_FLAGS), *(san if host_only else []), *inc, "-c", src,
+        keep_nans = host_only or os.path.basename(src) in NAN_SOURCES
+        cmd = [hipcc(), *COMMON, *([] if keep_nans else KERNEL_FLAGS), *(san if host_only else []), *inc, "-c", src,
                "-o", obj]
         if verbose:
             print(" ".join(cmd), flush=True)

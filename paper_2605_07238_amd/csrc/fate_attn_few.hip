@@ -1,0 +1,333 @@
+// Attention of few new tokens per sequence over a paged cache (one token of
+// an answer, some drafted tokens), and the joining of parts of the key axis.
+//
+// With few rows the call reads each key and value once and computes little:
+// memory bounds it.  k_attn_few: one workgroup of four waves per (sequence,
+// key head, 16 to 64 packed rows, part of the key axis); the parts are sized
+// from the lengths on the device so that the whole call makes about as many
+// pieces as the chip holds workgroups, whatever the mix of lengths.  A wave
+// takes every fourth block of 32 keys by itself: keys go from memory to
+// registers as the first product's operand (16-byte loads, 64 bytes of each of
+// 16 rows at a time), values through the wave's own LDS rows, because the
+// second product needs them transposed.  The products are transposed as in
+// the tile kernel (S^T = k q^T, O^T = v^T p^T), on 16 x 16 x 32 matrix
+// instructions: 16 packed rows are one column block.  The four waves'
+// statistics and outputs meet in LDS at the end.
+//
+// k_attn_join: the parts of a row tile, o = sum 2^(m_i - M) o_i / sum 2^(m_i - M) l_i.
+#include "fate_attn.h"
+
+namespace fate {
+namespace {
+
+template <class T, int D, int RT>
+__global__ __launch_bounds__(256) void k_attn_few(AttnLaunch a) {
+    typedef typename T::el el;
+    typedef typename T::x4 x4;
+    typedef typename T::x8 x8;
+    constexpr int M = 16 * RT, KS = D / 32, DT = D / 16;
+    constexpr int VS = D + 8;   // row of a wave's value rows in LDS: eight elements of padding against bank conflicts
+    constexpr int OS = D + 4;   // row of the waves' outputs in LDS
+    constexpr int kBytes = 4 * 32 * VS * 2 > 4 * 16 * OS * 4 ? 4 * 32 * VS * 2 : 4 * 16 * OS * 4;
+    __shared__ __align__(16) char raw[kBytes];
+    __shared__ float sm[4][M], sl[4][M];
+
+    const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
+    const int hk = blockIdx.x % a.hkv, item = blockIdx.x / a.hkv;
+    const int chunk = chunk_of<true>(a, M, kFewLeast, lane);
+    const Piece p = find_piece<true, false>(a, M, chunk, item, lane, hk == 0 && item == 0 && w == 0);
+    if (!p.ok) return;
+
+    const int rows = p.n * a.G, row0 = p.tile * M;
+    const int first = p.L - p.n + 1;
+    const int last_row = min(row0 + M, rows) - 1;
+    const int most = min(p.L, max(0, last_row / a.G + first));
+    const int least = max(0, min(p.L, row0 / a.G + first));
+    int k_lo = 0, k_hi = most;
+    if (p.splits > 1) {
+        k_lo = p.split * chunk * kKeyTile;
+        k_hi = (int)min((int64_t)most, (int64_t)k_lo + (int64_t)chunk * kKeyTile);
+    }
+
+    const int c = lane & 15, g = lane >> 4;
+    x8 q[RT][KS];
+    int ends[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int row = row0 + rt * 16 + c;
+        const bool live = row < rows;
+        const int tok = live ? row / a.G : 0;
+        ends[rt] = live ? max(0, min(p.L, tok + first)) : 0;
+        const el *src = (const el *)a.q.data + (p.lo_row + (int64_t)tok) * a.q.token +
+                        (int64_t)(hk * a.G + row - tok * a.G) * a.q.head + g * 8;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            u32x4 x = {0, 0, 0, 0};
+            if (live && s * 32 + g * 8 < a.d) x = *(const u32x4 *)(src + s * 32);
+            q[rt][s] = __builtin_bit_cast(x8, x);
+        }
+    }
+    f32x4 o[RT][DT];
+    float m[RT], l[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        m[rt] = kLowest;
+        l[rt] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) o[rt][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+
+    el *const vrow = (el *)raw + w * 32 * VS;
+    const int32_t *const table = a.s.pages + p.b * a.s.pages_stride;
+    const int mask = (1 << a.c.page_shift) - 1;
+    int pg[2];
+    auto find_pages = [&](int kb) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int key = kb + 16 * i + c;
+            pg[i] = key < k_hi ? table[key >> a.c.page_shift] : 0;
+        }
+    };
+    find_pages(k_lo + 32 * w);
+    for (int kb = k_lo + 32 * w; kb < k_hi; kb += 128) {
+        u32x4 rk[2][KS], rv[2][KS];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int key = kb + 16 * i + c;
+            bool in = key < k_hi;
+            if (in && (uint32_t)pg[i] >= (uint32_t)a.c.n_pages) {
+                in = false;
+                if (a.status) a.status[p.b] = FATE_EINVAL;
+            }
+            const int64_t at = pg[i] * a.c.page + (int64_t)hk * a.c.head + (key & mask) * a.c.token + g * 8;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const bool ld = in && s * 32 + g * 8 < a.d;
+                rk[i][s] = u32x4{0, 0, 0, 0};
+                rv[i][s] = u32x4{0, 0, 0, 0};
+                if (ld) {
+                    rk[i][s] = *(const u32x4 *)((const el *)a.c.k + at + s * 32);
+                    rv[i][s] = *(const u32x4 *)((const el *)a.c.v + at + s * 32);
+                }
+            }
+        }
+        find_pages(kb + 128);
+        const bool edge = kb + 32 > least;  // uniform
+        bool odd = false;
+        if (edge) {
+            uint32_t bad = 0;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int s = 0; s < KS; ++s)
+                    bad |= not_finite<T>(rv[i][s][0]) | not_finite<T>(rv[i][s][1]) | not_finite<T>(rv[i][s][2]) |
+                           not_finite<T>(rv[i][s][3]);
+            odd = __any(bad != 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int s = 0; s < KS; ++s) *(u32x4 *)&vrow[(16 * i + c) * VS + s * 32 + g * 8] = rv[i][s];
+
+        x8 pr[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            f32x4 s2[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                s2[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int s = 0; s < KS; ++s) s2[i] = T::mfma16(__builtin_bit_cast(x8, rk[i][s]), q[rt][s], s2[i]);
+            }
+            // s2[i][j]: key 16 i + 4 g + j of the block, packed row c
+            if (edge || kb + 32 > k_hi) {
+                const int left = min(ends[rt], k_hi) - kb - 4 * g;
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (16 * i + j >= left) s2[i][j] = -INFINITY;
+            }
+            float top = fmaxf(fmaxf(fmaxf(s2[0][0], s2[0][1]), fmaxf(s2[0][2], s2[0][3])),
+                              fmaxf(fmaxf(s2[1][0], s2[1][1]), fmaxf(s2[1][2], s2[1][3])));
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            top = fmaxf(top * a.scale_log2, kLowest);
+            if (__any(top > m[rt] + 8.0f)) {
+                const float next = fmaxf(m[rt], top), f = exp2_fast(m[rt] - next);
+                m[rt] = next;
+                l[rt] *= f;
+#pragma unroll
+                for (int i = 0; i < DT; ++i) o[rt][i] *= f;
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float x = exp2_fast(__builtin_fmaf(s2[i][j], a.scale_log2, -m[rt]));
+                    l[rt] += x;
+                    pr[rt][4 * i + j] = (el)x;
+                }
+        }
+        __builtin_amdgcn_wave_barrier();
+        const int vr = 4 * g + c / 4, vc = 4 * (c & 3);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+            const x4 v1 = T::read_tr(&vrow[vr * VS + dt * 16 + vc]);
+            const x4 v2 = T::read_tr(&vrow[(vr + 16) * VS + dt * 16 + vc]);
+            const x8 vf = __builtin_shufflevector(v1, v2, 0, 1, 2, 3, 4, 5, 6, 7);
+            if (!odd) {
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) o[rt][dt] = T::mfma16(vf, pr[rt], o[rt][dt]);
+            } else {
+                // a value that some row must not see is not finite: key by key
+                for (int key = 0; key < 32; ++key) {
+                    x8 one = vf;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (16 * (e / 4) + 4 * g + e % 4 != key) one[e] = (el)0.0f;
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) {
+                        const f32x4 z = T::mfma16(one, pr[rt], f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+                        if (kb + key < ends[rt]) o[rt][dt] += z;
+                    }
+                }
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+
+    // the four waves' rows: common maximum, sums
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        l[rt] += __shfl_xor(l[rt], 16);
+        l[rt] += __shfl_xor(l[rt], 32);
+        if (g == 0) {
+            sm[w][rt * 16 + c] = m[rt];
+            sl[w][rt * 16 + c] = l[rt];
+        }
+    }
+    float *const so = (float *)raw;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        __syncthreads();  // the value rows (rt = 0), or the last block's outputs, are done with
+        const int r = rt * 16 + c;
+        const float mm = fmaxf(fmaxf(sm[0][r], sm[1][r]), fmaxf(sm[2][r], sm[3][r]));
+        const float f = exp2_fast(m[rt] - mm);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) *(f32x4 *)&so[(w * 16 + c) * OS + dt * 16 + 4 * g] = o[rt][dt] * f;
+        __syncthreads();
+        for (int x = tid; x < 16 * (D / 8); x += 256) {
+            const int cc = x / (D / 8), d0 = x % (D / 8) * 8, rr = rt * 16 + cc, row = row0 + rr;
+            if (row >= rows || d0 >= a.d) continue;
+            const float top = fmaxf(fmaxf(sm[0][rr], sm[1][rr]), fmaxf(sm[2][rr], sm[3][rr]));
+            float sum = 0.0f;
+            f32x4 y0 = {0.0f, 0.0f, 0.0f, 0.0f}, y1 = y0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                sum += sl[k][rr] * exp2_fast(sm[k][rr] - top);
+                y0 += *(const f32x4 *)&so[(k * 16 + cc) * OS + d0];
+                y1 += *(const f32x4 *)&so[(k * 16 + cc) * OS + d0 + 4];
+            }
+            const int tok = row / a.G, qh = hk * a.G + row - tok * a.G;
+            const int64_t out_row = p.lo_row + (int64_t)tok;
+            if (p.splits > 1) {
+                if (p.slot >= a.slots) continue;
+                const int64_t at = ((int64_t)p.slot * a.hkv + hk) * M + rr;
+                *(f32x4 *)(a.part + at * a.d + d0) = y0;
+                *(f32x4 *)(a.part + at * a.d + d0 + 4) = y1;
+                if (d0 == 0) {
+                    float *ml = a.part + (int64_t)a.slots * a.hkv * M * a.d + at * 2;
+                    ml[0] = top;
+                    ml[1] = sum;
+                }
+                continue;
+            }
+            const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+            x8 y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                y[e] = (el)(y0[e] * inv);
+                y[4 + e] = (el)(y1[e] * inv);
+            }
+            *(x8 *)((el *)a.out.data + out_row * a.out.token + (int64_t)qh * a.out.head + d0) = y;
+            if (d0 == 0 && a.lse)
+                a.lse[out_row * a.hq + qh] = sum != 0.0f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+        }
+    }
+}
+
+// One workgroup per (split row tile, key head): each thread joins eight
+// dimensions of a row over the parts.
+template <class T>
+__global__ __launch_bounds__(256) void k_attn_join(AttnLaunch a, int M, int least) {
+    typedef typename T::el el;
+    typedef typename T::x8 x8;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int hk = blockIdx.x % a.hkv, item = blockIdx.x / a.hkv;
+    const int chunk = chunk_of<true>(a, M, least, lane);
+    const Piece p = find_piece<true, true>(a, M, chunk, item, lane, false);
+    if (!p.ok || p.slot + p.splits > a.slots) return;
+    const int rows = p.n * a.G, row0 = p.tile * M, per = a.d / 8;
+    const float *ml0 = a.part + (int64_t)a.slots * a.hkv * M * a.d;
+    for (int x = tid; x < min(M, rows - row0) * per; x += 256) {
+        const int rr = x / per, d0 = (x - rr * per) * 8, row = row0 + rr;
+        const int64_t at0 = ((int64_t)p.slot * a.hkv + hk) * M + rr, step = (int64_t)a.hkv * M;
+        float top = kLowest;
+        for (int i = 0; i < p.splits; ++i) top = fmaxf(top, ml0[(at0 + i * step) * 2]);
+        float sum = 0.0f;
+        f32x4 y0 = {0.0f, 0.0f, 0.0f, 0.0f}, y1 = y0;
+        for (int i = 0; i < p.splits; ++i) {
+            const int64_t at = at0 + i * step;
+            const float f = exp2_fast(ml0[at * 2] - top);
+            sum += ml0[at * 2 + 1] * f;
+            y0 += *(const f32x4 *)(a.part + at * a.d + d0) * f;
+            y1 += *(const f32x4 *)(a.part + at * a.d + d0 + 4) * f;
+        }
+        const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+        x8 y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            y[e] = (el)(y0[e] * inv);
+            y[4 + e] = (el)(y1[e] * inv);
+        }
+        const int tok = row / a.G, qh = hk * a.G + row - tok * a.G;
+        const int64_t out_row = p.lo_row + (int64_t)tok;
+        *(x8 *)((el *)a.out.data + out_row * a.out.token + (int64_t)qh * a.out.head + d0) = y;
+        if (d0 == 0 && a.lse)
+            a.lse[out_row * a.hq + qh] = sum != 0.0f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+    }
+}
+
+template <class T, int D>
+int go(const AttnLaunch &a, int rows, hipStream_t s) {
+    const dim3 grid((unsigned)a.grid * (unsigned)a.hkv);
+    if (rows == 16) hipLaunchKernelGGL((k_attn_few<T, D, 1>), grid, dim3(256), 0, s, a);
+    else if (rows == 32) hipLaunchKernelGGL((k_attn_few<T, D, 2>), grid, dim3(256), 0, s, a);
+    else if constexpr (D <= 128) hipLaunchKernelGGL((k_attn_few<T, D, 4>), grid, dim3(256), 0, s, a);
+    else return (int)hipErrorInvalidValue;
+    return (int)hipGetLastError();
+}
+
+template <class T>
+int go(const AttnLaunch &a, int rows, hipStream_t s) {
+    return a.d <= 64 ? go<T, 64>(a, rows, s) : a.d <= 128 ? go<T, 128>(a, rows, s) : go<T, 256>(a, rows, s);
+}
+
+}  // namespace
+
+int launch_attn_few(const AttnLaunch &a, int rows, void *stream) {
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    return a.dtype == FATE_BF16 ? go<BF16>(a, rows, s) : go<F16>(a, rows, s);
+}
+
+int launch_attn_join(const AttnLaunch &a, int rows, int tiles, void *stream) {
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    const dim3 grid((unsigned)tiles * (unsigned)a.hkv);
+    const int least = rows == kTileRows ? kTileLeast : kFewLeast;
+    if (a.dtype == FATE_BF16) hipLaunchKernelGGL(k_attn_join<BF16>, grid, dim3(256), 0, s, a, rows, least);
+    else hipLaunchKernelGGL(k_attn_join<F16>, grid, dim3(256), 0, s, a, rows, least);
+    return (int)hipGetLastError();
+}
+
+}  // namespace fate

@@ -13,6 +13,7 @@ the host-only :func:`fate_layout_dags` / :func:`fate_layout_state`.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 from typing import Optional
 
@@ -35,13 +36,15 @@ EXPORTS = ["fate_version", "fate_strerror", "fate_pack_dags_size", "fate_pack_da
            "fate_pack_dags_opt_size",
            "fate_pack_dags_opt", "fate_layout_dags_opt", "fate_score_sweep", "fate_topk_sweep", "fate_plan_wave",
            "fate_simulate", "fate_place_baseline", "fate_sim_ws_size", "fate_simulate_device",
-           "fate_place_baseline_device"]
+           "fate_place_baseline_device", "fate_kv_append", "fate_attn_paged_ws_size", "fate_attn_paged",
+           "fate_attn_prompt"]
 
 # Scoring variants and packing options (fate_params_t.flags, fate_pack_opts_t.levels).
 FATE_MEAN_PER_LEVEL, FATE_NO_WINDOWS = 1, 2
 FATE_LEVELS_HOP, FATE_LEVELS_TOPO = 0, 1
 FATE_MAX_SWEEP = 16
 FATE_PLACE_ROUND_ROBIN, FATE_PLACE_HEFT = 0, 1
+FATE_BF16, FATE_F16 = 0, 1
 FATE_NOALLOC_WS_BYTES = 32 << 20  # workspace the library holds per GPU for fate_commit_advance_noalloc
 
 
@@ -109,6 +112,24 @@ class StateH(C.Structure):
                 ("slice", C.c_int32), ("fr_off", C.c_void_p), ("order", C.c_void_p)]
 
 
+class Heads(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("heads_q", C.c_int32), ("heads_kv", C.c_int32), ("head_dim", C.c_int32)]
+
+
+class Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token", C.c_int64), ("head", C.c_int64)]
+
+
+class KvCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page", C.c_int64), ("head", C.c_int64),
+                ("token", C.c_int64), ("n_pages", C.c_int32), ("page_size", C.c_int32)]
+
+
+class Seqs(C.Structure):
+    _fields_ = [("B", C.c_int32), ("max_pages", C.c_int32), ("T", C.c_int64), ("pages_stride", C.c_int64),
+                ("off", C.c_void_p), ("kv_len", C.c_void_p), ("pages", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -165,6 +186,13 @@ def load(path: Optional[str] = None):
                                          C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
     lib.fate_place_baseline_device.argtypes = [P(Dags), P(StateH), C.c_int32, C.c_float, C.c_void_p, C.c_void_p,
                                                C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.fate_kv_append.argtypes = [P(Heads), P(Seqs), P(Rows), P(Rows), P(Rows), C.c_void_p, C.c_int64, C.c_int32,
+                                   C.c_int32, P(KvCache), P(Rows), C.c_void_p, C.c_void_p]
+    lib.fate_attn_paged_ws_size.argtypes = [P(Heads), P(Seqs), P(KvCache), C.c_int64, P(C.c_size_t)]
+    lib.fate_attn_paged.argtypes = [P(Heads), P(Seqs), P(Rows), P(KvCache), C.c_int64, C.c_float, P(Rows),
+                                    C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.fate_attn_prompt.argtypes = [P(Heads), P(Seqs), P(Rows), P(Rows), P(Rows), C.c_float, P(Rows), C.c_void_p,
+                                     C.c_void_p, C.c_void_p]
     for name in EXPORTS[2:]:
         getattr(lib, name).restype = st
     if path is None:
@@ -657,3 +685,228 @@ def desc_counts(packed: PackedDags):
     off = h.desc_off - packed.buf.data_ptr()
     do = packed.buf[off:off + 4 * (N + 1)].view(torch.int32).cpu().numpy().astype(np.int64)
     return np.diff(do)
+
+
+# ---- attention of a planned wave -------------------------------------------
+
+
+def _rows(t, name, heads, head_dim, dtype, device, tokens=None):
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != head_dim or (tokens is not None and t.shape[0] != tokens):
+        raise ValueError("%s must be [%s, %d, %d], got %s" % (name, "T" if tokens is None else tokens, heads, head_dim,
+                                                              tuple(t.shape)))
+    if t.dtype != dtype or t.device != device:
+        raise ValueError("%s must be %s on %s, got %s on %s" % (name, dtype, device, t.dtype, t.device))
+    if t.stride(2) != 1:
+        raise ValueError("%s: the elements of a head must be contiguous" % name)
+    # the stride of a dimension of one entry means nothing: any valid one will do
+    whole = heads * head_dim
+    return Rows(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else whole, t.stride(1) if heads > 1 else head_dim)
+
+
+def _ints(t, name, dims, device):
+    import torch
+    if t.dtype != torch.int32 or t.device != device or t.dim() != dims or (t.numel() and t.stride(-1) != 1):
+        raise ValueError("%s must be an int32 tensor of %d dimensions on %s, contiguous in the last" % (name, dims, device))
+    return t.data_ptr()
+
+
+def _attn_heads(q_heads, kv_heads, head_dim, dtype) -> Heads:
+    import torch
+    if dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError("attention takes bfloat16 or float16, got %s" % dtype)
+    return Heads(FATE_BF16 if dtype == torch.bfloat16 else FATE_F16, q_heads, kv_heads, head_dim)
+
+
+def _attn_seqs(off, kv_len, pages, page_size, T, device) -> Seqs:
+    B = off.shape[0] - 1
+    if off.dim() != 1 or B < 0:
+        raise ValueError("off must hold B + 1 entries")
+    s = Seqs(B, 0, T, 0, _ints(off, "off", 1, device))
+    if pages is not None:
+        s.kv_len, s.pages = _ints(kv_len, "kv_len", 1, device), _ints(pages, "pages", 2, device)
+        if kv_len.shape[0] != B or pages.shape[0] != B:
+            raise ValueError("kv_len and pages must have a row for each of the %d sequences" % B)
+        s.max_pages, s.pages_stride = pages.shape[1], pages.stride(0)
+    return s
+
+
+def _attn_cache(k_cache, v_cache, device) -> KvCache:
+    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or k_cache.stride() != v_cache.stride():
+        raise ValueError("k_cache and v_cache must be [pages, heads_kv, page_size, head_dim] with the same strides")
+    if k_cache.dtype != v_cache.dtype or k_cache.device != device or v_cache.device != device:
+        raise ValueError("k_cache and v_cache must have one type, on %s" % device)
+    if k_cache.stride(3) != 1:
+        raise ValueError("the elements of a cached head must be contiguous")
+    n, hkv, size, d = k_cache.shape
+    return KvCache(k_cache.data_ptr(), v_cache.data_ptr(), k_cache.stride(0) if n > 1 else hkv * size * d,
+                   k_cache.stride(1) if hkv > 1 else size * d, k_cache.stride(2) if size > 1 else d, n, size)
+
+
+def _attn_status(status, B, device):
+    import torch
+    if status is None:
+        return None
+    if status.dtype != torch.int32 or status.device != device or not status.is_contiguous() or status.numel() < B:
+        raise ValueError("status must be a contiguous int32 tensor of B elements on %s" % device)
+    return status.data_ptr()
+
+
+class _On:
+    """The device and stream that a call and its allocations use: memory
+    taken inside belongs to the stream the kernels run on, so that the
+    allocator hands it out again only behind them."""
+
+    def __init__(self, device, stream):
+        import torch
+        if device.type != "cuda":
+            raise ValueError("attention takes tensors on a GPU, got %s" % device)
+        if stream is not None and stream.device != device:
+            raise ValueError("the stream is on %s, the tensors are on %s" % (stream.device, device))
+        self.guards = []
+        if device.index != torch.cuda.current_device():
+            self.guards.append(torch.cuda.device(device))
+        if stream is not None:
+            self.guards.append(torch.cuda.stream(stream))
+        self.device = device
+
+    def __enter__(self):
+        import torch
+        for g in self.guards:
+            g.__enter__()
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def __exit__(self, *exc):
+        for g in reversed(self.guards):
+            g.__exit__(*exc)
+        return False
+
+
+def fate_kv_append(q, k, v, k_cache, v_cache, off, kv_len, pages, table=None, interleaved: bool = False, q_out=None,
+                   status=None, stream=None):
+    """Store new keys, rotated to their positions, and values in a paged cache
+    and rotate the queries.
+
+    q [T, heads_q, head_dim] or None; k, v [T, heads_kv, head_dim] (bfloat16 or
+    float16; any token and head strides that are multiples of 8); k_cache,
+    v_cache [pages, heads_kv, page_size, head_dim]; off [B + 1], kv_len [B] and
+    pages [B, max_pages] int32: sequence b has rows off[b] .. off[b + 1] and,
+    these included, kv_len[b] keys.  table [positions, rot] float32 (see
+    :func:`rotation_table`): cosines, then sines of the first rot dimensions,
+    paired (j, j + rot / 2) or, interleaved, (2 j, 2 j + 1); None leaves all
+    unrotated.  Returns q_out (None without q), which may be q itself.
+    ``status`` (int32 [B], cleared by the caller) receives FATE_EINVAL for
+    sequences whose device arrays are out of range."""
+    import torch
+    T, hkv, d = k.shape
+    dev, dtype = k.device, k.dtype
+    h = _attn_heads(hkv if q is None else q.shape[1], hkv, d, dtype)
+    rk, rv = _rows(k, "k", hkv, d, dtype, dev), _rows(v, "v", hkv, d, dtype, dev, T)
+    c = _attn_cache(k_cache, v_cache, dev)
+    if k_cache.dtype != dtype or k_cache.shape[1] != hkv or k_cache.shape[3] != d:
+        raise ValueError("the cache must hold %d heads of %d %s" % (hkv, d, dtype))
+    s = _attn_seqs(off, kv_len, pages, c.page_size, T, dev)
+    rot = rows = 0
+    if table is not None:
+        if table.dtype != torch.float32 or table.dim() != 2 or table.device != dev or not table.is_contiguous():
+            raise ValueError("table must be a contiguous float32 [positions, rot] tensor on %s" % dev)
+        rows, rot = table.shape
+    with _On(dev, stream) as sp:
+        rq = ro = None
+        if q is not None:
+            rq = _rows(q, "q", h.heads_q, d, dtype, dev, T)
+            if q_out is None:
+                q_out = torch.empty((T, h.heads_q, d), dtype=dtype, device=dev)
+            ro = _rows(q_out, "q_out", h.heads_q, d, dtype, dev, T)
+        elif q_out is not None:
+            raise ValueError("q_out without q")
+        st = load().fate_kv_append(h, s, rq, rk, rv, table.data_ptr() if rot else None, rows, rot, int(interleaved), c,
+                                   ro, _attn_status(status, s.B, dev), sp)
+    if st != FATE_OK:
+        raise FateError(st, "fate_kv_append")
+    return q_out
+
+
+def fate_attn_paged(q, k_cache, v_cache, off, kv_len, pages, max_new: Optional[int] = None, scale: Optional[float] = None,
+                    lse: bool = False, out=None, status=None, ws=None, stream=None):
+    """Causal attention of new tokens q [T, heads_q, head_dim] over their
+    sequences' keys and values in a paged cache (append first); arguments as
+    for :func:`fate_kv_append`.  ``max_new`` bounds the tokens per sequence
+    (default T): a small bound picks the kernels for few tokens.  ``scale``
+    defaults to 1 / sqrt(head_dim).  Returns (out, lse): lse [T, heads_q]
+    float32 if asked for, else None.  ``ws`` (uint8, as large as
+    :func:`fate_attn_paged_ws_size` says) is taken from the allocator if not
+    given."""
+    import torch
+    T, hq, d = q.shape
+    dev, dtype = q.device, q.dtype
+    c = _attn_cache(k_cache, v_cache, dev)
+    h = _attn_heads(hq, k_cache.shape[1], d, dtype)
+    if k_cache.dtype != dtype or k_cache.shape[3] != d:
+        raise ValueError("the cache must hold heads of %d %s" % (d, dtype))
+    rq = _rows(q, "q", hq, d, dtype, dev)
+    s = _attn_seqs(off, kv_len, pages, c.page_size, T, dev)
+    lib = load()
+    most = T if max_new is None else min(int(max_new), T)
+    with _On(dev, stream) as sp:
+        if out is None:
+            out = torch.empty((T, hq, d), dtype=dtype, device=dev)
+        ro = _rows(out, "out", hq, d, dtype, dev, T)
+        sums = torch.empty((T, hq), dtype=torch.float32, device=dev) if lse else None
+        nbytes = C.c_size_t(0)
+        st = lib.fate_attn_paged_ws_size(h, s, c, most, nbytes)
+        if st != FATE_OK:
+            raise FateError(st, "fate_attn_paged_ws_size")
+        if ws is None:
+            ws = torch.empty(max(1, nbytes.value), dtype=torch.uint8, device=dev)
+        elif ws.device != dev or not ws.is_contiguous():
+            raise ValueError("ws must be contiguous, on %s" % dev)
+        st = lib.fate_attn_paged(h, s, rq, c, most, 1.0 / math.sqrt(d) if scale is None else scale, ro,
+                                 sums.data_ptr() if lse else None, _attn_status(status, s.B, dev), ws.data_ptr(),
+                                 ws.numel() * ws.element_size(), sp)
+    if st != FATE_OK:
+        raise FateError(st, "fate_attn_paged")
+    return out, sums
+
+
+def fate_attn_paged_ws_size(T: int, heads_q: int, k_cache, B: int, max_pages: int, max_new: int) -> int:
+    """Workspace bytes of :func:`fate_attn_paged` for a call of these sizes."""
+    c = _attn_cache(k_cache, k_cache, k_cache.device)
+    h = _attn_heads(heads_q, k_cache.shape[1], k_cache.shape[3], k_cache.dtype)
+    nbytes = C.c_size_t(0)
+    _check(load().fate_attn_paged_ws_size(h, Seqs(B, max_pages, T), c, max_new, nbytes), "fate_attn_paged_ws_size")
+    return int(nbytes.value)
+
+
+def fate_attn_prompt(q, k, v, off, scale: Optional[float] = None, lse: bool = False, out=None, status=None,
+                     stream=None):
+    """Causal attention of whole prompts, packed: q [T, heads_q, head_dim]
+    over k, v [T, heads_kv, head_dim] (views of one projection will do),
+    sequence b in rows off[b] .. off[b + 1].  Returns (out, lse) as
+    :func:`fate_attn_paged`."""
+    import torch
+    T, hq, d = q.shape
+    dev, dtype = q.device, q.dtype
+    h = _attn_heads(hq, k.shape[1], d, dtype)
+    rq = _rows(q, "q", hq, d, dtype, dev)
+    rk, rv = (_rows(t, n, h.heads_kv, d, dtype, dev, T) for t, n in ((k, "k"), (v, "v")))
+    s = _attn_seqs(off, None, None, 0, T, dev)
+    with _On(dev, stream) as sp:
+        if out is None:
+            out = torch.empty((T, hq, d), dtype=dtype, device=dev)
+        ro = _rows(out, "out", hq, d, dtype, dev, T)
+        sums = torch.empty((T, hq), dtype=torch.float32, device=dev) if lse else None
+        st = load().fate_attn_prompt(h, s, rq, rk, rv, 1.0 / math.sqrt(d) if scale is None else scale, ro,
+                                     sums.data_ptr() if lse else None, _attn_status(status, s.B, dev), sp)
+    if st != FATE_OK:
+        raise FateError(st, "fate_attn_prompt")
+    return out, sums
+
+
+def rotation_table(positions: int, rot: int, base: float = 10000.0, device="cuda"):
+    """Cosines and sines for :func:`fate_kv_append`: float32 [positions, rot],
+    angle p * base ** (-j / (rot / 2)) of pair j, computed in float64."""
+    import torch
+    half = rot // 2
+    angle = torch.outer(torch.arange(positions, dtype=torch.float64),
+                        base ** (-torch.arange(half, dtype=torch.float64) / max(1, half)))
+    return torch.cat([angle.cos(), angle.sin()], 1).float().to(device)
