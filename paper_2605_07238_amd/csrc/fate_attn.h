@@ -118,6 +118,13 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t x) {
     return ((x & T::kExp) + T::kOne) & 0x80008000u;
 }
 
+// The pair with halves that are infinite or NaN set to zero.
+template <class T>
+__device__ __forceinline__ uint32_t only_finite(uint32_t x) {
+    const uint32_t bad = not_finite<T>(x);
+    return x & ~((bad & 0x8000u ? 0xffffu : 0u) | (bad & 0x80000000u ? 0xffff0000u : 0u));
+}
+
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }

@@ -89,6 +89,7 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnLaunch a) {
         }
     };
     find_pages(k_lo + 32 * w);
+    bool odd = false;  // a value on some row's edge is infinite or NaN
     for (int kb = k_lo + 32 * w; kb < k_hi; kb += 128) {
         u32x4 rk[2][KS], rv[2][KS];
 #pragma unroll
@@ -113,7 +114,6 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnLaunch a) {
         }
         find_pages(kb + 128);
         const bool edge = kb + 32 > least;  // uniform
-        bool odd = false;
         if (edge) {
             uint32_t bad = 0;
 #pragma unroll
@@ -122,7 +122,15 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnLaunch a) {
                 for (int s = 0; s < KS; ++s)
                     bad |= not_finite<T>(rv[i][s][0]) | not_finite<T>(rv[i][s][1]) | not_finite<T>(rv[i][s][2]) |
                            not_finite<T>(rv[i][s][3]);
-            odd = __any(bad != 0);
+            if (__any(bad != 0)) {  // left out here, added at the end to the rows that see them
+                odd = true;
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int s = 0; s < KS; ++s)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) rv[i][s][e] = only_finite<T>(rv[i][s][e]);
+            }
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -176,25 +184,31 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnLaunch a) {
             const x4 v1 = T::read_tr(&vrow[vr * VS + dt * 16 + vc]);
             const x4 v2 = T::read_tr(&vrow[(vr + 16) * VS + dt * 16 + vc]);
             const x8 vf = __builtin_shufflevector(v1, v2, 0, 1, 2, 3, 4, 5, 6, 7);
-            if (!odd) {
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) o[rt][dt] = T::mfma16(vf, pr[rt], o[rt][dt]);
-            } else {
-                // a value that some row must not see is not finite: key by key
-                for (int key = 0; key < 32; ++key) {
-                    x8 one = vf;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (16 * (e / 4) + 4 * g + e % 4 != key) one[e] = (el)0.0f;
-#pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) {
-                        const f32x4 z = T::mfma16(one, pr[rt], f32x4{0.0f, 0.0f, 0.0f, 0.0f});
-                        if (kb + key < ends[rt]) o[rt][dt] += z;
-                    }
-                }
-            }
+            for (int rt = 0; rt < RT; ++rt) o[rt][dt] = T::mfma16(vf, pr[rt], o[rt][dt]);
         }
         __builtin_amdgcn_wave_barrier();
+    }
+
+    if (odd) {  // uniform in the wave
+        for (int kb = k_lo + 32 * w; kb < k_hi; kb += 128)
+            for (int key = max(kb, least / 32 * 32); key < min(kb + 32, k_hi); ++key) {
+                const int page = table[key >> a.c.page_shift];
+                if ((uint32_t)page >= (uint32_t)a.c.n_pages) continue;
+                const el *src = (const el *)a.c.v + page * a.c.page + (int64_t)hk * a.c.head + (key & mask) * a.c.token;
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) {
+                    asm volatile("" ::: "memory");  // one load at a time: a rare path is to cost no registers
+                    const int d0 = dt * 16 + 4 * g;
+                    x4 x = {};
+                    if (d0 < a.d) x = *(const x4 *)(src + d0);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            o[rt][dt][e] += key < ends[rt] && !__builtin_isfinite((float)x[e]) ? (float)x[e] : 0.0f;
+                }
+            }
     }
 
     // the four waves' rows: common maximum, sums

@@ -21,23 +21,19 @@
 //
 // Key tiles go from the last to the first: the tiles on a row's causal edge
 // come first.  Values that a row must not see cannot be left out of a matrix
-// product by a zero weight when they are infinite or NaN (0 * inf): a tile on
-// an edge whose values hold one takes a slow product, key by key.
+// product by a zero weight when they are infinite or NaN (0 * inf): in the
+// tiles on an edge such values are stored as zeros, and added at the end to
+// the rows that do see them.
 #include "fate_attn.h"
 
 namespace fate {
 namespace {
 
-// Swizzles of the 16-byte chunks of a row in LDS (CH chunks a row).  Keys are
-// read by 32 rows at once, one chunk each: the chunk is xored with the row.
-// Values are read four rows times 64 bytes at once: whole groups of four
-// chunks are moved.
-template <int CH>
-__device__ __forceinline__ int key_chunk(int row, int c) { return c ^ (row & (CH < 16 ? CH - 1 : 15)); }
-template <int CH>
-__device__ __forceinline__ int val_chunk(int row, int c) {
-    return CH >= 16 ? c ^ ((row & 3) << 2) : c ^ (((row >> 1) & 1) << 2);
-}
+// Rows of a tile in LDS are padded against bank conflicts: keys are read by
+// eight rows at once, 16 bytes each (rows 16 bytes apart in the banks), values
+// four rows at once, 64 bytes each (rows 64 bytes apart).  Padding, unlike
+// xored chunks, leaves every address one register plus a constant.
+constexpr int kKeyPad = 8, kValPad = 32;
 
 template <class T, int D, bool PAGED>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch a) {
@@ -46,9 +42,10 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch 
     typedef typename T::x8 x8;
     constexpr int BK = kKeyTile, CH = D / 8;  // keys per tile, 16-byte chunks per row
     constexpr int NL = BK * CH / 256;         // chunks each thread loads of a key (and of a value) tile
-    __shared__ __align__(16) el sk[2][BK * D];
-    __shared__ __align__(16) el sv[2][BK * D];
-    __shared__ int odd_tile[2];  // the key tile whose values hold an infinity or a NaN, per buffer
+    constexpr int KS = D + kKeyPad, VS = D + kValPad;
+    __shared__ __align__(16) el sk[2][BK * KS];
+    __shared__ __align__(16) el sv[2][BK * VS];
+    __shared__ int odd;  // a value on the edge is infinite or NaN
 
     const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
     const int hk = blockIdx.x % a.hkv, item = blockIdx.x / a.hkv;
@@ -137,23 +134,29 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch 
     };
     const int wg_least = max(0, min(p.L, row0 / a.G + first));  // fewest keys a row of the workgroup sees
     auto store_tile = [&](int t, int buf) {
-#pragma unroll
-        for (int i = 0; i < NL; ++i) {
-            const int r = ld_row + i * (256 / CH);
-            *(u32x4 *)&sk[buf][r * D + key_chunk<CH>(r, ld_col) * 8] = rk[i];
-            *(u32x4 *)&sv[buf][r * D + val_chunk<CH>(r, ld_col) * 8] = rv[i];
-        }
         if ((t + 1) * BK > wg_least) {  // uniform: on the edge of some row
             uint32_t bad = 0;
 #pragma unroll
             for (int i = 0; i < NL; ++i)
                 bad |= not_finite<T>(rv[i][0]) | not_finite<T>(rv[i][1]) | not_finite<T>(rv[i][2]) | not_finite<T>(rv[i][3]);
-            if (bad) odd_tile[buf] = t;
+            if (bad) {
+                odd = 1;
+#pragma unroll
+                for (int i = 0; i < NL; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) rv[i][e] = only_finite<T>(rv[i][e]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const int r = ld_row + i * (256 / CH);
+            *(u32x4 *)&sk[buf][r * KS + ld_col * 8] = rk[i];
+            *(u32x4 *)&sv[buf][r * VS + ld_col * 8] = rv[i];
         }
     };
 
     int buf = 0;
-    if (tid < 2) odd_tile[tid] = -1;
+    if (tid == 0) odd = 0;
     if (t_hi > t_lo) {
         find_pages(t_hi - 1);
         load_tile(t_hi - 1);
@@ -177,7 +180,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch 
                 const int r = kt * 32 + (lane & 31);
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i) {
-                    const x8 kf = *(const x8 *)&sk[buf][r * D + key_chunk<CH>(r, i * 2 + half) * 8];
+                    const x8 kf = *(const x8 *)&sk[buf][r * KS + i * 16 + half * 8];
                     s[kt] = T::mfma32(kf, q[i], s[kt]);
                 }
             }
@@ -218,48 +221,45 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch 
                 }
             // second product: v transposed, four keys at a time, in the weights' order
             const int vr = 4 * half + (lane & 15) / 4, vc = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-            if (!edge || odd_tile[buf] != t) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int dt = 0; dt < D / 32; ++dt) {
-                        const int r1 = 16 * i + vr, r2 = r1 + 8, c = dt * 32 + vc;
-                        const x4 v1 = T::read_tr(&sv[buf][r1 * D + val_chunk<CH>(r1, c / 8) * 8 + c % 8]);
-                        const x4 v2 = T::read_tr(&sv[buf][r2 * D + val_chunk<CH>(r2, c / 8) * 8 + c % 8]);
-                        const x8 vf = __builtin_shufflevector(v1, v2, 0, 1, 2, 3, 4, 5, 6, 7);
-                        o[dt] = T::mfma32(vf, pr[i], o[dt]);
-                    }
-            } else {
-                // a value that some row must not see is not finite: one key at
-                // a time, its product kept by the rows that see it
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    for (int key = 0; key < 16; ++key) {
-                        const bool sees = t * BK + 16 * i + key < ends;
-#pragma unroll
-                        for (int dt = 0; dt < D / 32; ++dt) {
-                            const int r1 = 16 * i + vr, r2 = r1 + 8, c = dt * 32 + vc;
-                            const x4 v1 = T::read_tr(&sv[buf][r1 * D + val_chunk<CH>(r1, c / 8) * 8 + c % 8]);
-                            const x4 v2 = T::read_tr(&sv[buf][r2 * D + val_chunk<CH>(r2, c / 8) * 8 + c % 8]);
-                            x8 vf = __builtin_shufflevector(v1, v2, 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                if (8 * (e / 4) + 4 * half + e % 4 != key) vf[e] = (el)0.0f;
-                            f32x16 z;
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) z[j] = 0.0f;
-                            z = T::mfma32(vf, pr[i], z);
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) o[dt][j] += sees ? z[j] : 0.0f;
-                        }
-                    }
-            }
+                for (int dt = 0; dt < D / 32; ++dt) {
+                    const int r1 = 16 * i + vr, r2 = r1 + 8, c = dt * 32 + vc;
+                    const x4 v1 = T::read_tr(&sv[buf][r1 * VS + c]);
+                    const x4 v2 = T::read_tr(&sv[buf][r2 * VS + c]);
+                    const x8 vf = __builtin_shufflevector(v1, v2, 0, 1, 2, 3, 4, 5, 6, 7);
+                    o[dt] = T::mfma32(vf, pr[i], o[dt]);
+                }
         }
         if (t > t_lo) store_tile(t - 1, buf ^ 1);
         __syncthreads();
         buf ^= 1;
     }
 
+    if (odd) {  // values that the tiles left out, for the rows that see them (any weight makes them what they are)
+        for (int key = max(t_lo, wg_least / BK) * BK; key < min(ends, t_hi * BK); ++key) {
+            const el *src;
+            if (PAGED) {
+                const int page = a.s.pages[p.b * a.s.pages_stride + (key >> a.c.page_shift)];
+                if ((uint32_t)page >= (uint32_t)a.c.n_pages) continue;
+                src = (const el *)a.c.v + page * a.c.page + (int64_t)hk * a.c.head +
+                      (key & ((1 << a.c.page_shift) - 1)) * a.c.token;
+            } else {
+                src = (const el *)a.v.data + (p.lo_row + (int64_t)key) * a.v.token + (int64_t)hk * a.v.head;
+            }
+#pragma unroll
+            for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int c = dt * 32 + 8 * j + 4 * half;
+                    x4 x = {};
+                    if (c < a.d) x = *(const x4 *)(src + c);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[dt][4 * j + e] += __builtin_isfinite((float)x[e]) ? 0.0f : (float)x[e];
+                }
+        }
+    }
     l += __shfl_xor(l, 32);
     if (!live) return;
     const int64_t out_row = p.lo_row + (int64_t)tok;
