@@ -47,20 +47,19 @@ struct AttnLaunch {
     CacheArg c;
     float *lse;       // [T][hq] or null
     int32_t *status;  // [B] or null
-    float *part;      // partial outputs [slots][hkv][rows][d], then (max, sum) pairs [slots][hkv][rows][2]
+    float *part;      // partial outputs [2 pieces][hkv][rows][d], then (max, sum) pairs [2 pieces][hkv][rows][2]
     float scale_log2; // scale * log2(e)
     int32_t hq, hkv, G, d, dtype;
-    int32_t pieces;   // target pieces of work per key head (splitting); 0 = never split
-    int32_t slots;    // partial slots per key head
-    int32_t grid;     // pieces launched per key head
+    int32_t pieces;   // paged calls: shares of the work axis (few rows), or parts aimed at (row tiles), per key head
+    int32_t grid;     // workgroups per key head
 };
 int launch_attn_tile(const AttnLaunch &a, bool paged, void *stream);
 int launch_attn_few(const AttnLaunch &a, int rows, void *stream);
-int launch_attn_join(const AttnLaunch &a, int rows, int tiles, void *stream);
+int launch_attn_join(const AttnLaunch &a, int rows, int tiles, int groups, void *stream);
 
 constexpr int kKeyTile = 64;    // keys per tile: the unit in which the key axis is split
 constexpr int kTileRows = 128;  // packed rows of a workgroup of the tile kernel
-// Fewest key tiles of a part: one block of 32 keys for each wave of the
+// Fewest key tiles of a share: one block of 32 keys for each wave of the
 // few-row kernel; enough work to pay for the join in the tile kernel.
 constexpr int kFewLeast = 2, kTileLeast = 4;
 
@@ -129,117 +128,265 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
-// A workgroup's piece of work: packed rows [tile * M, ...) of sequence b over
-// key tiles [lo, hi) of its keys.
-struct Piece {
-    int b, n, lo_row;  // sequence, its tokens, first token row (off[b])
-    int L;             // its keys
-    int tile;          // row tile
-    int split, splits; // which part of the key axis, of how many
-    int slot;          // partial slot (splits > 1)
-    int chunk;         // key tiles per split
-    bool ok;
+// One sequence as the kernels see it: its first row, tokens and keys; no
+// tokens and no keys past the last sequence and where the device arrays are
+// out of range (`report`: say so in the status).
+struct Lens {
+    int lo, n, L;
 };
 
-// One sequence as the kernels see it: token count and keys, both zero where
-// the device arrays are out of range.
-template <bool PAGED>
-__device__ __forceinline__ void read_seq(const AttnLaunch &a, int b, int &lo, int &n, int &L, bool &bad) {
-    lo = a.s.off[b];
+template <bool PAGED, class A>
+__device__ __forceinline__ Lens read_lens(const A &a, int b, bool report) {
+    Lens s = {0, 0, 0};
+    if (b >= a.s.B) return s;
+    s.lo = a.s.off[b];
     const int hi = a.s.off[b + 1];
-    bad = lo < 0 || hi < lo || (int64_t)hi > a.s.T;
-    n = bad ? 0 : hi - lo;
-    L = n;
+    bool bad = s.lo < 0 || hi < s.lo || (int64_t)hi > a.s.T;
+    s.n = s.L = hi - s.lo;
     if (PAGED) {
-        L = a.s.kv_len[b];
-        if (L < 0 || (int64_t)L > a.s.max_keys) bad = true;
-        if (bad) L = n = 0;
+        s.L = a.s.kv_len[b];
+        bad = bad || s.L < 0 || (int64_t)s.L > a.s.max_keys;
     }
+    if (bad) {
+        s.lo = s.n = s.L = 0;
+        if (report && a.status) a.status[b] = FATE_EINVAL;
+    }
+    return s;
 }
 
-__device__ __forceinline__ int wave_scan_add(int x, int lane) {  // inclusive
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int y = __shfl_up(x, d);
-        if (lane >= d) x += y;
-    }
+// Inclusive sums over the 64 lanes (all active): shifts right by 1, 2, 4 and 8
+// within each row of 16 lanes, then the last lanes of rows 0 and 2, and of row
+// 1, to the rows after them, in DPP moves as wave_exscan_u32.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int moved(int x) {
+    return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, false);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int64_t moved(int64_t x) {
+    return (int64_t)(((uint64_t)(uint32_t)moved<CTRL, ROWS>((int)(x >> 32)) << 32) |
+                     (uint32_t)moved<CTRL, ROWS>((int)x));
+}
+template <class I>
+__device__ __forceinline__ I wave_scan_add(I x) {
+    x += moved<0x111, 0xF>(x);
+    x += moved<0x112, 0xF>(x);
+    x += moved<0x114, 0xF>(x);
+    x += moved<0x118, 0xF>(x);
+    x += moved<0x142, 0xA>(x);
+    x += moved<0x143, 0xC>(x);
     return x;
 }
 
-__device__ __forceinline__ int64_t wave_sum(int64_t x) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d);
+// Lane i's value, i the same in all lanes.
+__device__ __forceinline__ int lane_of(int x, int i) { return __builtin_amdgcn_readlane(x, i); }
+__device__ __forceinline__ int64_t lane_of(int64_t x, int i) {
+    return (int64_t)(((uint64_t)(uint32_t)lane_of((int)(x >> 32), i) << 32) | (uint32_t)lane_of((int)x, i));
+}
+
+template <class I>
+__device__ __forceinline__ I wave_sum(I x) { return lane_of(wave_scan_add(x), 63); }
+
+// The launch arguments where the kernel finds them.  A workgroup that walks
+// through several pieces of work reads them again for each (and its thread
+// number goes through fresh()), or the compiler would keep everything that
+// does not change between pieces in registers, which the piece itself needs.
+typedef const __attribute__((address_space(4))) AttnLaunch Args;
+
+__device__ __forceinline__ const Args &launch_args() {
+    const Args *p = (const Args *)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *p;
+}
+
+__device__ __forceinline__ int fresh(int x) {
+    asm volatile("" : "+v"(x));
     return x;
 }
 
 __device__ __forceinline__ int tiles_of(int n, int tile) { return (int)(((int64_t)n + tile - 1) / tile); }
 
-// Key tiles per piece: the call's key tiles over all row tiles of M packed
-// rows, shared out over the target number of pieces.  The lengths are read on
-// the device (a serving step's lengths live there), so every workgroup adds
-// them up for itself: B / 64 loads per lane, which a small batch barely feels.
-template <bool PAGED>
-__device__ __forceinline__ int chunk_of(const AttnLaunch &a, int M, int least, int lane) {
-    if (!PAGED || a.pieces == 0) return 0x7fffffff;
-    int64_t sum = 0;
-    for (int b = lane; b < a.s.B; b += 64) {
-        int lo, n, L;
-        bool bad;
-        read_seq<PAGED>(a, b, lo, n, L, bad);
-        sum += (int64_t)tiles_of(n * a.G, M) * tiles_of(L, kKeyTile);
-    }
-    sum = wave_sum(sum);
-    const int64_t c = (sum + a.pieces - 1) / a.pieces;
-    return c < least ? least : (int)(c > 0x7fffffff ? 0x7fffffff : c);
+// A row tile: packed rows [tile * M, ...) of sequence b, which has n tokens in
+// rows from lo_row and L keys.
+struct Unit {
+    int b, n, lo_row, L, tile;
+    int64_t start, cost;  // its place on the work axis (paged calls)
+    bool ok;
+};
+
+// ---- calls of few rows: an axis of work, equal shares -----------------------
+// The work axis of a paged call.  Its row tiles lie on it one after the other,
+// each as long as its cost: G times the keys that its last row sees, to the
+// nearest tile, G A + (tile + 1) M for a sequence with A keys cached before the
+// call.  The axis is cut into equal shares, one workgroup each, whatever the
+// mix of lengths; a tile that a cut goes through is done in parts and joined.
+// The lengths are read on the device, where a serving step has them (and a
+// captured step finds the current ones), so that every workgroup adds them up
+// for itself: B / 64 steps of a wave.
+struct Axis {
+    int64_t total, share;
+};
+
+__device__ __forceinline__ int64_t tile_start(int t, int64_t GA, int M) { return t * GA + (int64_t)M * t * (t + 1) / 2; }
+
+__device__ __forceinline__ int64_t seq_cost(const Lens &s, int G, int M) {
+    return tile_start(tiles_of(s.n * G, M), (int64_t)G * max(0, s.L - s.n), M);
 }
 
-// The piece with number `item`: sequences in order, each with its row tiles
-// from the last (which sees the most keys) to the first, each of these split
-// over its keys.  JOIN: number only the row tiles of split sequences.
-template <bool PAGED, bool JOIN>
-__device__ __forceinline__ Piece find_piece(const AttnLaunch &a, int M, int chunk, int item, int lane, bool report) {
+// `first`: the lane's sequence of the first 64, which most calls end with.
+template <class A>
+__device__ __forceinline__ Axis axis_of(const A &a, int M, const Lens &first, int lane, bool report) {
+    int64_t sum = seq_cost(first, a.G, M);
+    for (int at = 64; at < a.s.B; at += 64) sum += seq_cost(read_lens<true>(a, at + lane, report), a.G, M);
+    Axis x;
+    x.total = wave_sum(sum);
+    const int64_t least_share = (int64_t)kFewLeast * kKeyTile * a.G;
+    x.share = (x.total + a.pieces - 1) / a.pieces;
+    if (x.share < least_share) x.share = least_share;
+    return x;
+}
+
+// The row tile at place x < total of the axis.
+template <class A>
+__device__ __forceinline__ Unit unit_at(const A &a, int M, const Lens &first, int64_t x, int lane) {
+    Unit u;
+    u.ok = false;
+    int64_t before = 0;
+    for (int at = 0; at < a.s.B; at += 64) {
+        const Lens s = at == 0 ? first : read_lens<true>(a, at + lane, false);
+        const int64_t mine = seq_cost(s, a.G, M);
+        const int64_t end = before + wave_scan_add(mine);
+        const uint64_t has = __ballot(x < end);
+        if (has) {
+            const int src = uniform(__ffsll((unsigned long long)has) - 1);
+            u.b = at + src;
+            u.n = lane_of(s.n, src);
+            u.lo_row = lane_of(s.lo, src);
+            u.L = lane_of(s.L, src);
+            const int64_t base = lane_of(end - mine, src), y = x - base;
+            const int64_t GA = (int64_t)a.G * max(0, u.L - u.n);
+            const int tiles = tiles_of(u.n * a.G, M);
+            int t = 0;
+            if (tiles > 1) {
+                // largest t with tile_start(t) <= y: the root of M t^2 / 2 + (GA + M / 2) t - y, then by one steps
+                const double h = (double)GA + 0.5 * M;
+                t = min(max((int)((__builtin_sqrt(h * h + 2.0 * M * (double)y) - h) / M), 0), tiles - 1);
+                while (t > 0 && tile_start(t, GA, M) > y) --t;
+                while (t + 1 < tiles && tile_start(t + 1, GA, M) <= y) ++t;
+            }
+            u.tile = uniform(t);
+            u.start = base + tile_start(u.tile, GA, M);
+            u.cost = GA + (int64_t)(u.tile + 1) * M;
+            u.ok = true;
+            return u;
+        }
+        before = lane_of(end, 63);
+    }
+    return u;
+}
+
+// The key tile at which a cut at place x of the axis, inside the unit, parts
+// its `tiles` key tiles: both sides compute the same number.
+__device__ __forceinline__ int cut_at(const Unit &u, int64_t x, int tiles) {
+    return min(tiles, (int)((double)(x - u.start) / (double)u.cost * tiles));
+}
+
+// ---- calls of many rows: row tiles in order of length -----------------------
+// A row tile is one workgroup's, or several workgroups' where the call has too
+// few for the chip or one is much longer than the others: its keys are then
+// done in parts of at most `chunk` key tiles.  Longest sequences go first and
+// neighbours walk the same keys at the same time, which their shared L2 sees;
+// an equal cut of all the work, as for few rows, lost that (737 against 884
+// TFLOP/s on 16384 new tokens).
+
+// A part of a row tile.
+struct Piece {
+    Unit u;
+    int split, splits, slot;  // which part of how many; its slot for partial results
+};
+
+// Sequences of a group of 64 by decreasing keys: what belongs in this lane's place.
+__device__ __forceinline__ void sort_longest(int group, int lane, int &b, Lens &s) {
+    int rank = 0;
+    for (int i = 0; i < group; ++i) {
+        const int other = lane_of(s.L, i);
+        rank += other > s.L || (other == s.L && i < lane);
+    }
+    if (lane >= group) rank = lane;
+    s.n = __builtin_amdgcn_ds_permute(rank << 2, s.n);
+    s.L = __builtin_amdgcn_ds_permute(rank << 2, s.L);
+    s.lo = __builtin_amdgcn_ds_permute(rank << 2, s.lo);
+    b = __builtin_amdgcn_ds_permute(rank << 2, b);
+}
+
+__device__ __forceinline__ int parts_of(int L, int chunk) {
+    const int tiles = tiles_of(L, kKeyTile);
+    return tiles > chunk ? (tiles + chunk - 1) / chunk : 1;
+}
+
+// Key tiles of a part.  With as many row tiles as parts wanted, only what is
+// over twice an even share is cut.  With fewer, the call's work over `pieces`
+// parts, raised by eighths, up to twice, until there are no more than `pieces`
+// parts (where the sequences fit the wave's lanes): one part over what runs at
+// once costs a whole round.
+template <class A>
+__device__ __forceinline__ int chunk_of(const A &a, int M, const Lens &first, int lane, bool report) {
+    const int nt = tiles_of(first.n * a.G, M), kt = tiles_of(first.L, kKeyTile);
+    int64_t sum = (int64_t)nt * kt;
+    int units = nt;
+    for (int at = 64; at < a.s.B; at += 64) {
+        const Lens s = read_lens<true>(a, at + lane, report);
+        const int t = tiles_of(s.n * a.G, M);
+        units += t;
+        sum += (int64_t)t * tiles_of(s.L, kKeyTile);
+    }
+    const int64_t least = max((wave_sum(sum) + a.pieces - 1) / a.pieces, (int64_t)kTileLeast);
+    const bool spare = wave_sum(units) < a.pieces;
+    int chunk = (int)min(spare ? least : 2 * least, (int64_t)0x7ffffffe);
+    if (spare && a.s.B <= 64) {
+        for (int k = 1; k <= 8; ++k) {
+            if (wave_sum(nt * (kt > chunk ? (kt + chunk - 1) / chunk : 1)) <= a.pieces) break;
+            chunk = (int)min(least + (least * k + 7) / 8, (int64_t)0x7ffffffe);
+        }
+    }
+    return chunk;
+}
+
+// The part with number `item`; JOIN: the row tile with number `item` among
+// those done in parts.  Row tiles of a sequence go from the last, which sees
+// the most keys, to the first.
+template <bool PAGED, bool JOIN, class A>
+__device__ __forceinline__ Piece find_piece(const A &a, int M, const Lens &first, int chunk, int item, int lane,
+                                            bool report) {
     Piece p;
-    p.ok = false;
-    p.chunk = chunk;
+    p.u.ok = false;
     int items = 0, slots = 0;  // before this group of 64 sequences
     for (int at = 0; at < a.s.B; at += 64) {
-        const int b = at + lane;
-        int lo = 0, n = 0, L = 0;
-        if (b < a.s.B) {
-            bool bad;
-            read_seq<PAGED>(a, b, lo, n, L, bad);
-            if (bad && report && a.status) a.status[b] = FATE_EINVAL;
-        }
-        const int nt = tiles_of(n * a.G, M);
-        int sp = 1;
-        if (PAGED && chunk != 0x7fffffff) {
-            sp = (tiles_of(L, kKeyTile) + chunk - 1) / chunk;
-            if (sp < 1) sp = 1;
-        }
-        const int mine = JOIN ? (sp > 1 ? nt : 0) : nt * sp;
-        const int my_slots = sp > 1 ? nt * sp : 0;
-        const int end = wave_scan_add(mine, lane) + items;
-        const int slot_end = wave_scan_add(my_slots, lane) + slots;
+        int b = at + lane;
+        Lens s = at == 0 ? first : read_lens<PAGED>(a, b, report);
+        const int group = min(64, a.s.B - at);
+        if (group > 1) sort_longest(group, lane, b, s);
+        const int nt = tiles_of(s.n * a.G, M), sp = PAGED ? parts_of(s.L, chunk) : 1;
+        const int mine = JOIN ? (sp > 1 ? nt : 0) : nt * sp, my_slots = sp > 1 ? nt * sp : 0;
+        const int end = items + wave_scan_add(mine);
+        const int slot_end = PAGED ? slots + wave_scan_add(my_slots) : 0;
         const uint64_t has = __ballot(item < end);
         if (has) {
-            const int src = __ffsll((unsigned long long)has) - 1;
-            const int local = item - __shfl(end - mine, src);
-            p.b = uniform(at + src);
-            p.n = uniform(__shfl(n, src));
-            p.lo_row = uniform(__shfl(lo, src));
-            p.L = uniform(__shfl(L, src));
-            p.splits = uniform(__shfl(sp, src));
-            const int tiles = uniform(__shfl(nt, src));
-            const int first_slot = uniform(__shfl(slot_end - my_slots, src));
-            const int from_last = uniform(JOIN ? local : local / p.splits);
-            p.split = uniform(JOIN ? 0 : local - from_last * p.splits);
-            p.tile = tiles - 1 - from_last;
-            p.slot = first_slot + from_last * p.splits + p.split;
-            p.ok = true;
+            const int src = uniform(__ffsll((unsigned long long)has) - 1);
+            const int local = item - lane_of(end - mine, src);
+            p.u.b = lane_of(b, src);
+            p.u.n = lane_of(s.n, src);
+            p.u.L = lane_of(s.L, src);
+            p.u.lo_row = lane_of(s.lo, src);
+            p.splits = PAGED ? lane_of(sp, src) : 1;
+            const int from_last = JOIN || p.splits == 1 ? local : local / p.splits;
+            p.split = JOIN ? 0 : local - from_last * p.splits;
+            p.u.tile = lane_of(nt, src) - 1 - from_last;
+            p.slot = (PAGED ? lane_of(slot_end - my_slots, src) : 0) + from_last * p.splits + p.split;
+            p.u.ok = true;
             return p;
         }
-        items = __shfl(end, 63);
-        slots = __shfl(slot_end, 63);
+        items = lane_of(end, 63);
+        slots = lane_of(slot_end, 63);
     }
     return p;
 }

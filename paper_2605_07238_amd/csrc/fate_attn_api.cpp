@@ -68,25 +68,24 @@ void set_cache(fate::CacheArg &out, const fate_kv_cache_t *c) {
 
 // Which kernel a paged call takes, and how its key axis is shared out.
 struct PagedPlan {
-    int rows;    // packed rows per workgroup: 16, 32 or 64 (few-row kernel) or kTileRows
-    int pieces;  // target pieces per key head
-    int slots;   // partial slots per key head (a split row tile's parts are fewer than twice its share)
+    int rows;    // packed rows per workgroup: 16 or 32 (few-row kernel) or kTileRows
+    int pieces;  // shares of the work axis, or parts aimed at, per key head; twice as many slots hold all partial results
     int tiles;   // most row tiles of the call
 };
 
 PagedPlan plan_paged(const fate_heads_t *h, const fate_seqs_t *s, int64_t max_new) {
-    const int64_t G = h->heads_q / h->heads_kv, packed = max_new * G, most = h->head_dim <= 128 ? 64 : 32;
+    const int64_t G = h->heads_q / h->heads_kv, packed = max_new * G, few = h->head_dim <= 128 ? 32 : 16;
     PagedPlan p;
-    p.rows = packed <= 16 ? 16 : packed <= 32 ? 32 : packed <= most ? 64 : fate::kTileRows;
-    const int target = p.rows == fate::kTileRows ? 512 : 1024;
+    p.rows = packed <= 16 ? 16 : packed <= few ? 32 : fate::kTileRows;
+    // what the chip runs at once: two workgroups a compute unit, one of head sizes over 128
+    const int target = h->head_dim <= 128 ? 512 : 256;
     p.pieces = target / h->heads_kv > 0 ? target / h->heads_kv : 1;
-    p.slots = 2 * p.pieces;
     p.tiles = (int)(s->T * G / p.rows + (s->B < s->T ? s->B : s->T));
     return p;
 }
 
 size_t ws_of(const fate_heads_t *h, const PagedPlan &p) {
-    return (size_t)p.slots * h->heads_kv * p.rows * (h->head_dim + 2) * sizeof(float);
+    return 2 * (size_t)p.pieces * h->heads_kv * p.rows * (h->head_dim + 2) * sizeof(float);
 }
 
 fate_status_t fill(AttnLaunch &a, const fate_heads_t *h, const fate_rows_t *q, const fate_rows_t *out, float scale,
@@ -176,16 +175,19 @@ fate_status_t fate_attn_paged(const fate_heads_t *heads, const fate_seqs_t *seqs
     set_cache(a.c, cache);
     a.part = static_cast<float *>(d_ws);
     a.pieces = p.pieces;
-    a.slots = p.slots;
-    a.grid = p.pieces + p.tiles;
-    const int rc = p.rows == fate::kTileRows ? fate::launch_attn_tile(a, true, stream)
+    const bool tile = p.rows == fate::kTileRows;
+    a.grid = tile ? p.pieces + p.tiles : p.pieces;
+    const int rc = tile ? fate::launch_attn_tile(a, true, stream)
                                              : fate::launch_attn_few(a, p.rows, stream);
     if (rc) return FATE_EHIP;
-    // no sequence can be split that has no more keys than the smallest part
-    const int least = p.rows == fate::kTileRows ? fate::kTileLeast : fate::kFewLeast;
-    if (a.s.max_keys <= (int64_t)least * fate::kKeyTile) return FATE_OK;
-    const int tiles = p.tiles < p.pieces ? p.tiles : p.pieces;
-    return fate::launch_attn_join(a, p.rows, tiles, stream) == 0 ? FATE_OK : FATE_EHIP;
+    // row tiles done in parts: each has a part more than it has cuts, so fewer than there are shares; of those in
+    // order of length (each with over `chunk` key tiles of the sum) fewer than pieces, and no more than there are
+    const int tiles = !tile ? p.pieces - 1 : p.tiles < p.pieces ? p.tiles : p.pieces;
+    if (tiles < 1) return FATE_OK;
+    // four rows a workgroup at a time, sixteen at most: as many workgroups as max_new tokens have rows for
+    const int64_t most = max_new * a.G < p.rows ? max_new * a.G : p.rows;
+    const int groups = most > 64 ? 8 : most > 4 ? (int)((most + 3) / 4) : 1;
+    return fate::launch_attn_join(a, p.rows, tiles, groups, stream) == 0 ? FATE_OK : FATE_EHIP;
 }
 
 fate_status_t fate_attn_prompt(const fate_heads_t *heads, const fate_seqs_t *seqs, const fate_rows_t *q,

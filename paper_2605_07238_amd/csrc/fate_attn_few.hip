@@ -3,7 +3,7 @@
 //
 // With few rows the call reads each key and value once and computes little:
 // memory bounds it.  k_attn_few: one workgroup of four waves per (sequence,
-// key head, 16 to 64 packed rows, part of the key axis); the parts are sized
+// key head, 16 or 32 packed rows, part of the key axis); the parts are sized
 // from the lengths on the device so that the whole call makes about as many
 // pieces as the chip holds workgroups, whatever the mix of lengths.  A wave
 // takes every fourth block of 32 keys by itself: keys go from memory to
@@ -21,7 +21,7 @@ namespace fate {
 namespace {
 
 template <class T, int D, int RT>
-__global__ __launch_bounds__(256) void k_attn_few(AttnLaunch a) {
+__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_few(AttnLaunch) {
     typedef typename T::el el;
     typedef typename T::x4 x4;
     typedef typename T::x8 x8;
@@ -32,22 +32,34 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnLaunch a) {
     __shared__ __align__(16) char raw[kBytes];
     __shared__ float sm[4][M], sl[4][M];
 
-    const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
-    const int hk = blockIdx.x % a.hkv, item = blockIdx.x / a.hkv;
-    const int chunk = chunk_of<true>(a, M, kFewLeast, lane);
-    const Piece p = find_piece<true, false>(a, M, chunk, item, lane, hk == 0 && item == 0 && w == 0);
+    int hk, piece;
+    int64_t from, to;
+    Lens lens;
+    {
+        const Args &a = launch_args();
+        const bool report = blockIdx.x == 0 && threadIdx.x < 64;
+        hk = blockIdx.x % a.hkv, piece = blockIdx.x / a.hkv;
+        lens = read_lens<true>(a, threadIdx.x & 63, report);
+        const Axis axis = axis_of(a, M, lens, threadIdx.x & 63, report);
+        from = piece * axis.share;
+        to = min(from + axis.share, axis.total);
+    }
+    for (int64_t x = from; x < to;) {  // the row tiles of this share
+    const Args &a = launch_args();
+    const int tid = fresh(threadIdx.x), lane = tid & 63, w = uniform(tid >> 6);
+    const Unit p = unit_at(a, M, lens, x, lane);
     if (!p.ok) return;
+    x = p.start + p.cost;
 
     const int rows = p.n * a.G, row0 = p.tile * M;
     const int first = p.L - p.n + 1;
     const int last_row = min(row0 + M, rows) - 1;
     const int most = min(p.L, max(0, last_row / a.G + first));
     const int least = max(0, min(p.L, row0 / a.G + first));
-    int k_lo = 0, k_hi = most;
-    if (p.splits > 1) {
-        k_lo = p.split * chunk * kKeyTile;
-        k_hi = (int)min((int64_t)most, (int64_t)k_lo + (int64_t)chunk * kKeyTile);
-    }
+    const int blocks = (most + 31) / 32;
+    const bool part = p.start < from || p.start + p.cost > to;
+    const int k_lo = p.start < from ? 32 * cut_at(p, from, blocks) : 0;
+    const int k_hi = p.start + p.cost > to ? min(most, 32 * cut_at(p, to, blocks)) : most;
 
     const int c = lane & 15, g = lane >> 4;
     x8 q[RT][KS];
@@ -245,13 +257,12 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnLaunch a) {
             }
             const int tok = row / a.G, qh = hk * a.G + row - tok * a.G;
             const int64_t out_row = p.lo_row + (int64_t)tok;
-            if (p.splits > 1) {
-                if (p.slot >= a.slots) continue;
-                const int64_t at = ((int64_t)p.slot * a.hkv + hk) * M + rr;
+            if (part) {  // unscaled sums, joined by k_attn_join
+                const int64_t at = ((int64_t)(2 * piece + (p.start > from)) * a.hkv + hk) * M + rr;
                 *(f32x4 *)(a.part + at * a.d + d0) = y0;
                 *(f32x4 *)(a.part + at * a.d + d0 + 4) = y1;
                 if (d0 == 0) {
-                    float *ml = a.part + (int64_t)a.slots * a.hkv * M * a.d + at * 2;
+                    float *ml = a.part + 2 * (int64_t)a.pieces * a.hkv * M * a.d + at * 2;
                     ml[0] = top;
                     ml[1] = sum;
                 }
@@ -269,46 +280,87 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnLaunch a) {
                 a.lse[out_row * a.hq + qh] = sum != 0.0f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
         }
     }
+    __syncthreads();  // the outputs' and statistics' rows serve the next row tile
+    }
 }
 
-// One workgroup per (split row tile, key head): each thread joins eight
-// dimensions of a row over the parts.
-template <class T>
-__global__ __launch_bounds__(256) void k_attn_join(AttnLaunch a, int M, int least) {
+// One wave per row of a row tile done in parts (a workgroup takes four rows, and every
+// `groups`-th four after them): its lanes are sixteen chunks of eight
+// dimensions times four parts at a time, so that a row's parts are read side
+// by side and the chain of reads stays short however many parts there are.
+template <class T, bool TILE>
+__global__ __launch_bounds__(256) void k_attn_join(AttnLaunch a, int M, int groups) {
     typedef typename T::el el;
     typedef typename T::x8 x8;
-    const int tid = threadIdx.x, lane = tid & 63;
-    const int hk = blockIdx.x % a.hkv, item = blockIdx.x / a.hkv;
-    const int chunk = chunk_of<true>(a, M, least, lane);
-    const Piece p = find_piece<true, true>(a, M, chunk, item, lane, false);
-    if (!p.ok || p.slot + p.splits > a.slots) return;
-    const int rows = p.n * a.G, row0 = p.tile * M, per = a.d / 8;
-    const float *ml0 = a.part + (int64_t)a.slots * a.hkv * M * a.d;
-    for (int x = tid; x < min(M, rows - row0) * per; x += 256) {
-        const int rr = x / per, d0 = (x - rr * per) * 8, row = row0 + rr;
-        const int64_t at0 = ((int64_t)p.slot * a.hkv + hk) * M + rr, step = (int64_t)a.hkv * M;
-        float top = kLowest;
-        for (int i = 0; i < p.splits; ++i) top = fmaxf(top, ml0[(at0 + i * step) * 2]);
-        float sum = 0.0f;
-        f32x4 y0 = {0.0f, 0.0f, 0.0f, 0.0f}, y1 = y0;
-        for (int i = 0; i < p.splits; ++i) {
-            const int64_t at = at0 + i * step;
-            const float f = exp2_fast(ml0[at * 2] - top);
-            sum += ml0[at * 2 + 1] * f;
-            y0 += *(const f32x4 *)(a.part + at * a.d + d0) * f;
-            y1 += *(const f32x4 *)(a.part + at * a.d + d0 + 4) * f;
-        }
-        const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
-        x8 y;
+    const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
+    const int group = blockIdx.x % groups, hk = blockIdx.x / groups % a.hkv, item = blockIdx.x / groups / a.hkv;
+    const Lens lens = read_lens<true>(a, lane, false);
+    // part i lies in slot first_slot (i = 0), next_slot + step * i (others)
+    Unit p;
+    int splits, first_slot, next_slot, step;
+    if (TILE) {
+        const Piece piece = find_piece<true, true>(a, M, lens, chunk_of(a, M, lens, lane, false), item, lane, false);
+        p = piece.u;
+        if (!p.ok) return;
+        splits = piece.splits;
+        first_slot = next_slot = piece.slot;
+        step = 1;
+    } else {
+        const Axis axis = axis_of(a, M, lens, lane, false);
+        const int64_t cut = (item + 1) * axis.share;
+        if (cut >= axis.total) return;
+        p = unit_at(a, M, lens, cut, lane);
+        if (!p.ok || p.start >= cut || p.start < cut - axis.share) return;  // this row tile's first cut alone
+        splits = uniform((int)((p.start + p.cost - 1) / axis.share)) - item + 1;
+        first_slot = 2 * item + (p.start > cut - axis.share);  // behind the share's first where the tile begins within
+        next_slot = 2 * item;
+        step = 2;
+    }
+    const int rows = p.n * a.G, row0 = p.tile * M;
+    const float *ml0 = a.part + 2 * (int64_t)a.pieces * a.hkv * M * a.d;
+    auto place = [&](int i, int rr) {
+        return ((int64_t)(i == 0 ? first_slot : next_slot + step * i) * a.hkv + hk) * M + rr;
+    };
+    for (int rr = group * 4 + w; rr < min(M, rows - row0); rr += groups * 4) {
+        float top = kLowest, sum = 0.0f;
+        for (int i = lane; i < splits; i += 64) top = fmaxf(top, ml0[place(i, rr) * 2]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            y[e] = (el)(y0[e] * inv);
-            y[4 + e] = (el)(y1[e] * inv);
+        for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x));
+        for (int i = lane; i < splits; i += 64) {
+            const float *ml = ml0 + place(i, rr) * 2;
+            sum += ml[1] * exp2_fast(ml[0] - top);
         }
-        const int tok = row / a.G, qh = hk * a.G + row - tok * a.G;
+#pragma unroll
+        for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x);
+        const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+        const int row = row0 + rr, tok = row / a.G, qh = hk * a.G + row - tok * a.G;
         const int64_t out_row = p.lo_row + (int64_t)tok;
-        *(x8 *)((el *)a.out.data + out_row * a.out.token + (int64_t)qh * a.out.head + d0) = y;
-        if (d0 == 0 && a.lse)
+        el *dst = (el *)a.out.data + out_row * a.out.token + (int64_t)qh * a.out.head;
+        for (int c0 = 0; c0 < a.d; c0 += 128) {
+            const int d0 = c0 + (lane & 15) * 8;
+            f32x4 y0 = {0.0f, 0.0f, 0.0f, 0.0f}, y1 = y0;
+            if (d0 < a.d) {
+#pragma unroll 4
+                for (int i = lane >> 4; i < splits; i += 4) {
+                    const int64_t at = place(i, rr);
+                    const float f = exp2_fast(ml0[at * 2] - top);
+                    y0 += *(const f32x4 *)(a.part + at * a.d + d0) * f;
+                    y1 += *(const f32x4 *)(a.part + at * a.d + d0 + 4) * f;
+                }
+            }
+            x8 y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                y0[e] += __shfl_xor(y0[e], 16);
+                y1[e] += __shfl_xor(y1[e], 16);
+                y0[e] += __shfl_xor(y0[e], 32);
+                y1[e] += __shfl_xor(y1[e], 32);
+                y[e] = (el)(y0[e] * inv);
+                y[4 + e] = (el)(y1[e] * inv);
+            }
+            if (lane < 16 && d0 < a.d) *(x8 *)(dst + d0) = y;
+        }
+        if (lane == 0 && a.lse)
             a.lse[out_row * a.hq + qh] = sum != 0.0f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
     }
 }
@@ -317,8 +369,7 @@ template <class T, int D>
 int go(const AttnLaunch &a, int rows, hipStream_t s) {
     const dim3 grid((unsigned)a.grid * (unsigned)a.hkv);
     if (rows == 16) hipLaunchKernelGGL((k_attn_few<T, D, 1>), grid, dim3(256), 0, s, a);
-    else if (rows == 32) hipLaunchKernelGGL((k_attn_few<T, D, 2>), grid, dim3(256), 0, s, a);
-    else if constexpr (D <= 128) hipLaunchKernelGGL((k_attn_few<T, D, 4>), grid, dim3(256), 0, s, a);
+    else if constexpr (D <= 128) hipLaunchKernelGGL((k_attn_few<T, D, 2>), grid, dim3(256), 0, s, a);
     else return (int)hipErrorInvalidValue;
     return (int)hipGetLastError();
 }
@@ -335,12 +386,14 @@ int launch_attn_few(const AttnLaunch &a, int rows, void *stream) {
     return a.dtype == FATE_BF16 ? go<BF16>(a, rows, s) : go<F16>(a, rows, s);
 }
 
-int launch_attn_join(const AttnLaunch &a, int rows, int tiles, void *stream) {
+int launch_attn_join(const AttnLaunch &a, int rows, int tiles, int groups, void *stream) {
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    const dim3 grid((unsigned)tiles * (unsigned)a.hkv);
-    const int least = rows == kTileRows ? kTileLeast : kFewLeast;
-    if (a.dtype == FATE_BF16) hipLaunchKernelGGL(k_attn_join<BF16>, grid, dim3(256), 0, s, a, rows, least);
-    else hipLaunchKernelGGL(k_attn_join<F16>, grid, dim3(256), 0, s, a, rows, least);
+    const dim3 grid((unsigned)tiles * (unsigned)a.hkv * (unsigned)groups);
+    const bool bf = a.dtype == FATE_BF16, tile = rows == kTileRows;
+    if (bf && tile) hipLaunchKernelGGL((k_attn_join<BF16, true>), grid, dim3(256), 0, s, a, rows, groups);
+    else if (bf) hipLaunchKernelGGL((k_attn_join<BF16, false>), grid, dim3(256), 0, s, a, rows, groups);
+    else if (tile) hipLaunchKernelGGL((k_attn_join<F16, true>), grid, dim3(256), 0, s, a, rows, groups);
+    else hipLaunchKernelGGL((k_attn_join<F16, false>), grid, dim3(256), 0, s, a, rows, groups);
     return (int)hipGetLastError();
 }
 

@@ -49,8 +49,11 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch 
 
     const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
     const int hk = blockIdx.x % a.hkv, item = blockIdx.x / a.hkv;
-    const int chunk = chunk_of<PAGED>(a, kTileRows, kTileLeast, lane);
-    const Piece p = find_piece<PAGED, false>(a, kTileRows, chunk, item, lane, hk == 0 && item == 0 && w == 0);
+    const bool report = blockIdx.x == 0 && tid < 64;
+    const Lens lens = read_lens<PAGED>(a, lane, report);
+    const int chunk = PAGED ? chunk_of(a, kTileRows, lens, lane, report) : 0x7fffffff;
+    const Piece piece = find_piece<PAGED, false>(a, kTileRows, lens, chunk, item, lane, !PAGED && report);
+    const Unit &p = piece.u;
     if (!p.ok) return;
 
     // rows of this workgroup and wave: keys that a row sees are [0, token + first)
@@ -58,9 +61,11 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch 
     const int first = p.L - p.n + 1;
     const int wg_last = min(row0 + kTileRows, rows) - 1;
     const int wg_most = min(p.L, max(0, wg_last / a.G + first));  // most keys a row of the workgroup sees
-    const int t_lo = PAGED ? min((int64_t)p.split * chunk, (int64_t)0x7fffffff) : 0;
-    int t_hi = (wg_most + BK - 1) / BK;
-    if (PAGED && p.splits > 1) t_hi = min(t_hi, t_lo + chunk);
+    int t_lo = 0, t_hi = (wg_most + BK - 1) / BK;
+    if (PAGED && piece.splits > 1) {
+        t_lo = piece.split * chunk;
+        t_hi = min(t_hi, t_lo + chunk);
+    }
 
     const int wrow0 = row0 + w * 32;
     const int row = wrow0 + (lane & 31), half = lane >> 5;
@@ -187,6 +192,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch 
             // s[kt][j]: key kt * 32 + 8 (j / 4) + 4 half + j % 4 of the tile, row lane % 32
             const bool edge = (t + 1) * BK > w_least;
             if (edge) {
+                asm volatile("");  // a branch, not selects in every tile
                 const int left = ends - t * BK - 4 * half;
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt)
@@ -263,9 +269,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch 
     l += __shfl_xor(l, 32);
     if (!live) return;
     const int64_t out_row = p.lo_row + (int64_t)tok;
-    if (PAGED && p.splits > 1) {  // a part of the keys: unscaled sums, joined by k_attn_join
-        if (p.slot >= a.slots) return;
-        const int64_t at = ((int64_t)p.slot * a.hkv + hk) * kTileRows + (row - row0);
+    if (PAGED && piece.splits > 1) {  // a part of the keys: unscaled sums, joined by k_attn_join
+        const int64_t at = ((int64_t)piece.slot * a.hkv + hk) * kTileRows + (row - row0);
         float *dst = a.part + at * a.d;
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt)
@@ -275,7 +280,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch 
                 if (c < a.d) *(f32x4 *)(dst + c) = f32x4{o[dt][4 * j], o[dt][4 * j + 1], o[dt][4 * j + 2], o[dt][4 * j + 3]};
             }
         if (half == 0) {
-            float *ml = a.part + (int64_t)a.slots * a.hkv * kTileRows * a.d + at * 2;
+            float *ml = a.part + 2 * (int64_t)a.pieces * a.hkv * kTileRows * a.d + at * 2;
             ml[0] = m;
             ml[1] = l;
         }

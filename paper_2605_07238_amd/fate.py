@@ -688,97 +688,100 @@ def desc_counts(packed: PackedDags):
 
 
 # ---- attention of a planned wave -------------------------------------------
+# A serving step makes these calls tens of thousands of times a second, so the
+# checks are written to be cheap.
 
 
-def _rows(t, name, heads, head_dim, dtype, device, tokens=None):
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != head_dim or (tokens is not None and t.shape[0] != tokens):
-        raise ValueError("%s must be [%s, %d, %d], got %s" % (name, "T" if tokens is None else tokens, heads, head_dim,
-                                                              tuple(t.shape)))
-    if t.dtype != dtype or t.device != device:
-        raise ValueError("%s must be %s on %s, got %s on %s" % (name, dtype, device, t.dtype, t.device))
-    if t.stride(2) != 1:
+def _rows(t, name, T, heads, head_dim, dtype, device):
+    """A [T, heads, head_dim] tensor of the call as packed rows."""
+    if t.shape != (T, heads, head_dim) or t.dtype is not dtype or t.device != device:
+        raise ValueError("%s must be [%d, %d, %d] %s on %s, got %s %s on %s" % (
+            name, T, heads, head_dim, dtype, device, list(t.shape), t.dtype, t.device))
+    token, head, one = t.stride()
+    if one != 1:
         raise ValueError("%s: the elements of a head must be contiguous" % name)
     # the stride of a dimension of one entry means nothing: any valid one will do
-    whole = heads * head_dim
-    return Rows(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else whole, t.stride(1) if heads > 1 else head_dim)
+    return Rows(t.data_ptr(), token if T > 1 else heads * head_dim, head if heads > 1 else head_dim)
 
 
-def _ints(t, name, dims, device):
+def _three(t, name):
+    if t.dim() != 3:
+        raise ValueError("%s must be [tokens, heads, head_dim], got %s" % (name, list(t.shape)))
+    return t.shape
+
+
+def _attn_dtype(dtype):
     import torch
-    if t.dtype != torch.int32 or t.device != device or t.dim() != dims or (t.numel() and t.stride(-1) != 1):
-        raise ValueError("%s must be an int32 tensor of %d dimensions on %s, contiguous in the last" % (name, dims, device))
-    return t.data_ptr()
+    if dtype is torch.bfloat16:
+        return FATE_BF16
+    if dtype is torch.float16:
+        return FATE_F16
+    raise ValueError("attention takes bfloat16 or float16, got %s" % dtype)
 
 
-def _attn_heads(q_heads, kv_heads, head_dim, dtype) -> Heads:
+def _is_ints(t, dims, device):
     import torch
-    if dtype not in (torch.bfloat16, torch.float16):
-        raise ValueError("attention takes bfloat16 or float16, got %s" % dtype)
-    return Heads(FATE_BF16 if dtype == torch.bfloat16 else FATE_F16, q_heads, kv_heads, head_dim)
+    return t.dtype is torch.int32 and t.device == device and t.dim() == dims and (t.stride(-1) == 1 or t.numel() <= 1)
 
 
-def _attn_seqs(off, kv_len, pages, page_size, T, device) -> Seqs:
+def _attn_seqs(off, kv_len, pages, T, device) -> Seqs:
+    if not _is_ints(off, 1, device) or off.shape[0] < 1:
+        raise ValueError("off must be a contiguous int32 tensor of B + 1 elements on %s" % device)
     B = off.shape[0] - 1
-    if off.dim() != 1 or B < 0:
-        raise ValueError("off must hold B + 1 entries")
-    s = Seqs(B, 0, T, 0, _ints(off, "off", 1, device))
-    if pages is not None:
-        s.kv_len, s.pages = _ints(kv_len, "kv_len", 1, device), _ints(pages, "pages", 2, device)
-        if kv_len.shape[0] != B or pages.shape[0] != B:
-            raise ValueError("kv_len and pages must have a row for each of the %d sequences" % B)
-        s.max_pages, s.pages_stride = pages.shape[1], pages.stride(0)
-    return s
+    if pages is None:
+        return Seqs(B, 0, T, 0, off.data_ptr(), None, None)
+    if not _is_ints(kv_len, 1, device) or not _is_ints(pages, 2, device):
+        raise ValueError("kv_len [B] and pages [B, max_pages] must be int32 on %s, contiguous in the last dimension" % device)
+    n, width = pages.shape
+    if n != B or kv_len.shape[0] != B:
+        raise ValueError("kv_len and pages must have a row for each of the %d sequences" % B)
+    return Seqs(B, width, T, pages.stride(0) if n > 1 else width, off.data_ptr(), kv_len.data_ptr(), pages.data_ptr())
 
 
-def _attn_cache(k_cache, v_cache, device) -> KvCache:
-    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or k_cache.stride() != v_cache.stride():
-        raise ValueError("k_cache and v_cache must be [pages, heads_kv, page_size, head_dim] with the same strides")
-    if k_cache.dtype != v_cache.dtype or k_cache.device != device or v_cache.device != device:
-        raise ValueError("k_cache and v_cache must have one type, on %s" % device)
-    if k_cache.stride(3) != 1:
+def _attn_cache(k_cache, v_cache, heads, head_dim, dtype, device) -> KvCache:
+    shape, strides = k_cache.shape, k_cache.stride()
+    if len(shape) != 4 or shape[1] != heads or shape[3] != head_dim or v_cache.shape != shape or v_cache.stride() != strides:
+        raise ValueError("k_cache and v_cache must be [pages, %d, page_size, %d] with the same strides, got %s and %s" % (
+            heads, head_dim, list(shape), list(v_cache.shape)))
+    if k_cache.dtype is not dtype or v_cache.dtype is not dtype or k_cache.device != device or v_cache.device != device:
+        raise ValueError("k_cache and v_cache must be %s on %s" % (dtype, device))
+    if strides[3] != 1:
         raise ValueError("the elements of a cached head must be contiguous")
-    n, hkv, size, d = k_cache.shape
-    return KvCache(k_cache.data_ptr(), v_cache.data_ptr(), k_cache.stride(0) if n > 1 else hkv * size * d,
-                   k_cache.stride(1) if hkv > 1 else size * d, k_cache.stride(2) if size > 1 else d, n, size)
+    n, _, size, _ = shape
+    return KvCache(k_cache.data_ptr(), v_cache.data_ptr(), strides[0] if n > 1 else heads * size * head_dim,
+                   strides[1] if heads > 1 else size * head_dim, strides[2] if size > 1 else head_dim, n, size)
 
 
 def _attn_status(status, B, device):
     import torch
     if status is None:
         return None
-    if status.dtype != torch.int32 or status.device != device or not status.is_contiguous() or status.numel() < B:
+    if status.dtype is not torch.int32 or status.device != device or not status.is_contiguous() or status.numel() < B:
         raise ValueError("status must be a contiguous int32 tensor of B elements on %s" % device)
     return status.data_ptr()
 
 
-class _On:
-    """The device and stream that a call and its allocations use: memory
-    taken inside belongs to the stream the kernels run on, so that the
-    allocator hands it out again only behind them."""
+def _elsewhere(device, stream):
+    """Whether a call has to enter another device or stream than the current ones (:func:`_there`)."""
+    import torch
+    if device.type != "cuda":
+        raise ValueError("attention takes tensors on a GPU, got %s" % device)
+    if stream is None:
+        return device.index != torch.cuda.current_device()
+    if stream.device != device:
+        raise ValueError("the stream is on %s, the tensors are on %s" % (stream.device, device))
+    return True
 
-    def __init__(self, device, stream):
-        import torch
-        if device.type != "cuda":
-            raise ValueError("attention takes tensors on a GPU, got %s" % device)
-        if stream is not None and stream.device != device:
-            raise ValueError("the stream is on %s, the tensors are on %s" % (stream.device, device))
-        self.guards = []
-        if device.index != torch.cuda.current_device():
-            self.guards.append(torch.cuda.device(device))
-        if stream is not None:
-            self.guards.append(torch.cuda.stream(stream))
-        self.device = device
 
-    def __enter__(self):
-        import torch
-        for g in self.guards:
-            g.__enter__()
-        return torch.cuda.current_stream(self.device).cuda_stream
-
-    def __exit__(self, *exc):
-        for g in reversed(self.guards):
-            g.__exit__(*exc)
-        return False
+def _there(device, stream, call, *args, **more):
+    """A call made with the tensors' device and `stream` current: what it takes from the allocator then belongs to the
+    stream its kernels run on, and is handed out again only behind them."""
+    import torch
+    with torch.cuda.device(device):
+        if stream is None:
+            return call(*args, **more)
+        with torch.cuda.stream(stream):
+            return call(*args, **more)
 
 
 def fate_kv_append(q, k, v, k_cache, v_cache, off, kv_len, pages, table=None, interleaved: bool = False, q_out=None,
@@ -797,30 +800,33 @@ def fate_kv_append(q, k, v, k_cache, v_cache, off, kv_len, pages, table=None, in
     ``status`` (int32 [B], cleared by the caller) receives FATE_EINVAL for
     sequences whose device arrays are out of range."""
     import torch
-    T, hkv, d = k.shape
     dev, dtype = k.device, k.dtype
-    h = _attn_heads(hkv if q is None else q.shape[1], hkv, d, dtype)
-    rk, rv = _rows(k, "k", hkv, d, dtype, dev), _rows(v, "v", hkv, d, dtype, dev, T)
-    c = _attn_cache(k_cache, v_cache, dev)
-    if k_cache.dtype != dtype or k_cache.shape[1] != hkv or k_cache.shape[3] != d:
-        raise ValueError("the cache must hold %d heads of %d %s" % (hkv, d, dtype))
-    s = _attn_seqs(off, kv_len, pages, c.page_size, T, dev)
-    rot = rows = 0
+    if _elsewhere(dev, stream):
+        return _there(dev, stream, fate_kv_append, q, k, v, k_cache, v_cache, off, kv_len, pages, table, interleaved,
+                      q_out, status)
+    T, hkv, d = _three(k, "k")
+    hq = hkv
+    c = _attn_cache(k_cache, v_cache, hkv, d, dtype, dev)
+    s = _attn_seqs(off, kv_len, pages, T, dev)
+    rk, rv = _rows(k, "k", T, hkv, d, dtype, dev), _rows(v, "v", T, hkv, d, dtype, dev)
+    rq = ro = turns = None
+    rot = positions = 0
+    if q is not None:
+        hq = _three(q, "q")[1]
+        rq = _rows(q, "q", T, hq, d, dtype, dev)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
     if table is not None:
-        if table.dtype != torch.float32 or table.dim() != 2 or table.device != dev or not table.is_contiguous():
+        if table.dtype is not torch.float32 or table.dim() != 2 or table.device != dev or not table.is_contiguous():
             raise ValueError("table must be a contiguous float32 [positions, rot] tensor on %s" % dev)
-        rows, rot = table.shape
-    with _On(dev, stream) as sp:
-        rq = ro = None
-        if q is not None:
-            rq = _rows(q, "q", h.heads_q, d, dtype, dev, T)
-            if q_out is None:
-                q_out = torch.empty((T, h.heads_q, d), dtype=dtype, device=dev)
-            ro = _rows(q_out, "q_out", h.heads_q, d, dtype, dev, T)
-        elif q_out is not None:
-            raise ValueError("q_out without q")
-        st = load().fate_kv_append(h, s, rq, rk, rv, table.data_ptr() if rot else None, rows, rot, int(interleaved), c,
-                                   ro, _attn_status(status, s.B, dev), sp)
+        positions, rot = table.shape
+        turns = table.data_ptr()
+    if q is not None:
+        if q_out is None:
+            q_out = torch.empty((T, hq, d), dtype=dtype, device=dev)
+        ro = _rows(q_out, "q_out", T, hq, d, dtype, dev)
+    st = load().fate_kv_append(Heads(_attn_dtype(dtype), hq, hkv, d), s, rq, rk, rv, turns, positions, rot,
+                               1 if interleaved else 0, c, ro, _attn_status(status, s.B, dev), _raw_stream(dev.index))
     if st != FATE_OK:
         raise FateError(st, "fate_kv_append")
     return q_out
@@ -837,44 +843,48 @@ def fate_attn_paged(q, k_cache, v_cache, off, kv_len, pages, max_new: Optional[i
     :func:`fate_attn_paged_ws_size` says) is taken from the allocator if not
     given."""
     import torch
-    T, hq, d = q.shape
     dev, dtype = q.device, q.dtype
-    c = _attn_cache(k_cache, v_cache, dev)
-    h = _attn_heads(hq, k_cache.shape[1], d, dtype)
-    if k_cache.dtype != dtype or k_cache.shape[3] != d:
-        raise ValueError("the cache must hold heads of %d %s" % (d, dtype))
-    rq = _rows(q, "q", hq, d, dtype, dev)
-    s = _attn_seqs(off, kv_len, pages, c.page_size, T, dev)
-    lib = load()
-    most = T if max_new is None else min(int(max_new), T)
-    with _On(dev, stream) as sp:
-        if out is None:
-            out = torch.empty((T, hq, d), dtype=dtype, device=dev)
-        ro = _rows(out, "out", hq, d, dtype, dev, T)
-        sums = torch.empty((T, hq), dtype=torch.float32, device=dev) if lse else None
-        nbytes = C.c_size_t(0)
-        st = lib.fate_attn_paged_ws_size(h, s, c, most, nbytes)
-        if st != FATE_OK:
-            raise FateError(st, "fate_attn_paged_ws_size")
-        if ws is None:
-            ws = torch.empty(max(1, nbytes.value), dtype=torch.uint8, device=dev)
-        elif ws.device != dev or not ws.is_contiguous():
-            raise ValueError("ws must be contiguous, on %s" % dev)
-        st = lib.fate_attn_paged(h, s, rq, c, most, 1.0 / math.sqrt(d) if scale is None else scale, ro,
-                                 sums.data_ptr() if lse else None, _attn_status(status, s.B, dev), ws.data_ptr(),
-                                 ws.numel() * ws.element_size(), sp)
+    if _elsewhere(dev, stream):
+        return _there(dev, stream, fate_attn_paged, q, k_cache, v_cache, off, kv_len, pages, max_new, scale, lse, out,
+                      status, ws)
+    T, hq, d = _three(q, "q")
+    hkv = k_cache.shape[1] if k_cache.dim() == 4 else 0
+    c = _attn_cache(k_cache, v_cache, hkv, d, dtype, dev)
+    s = _attn_seqs(off, kv_len, pages, T, dev)
+    most = T if max_new is None or max_new > T else int(max_new)
+    rq = _rows(q, "q", T, hq, d, dtype, dev)
+    h = Heads(_attn_dtype(dtype), hq, hkv, d)
+    if out is None:
+        out = torch.empty((T, hq, d), dtype=dtype, device=dev)
+    ro = _rows(out, "out", T, hq, d, dtype, dev)
+    sums = torch.empty((T, hq), dtype=torch.float32, device=dev) if lse else None
+    if ws is None:
+        ws = torch.empty(_paged_ws(h, s, c, most), dtype=torch.uint8, device=dev)
+    elif ws.device != dev or not ws.is_contiguous():
+        raise ValueError("ws must be contiguous, on %s" % dev)
+    st = load().fate_attn_paged(h, s, rq, c, most, 1.0 / math.sqrt(d) if scale is None else scale, ro,
+                                sums.data_ptr() if lse else None, _attn_status(status, s.B, dev), ws.data_ptr(),
+                                ws.nbytes, _raw_stream(dev.index))
     if st != FATE_OK:
         raise FateError(st, "fate_attn_paged")
     return out, sums
 
 
+def _paged_ws(h, s, c, most) -> int:
+    nbytes = C.c_size_t(0)
+    st = load().fate_attn_paged_ws_size(h, s, c, most, nbytes)
+    if st != FATE_OK:
+        raise FateError(st, "fate_attn_paged_ws_size")
+    return nbytes.value
+
+
 def fate_attn_paged_ws_size(T: int, heads_q: int, k_cache, B: int, max_pages: int, max_new: int) -> int:
     """Workspace bytes of :func:`fate_attn_paged` for a call of these sizes."""
-    c = _attn_cache(k_cache, k_cache, k_cache.device)
-    h = _attn_heads(heads_q, k_cache.shape[1], k_cache.shape[3], k_cache.dtype)
-    nbytes = C.c_size_t(0)
-    _check(load().fate_attn_paged_ws_size(h, Seqs(B, max_pages, T), c, max_new, nbytes), "fate_attn_paged_ws_size")
-    return int(nbytes.value)
+    if k_cache.dim() != 4:
+        raise ValueError("k_cache must be [pages, heads_kv, page_size, head_dim]")
+    hkv, d = k_cache.shape[1], k_cache.shape[3]
+    c = _attn_cache(k_cache, k_cache, hkv, d, k_cache.dtype, k_cache.device)
+    return _paged_ws(Heads(_attn_dtype(k_cache.dtype), heads_q, hkv, d), Seqs(B, max_pages, T), c, max_new)
 
 
 def fate_attn_prompt(q, k, v, off, scale: Optional[float] = None, lse: bool = False, out=None, status=None,
@@ -884,22 +894,29 @@ def fate_attn_prompt(q, k, v, off, scale: Optional[float] = None, lse: bool = Fa
     sequence b in rows off[b] .. off[b + 1].  Returns (out, lse) as
     :func:`fate_attn_paged`."""
     import torch
-    T, hq, d = q.shape
     dev, dtype = q.device, q.dtype
-    h = _attn_heads(hq, k.shape[1], d, dtype)
-    rq = _rows(q, "q", hq, d, dtype, dev)
-    rk, rv = (_rows(t, n, h.heads_kv, d, dtype, dev, T) for t, n in ((k, "k"), (v, "v")))
-    s = _attn_seqs(off, None, None, 0, T, dev)
-    with _On(dev, stream) as sp:
-        if out is None:
-            out = torch.empty((T, hq, d), dtype=dtype, device=dev)
-        ro = _rows(out, "out", hq, d, dtype, dev, T)
-        sums = torch.empty((T, hq), dtype=torch.float32, device=dev) if lse else None
-        st = load().fate_attn_prompt(h, s, rq, rk, rv, 1.0 / math.sqrt(d) if scale is None else scale, ro,
-                                     sums.data_ptr() if lse else None, _attn_status(status, s.B, dev), sp)
+    if _elsewhere(dev, stream):
+        return _there(dev, stream, fate_attn_prompt, q, k, v, off, scale, lse, out, status)
+    T, hq, d = _three(q, "q")
+    hkv = _three(k, "k")[1]
+    s = _attn_seqs(off, None, None, T, dev)
+    rq, rk, rv = _rows(q, "q", T, hq, d, dtype, dev), _rows(k, "k", T, hkv, d, dtype, dev), _rows(v, "v", T, hkv, d, dtype, dev)
+    if out is None:
+        out = torch.empty((T, hq, d), dtype=dtype, device=dev)
+    ro = _rows(out, "out", T, hq, d, dtype, dev)
+    sums = torch.empty((T, hq), dtype=torch.float32, device=dev) if lse else None
+    st = load().fate_attn_prompt(Heads(_attn_dtype(dtype), hq, hkv, d), s, rq, rk, rv,
+                                 1.0 / math.sqrt(d) if scale is None else scale, ro, sums.data_ptr() if lse else None,
+                                 _attn_status(status, s.B, dev), _raw_stream(dev.index))
     if st != FATE_OK:
         raise FateError(st, "fate_attn_prompt")
     return out, sums
+
+
+def _raw_stream(index: int) -> int:
+    """The current stream of a device as a hipStream_t."""
+    import torch
+    return torch._C._cuda_getCurrentRawStream(index)
 
 
 def rotation_table(positions: int, rot: int, base: float = 10000.0, device="cuda"):
