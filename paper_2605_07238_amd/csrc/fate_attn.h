@@ -35,6 +35,7 @@ struct AppendLaunch {
     int32_t *status;
     int64_t table_rows;
     int32_t hq, hkv, d, rot, interleaved, dtype;
+    int32_t past_cache;  // the call moves more than the last-level cache holds
 };
 int launch_append(const AppendLaunch &a, void *stream);
 

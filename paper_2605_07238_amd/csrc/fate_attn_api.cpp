@@ -144,6 +144,8 @@ fate_status_t fate_kv_append(const fate_heads_t *heads, const fate_seqs_t *seqs,
     a.rot = rot;
     a.interleaved = interleaved;
     a.dtype = heads->dtype;
+    const int64_t bytes = seqs->T * (2 * (int64_t)a.hq + 4 * (int64_t)a.hkv) * a.d * 2;
+    a.past_cache = bytes > (int64_t(256) << 20);
     return fate::launch_append(a, stream) == 0 ? FATE_OK : FATE_EHIP;
 }
 

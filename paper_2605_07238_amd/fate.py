@@ -688,54 +688,92 @@ def desc_counts(packed: PackedDags):
 
 
 # ---- attention of a planned wave -------------------------------------------
-# A serving step makes these calls tens of thousands of times a second, so the
-# checks are written to be cheap.
+# A serving step makes these calls tens of thousands of times a second and the
+# small ones are over in a few microseconds, so the checks are written to be
+# cheap: torch is looked up once, and each property of a tensor is asked for once.
+
+_t = None  # the parts of torch that the calls use
 
 
-def _rows(t, name, T, heads, head_dim, dtype, device):
+class _Torch:
+    def __init__(self):
+        import torch
+        self.types = {torch.bfloat16: FATE_BF16, torch.float16: FATE_F16}
+        self.int32, self.float32, self.uint8 = torch.int32, torch.float32, torch.uint8
+        self.empty, self.empty_like = torch.empty, torch.empty_like
+        self.device, self.stream = torch.cuda.device, torch.cuda.stream
+        self.current_device = torch.cuda.current_device
+        self.raw_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _here(device, stream) -> bool:
+    """Whether a call's device and stream are the current ones (else :func:`_there`)."""
+    global _t
+    if _t is None:
+        _t = _Torch()
+    if stream is None and device.index is not None and device.index == _t.current_device():
+        return True
+    if device.type != "cuda":
+        raise ValueError("attention takes tensors on a GPU, got %s" % device)
+    if stream is not None and stream.device != device:
+        raise ValueError("the stream is on %s, the tensors are on %s" % (stream.device, device))
+    return False
+
+
+def _there(device, stream, call, *args, **more):
+    """A call made with the tensors' device and `stream` current: what it takes from the allocator then belongs to the
+    stream its kernels run on, and is handed out again only behind them."""
+    with _t.device(device):
+        if stream is None:
+            return call(*args, **more)
+        with _t.stream(stream):
+            return call(*args, **more)
+
+
+def _rows(t, name, shape, dtype, device):
     """A [T, heads, head_dim] tensor of the call as packed rows."""
-    if t.shape != (T, heads, head_dim) or t.dtype is not dtype or t.device != device:
-        raise ValueError("%s must be [%d, %d, %d] %s on %s, got %s %s on %s" % (
-            name, T, heads, head_dim, dtype, device, list(t.shape), t.dtype, t.device))
+    if t.shape != shape or t.dtype is not dtype or t.device != device:
+        raise ValueError("%s must be %s %s on %s, got %s %s on %s" % (
+            name, list(shape), dtype, device, list(t.shape), t.dtype, t.device))
     token, head, one = t.stride()
     if one != 1:
         raise ValueError("%s: the elements of a head must be contiguous" % name)
+    T, heads, d = shape
     # the stride of a dimension of one entry means nothing: any valid one will do
-    return Rows(t.data_ptr(), token if T > 1 else heads * head_dim, head if heads > 1 else head_dim)
+    return Rows(t.data_ptr(), token if T > 1 else heads * d, head if heads > 1 else d)
+
+
+def _attn_heads(dtype, shape, hkv) -> Heads:
+    kind = _t.types.get(dtype)
+    if kind is None:
+        raise ValueError("attention takes bfloat16 or float16, got %s" % dtype)
+    return Heads(kind, shape[1], hkv, shape[2])
 
 
 def _three(t, name):
-    if t.dim() != 3:
-        raise ValueError("%s must be [tokens, heads, head_dim], got %s" % (name, list(t.shape)))
-    return t.shape
-
-
-def _attn_dtype(dtype):
-    import torch
-    if dtype is torch.bfloat16:
-        return FATE_BF16
-    if dtype is torch.float16:
-        return FATE_F16
-    raise ValueError("attention takes bfloat16 or float16, got %s" % dtype)
-
-
-def _is_ints(t, dims, device):
-    import torch
-    return t.dtype is torch.int32 and t.device == device and t.dim() == dims and (t.stride(-1) == 1 or t.numel() <= 1)
+    shape = t.shape
+    if len(shape) != 3:
+        raise ValueError("%s must be [tokens, heads, head_dim], got %s" % (name, list(shape)))
+    return shape
 
 
 def _attn_seqs(off, kv_len, pages, T, device) -> Seqs:
-    if not _is_ints(off, 1, device) or off.shape[0] < 1:
+    int32 = _t.int32
+    if off.dtype is not int32 or off.device != device or off.dim() != 1 or off.stride(0) != 1 or off.shape[0] < 1:
         raise ValueError("off must be a contiguous int32 tensor of B + 1 elements on %s" % device)
     B = off.shape[0] - 1
     if pages is None:
         return Seqs(B, 0, T, 0, off.data_ptr(), None, None)
-    if not _is_ints(kv_len, 1, device) or not _is_ints(pages, 2, device):
-        raise ValueError("kv_len [B] and pages [B, max_pages] must be int32 on %s, contiguous in the last dimension" % device)
-    n, width = pages.shape
-    if n != B or kv_len.shape[0] != B:
-        raise ValueError("kv_len and pages must have a row for each of the %d sequences" % B)
-    return Seqs(B, width, T, pages.stride(0) if n > 1 else width, off.data_ptr(), kv_len.data_ptr(), pages.data_ptr())
+    n, width = pages.shape if pages.dim() == 2 else (-1, 0)
+    if n != B or kv_len.shape != (B,):
+        raise ValueError("kv_len must be [%d] and pages [%d, max_pages], got %s and %s" % (
+            B, B, list(kv_len.shape), list(pages.shape)))
+    if kv_len.dtype is not int32 or pages.dtype is not int32 or kv_len.device != device or pages.device != device:
+        raise ValueError("kv_len and pages must be int32 on %s" % device)
+    row, one = pages.stride()
+    if (one != 1 and width > 1) or (B > 1 and kv_len.stride(0) != 1):
+        raise ValueError("kv_len, and each row of pages, must be contiguous")
+    return Seqs(B, width, T, row if B > 1 else width, off.data_ptr(), kv_len.data_ptr(), pages.data_ptr())
 
 
 def _attn_cache(k_cache, v_cache, heads, head_dim, dtype, device) -> KvCache:
@@ -745,43 +783,20 @@ def _attn_cache(k_cache, v_cache, heads, head_dim, dtype, device) -> KvCache:
             heads, head_dim, list(shape), list(v_cache.shape)))
     if k_cache.dtype is not dtype or v_cache.dtype is not dtype or k_cache.device != device or v_cache.device != device:
         raise ValueError("k_cache and v_cache must be %s on %s" % (dtype, device))
-    if strides[3] != 1:
+    page, head, token, one = strides
+    if one != 1:
         raise ValueError("the elements of a cached head must be contiguous")
     n, _, size, _ = shape
-    return KvCache(k_cache.data_ptr(), v_cache.data_ptr(), strides[0] if n > 1 else heads * size * head_dim,
-                   strides[1] if heads > 1 else size * head_dim, strides[2] if size > 1 else head_dim, n, size)
+    return KvCache(k_cache.data_ptr(), v_cache.data_ptr(), page if n > 1 else heads * size * head_dim,
+                   head if heads > 1 else size * head_dim, token if size > 1 else head_dim, n, size)
 
 
 def _attn_status(status, B, device):
-    import torch
     if status is None:
         return None
-    if status.dtype is not torch.int32 or status.device != device or not status.is_contiguous() or status.numel() < B:
+    if status.dtype is not _t.int32 or status.device != device or not status.is_contiguous() or status.numel() < B:
         raise ValueError("status must be a contiguous int32 tensor of B elements on %s" % device)
     return status.data_ptr()
-
-
-def _elsewhere(device, stream):
-    """Whether a call has to enter another device or stream than the current ones (:func:`_there`)."""
-    import torch
-    if device.type != "cuda":
-        raise ValueError("attention takes tensors on a GPU, got %s" % device)
-    if stream is None:
-        return device.index != torch.cuda.current_device()
-    if stream.device != device:
-        raise ValueError("the stream is on %s, the tensors are on %s" % (stream.device, device))
-    return True
-
-
-def _there(device, stream, call, *args, **more):
-    """A call made with the tensors' device and `stream` current: what it takes from the allocator then belongs to the
-    stream its kernels run on, and is handed out again only behind them."""
-    import torch
-    with torch.cuda.device(device):
-        if stream is None:
-            return call(*args, **more)
-        with torch.cuda.stream(stream):
-            return call(*args, **more)
 
 
 def fate_kv_append(q, k, v, k_cache, v_cache, off, kv_len, pages, table=None, interleaved: bool = False, q_out=None,
@@ -799,34 +814,34 @@ def fate_kv_append(q, k, v, k_cache, v_cache, off, kv_len, pages, table=None, in
     unrotated.  Returns q_out (None without q), which may be q itself.
     ``status`` (int32 [B], cleared by the caller) receives FATE_EINVAL for
     sequences whose device arrays are out of range."""
-    import torch
     dev, dtype = k.device, k.dtype
-    if _elsewhere(dev, stream):
+    if not _here(dev, stream):
         return _there(dev, stream, fate_kv_append, q, k, v, k_cache, v_cache, off, kv_len, pages, table, interleaved,
                       q_out, status)
-    T, hkv, d = _three(k, "k")
-    hq = hkv
+    shape = _three(k, "k")
+    T, hkv, d = shape
     c = _attn_cache(k_cache, v_cache, hkv, d, dtype, dev)
     s = _attn_seqs(off, kv_len, pages, T, dev)
-    rk, rv = _rows(k, "k", T, hkv, d, dtype, dev), _rows(v, "v", T, hkv, d, dtype, dev)
+    rk, rv = _rows(k, "k", shape, dtype, dev), _rows(v, "v", shape, dtype, dev)
     rq = ro = turns = None
     rot = positions = 0
-    if q is not None:
-        hq = _three(q, "q")[1]
-        rq = _rows(q, "q", T, hq, d, dtype, dev)
-    elif q_out is not None:
-        raise ValueError("q_out without q")
     if table is not None:
-        if table.dtype is not torch.float32 or table.dim() != 2 or table.device != dev or not table.is_contiguous():
+        if table.dtype is not _t.float32 or table.dim() != 2 or table.device != dev or not table.is_contiguous():
             raise ValueError("table must be a contiguous float32 [positions, rot] tensor on %s" % dev)
         positions, rot = table.shape
         turns = table.data_ptr()
     if q is not None:
+        shape = _three(q, "q")
+        if shape[0] != T or shape[2] != d:
+            raise ValueError("q must be [%d, heads_q, %d], got %s" % (T, d, list(shape)))
+        rq = _rows(q, "q", shape, dtype, dev)
         if q_out is None:
-            q_out = torch.empty((T, hq, d), dtype=dtype, device=dev)
-        ro = _rows(q_out, "q_out", T, hq, d, dtype, dev)
-    st = load().fate_kv_append(Heads(_attn_dtype(dtype), hq, hkv, d), s, rq, rk, rv, turns, positions, rot,
-                               1 if interleaved else 0, c, ro, _attn_status(status, s.B, dev), _raw_stream(dev.index))
+            q_out = _t.empty_like(q)
+        ro = _rows(q_out, "q_out", shape, dtype, dev)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    st = load().fate_kv_append(_attn_heads(dtype, shape, hkv), s, rq, rk, rv, turns, positions, rot,
+                               1 if interleaved else 0, c, ro, _attn_status(status, s.B, dev), _t.raw_stream(dev.index))
     if st != FATE_OK:
         raise FateError(st, "fate_kv_append")
     return q_out
@@ -842,29 +857,29 @@ def fate_attn_paged(q, k_cache, v_cache, off, kv_len, pages, max_new: Optional[i
     float32 if asked for, else None.  ``ws`` (uint8, as large as
     :func:`fate_attn_paged_ws_size` says) is taken from the allocator if not
     given."""
-    import torch
     dev, dtype = q.device, q.dtype
-    if _elsewhere(dev, stream):
+    if not _here(dev, stream):
         return _there(dev, stream, fate_attn_paged, q, k_cache, v_cache, off, kv_len, pages, max_new, scale, lse, out,
                       status, ws)
-    T, hq, d = _three(q, "q")
+    shape = _three(q, "q")
+    T, hq, d = shape
     hkv = k_cache.shape[1] if k_cache.dim() == 4 else 0
+    h = _attn_heads(dtype, shape, hkv)
     c = _attn_cache(k_cache, v_cache, hkv, d, dtype, dev)
     s = _attn_seqs(off, kv_len, pages, T, dev)
     most = T if max_new is None or max_new > T else int(max_new)
-    rq = _rows(q, "q", T, hq, d, dtype, dev)
-    h = Heads(_attn_dtype(dtype), hq, hkv, d)
+    rq = _rows(q, "q", shape, dtype, dev)
     if out is None:
-        out = torch.empty((T, hq, d), dtype=dtype, device=dev)
-    ro = _rows(out, "out", T, hq, d, dtype, dev)
-    sums = torch.empty((T, hq), dtype=torch.float32, device=dev) if lse else None
+        out = _t.empty_like(q)
+    ro = _rows(out, "out", shape, dtype, dev)
+    sums = _t.empty((T, hq), dtype=_t.float32, device=dev) if lse else None
     if ws is None:
-        ws = torch.empty(_paged_ws(h, s, c, most), dtype=torch.uint8, device=dev)
+        ws = _t.empty(_paged_ws(h, s, c, most), dtype=_t.uint8, device=dev)
     elif ws.device != dev or not ws.is_contiguous():
         raise ValueError("ws must be contiguous, on %s" % dev)
     st = load().fate_attn_paged(h, s, rq, c, most, 1.0 / math.sqrt(d) if scale is None else scale, ro,
                                 sums.data_ptr() if lse else None, _attn_status(status, s.B, dev), ws.data_ptr(),
-                                ws.nbytes, _raw_stream(dev.index))
+                                ws.nbytes, _t.raw_stream(dev.index))
     if st != FATE_OK:
         raise FateError(st, "fate_attn_paged")
     return out, sums
@@ -883,8 +898,9 @@ def fate_attn_paged_ws_size(T: int, heads_q: int, k_cache, B: int, max_pages: in
     if k_cache.dim() != 4:
         raise ValueError("k_cache must be [pages, heads_kv, page_size, head_dim]")
     hkv, d = k_cache.shape[1], k_cache.shape[3]
+    _here(k_cache.device, None)
     c = _attn_cache(k_cache, k_cache, hkv, d, k_cache.dtype, k_cache.device)
-    return _paged_ws(Heads(_attn_dtype(k_cache.dtype), heads_q, hkv, d), Seqs(B, max_pages, T), c, max_new)
+    return _paged_ws(_attn_heads(k_cache.dtype, (T, heads_q, d), hkv), Seqs(B, max_pages, T), c, max_new)
 
 
 def fate_attn_prompt(q, k, v, off, scale: Optional[float] = None, lse: bool = False, out=None, status=None,
@@ -893,30 +909,27 @@ def fate_attn_prompt(q, k, v, off, scale: Optional[float] = None, lse: bool = Fa
     over k, v [T, heads_kv, head_dim] (views of one projection will do),
     sequence b in rows off[b] .. off[b + 1].  Returns (out, lse) as
     :func:`fate_attn_paged`."""
-    import torch
     dev, dtype = q.device, q.dtype
-    if _elsewhere(dev, stream):
+    if not _here(dev, stream):
         return _there(dev, stream, fate_attn_prompt, q, k, v, off, scale, lse, out, status)
-    T, hq, d = _three(q, "q")
-    hkv = _three(k, "k")[1]
+    shape, kv_shape = _three(q, "q"), _three(k, "k")
+    T, hq, d = shape
+    if kv_shape[0] != T or kv_shape[2] != d:
+        raise ValueError("k must be [%d, heads_kv, %d], got %s" % (T, d, list(kv_shape)))
+    h = _attn_heads(dtype, shape, kv_shape[1])
     s = _attn_seqs(off, None, None, T, dev)
-    rq, rk, rv = _rows(q, "q", T, hq, d, dtype, dev), _rows(k, "k", T, hkv, d, dtype, dev), _rows(v, "v", T, hkv, d, dtype, dev)
+    rq = _rows(q, "q", shape, dtype, dev)
+    rk, rv = _rows(k, "k", kv_shape, dtype, dev), _rows(v, "v", kv_shape, dtype, dev)
     if out is None:
-        out = torch.empty((T, hq, d), dtype=dtype, device=dev)
-    ro = _rows(out, "out", T, hq, d, dtype, dev)
-    sums = torch.empty((T, hq), dtype=torch.float32, device=dev) if lse else None
-    st = load().fate_attn_prompt(Heads(_attn_dtype(dtype), hq, hkv, d), s, rq, rk, rv,
-                                 1.0 / math.sqrt(d) if scale is None else scale, ro, sums.data_ptr() if lse else None,
-                                 _attn_status(status, s.B, dev), _raw_stream(dev.index))
+        out = _t.empty_like(q)
+    ro = _rows(out, "out", shape, dtype, dev)
+    sums = _t.empty((T, hq), dtype=_t.float32, device=dev) if lse else None
+    st = load().fate_attn_prompt(h, s, rq, rk, rv, 1.0 / math.sqrt(d) if scale is None else scale, ro,
+                                 sums.data_ptr() if lse else None, _attn_status(status, s.B, dev),
+                                 _t.raw_stream(dev.index))
     if st != FATE_OK:
         raise FateError(st, "fate_attn_prompt")
     return out, sums
-
-
-def _raw_stream(index: int) -> int:
-    """The current stream of a device as a hipStream_t."""
-    import torch
-    return torch._C._cuda_getCurrentRawStream(index)
 
 
 def rotation_table(positions: int, rot: int, base: float = 10000.0, device="cuda"):
