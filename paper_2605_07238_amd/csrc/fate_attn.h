@@ -86,6 +86,9 @@ struct BF16 {
     static __device__ __forceinline__ x4 read_tr(const el *p) {
         return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) x4 *)p);
     }
+    static __device__ __forceinline__ x4 read_tr_at(uint32_t at) {  // LDS byte address
+        return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) x4 *)at);
+    }
 };
 
 struct F16 {
@@ -103,6 +106,10 @@ struct F16 {
     static __device__ __forceinline__ x4 read_tr(const el *p) {
         typedef __fp16 h4 __attribute__((ext_vector_type(4)));
         return __builtin_bit_cast(x4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((__attribute__((address_space(3))) h4 *)p));
+    }
+    static __device__ __forceinline__ x4 read_tr_at(uint32_t at) {
+        typedef __fp16 h4 __attribute__((ext_vector_type(4)));
+        return __builtin_bit_cast(x4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((__attribute__((address_space(3))) h4 *)at));
     }
 };
 
@@ -128,6 +135,9 @@ __device__ __forceinline__ uint32_t only_finite(uint32_t x) {
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform64(int64_t x) {
+    return (int64_t)(((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32) | (uint32_t)uniform((int)x));
+}
 
 // One sequence as the kernels see it: its first row, tokens and keys; no
 // tokens and no keys past the last sequence and where the device arrays are

@@ -121,7 +121,7 @@ fate_status_t fate_kv_append(const fate_heads_t *heads, const fate_seqs_t *seqs,
     if (rot && (!table || reinterpret_cast<uintptr_t>(table) % 4)) return FATE_EINVAL;
     if (!q != !q_out) return FATE_EINVAL;
     if (seqs->T == 0 || seqs->B == 0) return FATE_OK;
-    if (!seqs->off || !seqs->kv_len || !seqs->pages || !good_rows(k) || !good_rows(v)) return FATE_EINVAL;
+    if (cache->n_pages < 1 || !seqs->off || !seqs->kv_len || !seqs->pages || !good_rows(k) || !good_rows(v)) return FATE_EINVAL;
     if (q && (!good_rows(q) || !good_out(q_out, heads))) return FATE_EINVAL;
     if (q && q->data == q_out->data && (q->token != q_out->token || q->head != q_out->head)) return FATE_EINVAL;
     AppendLaunch a = {};
@@ -167,7 +167,7 @@ fate_status_t fate_attn_paged(const fate_heads_t *heads, const fate_seqs_t *seqs
         return st;
     if (max_new < 0 || max_new > seqs->T) return FATE_EINVAL;
     if (seqs->T == 0 || seqs->B == 0) return FATE_OK;
-    if (!seqs->off || !seqs->kv_len || !seqs->pages) return FATE_EINVAL;
+    if (cache->n_pages < 1 || !seqs->off || !seqs->kv_len || !seqs->pages) return FATE_EINVAL;
     AttnLaunch a = {};
     if ((st = fill(a, heads, q, out, scale, d_lse, d_status)) != FATE_OK) return st;
     const PagedPlan p = plan_paged(heads, seqs, max_new);

@@ -19,32 +19,59 @@
 // the order of the keys in that product's sum is free, and v is read from LDS
 // in the order that the first product's result has (transposing reads).
 //
+// Keys and values come from memory straight into LDS (no registers hold them
+// on the way), values one tile ahead and keys two, so that a step works out the
+// next tile's scores on the matrix cores beside the softmax of this one's in
+// the vector units.  With tiles that passed through registers, one ahead, and
+// each tile's scores in its own step: 2346 us for 16384 tokens against 2034
+// (1081 TFLOP/s; a large library product reaches 1241).
+//
 // Key tiles go from the last to the first: the tiles on a row's causal edge
 // come first.  Values that a row must not see cannot be left out of a matrix
 // product by a zero weight when they are infinite or NaN (0 * inf): in the
-// tiles on an edge such values are stored as zeros, and added at the end to
-// the rows that do see them.
+// tiles on an edge such values are made zeros, and added at the end to the
+// rows that do see them.
+#include <type_traits>
+
 #include "fate_attn.h"
 
 namespace fate {
 namespace {
 
-// Rows of a tile in LDS are padded against bank conflicts: keys are read by
-// eight rows at once, 16 bytes each (rows 16 bytes apart in the banks), values
-// four rows at once, 64 bytes each (rows 64 bytes apart).  Padding, unlike
-// xored chunks, leaves every address one register plus a constant.
-constexpr int kKeyPad = 8, kValPad = 32;
+__device__ const uint4 kZeros[1] = {};  // what is loaded past a head's last dimension, and for a page that is none
+
+// Sixteen bytes a lane from memory straight to LDS: lane i's land at dst + 16 i
+// bytes.  Lane addresses are base + off bytes (base the same in all lanes), or
+// p.  The wave waits for them with dma_wait before the barrier behind which
+// the tile is read.
+__device__ __forceinline__ void dma16(const void *base, uint32_t off, uint32_t dst) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(uniform((int)dst)),
+                 "v"(off), "s"(uniform64((int64_t)base))
+                 : "memory", "m0");
+}
+__device__ __forceinline__ void dma16(const void *p, uint32_t dst) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(uniform((int)dst)), "v"(p)
+                 : "memory", "m0");
+}
+__device__ __forceinline__ void dma_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// The larger of this lane's value and that of the lane 32 away.
+__device__ __forceinline__ float both_halves_max(float x) {
+    const uint32_t y = __builtin_bit_cast(uint32_t, x);
+    const u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(y, y, false, false));
+    const uint32_t a = r[0], b = r[1];  // the lower half's values in both, the upper half's in both
+    return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+}
 
 template <class T, int D, bool PAGED>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch a) {
     typedef typename T::el el;
     typedef typename T::x4 x4;
     typedef typename T::x8 x8;
-    constexpr int BK = kKeyTile, CH = D / 8;  // keys per tile, 16-byte chunks per row
-    constexpr int NL = BK * CH / 256;         // chunks each thread loads of a key (and of a value) tile
-    constexpr int KS = D + kKeyPad, VS = D + kValPad;
-    __shared__ __align__(16) el sk[2][BK * KS];
-    __shared__ __align__(16) el sv[2][BK * VS];
+    constexpr int BK = kKeyTile, CH = D / 8;   // keys per tile, 16-byte chunks per row
+    constexpr int RI = 64 / CH, NI = 16 / RI;  // rows of one load of a wave; loads of its 16 rows of a tile
+    constexpr uint32_t kTile = BK * D * 2;     // bytes
+    __shared__ __align__(1024) char smem[4 * kTile];  // keys of two tiles, values of two
     __shared__ int odd;  // a value on the edge is infinite or NaN
 
     const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
@@ -96,117 +123,135 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch 
         for (int j = 0; j < 16; ++j) o[i][j] = 0.0f;
     float m = kLowest, l = 0.0f;
 
-    // key and value chunks of this thread: rows ld_row + i * (256 / CH), chunk ld_col
-    const int ld_row = tid / CH, ld_col = tid % CH;
-    const bool ld_in = ld_col * 8 < a.d;
-    u32x4 rk[NL], rv[NL];
-    int pg[NL];  // pages of the tile to load next
-    auto find_pages = [&](int t) {
-        if (PAGED) {
-#pragma unroll
-            for (int i = 0; i < NL; ++i) {
-                const int key = t * BK + ld_row + i * (256 / CH);
-                pg[i] = key < wg_most ? a.s.pages[p.b * a.s.pages_stride + (key >> a.c.page_shift)] : 0;
+    int ids1 = 0, ids2 = 0;
+    // Loads of a tile: wave w brings rows [16 w, 16 w + 16), RI rows a load.  A
+    // row's chunks are xored in LDS against bank conflicts: keys, read by many
+    // rows at once, by the row; values, read four rows times 64 bytes at once,
+    // in groups of four chunks.  Lane i's chunk is the one that belongs at its place.
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
+    const int lr = lane / CH, lc = lane % CH;
+    const int64_t tok_k = PAGED ? a.c.token : a.k.token, tok_v = PAGED ? a.c.token : a.v.token;
+    const char *base_k = PAGED ? a.c.k + (int64_t)hk * a.c.head * 2
+                               : a.k.data + (p.lo_row * a.k.token + (int64_t)hk * a.k.head) * 2;
+    const char *base_v = PAGED ? a.c.v + (int64_t)hk * a.c.head * 2
+                               : a.v.data + (p.lo_row * a.v.token + (int64_t)hk * a.v.head) * 2;
+    auto chunk_k = [&](int i) { return lc ^ ((i * RI + lr) & (CH < 16 ? CH - 1 : 15)); };
+    auto chunk_v = [&](int i) { return CH < 16 ? lc ^ ((((i * RI + lr) >> 1) & 1) << 2) : lc ^ (((i * RI + lr) & 3) << 2); };
+    // one page for the rows of a load, whole rows, offsets within 32 bits: addresses are a scalar and a lane's constant
+    const bool plain = a.d == D && tok_k < (1 << 24) && tok_v < (1 << 24) && (!PAGED || (1 << a.c.page_shift) >= RI);
+    const int page_mask = (1 << a.c.page_shift) - 1;
+    // lane i's entry is the page of load i (one that may be read, where none belongs); 0 where the pages are not used
+    auto pages_of = [&](int t) {
+        int id = 0;
+        if (PAGED && plain && lane < NI && t >= t_lo) {
+            const int key = t * BK + w * 16 + lane * RI;
+            if (key < wg_most) {
+                id = a.s.pages[p.b * a.s.pages_stride + (key >> a.c.page_shift)];
+                if ((uint32_t)id >= (uint32_t)a.c.n_pages) {
+                    id = 0;
+                    if (a.status) a.status[p.b] = FATE_EINVAL;
+                }
             }
         }
+        return id;
     };
-    auto load_tile = [&](int t) {
+    auto load_rows = [&](bool keys, int t, int ids, uint32_t dst) {
+        dst += w * 16 * D * 2;
+        const int key0 = t * BK + w * 16;
+        const int64_t tok = keys ? tok_k : tok_v;
+        const char *base = keys ? base_k : base_v;
+        // rows past the last key: of their page's own slots, or (prompts, page of less than a load) the last key's row
+        if (plain && (PAGED || key0 + 16 <= wg_most)) {
 #pragma unroll
-        for (int i = 0; i < NL; ++i) {
-            const int key = t * BK + ld_row + i * (256 / CH);
-            bool in = ld_in && key < wg_most;
-            rk[i] = u32x4{0, 0, 0, 0};
-            rv[i] = u32x4{0, 0, 0, 0};
+            for (int i = 0; i < NI; ++i) {
+                const int key = key0 + i * RI;
+                const char *src = PAGED ? base + (lane_of(ids, i) * a.c.page + (key & page_mask) * tok) * 2
+                                        : base + (int64_t)key * tok * 2;
+                dma16(src, (uint32_t)(lr * (int)tok * 2 + (keys ? chunk_k(i) : chunk_v(i)) * 16), dst + i * 1024);
+            }
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            const int key = min(key0 + i * RI + lr, wg_most - 1), c = keys ? chunk_k(i) : chunk_v(i);
+            const char *src = base;
+            bool in = c * 8 < a.d;
             if (PAGED) {
-                if (in && (uint32_t)pg[i] >= (uint32_t)a.c.n_pages) {
+                const int id = a.s.pages[p.b * a.s.pages_stride + (key >> a.c.page_shift)];
+                if ((uint32_t)id >= (uint32_t)a.c.n_pages) {
                     in = false;
                     if (a.status) a.status[p.b] = FATE_EINVAL;
                 }
-                const int64_t at = pg[i] * a.c.page + (int64_t)hk * a.c.head +
-                                   (key & ((1 << a.c.page_shift) - 1)) * a.c.token + ld_col * 8;
-                if (in) {
-                    rk[i] = *(const u32x4 *)((const el *)a.c.k + at);
-                    rv[i] = *(const u32x4 *)((const el *)a.c.v + at);
-                }
+                src += (id * a.c.page + (key & page_mask) * tok) * 2;
             } else {
-                const int64_t r = p.lo_row + (int64_t)key;
-                if (in) {
-                    rk[i] = *(const u32x4 *)((const el *)a.k.data + r * a.k.token + (int64_t)hk * a.k.head + ld_col * 8);
-                    rv[i] = *(const u32x4 *)((const el *)a.v.data + r * a.v.token + (int64_t)hk * a.v.head + ld_col * 8);
-                }
+                src += (int64_t)key * tok * 2;
             }
+            dma16(in ? src + c * 16 : (const char *)kZeros, dst + i * 1024);
         }
     };
     const int wg_least = max(0, min(p.L, row0 / a.G + first));  // fewest keys a row of the workgroup sees
-    auto store_tile = [&](int t, int buf) {
-        if ((t + 1) * BK > wg_least) {  // uniform: on the edge of some row
-            uint32_t bad = 0;
+
+    // LDS addresses of the products' operands (the xors as above)
+    const int r32 = lane & 31;
+    const uint32_t k0 = lds0 + r32 * D * 2 + ((half ^ (r32 & (CH < 16 ? CH - 1 : 15))) * 16);
+    const int vr = 4 * half + (lane & 15) / 4;
+    const int vx = CH < 16 ? (vr >> 1) & 1 : vr & 3;
+    const uint32_t v0 = lds0 + 2 * kTile + vr * D * 2 + vx * 64 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+    auto scores = [&](f32x16 (&s)[2], uint32_t buf) {
 #pragma unroll
-            for (int i = 0; i < NL; ++i)
-                bad |= not_finite<T>(rv[i][0]) | not_finite<T>(rv[i][1]) | not_finite<T>(rv[i][2]) | not_finite<T>(rv[i][3]);
-            if (bad) {
-                odd = 1;
+        for (int kt = 0; kt < 2; ++kt) {
 #pragma unroll
-                for (int i = 0; i < NL; ++i)
+            for (int j = 0; j < 16; ++j) s[kt][j] = 0.0f;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) rv[i][e] = only_finite<T>(rv[i][e]);
+            for (int i = 0; i < D / 16; ++i) {
+                const x8 kf = *(__attribute__((address_space(3))) const x8 *)(uintptr_t)((k0 ^ (i * 32)) + (kt * 32 * D * 2 + buf));
+                s[kt] = T::mfma32(kf, q[i], s[kt]);
             }
-        }
-#pragma unroll
-        for (int i = 0; i < NL; ++i) {
-            const int r = ld_row + i * (256 / CH);
-            *(u32x4 *)&sk[buf][r * KS + ld_col * 8] = rk[i];
-            *(u32x4 *)&sv[buf][r * VS + ld_col * 8] = rv[i];
         }
     };
 
-    int buf = 0;
-    if (tid == 0) odd = 0;
-    if (t_hi > t_lo) {
-        find_pages(t_hi - 1);
-        load_tile(t_hi - 1);
-        if (t_hi - 1 > t_lo) find_pages(t_hi - 2);
-    }
-    __syncthreads();
-    if (t_hi > t_lo) store_tile(t_hi - 1, 0);
-    __syncthreads();
-
-    for (int t = t_hi - 1; t >= t_lo; --t) {
-        if (t > t_lo) {
-            load_tile(t - 1);
-            if (t - 1 > t_lo) find_pages(t - 2);
-        }
-        if (t * BK < w_most) {  // uniform in the wave
-            f32x16 s[2];
+    // Tile t is in buffer B: its scores are in `cur` when its turn comes, and
+    // the next tile's are worked out beside its softmax.
+    auto step = [&](auto which, int t, f32x16 (&cur)[2], f32x16 (&nxt)[2]) {
+        constexpr uint32_t B = decltype(which)::value;
+        if (t - 1 >= t_lo) load_rows(false, t - 1, ids1, lds0 + (2 + (B ^ 1)) * kTile);
+        if (t - 2 >= t_lo) load_rows(true, t - 2, ids2, lds0 + B * kTile);
+        ids1 = ids2;
+        ids2 = pages_of(t - 3);
+        if ((t + 1) * BK > wg_least) {  // uniform: on the edge of some row
+            bool any = false;
 #pragma unroll
-            for (int kt = 0; kt < 2; ++kt) {
+            for (int j = 0; j < BK * CH / 256; ++j) {
+                const int c = tid + 256 * j;
+                u32x4 *at = (u32x4 *)(smem + (2 + B) * kTile + c * 16);
+                u32x4 x = *at;
+                if (not_finite<T>(x[0]) | not_finite<T>(x[1]) | not_finite<T>(x[2]) | not_finite<T>(x[3])) {
+                    any = any || t * BK + c / CH < wg_most;
 #pragma unroll
-                for (int j = 0; j < 16; ++j) s[kt][j] = 0.0f;
-                const int r = kt * 32 + (lane & 31);
-#pragma unroll
-                for (int i = 0; i < D / 16; ++i) {
-                    const x8 kf = *(const x8 *)&sk[buf][r * KS + i * 16 + half * 8];
-                    s[kt] = T::mfma32(kf, q[i], s[kt]);
+                    for (int e = 0; e < 4; ++e) x[e] = only_finite<T>(x[e]);
+                    *at = x;
                 }
             }
-            // s[kt][j]: key kt * 32 + 8 (j / 4) + 4 half + j % 4 of the tile, row lane % 32
-            const bool edge = (t + 1) * BK > w_least;
-            if (edge) {
+            if (any) odd = 1;
+            __syncthreads();
+        }
+        if (t * BK < w_most) {  // uniform in the wave
+            // cur[kt][j]: key kt * 32 + 8 (j / 4) + 4 half + j % 4 of the tile, row lane % 32
+            if ((t + 1) * BK > w_least) {
                 asm volatile("");  // a branch, not selects in every tile
                 const int left = ends - t * BK - 4 * half;
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
-                        if (kt * 32 + 8 * (j / 4) + j % 4 >= left) s[kt][j] = -INFINITY;
+                        if (kt * 32 + 8 * (j / 4) + j % 4 >= left) cur[kt][j] = -INFINITY;
             }
-            float top = s[0][0];
+            float top = cur[0][0];
 #pragma unroll
-            for (int j = 1; j < 16; ++j) top = fmaxf(top, s[0][j]);
+            for (int j = 1; j < 16; ++j) top = fmaxf(top, cur[0][j]);
 #pragma unroll
-            for (int j = 0; j < 16; ++j) top = fmaxf(top, s[1][j]);
-            top = fmaxf(top, __shfl_xor(top, 32));
-            top = fmaxf(top * a.scale_log2, kLowest);
+            for (int j = 0; j < 16; ++j) top = fmaxf(top, cur[1][j]);
+            top = fmaxf(both_halves_max(top) * a.scale_log2, kLowest);
             if (__any(top > m + 8.0f)) {
                 const float next = fmaxf(m, top), f = exp2_fast(m - next);
                 m = next;
@@ -216,31 +261,51 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch 
 #pragma unroll
                     for (int j = 0; j < 16; ++j) o[i][j] *= f;
             }
-            x8 pr[4];  // weights of keys 16 i + 8 (e / 4) + 4 half + e % 4
+            scores(nxt, (B ^ 1) * kTile);  // past the last tile: of nothing, and not used
+            x8 pr[4];                      // weights of keys 16 i + 8 (e / 4) + 4 half + e % 4
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float x = exp2_fast(__builtin_fmaf(s[i / 2][8 * (i % 2) + e], a.scale_log2, -m));
+                    const float x = exp2_fast(__builtin_fmaf(cur[i / 2][8 * (i % 2) + e], a.scale_log2, -m));
                     l += x;
                     pr[i][e] = (el)x;
                 }
             // second product: v transposed, four keys at a time, in the weights' order
-            const int vr = 4 * half + (lane & 15) / 4, vc = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int dt = 0; dt < D / 32; ++dt) {
-                    const int r1 = 16 * i + vr, r2 = r1 + 8, c = dt * 32 + vc;
-                    const x4 v1 = T::read_tr(&sv[buf][r1 * VS + c]);
-                    const x4 v2 = T::read_tr(&sv[buf][r2 * VS + c]);
+                    const uint32_t at = (v0 ^ (dt * 64)) + (i * 16 * D * 2 + B * kTile);
+                    const x4 v1 = T::read_tr_at(at);
+                    const x4 v2 = T::read_tr_at(at + 8 * D * 2);
                     const x8 vf = __builtin_shufflevector(v1, v2, 0, 1, 2, 3, 4, 5, 6, 7);
                     o[dt] = T::mfma32(vf, pr[i], o[dt]);
                 }
+        } else if (t - 1 >= t_lo && (t - 1) * BK < w_most) {
+            scores(nxt, (B ^ 1) * kTile);
         }
-        if (t > t_lo) store_tile(t - 1, buf ^ 1);
+        dma_wait();
         __syncthreads();
-        buf ^= 1;
+    };
+
+    if (tid == 0) odd = 0;
+    if (t_hi > t_lo) {
+        const int ids0 = pages_of(t_hi - 1);
+        load_rows(true, t_hi - 1, ids0, lds0);
+        load_rows(false, t_hi - 1, ids0, lds0 + 2 * kTile);
+        ids1 = pages_of(t_hi - 2);
+        if (t_hi - 2 >= t_lo) load_rows(true, t_hi - 2, ids1, lds0 + kTile);
+        ids2 = pages_of(t_hi - 3);
+    }
+    dma_wait();
+    __syncthreads();
+    f32x16 sa[2], sb[2];
+    scores(sa, 0);
+    __syncthreads();  // the first step loads over these keys
+    for (int t = t_hi - 1; t >= t_lo; t -= 2) {
+        step(std::integral_constant<uint32_t, 0>(), t, sa, sb);
+        if (t - 1 >= t_lo) step(std::integral_constant<uint32_t, 1>(), t - 1, sb, sa);
     }
 
     if (odd) {  // values that the tiles left out, for the rows that see them (any weight makes them what they are)
