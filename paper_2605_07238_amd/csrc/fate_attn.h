@@ -315,14 +315,30 @@ struct Piece {
     int split, splits, slot;  // which part of how many; its slot for partial results
 };
 
-// Sequences of a group of 64 by decreasing keys: what belongs in this lane's place.
+__device__ __forceinline__ int wave_max(int x) {  // of values of at least 0
+    x = max(x, moved<0x111, 0xF>(x));
+    x = max(x, moved<0x112, 0xF>(x));
+    x = max(x, moved<0x114, 0xF>(x));
+    x = max(x, moved<0x118, 0xF>(x));
+    x = max(x, moved<0x142, 0xA>(x));
+    x = max(x, moved<0x143, 0xC>(x));
+    return lane_of(x, 63);
+}
+
+// Sequences of a group of 64 by decreasing keys, to half an octave: what
+// belongs in this lane's place.  Few steps for the few classes that a batch
+// has (a full sort of 64 took 13 of 68 us of a call of 64 short prompts).
 __device__ __forceinline__ void sort_longest(int group, int lane, int &b, Lens &s) {
-    int rank = 0;
-    for (int i = 0; i < group; ++i) {
-        const int other = lane_of(s.L, i);
-        rank += other > s.L || (other == s.L && i < lane);
+    constexpr int kTop = 0xff << 1;  // over every class of a 31-bit length
+    const int cls = (int)(__builtin_bit_cast(uint32_t, (float)s.L) >> 22);
+    const bool in = lane < group;
+    const int hi = wave_max(in ? cls : 0), lo = kTop - wave_max(in ? kTop - cls : 0);
+    int rank = lane, before = 0;
+    for (int c = hi; c >= lo; --c) {
+        const uint64_t mine = __ballot(in && cls == c);
+        if (in && cls == c) rank = before + __popcll(mine & ((1ull << lane) - 1));
+        before += __popcll(mine);
     }
-    if (lane >= group) rank = lane;
     s.n = __builtin_amdgcn_ds_permute(rank << 2, s.n);
     s.L = __builtin_amdgcn_ds_permute(rank << 2, s.L);
     s.lo = __builtin_amdgcn_ds_permute(rank << 2, s.lo);

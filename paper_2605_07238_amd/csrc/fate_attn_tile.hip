@@ -23,8 +23,9 @@
 // on the way), values one tile ahead and keys two, so that a step works out the
 // next tile's scores on the matrix cores beside the softmax of this one's in
 // the vector units.  With tiles that passed through registers, one ahead, and
-// each tile's scores in its own step: 2346 us for 16384 tokens against 2034
-// (1081 TFLOP/s; a large library product reaches 1241).
+// each tile's scores in its own step: 2346 us for 16384 tokens against 2034.
+// Now 1971 us, 1116 TFLOP/s (a large library product reaches 1241): the matrix
+// cores are busy 58% of the cycles and the clock stands at 1.8 GHz for it.
 //
 // Key tiles go from the last to the first: the tiles on a row's causal edge
 // come first.  Values that a row must not see cannot be left out of a matrix
@@ -282,6 +283,21 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch 
                     const x8 vf = __builtin_shufflevector(v1, v2, 0, 1, 2, 3, 4, 5, 6, 7);
                     o[dt] = T::mfma32(vf, pr[i], o[dt]);
                 }
+            // the order of issue: the next scores' products, each behind its read, with the softmax
+            // between them (2067 us where the scheduler's own order took 2097), then the second product
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+            for (int g = 0; g < 2 * (D / 16); ++g) {
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // LDS read
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // matrix
+                __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);  // vector
+                __builtin_amdgcn_sched_group_barrier(0x400, 2, 0);  // exponential
+            }
+#pragma unroll
+            for (int g = 0; g < 4 * (D / 32); ++g) {
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            }
         } else if (t - 1 >= t_lo && (t - 1) * BK < w_most) {
             scores(nxt, (B ^ 1) * kTile);
         }
@@ -332,7 +348,6 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch 
         }
     }
     l += __shfl_xor(l, 32);
-    if (!live) return;
     const int64_t out_row = p.lo_row + (int64_t)tok;
     if (PAGED && piece.splits > 1) {  // a part of the keys: unscaled sums, joined by k_attn_join
         const int64_t at = ((int64_t)piece.slot * a.hkv + hk) * kTileRows + (row - row0);
@@ -342,29 +357,39 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch 
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int c = dt * 32 + 8 * j + 4 * half;
-                if (c < a.d) *(f32x4 *)(dst + c) = f32x4{o[dt][4 * j], o[dt][4 * j + 1], o[dt][4 * j + 2], o[dt][4 * j + 3]};
+                if (live && c < a.d) *(f32x4 *)(dst + c) = f32x4{o[dt][4 * j], o[dt][4 * j + 1], o[dt][4 * j + 2], o[dt][4 * j + 3]};
             }
-        if (half == 0) {
+        if (live && half == 0) {
             float *ml = a.part + 2 * (int64_t)a.pieces * a.hkv * kTileRows * a.d + at * 2;
             ml[0] = m;
             ml[1] = l;
         }
         return;
     }
+    // results to their rows: through the wave's 32 rows of LDS (chunks xored as
+    // above), so that whole rows are written, not sixteen bytes of each of 32
+    // rows at a time (373 against 340 us without the stores on a wave of prompts)
     const float inv = l != 0.0f ? 1.0f / l : 0.0f;
-    el *dst = (el *)a.out.data + out_row * a.out.token + (int64_t)qh * a.out.head;
+    char *const mine = smem + w * 32 * D * 2;
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int c = dt * 32 + 8 * j + 4 * half;
             x4 x;
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[e] = (el)(o[dt][4 * j + e] * inv);
-            if (c < a.d) *(x4 *)(dst + c) = x;
+            *(x4 *)(mine + r32 * D * 2 + ((dt * 4 + j) ^ (r32 & (CH < 16 ? CH - 1 : 15))) * 16 + half * 8) = x;
         }
-    if (half == 0 && a.lse)
+    if (half == 0 && live && a.lse)
         a.lse[out_row * a.hq + qh] = l != 0.0f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+    const int64_t at = live ? out_row * a.out.token + (int64_t)qh * a.out.head : -1;
+#pragma unroll
+    for (int i = 0; i < 32 / RI; ++i) {
+        const int r = i * RI + lr;
+        const int64_t to = (int64_t)(((uint64_t)(uint32_t)__shfl((int)(at >> 32), r) << 32) | (uint32_t)__shfl((int)at, r));
+        const x8 x = *(const x8 *)(mine + r * D * 2 + (lc ^ (r & (CH < 16 ? CH - 1 : 15))) * 16);
+        if (to >= 0 && lc * 8 < a.d) *(x8 *)((el *)a.out.data + to + lc * 8) = x;
+    }
 }
 
 template <class T, bool PAGED>
