@@ -63,6 +63,9 @@ constexpr int kTileRows = 128;  // packed rows of a workgroup of the tile kernel
 // Fewest key tiles of a share: one block of 32 keys for each wave of the
 // few-row kernel; enough work to pay for the join in the tile kernel.
 constexpr int kFewLeast = 2, kTileLeast = 4;
+// What a row tile costs in the few-row kernel beside its keys (finding it, its
+// queries, the waves' join, its results), in key tiles.
+constexpr int kUnitTiles = 2;
 
 #if defined(__HIPCC__)
 
@@ -226,9 +229,10 @@ struct Unit {
 
 // ---- calls of few rows: an axis of work, equal shares -----------------------
 // The work axis of a paged call.  Its row tiles lie on it one after the other,
-// each as long as its cost: G times the keys that its last row sees, to the
-// nearest tile, G A + (tile + 1) M for a sequence with A keys cached before the
-// call.  The axis is cut into equal shares, one workgroup each, whatever the
+// each as long as its cost: G times the keys that its last row sees, about
+// G A + (tile + 1) M for a sequence with A keys cached before the call, and
+// kUnitTiles more (without these, 37 sequences of six keys were one workgroup's,
+// one after the other: 100 us).  The axis is cut into equal shares, one workgroup each, whatever the
 // mix of lengths; a tile that a cut goes through is done in parts and joined.
 // The lengths are read on the device, where a serving step has them (and a
 // captured step finds the current ones), so that every workgroup adds them up
@@ -239,8 +243,12 @@ struct Axis {
 
 __device__ __forceinline__ int64_t tile_start(int t, int64_t GA, int M) { return t * GA + (int64_t)M * t * (t + 1) / 2; }
 
+__device__ __forceinline__ int64_t axis_keys(int n, int L, int G) {
+    return (int64_t)G * (max(0, L - n) + kUnitTiles * kKeyTile);
+}
+
 __device__ __forceinline__ int64_t seq_cost(const Lens &s, int G, int M) {
-    return tile_start(tiles_of(s.n * G, M), (int64_t)G * max(0, s.L - s.n), M);
+    return tile_start(tiles_of(s.n * G, M), axis_keys(s.n, s.L, G), M);
 }
 
 // `first`: the lane's sequence of the first 64, which most calls end with.
@@ -274,7 +282,7 @@ __device__ __forceinline__ Unit unit_at(const A &a, int M, const Lens &first, in
             u.lo_row = lane_of(s.lo, src);
             u.L = lane_of(s.L, src);
             const int64_t base = lane_of(end - mine, src), y = x - base;
-            const int64_t GA = (int64_t)a.G * max(0, u.L - u.n);
+            const int64_t GA = axis_keys(u.n, u.L, a.G);
             const int tiles = tiles_of(u.n * a.G, M);
             int t = 0;
             if (tiles > 1) {
@@ -350,11 +358,12 @@ __device__ __forceinline__ int parts_of(int L, int chunk) {
     return tiles > chunk ? (tiles + chunk - 1) / chunk : 1;
 }
 
-// Key tiles of a part.  With as many row tiles as parts wanted, only what is
-// over twice an even share is cut.  With fewer, the call's work over `pieces`
-// parts, raised by eighths, up to twice, until there are no more than `pieces`
-// parts (where the sequences fit the wave's lanes): one part over what runs at
-// once costs a whole round.
+// Key tiles of a part: an even share of the call's work over `pieces` parts.
+// So no row tile outlasts the others' work (52 chunks of 42 to 162 tokens over
+// up to 14430: 396 us when only tiles over two shares were cut, 310 so).  With
+// fewer row tiles than parts it is raised by eighths, up to twice, until there
+// are no more than `pieces` parts (where the sequences fit the wave's lanes):
+// one part over what runs at once costs a whole round.
 template <class A>
 __device__ __forceinline__ int chunk_of(const A &a, int M, const Lens &first, int lane, bool report) {
     const int nt = tiles_of(first.n * a.G, M), kt = tiles_of(first.L, kKeyTile);
@@ -367,9 +376,8 @@ __device__ __forceinline__ int chunk_of(const A &a, int M, const Lens &first, in
         sum += (int64_t)t * tiles_of(s.L, kKeyTile);
     }
     const int64_t least = max((wave_sum(sum) + a.pieces - 1) / a.pieces, (int64_t)kTileLeast);
-    const bool spare = wave_sum(units) < a.pieces;
-    int chunk = (int)min(spare ? least : 2 * least, (int64_t)0x7ffffffe);
-    if (spare && a.s.B <= 64) {
+    int chunk = (int)min(least, (int64_t)0x7ffffffe);
+    if (a.s.B <= 64 && wave_sum(units) < a.pieces) {
         for (int k = 1; k <= 8; ++k) {
             if (wave_sum(nt * (kt > chunk ? (kt + chunk - 1) / chunk : 1)) <= a.pieces) break;
             chunk = (int)min(least + (least * k + 7) / 8, (int64_t)0x7ffffffe);

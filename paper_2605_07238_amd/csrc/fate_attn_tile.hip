@@ -65,7 +65,8 @@ __device__ __forceinline__ float both_halves_max(float x) {
 }
 
 template <class T, int D, bool PAGED>
-__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch a) {
+__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch) {
+    const Args &a = launch_args();
     typedef typename T::el el;
     typedef typename T::x4 x4;
     typedef typename T::x8 x8;
@@ -172,7 +173,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch 
             }
             return;
         }
-#pragma unroll
+#pragma unroll 1
         for (int i = 0; i < NI; ++i) {
             const int key = min(key0 + i * RI + lr, wg_most - 1), c = keys ? chunk_k(i) : chunk_v(i);
             const char *src = base;
