@@ -590,7 +590,7 @@ typedef struct {
 
 /* Paged cache: element i of head h in slot s of page p is k[p * page +
  * h * head + s * token + i], values likewise in v.  Strides and alignment as
- * for rows; page_size a power of two up to 1024. */
+ * for rows, the token stride under 2^24; page_size a power of two up to 1024. */
 typedef struct {
     void *k, *v;
     int64_t page, head, token;
@@ -658,7 +658,8 @@ fate_status_t fate_attn_paged(const fate_heads_t *heads, const fate_seqs_t *seqs
                               float *d_lse, int32_t *d_status, void *d_ws, size_t ws_bytes, void *stream);
 
 /* fate_attn_prompt: causal attention of whole prompts: row i of a sequence
- * sees the sequence's rows 0 .. i of k and v.  Otherwise as fate_attn_paged.
+ * sees the sequence's rows 0 .. i of k and v (token strides under 2^24).
+ * Otherwise as fate_attn_paged.
  * Errors: EINVAL, ERANGE, EHIP. */
 fate_status_t fate_attn_prompt(const fate_heads_t *heads, const fate_seqs_t *seqs, const fate_rows_t *q,
                                const fate_rows_t *k, const fate_rows_t *v, float scale, const fate_rows_t *out,

@@ -11,6 +11,9 @@ namespace {
 using fate::AppendLaunch;
 using fate::AttnLaunch;
 
+// Token strides of keys and values: offsets of neighbouring rows are 32-bit in the kernels.
+constexpr int64_t kMaxToken = int64_t(1) << 24;
+
 bool good_rows(const fate_rows_t *r) {
     return r && r->data && reinterpret_cast<uintptr_t>(r->data) % 16 == 0 && r->token >= 0 && r->head >= 0 &&
            r->token % 8 == 0 && r->head % 8 == 0;
@@ -42,7 +45,8 @@ fate_status_t check_sizes(const fate_heads_t *h, const fate_seqs_t *s) {
 fate_status_t check_cache(const fate_heads_t *h, const fate_seqs_t *s, const fate_kv_cache_t *c) {
     if (!c || s->max_pages < 0 || s->pages_stride < 0 || c->n_pages < 0) return FATE_EINVAL;
     if (c->page_size < 1 || (c->page_size & (c->page_size - 1))) return FATE_EINVAL;
-    if (c->page_size > 1024 || (int64_t)s->max_pages * c->page_size > (int64_t(1) << 30)) return FATE_ERANGE;
+    if (c->page_size > 1024 || (int64_t)s->max_pages * c->page_size > (int64_t(1) << 30) || c->token >= kMaxToken)
+        return FATE_ERANGE;
     const fate_rows_t k = {c->k, c->token, c->head}, v = {c->v, c->token, c->head};
     if (c->n_pages > 0 && (!good_out(&k, h) || !good_out(&v, h) || c->page < h->head_dim || c->page % 8))
         return FATE_EINVAL;
@@ -199,6 +203,7 @@ fate_status_t fate_attn_prompt(const fate_heads_t *heads, const fate_seqs_t *seq
     if (st != FATE_OK || (st = check_sizes(heads, seqs)) != FATE_OK) return st;
     if (seqs->T == 0 || seqs->B == 0) return FATE_OK;
     if (!seqs->off || !good_rows(k) || !good_rows(v)) return FATE_EINVAL;
+    if (k->token >= kMaxToken || v->token >= kMaxToken) return FATE_ERANGE;
     AttnLaunch a = {};
     if ((st = fill(a, heads, q, out, scale, d_lse, d_status)) != FATE_OK) return st;
     set_seqs(a.s, seqs, nullptr);

@@ -39,20 +39,20 @@
 namespace fate {
 namespace {
 
-__device__ const uint4 kZeros[1] = {};  // what is loaded past a head's last dimension, and for a page that is none
 
 // Sixteen bytes a lane from memory straight to LDS: lane i's land at dst + 16 i
 // bytes.  Lane addresses are base + off bytes (base the same in all lanes), or
 // p.  The wave waits for them with dma_wait before the barrier behind which
-// the tile is read.
+// the tile is read.  m0 holds the place in LDS; nothing else here uses m0 (on
+// this architecture only such loads and a few global-data instructions do).
 __device__ __forceinline__ void dma16(const void *base, uint32_t off, uint32_t dst) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(uniform((int)dst)),
                  "v"(off), "s"(uniform64((int64_t)base))
-                 : "memory", "m0");
+                 : "memory");
 }
 __device__ __forceinline__ void dma16(const void *p, uint32_t dst) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(uniform((int)dst)), "v"(p)
-                 : "memory", "m0");
+                 : "memory");
 }
 __device__ __forceinline__ void dma_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
@@ -64,7 +64,11 @@ __device__ __forceinline__ float both_halves_max(float x) {
     return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
 }
 
-template <class T, int D, bool PAGED>
+// Where keys and values are: packed rows, pages of at least the rows of one
+// load, smaller pages.
+enum Source { kRows, kPages, kSmallPages };
+
+template <class T, int D, Source FROM>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch) {
     const Args &a = launch_args();
     typedef typename T::el el;
@@ -73,6 +77,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
     constexpr int BK = kKeyTile, CH = D / 8;   // keys per tile, 16-byte chunks per row
     constexpr int RI = 64 / CH, NI = 16 / RI;  // rows of one load of a wave; loads of its 16 rows of a tile
     constexpr uint32_t kTile = BK * D * 2;     // bytes
+    constexpr bool PAGED = FROM != kRows;
     __shared__ __align__(1024) char smem[4 * kTile];  // keys of two tiles, values of two
     __shared__ int odd;  // a value on the edge is infinite or NaN
 
@@ -139,13 +144,14 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
                                : a.v.data + (p.lo_row * a.v.token + (int64_t)hk * a.v.head) * 2;
     auto chunk_k = [&](int i) { return lc ^ ((i * RI + lr) & (CH < 16 ? CH - 1 : 15)); };
     auto chunk_v = [&](int i) { return CH < 16 ? lc ^ ((((i * RI + lr) >> 1) & 1) << 2) : lc ^ (((i * RI + lr) & 3) << 2); };
-    // one page for the rows of a load, whole rows, offsets within 32 bits: addresses are a scalar and a lane's constant
-    const bool plain = a.d == D && tok_k < (1 << 24) && tok_v < (1 << 24) && (!PAGED || (1 << a.c.page_shift) >= RI);
+    // lanes past a head's last dimension load nothing: their places in LDS are zero from the start
+    const bool whole = a.d == D;
     const int page_mask = (1 << a.c.page_shift) - 1;
-    // lane i's entry is the page of load i (one that may be read, where none belongs); 0 where the pages are not used
+    // Rows of one page a load: addresses are a scalar and a lane's constant (token strides are under 2^24).  Lane i's
+    // entry is the page of load i, or one that may be read where none belongs.
     auto pages_of = [&](int t) {
         int id = 0;
-        if (PAGED && plain && lane < NI && t >= t_lo) {
+        if (FROM == kPages && lane < NI && t >= t_lo) {
             const int key = t * BK + w * 16 + lane * RI;
             if (key < wg_most) {
                 id = a.s.pages[p.b * a.s.pages_stride + (key >> a.c.page_shift)];
@@ -157,38 +163,61 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
         }
         return id;
     };
-    auto load_rows = [&](bool keys, int t, int ids, uint32_t dst) {
+    auto load_rows = [&](bool keys, int t, int ids, uint32_t dst) __attribute__((always_inline)) {
         dst += w * 16 * D * 2;
         const int key0 = t * BK + w * 16;
         const int64_t tok = keys ? tok_k : tok_v;
         const char *base = keys ? base_k : base_v;
-        // rows past the last key: of their page's own slots, or (prompts, page of less than a load) the last key's row
-        if (plain && (PAGED || key0 + 16 <= wg_most)) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            const int key = key0 + i * RI, c = keys ? chunk_k(i) : chunk_v(i);
+            const char *src = PAGED ? base + (lane_of(ids, i) * a.c.page + (key & page_mask) * tok) * 2
+                                    : base + (int64_t)key * tok * 2;
+            if (whole || c * 8 < a.d) dma16(src, (uint32_t)(lr * (int)tok * 2 + c * 16), dst + i * 1024);
+        }
+    };
+    // Row by row: pages of fewer rows than a load, and the last tile of a prompt (rows past its end: the last one
+    // again; a cached sequence's are of their page's own slots).  Both tiles' pages are looked up before either's rows.
+    auto load_by_row = [&](int tv, uint32_t dst_v, int tk, uint32_t dst_k) __attribute__((always_inline)) {
+        int id[2][NI];
+        if (PAGED) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int i = 0; i < NI; ++i) {
+                    const int t = x ? tk : tv, key = max(0, min(t * BK + w * 16 + i * RI + lr, wg_most - 1));
+                    id[x][i] = a.s.pages[p.b * a.s.pages_stride + (key >> a.c.page_shift)];
+                }
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int t = x ? tk : tv;
+            if (t < t_lo) continue;
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
-                const int key = key0 + i * RI;
-                const char *src = PAGED ? base + (lane_of(ids, i) * a.c.page + (key & page_mask) * tok) * 2
-                                        : base + (int64_t)key * tok * 2;
-                dma16(src, (uint32_t)(lr * (int)tok * 2 + (keys ? chunk_k(i) : chunk_v(i)) * 16), dst + i * 1024);
-            }
-            return;
-        }
-#pragma unroll 1
-        for (int i = 0; i < NI; ++i) {
-            const int key = min(key0 + i * RI + lr, wg_most - 1), c = keys ? chunk_k(i) : chunk_v(i);
-            const char *src = base;
-            bool in = c * 8 < a.d;
-            if (PAGED) {
-                const int id = a.s.pages[p.b * a.s.pages_stride + (key >> a.c.page_shift)];
-                if ((uint32_t)id >= (uint32_t)a.c.n_pages) {
-                    in = false;
-                    if (a.status) a.status[p.b] = FATE_EINVAL;
+                const int key = min(t * BK + w * 16 + i * RI + lr, wg_most - 1), c = x ? chunk_k(i) : chunk_v(i);
+                const char *src = (x ? base_k : base_v) + c * 16;
+                bool in = c * 8 < a.d;
+                if (PAGED) {
+                    if ((uint32_t)id[x][i] >= (uint32_t)a.c.n_pages) {
+                        in = false;
+                        if (a.status) a.status[p.b] = FATE_EINVAL;
+                    }
+                    src += (id[x][i] * a.c.page + (key & page_mask) * (x ? tok_k : tok_v)) * 2;
+                } else {
+                    src += (int64_t)key * (x ? tok_k : tok_v) * 2;
                 }
-                src += (id * a.c.page + (key & page_mask) * tok) * 2;
-            } else {
-                src += (int64_t)key * tok * 2;
+                if (in) dma16(src, (x ? dst_k : dst_v) + w * 16 * D * 2 + i * 1024);
             }
-            dma16(in ? src + c * 16 : (const char *)kZeros, dst + i * 1024);
+        }
+    };
+    // values of tile tv and keys of tile tk (those there are); last: the last tile is one of them
+    auto load_tiles = [&](bool last, int tv, int ids_v, uint32_t dst_v, int tk, int ids_k, uint32_t dst_k) __attribute__((always_inline)) {
+        if (FROM == kPages || (FROM == kRows && !last)) {
+            if (tv >= t_lo) load_rows(false, tv, ids_v, dst_v);
+            if (tk >= t_lo) load_rows(true, tk, ids_k, dst_k);
+        } else {
+            load_by_row(tv, dst_v, tk, dst_k);
         }
     };
     const int wg_least = max(0, min(p.L, row0 / a.G + first));  // fewest keys a row of the workgroup sees
@@ -216,8 +245,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
     // the next tile's are worked out beside its softmax.
     auto step = [&](auto which, int t, f32x16 (&cur)[2], f32x16 (&nxt)[2]) {
         constexpr uint32_t B = decltype(which)::value;
-        if (t - 1 >= t_lo) load_rows(false, t - 1, ids1, lds0 + (2 + (B ^ 1)) * kTile);
-        if (t - 2 >= t_lo) load_rows(true, t - 2, ids2, lds0 + B * kTile);
+        load_tiles(false, t - 1, ids1, lds0 + (2 + (B ^ 1)) * kTile, t - 2, ids2, lds0 + B * kTile);
         ids1 = ids2;
         ids2 = pages_of(t - 3);
         if ((t + 1) * BK > wg_least) {  // uniform: on the edge of some row
@@ -307,12 +335,16 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
     };
 
     if (tid == 0) odd = 0;
+    if (!whole) {
+#pragma unroll
+        for (int i = 0; i < (int)(4 * kTile / 4096); ++i) *(u32x4 *)(smem + (i * 256 + tid) * 16) = u32x4{0, 0, 0, 0};
+        __syncthreads();
+    }
     if (t_hi > t_lo) {
         const int ids0 = pages_of(t_hi - 1);
-        load_rows(true, t_hi - 1, ids0, lds0);
-        load_rows(false, t_hi - 1, ids0, lds0 + 2 * kTile);
+        load_tiles(true, t_hi - 1, ids0, lds0 + 2 * kTile, t_hi - 1, ids0, lds0);
         ids1 = pages_of(t_hi - 2);
-        if (t_hi - 2 >= t_lo) load_rows(true, t_hi - 2, ids1, lds0 + kTile);
+        load_tiles(false, t_lo - 1, 0, 0, t_hi - 2, ids1, lds0 + kTile);
         ids2 = pages_of(t_hi - 3);
     }
     dma_wait();
@@ -393,21 +425,27 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
     }
 }
 
-template <class T, bool PAGED>
+template <class T, Source FROM>
 int go(const AttnLaunch &a, hipStream_t s) {
     const dim3 grid((unsigned)a.grid * (unsigned)a.hkv);
-    if (a.d <= 64) hipLaunchKernelGGL((k_attn_tile<T, 64, PAGED>), grid, dim3(256), 0, s, a);
-    else if (a.d <= 128) hipLaunchKernelGGL((k_attn_tile<T, 128, PAGED>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((k_attn_tile<T, 256, PAGED>), grid, dim3(256), 0, s, a);
+    if (a.d <= 64) hipLaunchKernelGGL((k_attn_tile<T, 64, FROM>), grid, dim3(256), 0, s, a);
+    else if (a.d <= 128) hipLaunchKernelGGL((k_attn_tile<T, 128, FROM>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((k_attn_tile<T, 256, FROM>), grid, dim3(256), 0, s, a);
     return (int)hipGetLastError();
+}
+
+template <class T>
+int go(const AttnLaunch &a, bool paged, hipStream_t s) {
+    if (!paged) return go<T, kRows>(a, s);
+    const int rows = a.d <= 64 ? 8 : a.d <= 128 ? 4 : 2;  // of a load: 1024 bytes
+    return (1 << a.c.page_shift) >= rows ? go<T, kPages>(a, s) : go<T, kSmallPages>(a, s);
 }
 
 }  // namespace
 
 int launch_attn_tile(const AttnLaunch &a, bool paged, void *stream) {
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    if (a.dtype == FATE_BF16) return paged ? go<BF16, true>(a, s) : go<BF16, false>(a, s);
-    return paged ? go<F16, true>(a, s) : go<F16, false>(a, s);
+    return a.dtype == FATE_BF16 ? go<BF16>(a, paged, s) : go<F16>(a, paged, s);
 }
 
 }  // namespace fate
