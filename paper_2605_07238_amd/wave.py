@@ -1,0 +1,222 @@
+"""A planned wave, carried out: the attention calls that one device makes for
+the stages that the planner gave it.
+
+The planner (score, top-k, planning wave, commit; :mod:`.fate`) says which
+stages run on a device next and, through its prefix slots, which prompts start
+with a prefix whose keys and values the device still holds.  :class:`DeviceCache`
+is what such a slot stands for on the device: pages of a paged cache per prefix
+group.  :func:`run_stages` takes a wave's stages through one attention layer:
+
+  stages whose prefix is cached   their own tokens are appended behind the
+                                  shared pages and attend over them
+                                  (fate_kv_append, fate_attn_paged)
+  the others                      the whole prompt is attended and stored
+                                  (fate_kv_append, fate_attn_prompt), and the
+                                  prefix's full pages become the group's
+  then all of them                answer token by token (fate_kv_append,
+                                  fate_attn_paged)
+
+``python -m paper_2605_07238_amd.wave`` plans waves on a few fork-join
+workflows, carries out each device's share and prints per wave what cached
+prefixes saved.  Weights and tokens are random.
+"""
+
+from __future__ import annotations
+
+import dataclasses
+import time
+
+import torch
+
+from . import fate, synth
+
+
+@dataclasses.dataclass
+class Layer:
+    """One attention layer: heads, the fused projection and the rotation table."""
+
+    heads_q: int
+    heads_kv: int
+    head_dim: int
+    weight: torch.Tensor  # [hidden, (heads_q + 2 heads_kv) head_dim]
+    table: torch.Tensor   # [positions, head_dim]
+
+    @classmethod
+    def random(cls, hidden=512, heads_q=32, heads_kv=8, head_dim=128, positions=8192, dtype=torch.bfloat16, seed=0):
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+        weight = torch.randn(hidden, (heads_q + 2 * heads_kv) * head_dim, generator=gen, device="cuda") / hidden ** 0.5
+        return cls(heads_q, heads_kv, head_dim, weight.to(dtype), fate.rotation_table(positions, head_dim))
+
+    def project(self, x):
+        """Fused projection [T, heads_q + 2 heads_kv, head_dim] of token rows x [T, hidden]."""
+        return (x @ self.weight).view(x.shape[0], self.heads_q + 2 * self.heads_kv, self.head_dim)
+
+
+class DeviceCache:
+    """A device's paged key-value cache, and the pages of the prefix groups it holds."""
+
+    def __init__(self, layer: Layer, pages: int, page_size: int = 16):
+        shape = (pages, layer.heads_kv, page_size, layer.head_dim)
+        self.k = torch.empty(shape, dtype=layer.weight.dtype, device="cuda")
+        self.v = torch.empty_like(self.k)
+        self.page_size = page_size
+        self.free = list(range(pages - 1, -1, -1))
+        self.groups = {}  # prefix group -> its full pages
+
+    def take(self, n: int):
+        if n > len(self.free):
+            raise RuntimeError("the cache has %d free pages, %d are needed" % (len(self.free), n))
+        return [self.free.pop() for _ in range(n)]
+
+    def release(self, pages):
+        self.free.extend(pages)
+
+
+@dataclasses.dataclass
+class Stage:
+    """A stage of a wave: its prefix group (0 = none), the tokens of the shared prefix, its own tokens."""
+
+    group: int
+    prefix: torch.Tensor  # [P, hidden] token rows
+    own: torch.Tensor     # [n, hidden], at least one
+
+
+def _ints(values):
+    return torch.tensor(values, dtype=torch.int32, device="cuda")
+
+
+class Step:
+    """The device arrays of one call over several sequences: new tokens of each, keys with them, pages."""
+
+    def __init__(self, new, keys, pages):
+        off = [0]
+        for n in new:
+            off.append(off[-1] + n)
+        width = max(len(p) for p in pages)
+        self.off, self.kv_len = _ints(off), _ints(keys)
+        self.pages = _ints([p + [-1] * (width - len(p)) for p in pages])
+        self.max_new = max(new)
+
+
+def _store(layer, cache, step, x):
+    """Project token rows, rotate queries and keys in place and store keys and values: the fused projection's queries and
+    keys lie side by side, so one call rotates both (as query heads) while it stores.  Returns (q, k, v) views."""
+    qkv, hq, hk = layer.project(x), layer.heads_q, layer.heads_q + layer.heads_kv
+    k = qkv[:, hq:hk].clone()  # the call reads the keys as they come
+    fate.fate_kv_append(qkv[:, :hk], k, qkv[:, hk:], cache.k, cache.v, step.off, step.kv_len, step.pages, layer.table,
+                        q_out=qkv[:, :hk])
+    return qkv[:, :hq], qkv[:, hq:hk], qkv[:, hk:]
+
+
+def run_stages(layer: Layer, cache: DeviceCache, stages, answer_tokens: int = 0, reuse: bool = True):
+    """Attention outputs [n, heads_q, head_dim] of each stage's own tokens and of its answer tokens (list of
+    [answer_tokens, heads_q, head_dim]), and how many prefix tokens were found in the cache.  ``reuse`` False ignores the
+    cached prefixes (and caches none)."""
+    P, hq, d = cache.page_size, layer.heads_q, layer.head_dim
+    pages, mine, keys, cached, outs = [], [], [], [], [None] * len(stages)
+    for s in stages:
+        have = cache.groups.get(s.group, []) if reuse and s.group else []
+        have = have[:s.prefix.shape[0] // P]
+        total = s.prefix.shape[0] + s.own.shape[0]
+        extra = cache.take(-(-(total + answer_tokens) // P) - len(have))
+        pages.append(have + extra)
+        mine.append(extra)
+        keys.append(total)
+        cached.append(len(have) * P)
+    for hit in (False, True):
+        of = [i for i in range(len(stages)) if (cached[i] > 0) == hit]
+        if not of:
+            continue
+        # what is not in the cache: the prefix's last tokens (those short of a full page, or all) and the stage's own
+        rows = [torch.cat([stages[i].prefix[cached[i]:], stages[i].own]) for i in of]
+        step = Step([r.shape[0] for r in rows], [keys[i] for i in of], [pages[i] for i in of])
+        q, k, v = _store(layer, cache, step, torch.cat(rows))
+        if hit:
+            out, _ = fate.fate_attn_paged(q, cache.k, cache.v, step.off, step.kv_len, step.pages, max_new=step.max_new)
+        else:
+            out, _ = fate.fate_attn_prompt(q, k, v, step.off)
+        at = 0
+        for i, r in zip(of, rows):
+            at += r.shape[0]
+            outs[i] = out[at - stages[i].own.shape[0]:at]
+    answers = torch.empty((answer_tokens, len(stages), hq, d), dtype=layer.weight.dtype, device="cuda")
+    if answer_tokens:
+        step = Step([1] * len(stages), keys, pages)
+        for t in range(answer_tokens):
+            step.kv_len += 1
+            # a model would feed the token it sampled; the layer's own output stands in for its embedding
+            x = (answers[t - 1] if t else torch.stack([o[-1] for o in outs])).flatten(1)[:, :layer.weight.shape[0]]
+            q, _, _ = _store(layer, cache, step, x.contiguous())
+            fate.fate_attn_paged(q, cache.k, cache.v, step.off, step.kv_len, step.pages, max_new=1, out=answers[t])
+    for s, p, extra, n in zip(stages, pages, mine, cached):
+        keep = []
+        if reuse and s.group and n == 0 and s.group not in cache.groups:
+            keep = p[:s.prefix.shape[0] // P]
+            if keep:
+                cache.groups[s.group] = keep
+        cache.release([x for x in extra if x not in keep])
+    return outs, list(answers.unbind(1)), sum(cached)
+
+
+class Prompts:
+    """Random token rows for stages: a prefix per group (its length from the workload), own tokens per stage."""
+
+    def __init__(self, w, hidden, dtype, own_tokens=(16, 256), seed=0):
+        self.w, self.hidden, self.dtype, self.own = w, hidden, dtype, own_tokens
+        self.gen = torch.Generator(device="cuda").manual_seed(seed)
+        self.prefixes = {}
+
+    def rows(self, n):
+        return torch.randn(n, self.hidden, generator=self.gen, device="cuda").to(self.dtype)
+
+    def stage(self, flat: int) -> Stage:
+        group = int(self.w.prefix_hash[flat])
+        if group not in self.prefixes:
+            self.prefixes[group] = self.rows(int(self.w.prefix_tokens[flat]) if group else 0)
+        lo, hi = self.own
+        n = int(torch.randint(lo, hi + 1, (1,), generator=self.gen, device="cuda"))
+        return Stage(group, self.prefixes[group], self.rows(n))
+
+
+def plan_waves(w, waves: int, k: int = 4):
+    """Waves of a plan, one after the other: lists of (flat stage id, device) of the single-device placements."""
+    packed = fate.fate_pack_dags(w)
+    state = fate.fate_pack_state(packed, w, advance=True)
+    params = fate.make_params(w)
+    for _ in range(waves):
+        F = state.counts()[0]
+        if F == 0:
+            return
+        _, idx, val = fate.fate_score_topk(packed, state, params, k)
+        sel = fate.fate_plan_wave(state, idx, val)
+        flat = fate.frontier_table(state)[0]
+        chosen = sel[:F].cpu().tolist()
+        yield [(int(flat[f]), c) for f, c in enumerate(chosen) if 0 <= c < w.D]
+        fate.fate_commit_advance(packed, state, sel)
+
+
+def main(instances: int = 4, waves: int = 12, answer_tokens: int = 4):
+    """Plan waves and carry out every device's share here, one device after the other, each with a cache of its own."""
+    w = synth.make_workload("forkjoin-4096x1000-d16", B=instances)
+    layer = Layer.random()
+    caches = [DeviceCache(layer, pages=1 << 13) for _ in range(w.D)]
+    prompts = Prompts(w, layer.weight.shape[0], layer.weight.dtype)
+    run_stages(layer, caches[0], [Stage(0, prompts.rows(0), prompts.rows(8))], 1)  # libraries load at the first call
+    for number, wave in enumerate(plan_waves(w, waves)):
+        stages = [[prompts.stage(flat) for flat, on in wave if on == d] for d in range(w.D)]
+        took, found = [], 0
+        for reuse in (False, True):
+            torch.cuda.synchronize()
+            t = time.perf_counter()
+            hits = [run_stages(layer, caches[d], stages[d], answer_tokens, reuse)[2] for d in range(w.D) if stages[d]]
+            torch.cuda.synchronize()
+            took.append((time.perf_counter() - t) * 1e3)
+            found = sum(hits)
+        flat = [s for x in stages for s in x]
+        tokens = sum(s.prefix.shape[0] + s.own.shape[0] for s in flat)
+        print("wave %d: %d stages on %d devices, %d prompt tokens, %d of them cached: %.2f ms, %.2f without the cached ones"
+              % (number, len(flat), sum(map(bool, stages)), tokens, found, took[1], took[0]), flush=True)
+
+
+if __name__ == "__main__":
+    main()
