@@ -189,7 +189,8 @@ fate_status_t fate_attn_paged(const fate_heads_t *heads, const fate_seqs_t *seqs
     // row tiles done in parts: each has a part more than it has cuts, so fewer than there are shares; of those in
     // order of length (each with over `chunk` key tiles of the sum) fewer than pieces, and no more than there are
     const int tiles = !tile ? p.pieces - 1 : p.tiles < p.pieces ? p.tiles : p.pieces;
-    if (tiles < 1) return FATE_OK;
+    // (the tile kernel makes no part of fewer than kTileLeast key tiles)
+    if (tiles < 1 || (tile && a.s.max_keys <= (int64_t)fate::kTileLeast * fate::kKeyTile)) return FATE_OK;
     // four rows a workgroup at a time, sixteen at most: as many workgroups as max_new tokens have rows for
     const int64_t most = max_new * a.G < p.rows ? max_new * a.G : p.rows;
     const int groups = most > 64 ? 8 : most > 4 ? (int)((most + 3) / 4) : 1;

@@ -284,29 +284,34 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_few(AttnLaunch) 
     }
 }
 
-// One wave per row of a row tile done in parts (a workgroup takes four rows, and every
-// `groups`-th four after them): its lanes are sixteen chunks of eight
+// One wave per row of a row tile done in parts (a workgroup takes four rows and
+// every `groups`-th four after them): its lanes are sixteen chunks of eight
 // dimensions times four parts at a time, so that a row's parts are read side
 // by side and the chain of reads stays short however many parts there are.
 template <class T, bool TILE>
-__global__ __launch_bounds__(256) void k_attn_join(AttnLaunch a, int M, int groups) {
+__global__ __launch_bounds__(256) void k_attn_join(AttnLaunch a, int M, int items, int groups) {
     typedef typename T::el el;
     typedef typename T::x8 x8;
     const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
-    const int group = blockIdx.x % groups, hk = blockIdx.x / groups % a.hkv, item = blockIdx.x / groups / a.hkv;
+    const int hk = blockIdx.x % a.hkv;
     const Lens lens = read_lens<true>(a, lane, false);
+    Axis axis = {0, 0};
+    int chunk = 0;
+    if (TILE) chunk = chunk_of(a, M, lens, lane, false);
+    else axis = axis_of(a, M, lens, lane, false);
+    for (int at = blockIdx.x / a.hkv; at < items * groups; at += gridDim.x / a.hkv) {
+    const int item = at / groups, group = at - item * groups;
     // part i lies in slot first_slot (i = 0), next_slot + step * i (others)
     Unit p;
     int splits, first_slot, next_slot, step;
     if (TILE) {
-        const Piece piece = find_piece<true, true>(a, M, lens, chunk_of(a, M, lens, lane, false), item, lane, false);
+        const Piece piece = find_piece<true, true>(a, M, lens, chunk, item, lane, false);
         p = piece.u;
         if (!p.ok) return;
         splits = piece.splits;
         first_slot = next_slot = piece.slot;
         step = 1;
     } else {
-        const Axis axis = axis_of(a, M, lens, lane, false);
         const int64_t cut = (item + 1) * axis.share;
         if (cut >= axis.total) return;
         p = unit_at(a, M, lens, cut, lane);
@@ -363,6 +368,8 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnLaunch a, int M, int grou
         if (lane == 0 && a.lse)
             a.lse[out_row * a.hq + qh] = sum != 0.0f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
     }
+    if (!TILE) return;
+    }
 }
 
 template <class T, int D>
@@ -388,12 +395,14 @@ int launch_attn_few(const AttnLaunch &a, int rows, void *stream) {
 
 int launch_attn_join(const AttnLaunch &a, int rows, int tiles, int groups, void *stream) {
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    const dim3 grid((unsigned)tiles * (unsigned)a.hkv * (unsigned)groups);
+    // row tiles: at most about 1024 workgroups, each of which goes on a grid's length further; most calls cut few
     const bool bf = a.dtype == FATE_BF16, tile = rows == kTileRows;
-    if (bf && tile) hipLaunchKernelGGL((k_attn_join<BF16, true>), grid, dim3(256), 0, s, a, rows, groups);
-    else if (bf) hipLaunchKernelGGL((k_attn_join<BF16, false>), grid, dim3(256), 0, s, a, rows, groups);
-    else if (tile) hipLaunchKernelGGL((k_attn_join<F16, true>), grid, dim3(256), 0, s, a, rows, groups);
-    else hipLaunchKernelGGL((k_attn_join<F16, false>), grid, dim3(256), 0, s, a, rows, groups);
+    const int most = 1024 / a.hkv > 0 ? 1024 / a.hkv : 1, all = tiles * groups;
+    const dim3 grid((unsigned)(tile && all > most ? most : all) * (unsigned)a.hkv);
+    if (bf && tile) hipLaunchKernelGGL((k_attn_join<BF16, true>), grid, dim3(256), 0, s, a, rows, tiles, groups);
+    else if (bf) hipLaunchKernelGGL((k_attn_join<BF16, false>), grid, dim3(256), 0, s, a, rows, tiles, groups);
+    else if (tile) hipLaunchKernelGGL((k_attn_join<F16, true>), grid, dim3(256), 0, s, a, rows, tiles, groups);
+    else hipLaunchKernelGGL((k_attn_join<F16, false>), grid, dim3(256), 0, s, a, rows, tiles, groups);
     return (int)hipGetLastError();
 }
 
