@@ -619,7 +619,10 @@ typedef struct {
  *     rotated, the rest pass; pairs are (j, j + rot/2), or (2j, 2j + 1) with
  *     interleaved = 1: (x, y) -> (x cos - y sin, y cos + x sin), in float32,
  *     rounded once.  rot = 0: no rotation, table may be null.
- *   q, q_out  both null for no queries; q_out may be q itself (same strides).
+ *   q, q_out  both null for no queries; q_out may be q itself (same strides),
+ *     and must not overlap k, v or the cache otherwise.  Every row of q is
+ *     rotated alike, so that keys laid beside the queries can come out rotated
+ *     with them (fate_attn_prompt takes rotated keys).
  * A row at a negative position (more new tokens than keys) has no place: its
  * key and value are not stored, its query comes out zero.  A position at or
  * past table_rows or max_pages * page_size, or a page outside 0 .. n_pages - 1,
@@ -651,7 +654,8 @@ fate_status_t fate_attn_paged_ws_size(const fate_heads_t *heads, const fate_seqs
  *             the kernels; a larger sequence is still computed, slower
  *   scale     positive and finite
  *   d_lse     [T][heads_q] float32, or null
- *   d_ws      fate_attn_paged_ws_size bytes, aligned to 16, contents irrelevant
+ *   d_ws      fate_attn_paged_ws_size bytes, aligned to 16, contents irrelevant;
+ *             calls that may overlap in time need one each
  * Errors: EINVAL, ERANGE, ESIZE (workspace), EHIP. */
 fate_status_t fate_attn_paged(const fate_heads_t *heads, const fate_seqs_t *seqs, const fate_rows_t *q,
                               const fate_kv_cache_t *cache, int64_t max_new, float scale, const fate_rows_t *out,

@@ -338,7 +338,7 @@ __device__ __forceinline__ int wave_max(int x) {  // of values of at least 0
 // has (a full sort of 64 took 13 of 68 us of a call of 64 short prompts).
 __device__ __forceinline__ void sort_longest(int group, int lane, int &b, Lens &s) {
     constexpr int kTop = 0xff << 1;  // over every class of a 31-bit length
-    const int cls = (int)(__builtin_bit_cast(uint32_t, (float)s.L) >> 22);
+    const int cls = (int)(__builtin_bit_cast(uint32_t, (float)max(s.L, 1)) >> 22);  // 254 to 314
     const bool in = lane < group;
     const int hi = wave_max(in ? cls : 0), lo = kTop - wave_max(in ? kTop - cls : 0);
     int rank = lane, before = 0;

@@ -34,7 +34,8 @@ struct Place {
 
 // VEC: chunks are 16-byte loads (rot / 2 a multiple of 8, or pairs
 // interleaved with rot a multiple of 8); otherwise element by element.
-template <class T, bool VEC>
+// PAST: rows are read past the last-level cache.
+template <class T, bool VEC, bool PAST>
 __global__ __launch_bounds__(256) void k_kv_append(AppendLaunch a, int per_wg, int units, int heads, uint32_t heads_inv) {
     typedef typename T::el el;
     typedef typename T::x8 x8;
@@ -110,7 +111,7 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendLaunch a, int per_wg, i
                        : (el *)(is_k ? a.ck : a.cv) + p.cache + (int64_t)kh * a.c.head;
         x8 x0 = {}, x1 = {};
         if (p.pos >= 0) {  // a query without a place comes out zero
-            if (VEC && a.past_cache) {
+            if (VEC && PAST) {
                 if (len0 > 0) x0 = __builtin_nontemporal_load((const x8 *)(src + e0));
                 if (len1 > 0) x1 = __builtin_nontemporal_load((const x8 *)(src + e1));
             } else if (VEC) {
@@ -185,8 +186,10 @@ int go(const AppendLaunch &a, hipStream_t s) {
     const unsigned grid = (unsigned)((a.s.T + per_wg - 1) / per_wg);
     // multiplier of __umulhi for x / heads: ceil(2^32 / heads), exact while x * heads < 2^32 (x < kAppendTokens * heads)
     const uint32_t inv = heads > 1 ? (uint32_t)((0x100000000ull + heads - 1) / heads) : 0u;
-    if (vec) hipLaunchKernelGGL((k_kv_append<T, true>), dim3(grid), dim3(256), 0, s, a, per_wg, units, heads, inv);
-    else hipLaunchKernelGGL((k_kv_append<T, false>), dim3(grid), dim3(256), 0, s, a, per_wg, units, heads, inv);
+    const dim3 g(grid), b(256);
+    if (vec && a.past_cache) hipLaunchKernelGGL((k_kv_append<T, true, true>), g, b, 0, s, a, per_wg, units, heads, inv);
+    else if (vec) hipLaunchKernelGGL((k_kv_append<T, true, false>), g, b, 0, s, a, per_wg, units, heads, inv);
+    else hipLaunchKernelGGL((k_kv_append<T, false, false>), g, b, 0, s, a, per_wg, units, heads, inv);
     return (int)hipGetLastError();
 }
 
