@@ -76,7 +76,6 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 struct BF16 {
     typedef __bf16 el;
-    typedef __bf16 x2 __attribute__((ext_vector_type(2)));
     typedef __bf16 x4 __attribute__((ext_vector_type(4)));
     typedef __bf16 x8 __attribute__((ext_vector_type(8)));
     static constexpr uint32_t kExp = 0x7f807f80u, kOne = 0x00800080u;  // exponent bits of a pair; their lowest
@@ -96,7 +95,6 @@ struct BF16 {
 
 struct F16 {
     typedef _Float16 el;
-    typedef _Float16 x2 __attribute__((ext_vector_type(2)));
     typedef _Float16 x4 __attribute__((ext_vector_type(4)));
     typedef _Float16 x8 __attribute__((ext_vector_type(8)));
     static constexpr uint32_t kExp = 0x7c007c00u, kOne = 0x04000400u;
@@ -108,11 +106,13 @@ struct F16 {
     }
     static __device__ __forceinline__ x4 read_tr(const el *p) {
         typedef __fp16 h4 __attribute__((ext_vector_type(4)));
-        return __builtin_bit_cast(x4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((__attribute__((address_space(3))) h4 *)p));
+        return __builtin_bit_cast(
+            x4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((__attribute__((address_space(3))) h4 *)p));
     }
     static __device__ __forceinline__ x4 read_tr_at(uint32_t at) {
         typedef __fp16 h4 __attribute__((ext_vector_type(4)));
-        return __builtin_bit_cast(x4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((__attribute__((address_space(3))) h4 *)at));
+        return __builtin_bit_cast(
+            x4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((__attribute__((address_space(3))) h4 *)at));
     }
 };
 
@@ -241,7 +241,9 @@ struct Axis {
     int64_t total, share;
 };
 
-__device__ __forceinline__ int64_t tile_start(int t, int64_t GA, int M) { return t * GA + (int64_t)M * t * (t + 1) / 2; }
+__device__ __forceinline__ int64_t tile_start(int t, int64_t GA, int M) {
+    return t * GA + (int64_t)M * t * (t + 1) / 2;
+}
 
 __device__ __forceinline__ int64_t axis_keys(int n, int L, int G) {
     return (int64_t)G * (max(0, L - n) + kUnitTiles * kKeyTile);

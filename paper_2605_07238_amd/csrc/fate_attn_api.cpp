@@ -73,7 +73,7 @@ void set_cache(fate::CacheArg &out, const fate_kv_cache_t *c) {
 // Which kernel a paged call takes, and how its key axis is shared out.
 struct PagedPlan {
     int rows;    // packed rows per workgroup: 16 or 32 (few-row kernel) or kTileRows
-    int pieces;  // shares of the work axis, or parts aimed at, per key head; twice as many slots hold all partial results
+    int pieces;  // shares of the work axis, or parts aimed at, per key head; twice as many slots hold all partials
     int tiles;   // most row tiles of the call
 };
 
@@ -118,14 +118,16 @@ fate_status_t fate_kv_append(const fate_heads_t *heads, const fate_seqs_t *seqs,
                              int32_t rot, int32_t interleaved, const fate_kv_cache_t *cache,
                              const fate_rows_t *q_out, int32_t *d_status, void *stream) {
     fate_status_t st = check_heads(heads);
-    if (st != FATE_OK || (st = check_sizes(heads, seqs)) != FATE_OK || (st = check_cache(heads, seqs, cache)) != FATE_OK)
+    if (st != FATE_OK || (st = check_sizes(heads, seqs)) != FATE_OK ||
+        (st = check_cache(heads, seqs, cache)) != FATE_OK)
         return st;
     if (rot < 0 || rot > heads->head_dim || rot % 2 || table_rows < 0 || (interleaved != 0 && interleaved != 1))
         return FATE_EINVAL;
     if (rot && (!table || reinterpret_cast<uintptr_t>(table) % 4)) return FATE_EINVAL;
     if (!q != !q_out) return FATE_EINVAL;
     if (seqs->T == 0 || seqs->B == 0) return FATE_OK;
-    if (cache->n_pages < 1 || !seqs->off || !seqs->kv_len || !seqs->pages || !good_rows(k) || !good_rows(v)) return FATE_EINVAL;
+    if (cache->n_pages < 1 || !seqs->off || !seqs->kv_len || !seqs->pages || !good_rows(k) || !good_rows(v))
+        return FATE_EINVAL;
     if (q && (!good_rows(q) || !good_out(q_out, heads))) return FATE_EINVAL;
     if (q && q->data == q_out->data && (q->token != q_out->token || q->head != q_out->head)) return FATE_EINVAL;
     AppendLaunch a = {};
@@ -156,7 +158,8 @@ fate_status_t fate_kv_append(const fate_heads_t *heads, const fate_seqs_t *seqs,
 fate_status_t fate_attn_paged_ws_size(const fate_heads_t *heads, const fate_seqs_t *seqs,
                                       const fate_kv_cache_t *cache, int64_t max_new, size_t *bytes) {
     fate_status_t st = check_heads(heads);
-    if (st != FATE_OK || (st = check_sizes(heads, seqs)) != FATE_OK || (st = check_cache(heads, seqs, cache)) != FATE_OK)
+    if (st != FATE_OK || (st = check_sizes(heads, seqs)) != FATE_OK ||
+        (st = check_cache(heads, seqs, cache)) != FATE_OK)
         return st;
     if (!bytes || max_new < 0 || max_new > seqs->T) return FATE_EINVAL;
     *bytes = seqs->T == 0 || seqs->B == 0 ? 0 : ws_of(heads, plan_paged(heads, seqs, max_new));
@@ -167,7 +170,8 @@ fate_status_t fate_attn_paged(const fate_heads_t *heads, const fate_seqs_t *seqs
                               const fate_kv_cache_t *cache, int64_t max_new, float scale, const fate_rows_t *out,
                               float *d_lse, int32_t *d_status, void *d_ws, size_t ws_bytes, void *stream) {
     fate_status_t st = check_heads(heads);
-    if (st != FATE_OK || (st = check_sizes(heads, seqs)) != FATE_OK || (st = check_cache(heads, seqs, cache)) != FATE_OK)
+    if (st != FATE_OK || (st = check_sizes(heads, seqs)) != FATE_OK ||
+        (st = check_cache(heads, seqs, cache)) != FATE_OK)
         return st;
     if (max_new < 0 || max_new > seqs->T) return FATE_EINVAL;
     if (seqs->T == 0 || seqs->B == 0) return FATE_OK;

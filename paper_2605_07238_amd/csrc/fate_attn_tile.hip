@@ -39,11 +39,12 @@
 namespace fate {
 namespace {
 
-
 // Sixteen bytes a lane from memory straight to LDS: lane i's land at dst + 16 i
 // bytes.  Lane addresses are base + off bytes (base the same in all lanes), or
-// p.  The wave waits for them with dma_wait before the barrier behind which
-// the tile is read.  m0 holds the place in LDS; nothing else here uses m0 (on
+// p.  Nothing arrives in a register, so nothing that the compiler placed can be
+// overwritten on the way; the wave waits for them with dma_wait before the
+// barrier behind which the tile is read, and the waits that the compiler counts
+// for its own loads can only wait for more.  m0 holds the place in LDS; nothing else here uses m0 (on
 // this architecture only such loads and a few global-data instructions do).
 __device__ __forceinline__ void dma16(const void *base, uint32_t off, uint32_t dst) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(uniform((int)dst)),
@@ -70,7 +71,7 @@ enum Source { kRows, kPages, kSmallPages };
 
 template <class T, int D, Source FROM>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch) {
-    const Args &a = launch_args();
+    const Args &a = launch_args();  // read where they lie: copied, they go to scratch and what uses them after them
     typedef typename T::el el;
     typedef typename T::x4 x4;
     typedef typename T::x8 x8;
@@ -113,7 +114,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
     // queries: the first product's second operand, column = row of the tile
     x8 q[D / 16];
     {
-        const el *src = (const el *)a.q.data + (p.lo_row + (int64_t)tok) * a.q.token + (int64_t)qh * a.q.head + half * 8;
+        const el *src =
+            (const el *)a.q.data + (p.lo_row + (int64_t)tok) * a.q.token + (int64_t)qh * a.q.head + half * 8;
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) {
             const bool in = live && s * 16 + half * 8 < a.d;
@@ -143,7 +145,10 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
     const char *base_v = PAGED ? a.c.v + (int64_t)hk * a.c.head * 2
                                : a.v.data + (p.lo_row * a.v.token + (int64_t)hk * a.v.head) * 2;
     auto chunk_k = [&](int i) { return lc ^ ((i * RI + lr) & (CH < 16 ? CH - 1 : 15)); };
-    auto chunk_v = [&](int i) { return CH < 16 ? lc ^ ((((i * RI + lr) >> 1) & 1) << 2) : lc ^ (((i * RI + lr) & 3) << 2); };
+    auto chunk_v = [&](int i) {
+        const int r = i * RI + lr;
+        return CH < 16 ? lc ^ (((r >> 1) & 1) << 2) : lc ^ ((r & 3) << 2);
+    };
     // lanes past a head's last dimension load nothing: their places in LDS are zero from the start
     const bool whole = a.d == D;
     const int page_mask = (1 << a.c.page_shift) - 1;
@@ -212,7 +217,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
         }
     };
     // values of tile tv and keys of tile tk (those there are); last: the last tile is one of them
-    auto load_tiles = [&](bool last, int tv, int ids_v, uint32_t dst_v, int tk, int ids_k, uint32_t dst_k) __attribute__((always_inline)) {
+    auto load_tiles = [&](bool last, int tv, int ids_v, uint32_t dst_v, int tk, int ids_k,
+                          uint32_t dst_k) __attribute__((always_inline)) {
         if (FROM == kPages || (FROM == kRows && !last)) {
             if (tv >= t_lo) load_rows(false, tv, ids_v, dst_v);
             if (tk >= t_lo) load_rows(true, tk, ids_k, dst_k);
@@ -235,7 +241,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
             for (int j = 0; j < 16; ++j) s[kt][j] = 0.0f;
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) {
-                const x8 kf = *(__attribute__((address_space(3))) const x8 *)(uintptr_t)((k0 ^ (i * 32)) + (kt * 32 * D * 2 + buf));
+                const uint32_t at = (k0 ^ (i * 32)) + (kt * 32 * D * 2 + buf);
+                const x8 kf = *(__attribute__((address_space(3))) const x8 *)(uintptr_t)at;
                 s[kt] = T::mfma32(kf, q[i], s[kt]);
             }
         }
@@ -376,7 +383,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
                     x4 x = {};
                     if (c < a.d) x = *(const x4 *)(src + c);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) o[dt][4 * j + e] += __builtin_isfinite((float)x[e]) ? 0.0f : (float)x[e];
+                    for (int e = 0; e < 4; ++e)
+                        o[dt][4 * j + e] += __builtin_isfinite((float)x[e]) ? 0.0f : (float)x[e];
                 }
         }
     }
@@ -390,7 +398,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int c = dt * 32 + 8 * j + 4 * half;
-                if (live && c < a.d) *(f32x4 *)(dst + c) = f32x4{o[dt][4 * j], o[dt][4 * j + 1], o[dt][4 * j + 2], o[dt][4 * j + 3]};
+                if (live && c < a.d)
+                    *(f32x4 *)(dst + c) = f32x4{o[dt][4 * j], o[dt][4 * j + 1], o[dt][4 * j + 2], o[dt][4 * j + 3]};
             }
         if (live && half == 0) {
             float *ml = a.part + 2 * (int64_t)a.pieces * a.hkv * kTileRows * a.d + at * 2;
@@ -419,7 +428,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
 #pragma unroll
     for (int i = 0; i < 32 / RI; ++i) {
         const int r = i * RI + lr;
-        const int64_t to = (int64_t)(((uint64_t)(uint32_t)__shfl((int)(at >> 32), r) << 32) | (uint32_t)__shfl((int)at, r));
+        const int64_t to =
+            (int64_t)(((uint64_t)(uint32_t)__shfl((int)(at >> 32), r) << 32) | (uint32_t)__shfl((int)at, r));
         const x8 x = *(const x8 *)(mine + r * D * 2 + (lc ^ (r & (CH < 16 ? CH - 1 : 15))) * 16);
         if (to >= 0 && lc * 8 < a.d) *(x8 *)((el *)a.out.data + to + lc * 8) = x;
     }

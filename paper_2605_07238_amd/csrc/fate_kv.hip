@@ -36,7 +36,8 @@ struct Place {
 // interleaved with rot a multiple of 8); otherwise element by element.
 // PAST: rows are read past the last-level cache.
 template <class T, bool VEC, bool PAST>
-__global__ __launch_bounds__(256) void k_kv_append(AppendLaunch a, int per_wg, int units, int heads, uint32_t heads_inv) {
+__global__ __launch_bounds__(256) void k_kv_append(AppendLaunch a, int per_wg, int units, int heads,
+                                                   uint32_t heads_inv) {
     typedef typename T::el el;
     typedef typename T::x8 x8;
     __shared__ Place place[kAppendTokens];
