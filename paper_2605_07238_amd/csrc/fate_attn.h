@@ -266,18 +266,26 @@ __device__ __forceinline__ Axis axis_of(const A &a, int M, const Lens &first, in
     return x;
 }
 
+// Where the search for a place of the axis stands: a group of 64 sequences and
+// the cost before it.  Places only grow, so it never goes back.
+struct Search {
+    int at;
+    int64_t before;
+};
+
 // The row tile at place x < total of the axis.
 template <class A>
-__device__ __forceinline__ Unit unit_at(const A &a, int M, const Lens &first, int64_t x, int lane) {
+__device__ __forceinline__ Unit unit_at(const A &a, int M, const Lens &first, int64_t x, int lane, Search &from) {
     Unit u;
     u.ok = false;
-    int64_t before = 0;
-    for (int at = 0; at < a.s.B; at += 64) {
+    int64_t before = from.before;
+    for (int at = from.at; at < a.s.B; at += 64) {
         const Lens s = at == 0 ? first : read_lens<true>(a, at + lane, false);
         const int64_t mine = seq_cost(s, a.G, M);
         const int64_t end = before + wave_scan_add(mine);
         const uint64_t has = __ballot(x < end);
         if (has) {
+            from = {at, before};
             const int src = uniform(__ffsll((unsigned long long)has) - 1);
             u.b = at + src;
             u.n = lane_of(s.n, src);
@@ -392,18 +400,31 @@ __device__ __forceinline__ int chunk_of(const A &a, int M, const Lens &first, in
 // those done in parts.  Row tiles of a sequence go from the last, which sees
 // the most keys, to the first.
 template <bool PAGED, bool JOIN, class A>
-__device__ __forceinline__ Piece find_piece(const A &a, int M, const Lens &first, int chunk, int item, int lane,
-                                            bool report) {
+__device__ __forceinline__ Piece find_piece(const A &a, int M, const Lens &first, int chunk, int item, int lane) {
     Piece p;
     p.u.ok = false;
     int items = 0, slots = 0;  // before this group of 64 sequences
     for (int at = 0; at < a.s.B; at += 64) {
         int b = at + lane;
-        Lens s = at == 0 ? first : read_lens<PAGED>(a, b, report);
+        Lens s = at == 0 ? first : read_lens<PAGED>(a, b, false);
+        int nt = tiles_of(s.n * a.G, M), sp = PAGED ? parts_of(s.L, chunk) : 1;
+        int mine = JOIN ? (sp > 1 ? nt : 0) : nt * sp, my_slots = sp > 1 ? nt * sp : 0;
         const int group = min(64, a.s.B - at);
-        if (group > 1) sort_longest(group, lane, b, s);
-        const int nt = tiles_of(s.n * a.G, M), sp = PAGED ? parts_of(s.L, chunk) : 1;
-        const int mine = JOIN ? (sp > 1 ? nt : 0) : nt * sp, my_slots = sp > 1 ? nt * sp : 0;
+        if (at + 64 < a.s.B) {  // not in this group: its sums alone
+            const int all = wave_sum(mine);
+            if (item >= items + all) {
+                items += all;
+                if (PAGED) slots += wave_sum(my_slots);
+                continue;
+            }
+        }
+        if (group > 1) {
+            sort_longest(group, lane, b, s);
+            nt = tiles_of(s.n * a.G, M);
+            sp = PAGED ? parts_of(s.L, chunk) : 1;
+            mine = JOIN ? (sp > 1 ? nt : 0) : nt * sp;
+            my_slots = sp > 1 ? nt * sp : 0;
+        }
         const int end = items + wave_scan_add(mine);
         const int slot_end = PAGED ? slots + wave_scan_add(my_slots) : 0;
         const uint64_t has = __ballot(item < end);
@@ -422,8 +443,7 @@ __device__ __forceinline__ Piece find_piece(const A &a, int M, const Lens &first
             p.u.ok = true;
             return p;
         }
-        items = lane_of(end, 63);
-        slots = lane_of(slot_end, 63);
+        return p;  // past the last
     }
     return p;
 }

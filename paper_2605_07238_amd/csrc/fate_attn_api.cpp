@@ -101,6 +101,7 @@ fate_status_t fill(AttnLaunch &a, const fate_heads_t *h, const fate_rows_t *q, c
     a.lse = d_lse;
     a.status = d_status;
     a.scale_log2 = (float)((double)scale * 1.4426950408889634);
+    if (!std::isfinite(a.scale_log2)) return FATE_EINVAL;
     a.hq = h->heads_q;
     a.hkv = h->heads_kv;
     a.G = h->heads_q / h->heads_kv;

@@ -47,10 +47,11 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_few(AttnLaunch) 
         from = piece * axis.share;
         to = min(from + axis.share, axis.total);
     }
+    Search search = {0, 0};
     for (int64_t x = from; x < to;) {  // the row tiles of this share
         const Args &a = launch_args();
         const int tid = fresh(threadIdx.x), lane = tid & 63, w = uniform(tid >> 6);
-        const Unit p = unit_at(a, M, lens, x, lane);
+        const Unit p = unit_at(a, M, lens, x, lane, search);
         if (!p.ok) return;
         x = p.start + p.cost;
 
@@ -308,16 +309,17 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnLaunch a, int M, int item
         Unit p;
         int splits, first_slot, next_slot, step;
         if (TILE) {
-            const Piece piece = find_piece<true, true>(a, M, lens, chunk, item, lane, false);
+            const Piece piece = find_piece<true, true>(a, M, lens, chunk, item, lane);
             p = piece.u;
             if (!p.ok) return;
             splits = piece.splits;
             first_slot = next_slot = piece.slot;
             step = 1;
         } else {
+            Search search = {0, 0};
             const int64_t cut = (item + 1) * axis.share;
             if (cut >= axis.total) return;
-            p = unit_at(a, M, lens, cut, lane);
+            p = unit_at(a, M, lens, cut, lane, search);
             if (!p.ok || p.start >= cut || p.start < cut - axis.share) return;  // this row tile's first cut alone
             splits = uniform((int)((p.start + p.cost - 1) / axis.share)) - item + 1;
             first_slot = 2 * item + (p.start > cut - axis.share);  // behind the share's first where the tile begins within
