@@ -13,6 +13,7 @@ the host-only :func:`fate_layout_dags` / :func:`fate_layout_state`.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import math
 import os
 from typing import Optional
@@ -874,7 +875,7 @@ def fate_attn_paged(q, k_cache, v_cache, off, kv_len, pages, max_new: Optional[i
     ro = _rows(out, "out", shape, dtype, dev)
     sums = _t.empty((T, hq), dtype=_t.float32, device=dev) if lse else None
     if ws is None:
-        ws = _t.empty(_paged_ws(h, s, c, most), dtype=_t.uint8, device=dev)
+        ws = _t.empty(_ws_bytes(h.dtype, hq, hkv, d, most), dtype=_t.uint8, device=dev)
     elif ws.device != dev or not ws.is_contiguous():
         raise ValueError("ws must be contiguous, on %s" % dev)
     st = load().fate_attn_paged(h, s, rq, c, most, 1.0 / math.sqrt(d) if scale is None else scale, ro,
@@ -885,9 +886,12 @@ def fate_attn_paged(q, k_cache, v_cache, off, kv_len, pages, max_new: Optional[i
     return out, sums
 
 
-def _paged_ws(h, s, c, most) -> int:
+@functools.lru_cache(maxsize=1024)
+def _ws_bytes(dtype: int, heads_q: int, heads_kv: int, head_dim: int, max_new: int) -> int:
+    """The library's workspace size, which depends on these alone (a call that is empty needs none)."""
     nbytes = C.c_size_t(0)
-    st = load().fate_attn_paged_ws_size(h, s, c, most, nbytes)
+    st = load().fate_attn_paged_ws_size(Heads(dtype, heads_q, heads_kv, head_dim), Seqs(1, 0, max(1, max_new)),
+                                        KvCache(page_size=1), max_new, nbytes)
     if st != FATE_OK:
         raise FateError(st, "fate_attn_paged_ws_size")
     return nbytes.value
@@ -899,8 +903,11 @@ def fate_attn_paged_ws_size(T: int, heads_q: int, k_cache, B: int, max_pages: in
         raise ValueError("k_cache must be [pages, heads_kv, page_size, head_dim]")
     hkv, d = k_cache.shape[1], k_cache.shape[3]
     _here(k_cache.device, None)
-    c = _attn_cache(k_cache, k_cache, hkv, d, k_cache.dtype, k_cache.device)
-    return _paged_ws(_attn_heads(k_cache.dtype, (T, heads_q, d), hkv), Seqs(B, max_pages, T), c, max_new)
+    if T == 0 or B == 0:
+        return 0
+    if max_new > T:
+        raise ValueError("max_new is at most T")
+    return _ws_bytes(_attn_heads(k_cache.dtype, (T, heads_q, d), hkv).dtype, heads_q, hkv, d, max_new)
 
 
 def fate_attn_prompt(q, k, v, off, scale: Optional[float] = None, lse: bool = False, out=None, status=None,
