@@ -701,7 +701,7 @@ class _Torch:
         import torch
         self.types = {torch.bfloat16: FATE_BF16, torch.float16: FATE_F16}
         self.int32, self.float32, self.uint8 = torch.int32, torch.float32, torch.uint8
-        self.empty, self.empty_like = torch.empty, torch.empty_like
+        self.empty, self.empty_like, self.Tensor = torch.empty, torch.empty_like, torch.Tensor
         self.device, self.stream = torch.cuda.device, torch.cuda.stream
         self.current_device = torch.cuda.current_device
         self.raw_stream = torch._C._cuda_getCurrentRawStream
@@ -723,12 +723,16 @@ def _here(device, stream) -> bool:
 
 def _there(device, stream, call, *args, **more):
     """A call made with the tensors' device and `stream` current: what it takes from the allocator then belongs to the
-    stream its kernels run on, and is handed out again only behind them."""
+    stream its kernels run on, and is handed out again only behind them; so are the caller's tensors, of whatever stream."""
     with _t.device(device):
         if stream is None:
             return call(*args, **more)
         with _t.stream(stream):
-            return call(*args, **more)
+            result = call(*args, **more)
+        for x in args:
+            if isinstance(x, _t.Tensor):
+                x.record_stream(stream)
+        return result
 
 
 def _rows(t, name, shape, dtype, device):
@@ -878,7 +882,7 @@ def fate_attn_paged(q, k_cache, v_cache, off, kv_len, pages, max_new: Optional[i
         ws = _t.empty(_ws_bytes(h.dtype, hq, hkv, d, most), dtype=_t.uint8, device=dev)
     elif ws.device != dev or not ws.is_contiguous():
         raise ValueError("ws must be contiguous, on %s" % dev)
-    st = load().fate_attn_paged(h, s, rq, c, most, 1.0 / math.sqrt(d) if scale is None else scale, ro,
+    st = load().fate_attn_paged(h, s, rq, c, most, 1.0 / math.sqrt(d or 1) if scale is None else scale, ro,
                                 sums.data_ptr() if lse else None, _attn_status(status, s.B, dev), ws.data_ptr(),
                                 ws.nbytes, _t.raw_stream(dev.index))
     if st != FATE_OK:
@@ -931,7 +935,7 @@ def fate_attn_prompt(q, k, v, off, scale: Optional[float] = None, lse: bool = Fa
         out = _t.empty_like(q)
     ro = _rows(out, "out", shape, dtype, dev)
     sums = _t.empty((T, hq), dtype=_t.float32, device=dev) if lse else None
-    st = load().fate_attn_prompt(h, s, rq, rk, rv, 1.0 / math.sqrt(d) if scale is None else scale, ro,
+    st = load().fate_attn_prompt(h, s, rq, rk, rv, 1.0 / math.sqrt(d or 1) if scale is None else scale, ro,
                                  sums.data_ptr() if lse else None, _attn_status(status, s.B, dev),
                                  _t.raw_stream(dev.index))
     if st != FATE_OK:
