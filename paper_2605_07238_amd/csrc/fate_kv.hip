@@ -71,7 +71,7 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendLaunch a, int per_wg, i
                         }
                     }
                     if (bad && a.status) a.status[b] = FATE_EINVAL;
-                } else if (a.status) {
+                } else if (a.status && (lo < 0 || hi < lo || (int64_t)hi > a.s.T)) {  // not a row before the sequence
                     a.status[b] = FATE_EINVAL;
                 }
             }
