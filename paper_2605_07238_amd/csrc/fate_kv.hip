@@ -45,34 +45,38 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendLaunch a, int per_wg, i
     const int64_t t0 = (int64_t)blockIdx.x * per_wg;
     const int toks = (int)min((int64_t)per_wg, a.s.T - t0);
     if (tid < 64) {
-        int b = 0;  // lane i: sequences that end at or before token t0 + i
-        for (int at = 0; at < a.s.B; at += 64) {
-            const int64_t end = at + tid < a.s.B ? (int64_t)a.s.off[at + tid + 1] : a.s.T + 1;
+        // Lane i: the sequence that holds token t0 + i.  The first workgroup goes through all sequences, which reports
+        // those that are out of range; the others stop at their last token's.
+        int b = 0, n = 0, L = -1, row = 0, found = 0;
+        for (int at = 0; at < a.s.B && (found < toks || blockIdx.x == 0); at += 64) {
+            const Lens s = read_lens<true>(a, at + tid, blockIdx.x == 0);
             for (int i = 0; i < toks; ++i) {
-                const int n = __popcll(__ballot(end <= t0 + i));
-                b += tid == i ? n : 0;
+                const uint64_t has = __ballot(t0 + i >= s.lo && t0 + i - s.lo < s.n);
+                if (!has) continue;
+                const int src = uniform(__ffsll((unsigned long long)has) - 1);
+                const int its_n = lane_of(s.n, src), its_L = lane_of(s.L, src), its_lo = lane_of(s.lo, src);
+                if (tid == i) {
+                    b = at + src;
+                    n = its_n;
+                    L = its_L;
+                    row = (int)(t0 + i - its_lo);
+                }
+                ++found;
             }
         }
         if (tid < toks) {
-            const int64_t t = t0 + tid;
             Place p = {-1, -2};  // in no sequence: not touched
-            if (b < a.s.B) {
-                const int lo = a.s.off[b], hi = a.s.off[b + 1], n = a.s.kv_len[b];
-                if (lo >= 0 && (int64_t)lo <= t && t < (int64_t)hi && (int64_t)hi <= a.s.T) {
-                    bool bad = n < 0 || (int64_t)n > a.s.max_keys;
-                    const int64_t pos = (int64_t)n - (hi - lo) + (t - lo);
-                    p.pos = -1;
-                    if (!bad && pos >= 0) {
-                        const int page = a.s.pages[b * a.s.pages_stride + (pos >> a.c.page_shift)];
-                        bad = page < 0 || page >= a.c.n_pages || (a.rot && pos >= a.table_rows);
-                        if (!bad) {
-                            p.pos = (int)pos;
-                            p.cache = page * a.c.page + (pos & ((1 << a.c.page_shift) - 1)) * a.c.token;
-                        }
+            if (L >= 0) {
+                const int64_t pos = (int64_t)L - n + row;
+                p.pos = -1;
+                if (pos >= 0) {
+                    const int page = a.s.pages[b * a.s.pages_stride + (pos >> a.c.page_shift)];
+                    if (page < 0 || page >= a.c.n_pages || (a.rot && pos >= a.table_rows)) {
+                        if (a.status) a.status[b] = FATE_EINVAL;
+                    } else {
+                        p.pos = (int)pos;
+                        p.cache = page * a.c.page + (pos & ((1 << a.c.page_shift) - 1)) * a.c.token;
                     }
-                    if (bad && a.status) a.status[b] = FATE_EINVAL;
-                } else if (a.status && (lo < 0 || hi < lo || (int64_t)hi > a.s.T)) {  // not a row before the sequence
-                    a.status[b] = FATE_EINVAL;
                 }
             }
             place[tid] = p;

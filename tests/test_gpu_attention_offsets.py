@@ -1,4 +1,5 @@
-"""Offsets of a call's sequences: rows outside every sequence are no error of any."""
+"""Offsets and lengths of a call's sequences: rows outside every sequence are no error of any, and what is an error in the
+attention calls is one in the append."""
 
 import math
 
@@ -10,6 +11,7 @@ from paper_2605_07238_amd import fate
 from test_gpu_attention import HF
 
 pytestmark = pytest.mark.gpu
+BAD = fate.FATE_EINVAL
 
 
 def ints(x):
@@ -47,3 +49,21 @@ def test_append_leaves_rows_outside_sequences_alone(new, kv, lead, trail):
     assert torch.equal(got_q[lead:lead + T], want_q)
     assert (got_q[:lead] == 3).all() and (got_q[lead + T:] == 3).all()
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("what", [-1, 33])
+@pytest.mark.parametrize("B", [3, 90])
+def test_append_reports_what_attention_reports(what, B):
+    """A length out of range on a sequence with no tokens in the call."""
+    off, kv, pages = [0] + [2] * (B - 1) + [5], [2] + [0] * (B - 2) + [7], [[0, 1]] + [[-1, -1]] * (B - 2) + [[2, 3]]
+    kv[B - 2] = what
+    qkv = torch.randn(5, 8, 64, device="cuda").half()
+    cache = empty_cache()
+    want = [BAD if b == B - 2 else 0 for b in range(B)]
+    q = torch.empty(5, 4, 64, dtype=HF, device="cuda")
+    assert append(qkv, 4, 2, cache, off, kv, pages, q) == want
+    assert torch.equal(cache[1][0, :, :2], qkv[:2, 6:].transpose(0, 1)) and cache[1][2, :, 4:7].any()
+    for most in (3, None):
+        status = torch.zeros(B, dtype=torch.int32, device="cuda")
+        fate.fate_attn_paged(q, *cache, ints(off), ints(kv), ints(pages), max_new=most, status=status)
+        assert status.tolist() == want
