@@ -598,8 +598,10 @@ typedef struct {
 } fate_kv_cache_t;
 
 /* The sequences of a call: B of them over T packed token rows.
- *   off[B+1]     sequence b's rows are off[b] .. off[b+1] (ascending); rows
- *                outside every sequence are neither read nor written
+ *   off[B+1]     sequence b's rows are off[b] .. off[b+1], within 0 .. T; rows
+ *                outside every sequence are neither read nor written.  A
+ *                sequence whose end lies before its start, or whose start
+ *                below any earlier entry, is in error
  *   kv_len[B]    keys of sequence b in the cache, the call's own tokens
  *                included: row i of n stands at position kv_len[b] - n + i
  *   pages        sequence b's page for positions [j * page_size,

@@ -142,32 +142,6 @@ __device__ __forceinline__ int64_t uniform64(int64_t x) {
     return (int64_t)(((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32) | (uint32_t)uniform((int)x));
 }
 
-// One sequence as the kernels see it: its first row, tokens and keys; no
-// tokens and no keys past the last sequence and where the device arrays are
-// out of range (`report`: say so in the status).
-struct Lens {
-    int lo, n, L;
-};
-
-template <bool PAGED, class A>
-__device__ __forceinline__ Lens read_lens(const A &a, int b, bool report) {
-    Lens s = {0, 0, 0};
-    if (b >= a.s.B) return s;
-    s.lo = a.s.off[b];
-    const int hi = a.s.off[b + 1];
-    bool bad = s.lo < 0 || hi < s.lo || (int64_t)hi > a.s.T;
-    s.n = s.L = hi - s.lo;
-    if (PAGED) {
-        s.L = a.s.kv_len[b];
-        bad = bad || s.L < 0 || (int64_t)s.L > a.s.max_keys;
-    }
-    if (bad) {
-        s.lo = s.n = s.L = 0;
-        if (report && a.status) a.status[b] = FATE_EINVAL;
-    }
-    return s;
-}
-
 // Inclusive sums over the 64 lanes (all active): shifts right by 1, 2, 4 and 8
 // within each row of 16 lanes, then the last lanes of rows 0 and 2, and of row
 // 1, to the rows after them, in DPP moves as wave_exscan_u32.
@@ -191,6 +165,16 @@ __device__ __forceinline__ I wave_scan_add(I x) {
     return x;
 }
 
+__device__ __forceinline__ int wave_scan_max(int x) {  // of values of at least 0, as which others count
+    x = max(x, moved<0x111, 0xF>(x));
+    x = max(x, moved<0x112, 0xF>(x));
+    x = max(x, moved<0x114, 0xF>(x));
+    x = max(x, moved<0x118, 0xF>(x));
+    x = max(x, moved<0x142, 0xA>(x));
+    x = max(x, moved<0x143, 0xC>(x));
+    return x;
+}
+
 // Lane i's value, i the same in all lanes.
 __device__ __forceinline__ int lane_of(int x, int i) { return __builtin_amdgcn_readlane(x, i); }
 __device__ __forceinline__ int64_t lane_of(int64_t x, int i) {
@@ -199,6 +183,40 @@ __device__ __forceinline__ int64_t lane_of(int64_t x, int i) {
 
 template <class I>
 __device__ __forceinline__ I wave_sum(I x) { return lane_of(wave_scan_add(x), 63); }
+
+// One sequence as the kernels see it: its first row, tokens and keys; no
+// tokens and no keys past the last sequence and where the device arrays are
+// out of range (`report`: say so in the status).
+struct Lens {
+    int lo, n, L;
+};
+
+// Lane i: sequence at + i.  `reach`: the largest offset before the group, 0
+// for the first; on return, before the next one.  A sequence that starts below
+// an earlier offset is out of range: those that are not hold different rows,
+// in order, so that the tiles that the host counts from T and B are enough.
+template <bool PAGED, class A>
+__device__ __forceinline__ Lens read_lens(const A &a, int at, int lane, int &reach, bool report) {
+    Lens s = {0, 0, 0};
+    const int b = at + lane;
+    int hi = 0;
+    if (b < a.s.B) {
+        s.lo = a.s.off[b];
+        hi = a.s.off[b + 1];
+        if (PAGED) s.L = a.s.kv_len[b];
+    }
+    const int before = max(reach, wave_scan_max(s.lo));  // its own offset among them
+    reach = lane_of(before, 63);
+    s.n = hi - s.lo;
+    bool bad = s.lo < before || hi < s.lo || (int64_t)hi > a.s.T;
+    if (PAGED) bad = bad || s.L < 0 || (int64_t)s.L > a.s.max_keys;
+    else s.L = s.n;
+    if (bad || b >= a.s.B) {
+        s.lo = s.n = s.L = 0;
+        if (report && a.status && b < a.s.B) a.status[b] = FATE_EINVAL;
+    }
+    return s;
+}
 
 // The launch arguments where the kernel finds them.  A workgroup that walks
 // through several pieces of work reads them again for each (and its thread
@@ -215,6 +233,28 @@ __device__ __forceinline__ const Args &launch_args() {
 __device__ __forceinline__ int fresh(int x) {
     asm volatile("" : "+v"(x));
     return x;
+}
+
+// The first 64 sequences, and the largest offset before the next.
+struct Group {
+    Lens lens;
+    int reach;
+};
+
+template <bool PAGED, class A>
+__device__ __forceinline__ Group first_group(const A &a, int lane, bool report) {
+    Group g;
+    g.reach = 0;
+    g.lens = read_lens<PAGED>(a, 0, lane, g.reach, report);
+    return g;
+}
+
+// The group from sequence `at` on: `first`, or read; `reach` as in read_lens.
+template <bool PAGED, class A>
+__device__ __forceinline__ Lens group_at(const A &a, int at, int lane, const Group &first, int &reach) {
+    if (at > 0) return read_lens<PAGED>(a, at, lane, reach, false);
+    reach = first.reach;
+    return first.lens;
 }
 
 __device__ __forceinline__ int tiles_of(int n, int tile) { return (int)(((int64_t)n + tile - 1) / tile); }
@@ -253,11 +293,12 @@ __device__ __forceinline__ int64_t seq_cost(const Lens &s, int G, int M) {
     return tile_start(tiles_of(s.n * G, M), axis_keys(s.n, s.L, G), M);
 }
 
-// `first`: the lane's sequence of the first 64, which most calls end with.
+// `first`: the first 64 sequences, which most calls end with.
 template <class A>
-__device__ __forceinline__ Axis axis_of(const A &a, int M, const Lens &first, int lane, bool report) {
-    int64_t sum = seq_cost(first, a.G, M);
-    for (int at = 64; at < a.s.B; at += 64) sum += seq_cost(read_lens<true>(a, at + lane, report), a.G, M);
+__device__ __forceinline__ Axis axis_of(const A &a, int M, const Group &first, int lane, bool report) {
+    int64_t sum = seq_cost(first.lens, a.G, M);
+    int reach = first.reach;
+    for (int at = 64; at < a.s.B; at += 64) sum += seq_cost(read_lens<true>(a, at, lane, reach, report), a.G, M);
     Axis x;
     x.total = wave_sum(sum);
     const int64_t least_share = (int64_t)kFewLeast * kKeyTile * a.G;
@@ -266,26 +307,28 @@ __device__ __forceinline__ Axis axis_of(const A &a, int M, const Lens &first, in
     return x;
 }
 
-// Where the search for a place of the axis stands: a group of 64 sequences and
-// the cost before it.  Places only grow, so it never goes back.
+// Where the search for a place of the axis stands: a group of 64 sequences,
+// the largest offset and the cost before it.  Places only grow, so it never goes back.
 struct Search {
-    int at;
+    int at, reach;
     int64_t before;
 };
 
 // The row tile at place x < total of the axis.
 template <class A>
-__device__ __forceinline__ Unit unit_at(const A &a, int M, const Lens &first, int64_t x, int lane, Search &from) {
+__device__ __forceinline__ Unit unit_at(const A &a, int M, const Group &first, int64_t x, int lane, Search &from) {
     Unit u;
     u.ok = false;
     int64_t before = from.before;
+    int reach = from.reach;
     for (int at = from.at; at < a.s.B; at += 64) {
-        const Lens s = at == 0 ? first : read_lens<true>(a, at + lane, false);
+        const int reach0 = reach;
+        const Lens s = group_at<true>(a, at, lane, first, reach);
         const int64_t mine = seq_cost(s, a.G, M);
         const int64_t end = before + wave_scan_add(mine);
         const uint64_t has = __ballot(x < end);
         if (has) {
-            from = {at, before};
+            from = {at, reach0, before};
             const int src = uniform(__ffsll((unsigned long long)has) - 1);
             u.b = at + src;
             u.n = lane_of(s.n, src);
@@ -333,15 +376,7 @@ struct Piece {
     int split, splits, slot;  // which part of how many; its slot for partial results
 };
 
-__device__ __forceinline__ int wave_max(int x) {  // of values of at least 0
-    x = max(x, moved<0x111, 0xF>(x));
-    x = max(x, moved<0x112, 0xF>(x));
-    x = max(x, moved<0x114, 0xF>(x));
-    x = max(x, moved<0x118, 0xF>(x));
-    x = max(x, moved<0x142, 0xA>(x));
-    x = max(x, moved<0x143, 0xC>(x));
-    return lane_of(x, 63);
-}
+__device__ __forceinline__ int wave_max(int x) { return lane_of(wave_scan_max(x), 63); }
 
 // Sequences of a group of 64 by decreasing keys, to half an octave: what
 // belongs in this lane's place.  Few steps for the few classes that a batch
@@ -375,12 +410,12 @@ __device__ __forceinline__ int parts_of(int L, int chunk) {
 // are no more than `pieces` parts (where the sequences fit the wave's lanes):
 // one part over what runs at once costs a whole round.
 template <class A>
-__device__ __forceinline__ int chunk_of(const A &a, int M, const Lens &first, int lane, bool report) {
-    const int nt = tiles_of(first.n * a.G, M), kt = tiles_of(first.L, kKeyTile);
+__device__ __forceinline__ int chunk_of(const A &a, int M, const Group &first, int lane, bool report) {
+    const int nt = tiles_of(first.lens.n * a.G, M), kt = tiles_of(first.lens.L, kKeyTile);
     int64_t sum = (int64_t)nt * kt;
-    int units = nt;
+    int units = nt, reach = first.reach;
     for (int at = 64; at < a.s.B; at += 64) {
-        const Lens s = read_lens<true>(a, at + lane, report);
+        const Lens s = read_lens<true>(a, at, lane, reach, report);
         const int t = tiles_of(s.n * a.G, M);
         units += t;
         sum += (int64_t)t * tiles_of(s.L, kKeyTile);
@@ -400,13 +435,13 @@ __device__ __forceinline__ int chunk_of(const A &a, int M, const Lens &first, in
 // those done in parts.  Row tiles of a sequence go from the last, which sees
 // the most keys, to the first.
 template <bool PAGED, bool JOIN, class A>
-__device__ __forceinline__ Piece find_piece(const A &a, int M, const Lens &first, int chunk, int item, int lane) {
+__device__ __forceinline__ Piece find_piece(const A &a, int M, const Group &first, int chunk, int item, int lane) {
     Piece p;
     p.u.ok = false;
-    int items = 0, slots = 0;  // before this group of 64 sequences
+    int items = 0, slots = 0, reach = 0;  // before this group of 64 sequences
     for (int at = 0; at < a.s.B; at += 64) {
         int b = at + lane;
-        Lens s = at == 0 ? first : read_lens<PAGED>(a, b, false);
+        Lens s = group_at<PAGED>(a, at, lane, first, reach);
         int nt = tiles_of(s.n * a.G, M), sp = PAGED ? parts_of(s.L, chunk) : 1;
         int mine = JOIN ? (sp > 1 ? nt : 0) : nt * sp, my_slots = sp > 1 ? nt * sp : 0;
         const int group = min(64, a.s.B - at);

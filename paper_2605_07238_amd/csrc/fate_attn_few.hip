@@ -37,17 +37,17 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_few(AttnLaunch) 
 
     int hk, piece;
     int64_t from, to;
-    Lens lens;
+    Group lens;
     {
         const Args &a = launch_args();
         const bool report = blockIdx.x == 0 && threadIdx.x < 64;
         hk = blockIdx.x % a.hkv, piece = blockIdx.x / a.hkv;
-        lens = read_lens<true>(a, threadIdx.x & 63, report);
+        lens = first_group<true>(a, threadIdx.x & 63, report);
         const Axis axis = axis_of(a, M, lens, threadIdx.x & 63, report);
         from = piece * axis.share;
         to = min(from + axis.share, axis.total);
     }
-    Search search = {0, 0};
+    Search search = {0, 0, 0};
     for (int64_t x = from; x < to;) {  // the row tiles of this share
         const Args &a = launch_args();
         const int tid = fresh(threadIdx.x), lane = tid & 63, w = uniform(tid >> 6);
@@ -298,7 +298,7 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnLaunch a, int M, int item
     typedef typename T::x8 x8;
     const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
     const int hk = blockIdx.x % a.hkv;
-    const Lens lens = read_lens<true>(a, lane, false);
+    const Group lens = first_group<true>(a, lane, false);
     Axis axis = {0, 0};
     int chunk = 0;
     if (TILE) chunk = chunk_of(a, M, lens, lane, false);
@@ -316,7 +316,7 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnLaunch a, int M, int item
             first_slot = next_slot = piece.slot;
             step = 1;
         } else {
-            Search search = {0, 0};
+            Search search = {0, 0, 0};
             const int64_t cut = (item + 1) * axis.share;
             if (cut >= axis.total) return;
             p = unit_at(a, M, lens, cut, lane, search);

@@ -85,9 +85,11 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
     const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
     const int hk = blockIdx.x % a.hkv, item = blockIdx.x / a.hkv;
     const bool report = blockIdx.x == 0 && tid < 64;
-    const Lens lens = read_lens<PAGED>(a, lane, report);
-    if (!PAGED && report)
-        for (int at = 64; at < a.s.B; at += 64) read_lens<false>(a, at + lane, true);
+    const Group lens = first_group<PAGED>(a, lane, report);
+    if (!PAGED && report) {
+        int reach = lens.reach;
+        for (int at = 64; at < a.s.B; at += 64) read_lens<false>(a, at, lane, reach, true);
+    }
     const int chunk = PAGED ? chunk_of(a, kTileRows, lens, lane, report) : 0x7fffffff;
     const Piece piece = find_piece<PAGED, false>(a, kTileRows, lens, chunk, item, lane);
     const Unit &p = piece.u;

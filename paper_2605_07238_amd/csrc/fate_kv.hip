@@ -47,9 +47,9 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendLaunch a, int per_wg, i
     if (tid < 64) {
         // Lane i: the sequence that holds token t0 + i.  The first workgroup goes through all sequences, which reports
         // those that are out of range; the others stop at their last token's.
-        int b = 0, n = 0, L = -1, row = 0, found = 0;
+        int b = 0, n = 0, L = -1, row = 0, found = 0, reach = 0;
         for (int at = 0; at < a.s.B && (found < toks || blockIdx.x == 0); at += 64) {
-            const Lens s = read_lens<true>(a, at + tid, blockIdx.x == 0);
+            const Lens s = read_lens<true>(a, at, tid, reach, blockIdx.x == 0);
             for (int i = 0; i < toks; ++i) {
                 const uint64_t has = __ballot(t0 + i >= s.lo && t0 + i - s.lo < s.n);
                 if (!has) continue;

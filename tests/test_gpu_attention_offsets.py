@@ -1,5 +1,5 @@
-"""Offsets and lengths of a call's sequences: rows outside every sequence are no error of any, and what is an error in the
-attention calls is one in the append."""
+"""Offsets that are sound but leave rows outside, and offsets, lengths and empty sequences that are not sound: all calls
+that read them hold the same ones for errors, report each, and leave the others' results as they are."""
 
 import math
 
@@ -7,8 +7,9 @@ import numpy as np
 import pytest
 import torch
 
+import attn_oracle as ao
 from paper_2605_07238_amd import fate
-from test_gpu_attention import HF
+from test_gpu_attention import BF, HF, compare, run_paged
 
 pytestmark = pytest.mark.gpu
 BAD = fate.FATE_EINVAL
@@ -67,3 +68,65 @@ def test_append_reports_what_attention_reports(what, B):
         status = torch.zeros(B, dtype=torch.int32, device="cuda")
         fate.fate_attn_paged(q, *cache, ints(off), ints(kv), ints(pages), max_new=most, status=status)
         assert status.tolist() == want
+
+
+def ascending_up_to(off, T):
+    """The sequences that are sound: within the rows, not descending, not from below an earlier entry."""
+    return [0 <= off[b] <= off[b + 1] <= T and off[b] >= max(off[:b + 1]) for b in range(len(off) - 1)]
+
+
+OFFSETS = {
+    "down": ([0, 10, 5, 20], 20),
+    "twice the same rows": ([0, 20, 0, 20], 20),
+    "first": ([6, 2, 20], 20),
+    "past the end": ([0, 8, 40, 12, 20], 20),
+    "negative": ([-3, 4, 20], 20),
+    "down in a later group": ([*range(70), 20, *range(71, 131)], 130),
+    "over a whole group": ([0, 1, 2, 100, *range(4, 131)], 130),
+    "many times the same rows": ([0, 130] * 60, 130),
+}
+
+
+@pytest.mark.parametrize("name", sorted(OFFSETS))
+def test_offsets_that_descend(name):
+    off, T = OFFSETS[name]
+    B = len(off) - 1
+    good = ascending_up_to(off, T)
+    want = [0 if x else BAD for x in good]
+    kv = [140 if b % 3 else 131 for b in range(B)]
+    P, need = 16, 9
+    gen = torch.Generator().manual_seed(B)
+    rng = np.random.default_rng(B)
+    pages = rng.permutation(B * need).reshape(B, need).astype(np.int32)
+    q = torch.randn(T, 4, 64, generator=gen).to(BF)
+    kc, vc = (torch.randn(B * need, 2, P, 64, generator=gen).to(BF) for _ in range(2))
+    for most in (4, None):
+        status = torch.zeros(B, dtype=torch.int32, device="cuda")
+        out, lse = run_paged(q, kc, vc, np.array(off, np.int32), np.array(kv, np.int32), pages, max_new=most, scale=0.125,
+                             status=status)
+        assert status.tolist() == want
+        for b in range(B):
+            if good[b] and off[b] < off[b + 1]:
+                lo, hi = off[b], off[b + 1]
+                ref = ao.paged(q[lo:hi], kc, vc, [0, hi - lo], [kv[b]], [pages[b].tolist()], 0.125)
+                compare(out[lo:hi], lse[lo:hi], ref)
+    k, v = (torch.randn(T, 2, 64, generator=gen).to(BF) for _ in range(2))
+    status.zero_()
+    out, lse = fate.fate_attn_prompt(q.cuda(), k.cuda(), v.cuda(), ints(off), lse=True, status=status)
+    assert status.tolist() == want
+    for b in range(B):
+        if good[b] and off[b] < off[b + 1]:
+            rows = slice(off[b], off[b + 1])
+            compare(out[rows], lse[rows], ao.prompt(q[rows], k[rows], v[rows], [0, off[b + 1] - off[b]], 0.125))
+    # append: rows of sound sequences are stored, no others are
+    nk, nv = torch.zeros_like(kc).cuda(), torch.zeros_like(vc).cuda()
+    status.zero_()
+    fate.fate_kv_append(None, k.cuda(), v.cuda(), nk, nv, ints(off), ints(kv), torch.from_numpy(pages).cuda(), status=status)
+    assert status.tolist() == want
+    ek, ev = torch.zeros_like(kc), torch.zeros_like(vc)
+    for b in range(B):
+        if good[b]:
+            for t in range(off[b], off[b + 1]):
+                pos = kv[b] - off[b + 1] + t
+                ek[pages[b, pos // P], :, pos % P], ev[pages[b, pos // P], :, pos % P] = k[t], v[t]
+    assert torch.equal(nk.cpu(), ek) and torch.equal(nv.cpu(), ev)
