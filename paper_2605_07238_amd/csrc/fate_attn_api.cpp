@@ -35,8 +35,8 @@ fate_status_t check_heads(const fate_heads_t *h) {
 
 fate_status_t check_sizes(const fate_heads_t *h, const fate_seqs_t *s) {
     if (!s || s->B < 0 || s->T < 0) return FATE_EINVAL;
-    // packed rows and piece numbers are 32-bit in the kernels
-    if (s->T * (int64_t)(h->heads_q + 2 * h->heads_kv) >= (int64_t(1) << 31) || s->T >= (int64_t(1) << 31) ||
+    // packed rows and piece numbers are 32-bit in the kernels (T first: the product is then within 64 bits)
+    if (s->T >= (int64_t(1) << 31) || s->T * (int64_t)(h->heads_q + 2 * h->heads_kv) >= (int64_t(1) << 31) ||
         s->B > (1 << 24))
         return FATE_ERANGE;
     return FATE_OK;
