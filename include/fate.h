@@ -631,7 +631,7 @@ typedef struct {
  * is an error of its sequence.  No page that is written may be another
  * sequence's in the same call.
  * Errors: EINVAL (null pointers, types, strides, alignment, rot, heads),
- * ERANGE (heads, head_dim, page_size, T * heads at 2^31), EHIP. */
+ * ERANGE (heads, head_dim, page_size, T * heads at 2^31, T past 2^26 - 4), EHIP. */
 fate_status_t fate_kv_append(const fate_heads_t *heads, const fate_seqs_t *seqs, const fate_rows_t *q,
                              const fate_rows_t *k, const fate_rows_t *v, const float *table, int64_t table_rows,
                              int32_t rot, int32_t interleaved, const fate_kv_cache_t *cache,
@@ -658,7 +658,9 @@ fate_status_t fate_attn_paged_ws_size(const fate_heads_t *heads, const fate_seqs
  *   d_lse     [T][heads_q] float32, or null
  *   d_ws      fate_attn_paged_ws_size bytes, aligned to 16, contents irrelevant;
  *             calls that may overlap in time need one each
- * Errors: EINVAL, ERANGE, ESIZE (workspace), EHIP. */
+ * Errors: EINVAL, ERANGE (sizes as above; a launch of 2^24 workgroups or more,
+ * as T heads_q / 128 + min(B, T) heads_kv of them for other than few tokens a
+ * sequence), ESIZE (workspace), EHIP. */
 fate_status_t fate_attn_paged(const fate_heads_t *heads, const fate_seqs_t *seqs, const fate_rows_t *q,
                               const fate_kv_cache_t *cache, int64_t max_new, float scale, const fate_rows_t *out,
                               float *d_lse, int32_t *d_status, void *d_ws, size_t ws_bytes, void *stream);

@@ -13,6 +13,8 @@ using fate::AttnLaunch;
 
 // Token strides of keys and values: offsets of neighbouring rows are 32-bit in the kernels.
 constexpr int64_t kMaxToken = int64_t(1) << 24;
+// A launch takes fewer than 2^32 threads: workgroups of 256.
+constexpr int64_t kMaxGrid = (int64_t(1) << 24) - 1;
 
 bool good_rows(const fate_rows_t *r) {
     return r && r->data && reinterpret_cast<uintptr_t>(r->data) % 16 == 0 && r->token >= 0 && r->head >= 0 &&
@@ -75,7 +77,13 @@ struct PagedPlan {
     int rows;    // packed rows per workgroup: 16 or 32 (few-row kernel) or kTileRows
     int pieces;  // shares of the work axis, or parts aimed at, per key head; twice as many slots hold all partials
     int tiles;   // most row tiles of the call
+    int grid;    // workgroups per key head
 };
+
+// Most row tiles of T tokens in B sequences.
+int tiles_of(const fate_seqs_t *s, int64_t G, int rows) {
+    return (int)(s->T * G / rows + (s->B < s->T ? s->B : s->T));
+}
 
 PagedPlan plan_paged(const fate_heads_t *h, const fate_seqs_t *s, int64_t max_new) {
     const int64_t G = h->heads_q / h->heads_kv, packed = max_new * G, few = h->head_dim <= 128 ? 32 : 16;
@@ -84,7 +92,8 @@ PagedPlan plan_paged(const fate_heads_t *h, const fate_seqs_t *s, int64_t max_ne
     // what the chip runs at once: two workgroups a compute unit, one of head sizes over 128
     const int target = h->head_dim <= 128 ? 512 : 256;
     p.pieces = target / h->heads_kv > 0 ? target / h->heads_kv : 1;
-    p.tiles = (int)(s->T * G / p.rows + (s->B < s->T ? s->B : s->T));
+    p.tiles = tiles_of(s, G, p.rows);
+    p.grid = p.rows == fate::kTileRows ? p.pieces + p.tiles : p.pieces;
     return p;
 }
 
@@ -127,6 +136,7 @@ fate_status_t fate_kv_append(const fate_heads_t *heads, const fate_seqs_t *seqs,
     if (rot && (!table || reinterpret_cast<uintptr_t>(table) % 4)) return FATE_EINVAL;
     if (!q != !q_out) return FATE_EINVAL;
     if (seqs->T == 0 || seqs->B == 0) return FATE_OK;
+    if (fate::append_grid(seqs->T) > kMaxGrid) return FATE_ERANGE;
     if (cache->n_pages < 1 || !seqs->off || !seqs->kv_len || !seqs->pages || !good_rows(k) || !good_rows(v))
         return FATE_EINVAL;
     if (q && (!good_rows(q) || !good_out(q_out, heads))) return FATE_EINVAL;
@@ -163,7 +173,13 @@ fate_status_t fate_attn_paged_ws_size(const fate_heads_t *heads, const fate_seqs
         (st = check_cache(heads, seqs, cache)) != FATE_OK)
         return st;
     if (!bytes || max_new < 0 || max_new > seqs->T) return FATE_EINVAL;
-    *bytes = seqs->T == 0 || seqs->B == 0 ? 0 : ws_of(heads, plan_paged(heads, seqs, max_new));
+    if (seqs->T == 0 || seqs->B == 0) {
+        *bytes = 0;
+        return FATE_OK;
+    }
+    const PagedPlan p = plan_paged(heads, seqs, max_new);
+    if ((int64_t)p.grid * heads->heads_kv > kMaxGrid) return FATE_ERANGE;
+    *bytes = ws_of(heads, p);
     return FATE_OK;
 }
 
@@ -177,9 +193,10 @@ fate_status_t fate_attn_paged(const fate_heads_t *heads, const fate_seqs_t *seqs
     if (max_new < 0 || max_new > seqs->T) return FATE_EINVAL;
     if (seqs->T == 0 || seqs->B == 0) return FATE_OK;
     if (cache->n_pages < 1 || !seqs->off || !seqs->kv_len || !seqs->pages) return FATE_EINVAL;
+    const PagedPlan p = plan_paged(heads, seqs, max_new);
+    if ((int64_t)p.grid * heads->heads_kv > kMaxGrid) return FATE_ERANGE;
     AttnLaunch a = {};
     if ((st = fill(a, heads, q, out, scale, d_lse, d_status)) != FATE_OK) return st;
-    const PagedPlan p = plan_paged(heads, seqs, max_new);
     if (!d_ws || reinterpret_cast<uintptr_t>(d_ws) % 16) return FATE_EINVAL;
     if (ws_bytes < ws_of(heads, p)) return FATE_ESIZE;
     set_seqs(a.s, seqs, cache);
@@ -187,9 +204,8 @@ fate_status_t fate_attn_paged(const fate_heads_t *heads, const fate_seqs_t *seqs
     a.part = static_cast<float *>(d_ws);
     a.pieces = p.pieces;
     const bool tile = p.rows == fate::kTileRows;
-    a.grid = tile ? p.pieces + p.tiles : p.pieces;
-    const int rc = tile ? fate::launch_attn_tile(a, true, stream)
-                                             : fate::launch_attn_few(a, p.rows, stream);
+    a.grid = p.grid;
+    const int rc = tile ? fate::launch_attn_tile(a, true, stream) : fate::launch_attn_few(a, p.rows, stream);
     if (rc) return FATE_EHIP;
     // row tiles done in parts: each has a part more than it has cuts, so fewer than there are shares; of those in
     // order of length (each with over `chunk` key tiles of the sum) fewer than pieces, and no more than there are
@@ -208,6 +224,9 @@ fate_status_t fate_attn_prompt(const fate_heads_t *heads, const fate_seqs_t *seq
     fate_status_t st = check_heads(heads);
     if (st != FATE_OK || (st = check_sizes(heads, seqs)) != FATE_OK) return st;
     if (seqs->T == 0 || seqs->B == 0) return FATE_OK;
+    const int64_t G = heads->heads_q / heads->heads_kv;
+    const int grid = tiles_of(seqs, G, fate::kTileRows);
+    if ((int64_t)grid * heads->heads_kv > kMaxGrid) return FATE_ERANGE;
     if (!seqs->off || !good_rows(k) || !good_rows(v)) return FATE_EINVAL;
     if (k->token >= kMaxToken || v->token >= kMaxToken) return FATE_ERANGE;
     AttnLaunch a = {};
@@ -215,7 +234,7 @@ fate_status_t fate_attn_prompt(const fate_heads_t *heads, const fate_seqs_t *seq
     set_seqs(a.s, seqs, nullptr);
     a.k = rows(k);
     a.v = rows(v);
-    a.grid = (int)(seqs->T * a.G / fate::kTileRows + (seqs->B < seqs->T ? seqs->B : seqs->T));
+    a.grid = grid;
     return fate::launch_attn_tile(a, false, stream) == 0 ? FATE_OK : FATE_EHIP;
 }
 

@@ -23,10 +23,6 @@
 namespace fate {
 namespace {
 
-// Tokens of a workgroup in large calls: its first wave finds them all at once.
-// Four: 98.8 us for 18261 tokens (48 heads of 128); eight 112, sixteen 109.
-constexpr int kAppendTokens = 4;
-
 struct Place {
     int64_t cache;  // element of the token's slot, head 0; negative: no place
     int pos;        // position; negative: no place
@@ -187,8 +183,8 @@ int go(const AppendLaunch &a, hipStream_t s) {
     // units of a head: rotated pairs of chunks, then the rest in sixteens
     const int units = a.interleaved ? (a.d + 15) / 16 : (half + 7) / 8 + (a.d - a.rot + 15) / 16;
     const bool vec = a.interleaved ? a.rot % 8 == 0 : half % 8 == 0;
-    const int per_wg = a.s.T <= 1024 ? 1 : kAppendTokens;
-    const unsigned grid = (unsigned)((a.s.T + per_wg - 1) / per_wg);
+    const int per_wg = append_tokens(a.s.T);
+    const unsigned grid = (unsigned)append_grid(a.s.T);
     // multiplier of __umulhi for x / heads: ceil(2^32 / heads), exact while x * heads < 2^32 (x < kAppendTokens * heads)
     const uint32_t inv = heads > 1 ? (uint32_t)((0x100000000ull + heads - 1) / heads) : 0u;
     const dim3 g(grid), b(256);
