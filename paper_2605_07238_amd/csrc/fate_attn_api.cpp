@@ -86,7 +86,8 @@ int tiles_of(const fate_seqs_t *s, int64_t G, int rows) {
 }
 
 PagedPlan plan_paged(const fate_heads_t *h, const fate_seqs_t *s, int64_t max_new) {
-    const int64_t G = h->heads_q / h->heads_kv, packed = max_new * G, few = h->head_dim <= 128 ? 32 : 16;
+    // a token's rows at least: the work axis of the few-row kernel is within 64 bits where they are 32 or fewer
+    const int64_t G = h->heads_q / h->heads_kv, packed = (max_new > 1 ? max_new : 1) * G, few = h->head_dim <= 128 ? 32 : 16;
     PagedPlan p;
     p.rows = packed <= 16 ? 16 : packed <= few ? 32 : fate::kTileRows;
     // what the chip runs at once: two workgroups a compute unit, one of head sizes over 128

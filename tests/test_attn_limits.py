@@ -39,3 +39,15 @@ def test_grids_past_the_launch():
     # few new tokens a sequence: as many workgroups as run at once, whatever the batch
     assert paged(h=h, s=seqs(B=600_000, T=600_000), most=1, q=none) == EINVAL
     assert fate.load().fate_attn_paged_ws_size(h, seqs(B=600_000, T=600_000), cache(), 1, n) == 0
+
+
+@pytest.mark.parametrize("heads_q,heads_kv,head_dim", [(64, 1, 64), (256, 1, 256), (32, 1, 128), (8, 8, 64), (20, 1, 256)])
+def test_no_bound_below_one_token(heads_q, heads_kv, head_dim):
+    """A call that has tokens is planned for one a sequence at least: the axis of work of few rows, its length in 64 bits,
+    holds 2^31 rows over 2^30 keys only where a token has no more packed rows than a workgroup."""
+    h = heads(heads_q=heads_q, heads_kv=heads_kv, head_dim=head_dim)
+    c = cache(page=1024 * head_dim, head=16 * head_dim, token=head_dim)
+    n = [C.c_size_t(0) for _ in range(2)]
+    for most in (0, 1):
+        assert fate.load().fate_attn_paged_ws_size(h, seqs(T=1000), c, most, n[most]) == 0
+    assert n[0].value == n[1].value > 0
