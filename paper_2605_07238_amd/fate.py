@@ -705,6 +705,7 @@ class _Torch:
         self.device, self.stream = torch.cuda.device, torch.cuda.stream
         self.current_device = torch.cuda.current_device
         self.raw_stream = torch._C._cuda_getCurrentRawStream
+        self.grad_enabled = torch.is_grad_enabled
 
 
 def _here(device, stream) -> bool:
@@ -733,6 +734,11 @@ def _there(device, stream, call, *args, **more):
             if isinstance(x, _t.Tensor):
                 x.record_stream(stream)
         return result
+
+
+def _no_gradient():
+    """The attention calls have no backward pass: what they return carries no graph."""
+    return ValueError("the attention calls have no gradient: pass detached tensors or call them under torch.no_grad()")
 
 
 def _rows(t, name, shape, dtype, device):
@@ -818,11 +824,18 @@ def fate_kv_append(q, k, v, k_cache, v_cache, off, kv_len, pages, table=None, in
     paired (j, j + rot / 2) or, interleaved, (2 j, 2 j + 1); None leaves all
     unrotated.  Returns q_out (None without q), which may be q itself.
     ``status`` (int32 [B], cleared by the caller) receives FATE_EINVAL for
-    sequences whose device arrays are out of range."""
+    sequences whose device arrays are out of range.
+
+    The attention calls have no backward pass: with gradients enabled, tensors
+    that require one are refused (ValueError)."""
     dev, dtype = k.device, k.dtype
     if not _here(dev, stream):
         return _there(dev, stream, fate_kv_append, q, k, v, k_cache, v_cache, off, kv_len, pages, table, interleaved,
                       q_out, status)
+    if _t.grad_enabled() and (k.requires_grad or v.requires_grad or k_cache.requires_grad or v_cache.requires_grad or
+                              (q is not None and q.requires_grad) or (table is not None and table.requires_grad) or
+                              (q_out is not None and q_out.requires_grad)):
+        raise _no_gradient()
     shape = _three(k, "k")
     T, hkv, d = shape
     c = _attn_cache(k_cache, v_cache, hkv, d, dtype, dev)
@@ -866,6 +879,9 @@ def fate_attn_paged(q, k_cache, v_cache, off, kv_len, pages, max_new: Optional[i
     if not _here(dev, stream):
         return _there(dev, stream, fate_attn_paged, q, k_cache, v_cache, off, kv_len, pages, max_new, scale, lse, out,
                       status, ws)
+    if _t.grad_enabled() and (q.requires_grad or k_cache.requires_grad or v_cache.requires_grad or
+                              (out is not None and out.requires_grad)):
+        raise _no_gradient()
     shape = _three(q, "q")
     T, hq, d = shape
     hkv = k_cache.shape[1] if k_cache.dim() == 4 else 0
@@ -923,6 +939,9 @@ def fate_attn_prompt(q, k, v, off, scale: Optional[float] = None, lse: bool = Fa
     dev, dtype = q.device, q.dtype
     if not _here(dev, stream):
         return _there(dev, stream, fate_attn_prompt, q, k, v, off, scale, lse, out, status)
+    if _t.grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad or
+                              (out is not None and out.requires_grad)):
+        raise _no_gradient()
     shape, kv_shape = _three(q, "q"), _three(k, "k")
     T, hq, d = shape
     if kv_shape[0] != T or kv_shape[2] != d:
