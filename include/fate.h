@@ -649,7 +649,8 @@ fate_status_t fate_attn_paged_ws_size(const fate_heads_t *heads, const fate_seqs
  *   out = sum_j softmax_j(scale q.k_j) v_j,  d_lse = log sum_j exp(scale q.k_j)
  * with the products of 16-bit operands summed in float32, the statistics in
  * float32 and the weights rounded to the operands' type for the second
- * product.  A row that sees no key (p < 0) gets zeros and -infinity.  Keys and
+ * product (in float16 by at most 2^-32 of the row's largest weight where that
+ * exceeds the rounding itself).  A row that sees no key (p < 0) gets zeros and -infinity.  Keys and
  * values that a row does not see never reach it, whatever they hold (a page's
  * slots past the last key may hold anything).
  *   max_new   an upper bound of the tokens per sequence (1 .. T), which picks

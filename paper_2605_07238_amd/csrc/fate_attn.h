@@ -80,7 +80,17 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
+// The running maximum m that a row's weights 2^(S - m) refer to (S in units of
+// log2) stands kLift below its largest score, or up to kLag above that: the
+// largest weight is 2^kLift to 2^(kLift + kLag).  Float16 gives up bits of
+// weights under 2^-14 and all of them under 2^-25, which many keys behind one
+// large score add up to: 100000 of 2^-25.6 are 0.2% of the result.  Lifted,
+// they lose at most 2^-32 of the largest weight each.  The range allows no
+// more (2^16); bfloat16 reaches as far down as float32.
+constexpr float kLag = 8.0f;
+
 struct BF16 {
+    static constexpr float kLift = 0.0f;
     typedef __bf16 el;
     typedef __bf16 x4 __attribute__((ext_vector_type(4)));
     typedef __bf16 x8 __attribute__((ext_vector_type(8)));
@@ -100,6 +110,7 @@ struct BF16 {
 };
 
 struct F16 {
+    static constexpr float kLift = 7.0f;
     typedef _Float16 el;
     typedef _Float16 x4 __attribute__((ext_vector_type(4)));
     typedef _Float16 x8 __attribute__((ext_vector_type(8)));

@@ -177,8 +177,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_few(AttnLaunch) 
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
                 top = fmaxf(top * a.scale_log2, kLowest);
-                if (__any(top > m[rt] + 8.0f)) {
-                    const float next = fmaxf(m[rt], top), f = exp2_fast(m[rt] - next);
+                if (__any(top > m[rt] + (kLag + T::kLift))) {
+                    const float next = fmaxf(m[rt], top - T::kLift), f = exp2_fast(m[rt] - next);
                     m[rt] = next;
                     l[rt] *= f;
 #pragma unroll

@@ -5,8 +5,8 @@
 // One pass over the keys with the running maximum m and sum l of each row:
 // per key tile, m' = max(m, max S), O = O 2^(m - m') + 2^(S - m') v (S in
 // units of log2), l likewise; at the end O / l.  m moves only when a tile
-// exceeds it by more than 8, so the weights stay under 2^8 and O is rescaled
-// rarely.
+// exceeds it by more than 8, so O is rescaled rarely and the weights stay under
+// 2^8 (in float16 under 2^15: kLift).
 //
 // k_attn_tile: one workgroup of four 64-lane waves per (sequence, key head,
 // 128 packed rows, part of the key axis).  The G query heads of a key head are
@@ -293,8 +293,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
 #pragma unroll
             for (int j = 0; j < 16; ++j) top = fmaxf(top, cur[1][j]);
             top = fmaxf(both_halves_max(top) * a.scale_log2, kLowest);
-            if (__any(top > m + 8.0f)) {
-                const float next = fmaxf(m, top), f = exp2_fast(m - next);
+            if (__any(top > m + (kLag + T::kLift))) {
+                const float next = fmaxf(m, top - T::kLift), f = exp2_fast(m - next);
                 m = next;
                 l *= f;
 #pragma unroll
