@@ -112,15 +112,24 @@ def run_stages(layer: Layer, cache: DeviceCache, stages, answer_tokens: int = 0,
     """Attention outputs [n, heads_q, head_dim] of each stage's own tokens and of its answer tokens (list of
     [answer_tokens, heads_q, head_dim]), and how many prefix tokens were found in the cache.  ``reuse`` False ignores the
     cached prefixes (and caches none)."""
+    mine = []  # the pages taken for each stage
+    try:
+        return _run_stages(layer, cache, stages, answer_tokens, reuse, mine)
+    finally:
+        kept = {p for group in cache.groups.values() for p in group}
+        cache.release([p for extra in mine for p in extra if p not in kept])
+
+
+def _run_stages(layer, cache, stages, answer_tokens, reuse, mine):
     P, hq, d = cache.page_size, layer.heads_q, layer.head_dim
-    pages, mine, keys, cached, outs = [], [], [], [], [None] * len(stages)
+    pages, keys, cached, outs = [], [], [], [None] * len(stages)
     for s in stages:
         have = cache.groups.get(s.group, []) if reuse and s.group else []
         have = have[:s.prefix.shape[0] // P]
         total = s.prefix.shape[0] + s.own.shape[0]
         extra = cache.take(-(-(total + answer_tokens) // P) - len(have))
-        pages.append(have + extra)
         mine.append(extra)
+        pages.append(have + extra)
         keys.append(total)
         cached.append(len(have) * P)
     for hit in (False, True):
@@ -148,13 +157,10 @@ def run_stages(layer: Layer, cache: DeviceCache, stages, answer_tokens: int = 0,
             x = (answers[t - 1] if t else torch.stack([o[-1] for o in outs])).flatten(1)[:, :layer.weight.shape[0]]
             q, _, _ = _store(layer, cache, step, x.contiguous())
             fate.fate_attn_paged(q, cache.k, cache.v, step.off, step.kv_len, step.pages, max_new=1, out=answers[t])
-    for s, p, extra, n in zip(stages, pages, mine, cached):
-        keep = []
-        if reuse and s.group and n == 0 and s.group not in cache.groups:
-            keep = p[:s.prefix.shape[0] // P]
-            if keep:
-                cache.groups[s.group] = keep
-        cache.release([x for x in extra if x not in keep])
+    for s, p, n in zip(stages, pages, cached):
+        full = p[:s.prefix.shape[0] // P]
+        if reuse and s.group and n == 0 and full and s.group not in cache.groups:
+            cache.groups[s.group] = full
     return outs, list(answers.unbind(1)), sum(cached)
 
 

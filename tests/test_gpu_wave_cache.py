@@ -1,0 +1,27 @@
+"""The wave example's page cache: what it holds, gives back and refuses."""
+
+import pytest
+import torch
+
+from paper_2605_07238_amd import wave
+
+pytestmark = pytest.mark.gpu
+
+
+def layer(positions=512, seed=3):
+    return wave.Layer.random(hidden=64, heads_q=4, heads_kv=2, head_dim=64, positions=positions, dtype=torch.float16, seed=seed)
+
+
+def rows(n, seed=0):
+    return torch.randn(n, 64, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda").half()
+
+
+def test_a_wave_that_does_not_fit_takes_no_pages():
+    one = layer()
+    cache = wave.DeviceCache(one, pages=12)
+    fits, more = wave.Stage(1, rows(64), rows(20)), wave.Stage(2, rows(64), rows(40))  # 6 and 7 pages
+    with pytest.raises(RuntimeError):
+        wave.run_stages(one, cache, [fits, more])
+    assert sorted(cache.free) == list(range(12)) and not cache.groups
+    outs, _, found = wave.run_stages(one, cache, [fits])
+    assert found == 0 and outs[0].shape == (20, 4, 64) and len(cache.free) == 8
