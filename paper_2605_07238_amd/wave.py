@@ -127,6 +127,9 @@ def _run_stages(layer, cache, stages, answer_tokens, reuse, mine):
         have = cache.groups.get(s.group, []) if reuse and s.group else []
         have = have[:s.prefix.shape[0] // P]
         total = s.prefix.shape[0] + s.own.shape[0]
+        if total + answer_tokens > layer.table.shape[0]:
+            raise ValueError("a stage of %d tokens with %d of an answer stands past the layer's %d positions" % (
+                total, answer_tokens, layer.table.shape[0]))
         extra = cache.take(-(-(total + answer_tokens) // P) - len(have))
         mine.append(extra)
         pages.append(have + extra)

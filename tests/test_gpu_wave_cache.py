@@ -25,3 +25,13 @@ def test_a_wave_that_does_not_fit_takes_no_pages():
     assert sorted(cache.free) == list(range(12)) and not cache.groups
     outs, _, found = wave.run_stages(one, cache, [fits])
     assert found == 0 and outs[0].shape == (20, 4, 64) and len(cache.free) == 8
+
+
+@pytest.mark.parametrize("prefix,own,answers", [(0, 513, 0), (500, 13, 0), (480, 20, 13)])
+def test_positions_past_the_rotation_table_are_refused(prefix, own, answers):
+    one = layer(positions=512)
+    cache = wave.DeviceCache(one, pages=64)
+    with pytest.raises(ValueError, match="positions"):
+        wave.run_stages(one, cache, [wave.Stage(1, rows(prefix), rows(own))], answers)
+    assert len(cache.free) == 64
+    wave.run_stages(one, cache, [wave.Stage(1, rows(prefix), rows(512 - prefix - answers))], answers)
