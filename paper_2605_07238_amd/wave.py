@@ -61,7 +61,7 @@ class DeviceCache:
         self.v = torch.empty_like(self.k)
         self.page_size = page_size
         self.free = list(range(pages - 1, -1, -1))
-        self.groups = {}  # prefix group -> its full pages
+        self.groups = {}  # Stage.key of a prefix -> its full pages
 
     def take(self, n: int):
         if n > len(self.free):
@@ -74,11 +74,17 @@ class DeviceCache:
 
 @dataclasses.dataclass
 class Stage:
-    """A stage of a wave: its prefix group (0 = none), the tokens of the shared prefix, its own tokens."""
+    """A stage of a wave: its prefix group (0 = none), the tokens of the shared prefix, its own tokens, its model."""
 
     group: int
     prefix: torch.Tensor  # [P, hidden] token rows
     own: torch.Tensor     # [n, hidden], at least one
+    model: int = 0
+
+    @property
+    def key(self):
+        """What the keys and values of the prefix depend on: the model that made them, too."""
+        return self.model, self.group
 
 
 def _ints(values):
@@ -109,9 +115,9 @@ def _store(layer, cache, step, x):
 
 
 def run_stages(layer: Layer, cache: DeviceCache, stages, answer_tokens: int = 0, reuse: bool = True):
-    """Attention outputs [n, heads_q, head_dim] of each stage's own tokens and of its answer tokens (list of
-    [answer_tokens, heads_q, head_dim]), and how many prefix tokens were found in the cache.  ``reuse`` False ignores the
-    cached prefixes (and caches none)."""
+    """Stages of one model, whose layer this is: attention outputs [n, heads_q, head_dim] of each stage's own tokens and of
+    its answer tokens (list of [answer_tokens, heads_q, head_dim]), and how many prefix tokens were found in the cache.
+    ``reuse`` False ignores the cached prefixes (and caches none)."""
     mine = []  # the pages taken for each stage
     try:
         return _run_stages(layer, cache, stages, answer_tokens, reuse, mine)
@@ -124,7 +130,7 @@ def _run_stages(layer, cache, stages, answer_tokens, reuse, mine):
     P, hq, d = cache.page_size, layer.heads_q, layer.head_dim
     pages, keys, cached, outs = [], [], [], [None] * len(stages)
     for s in stages:
-        have = cache.groups.get(s.group, []) if reuse and s.group else []
+        have = cache.groups.get(s.key, []) if reuse and s.group else []
         have = have[:s.prefix.shape[0] // P]
         total = s.prefix.shape[0] + s.own.shape[0]
         if total + answer_tokens > layer.table.shape[0]:
@@ -162,8 +168,8 @@ def _run_stages(layer, cache, stages, answer_tokens, reuse, mine):
             fate.fate_attn_paged(q, cache.k, cache.v, step.off, step.kv_len, step.pages, max_new=1, out=answers[t])
     for s, p, n in zip(stages, pages, cached):
         full = p[:s.prefix.shape[0] // P]
-        if reuse and s.group and n == 0 and full and s.group not in cache.groups:
-            cache.groups[s.group] = full
+        if reuse and s.group and n == 0 and full and s.key not in cache.groups:
+            cache.groups[s.key] = full
     return outs, list(answers.unbind(1)), sum(cached)
 
 
@@ -184,7 +190,7 @@ class Prompts:
             self.prefixes[group] = self.rows(int(self.w.prefix_tokens[flat]) if group else 0)
         lo, hi = self.own
         n = int(torch.randint(lo, hi + 1, (1,), generator=self.gen, device="cuda"))
-        return Stage(group, self.prefixes[group], self.rows(n))
+        return Stage(group, self.prefixes[group], self.rows(n), int(self.w.model[flat]))
 
 
 def plan_waves(w, waves: int, k: int = 4):
@@ -204,20 +210,29 @@ def plan_waves(w, waves: int, k: int = 4):
         fate.fate_commit_advance(packed, state, sel)
 
 
+def by_model(stages):
+    """The stages of each model: (model, its stages)."""
+    models = {}
+    for s in stages:
+        models.setdefault(s.model, []).append(s)
+    return sorted(models.items(), key=lambda x: x[0])
+
+
 def main(instances: int = 4, waves: int = 12, answer_tokens: int = 4):
     """Plan waves and carry out every device's share here, one device after the other, each with a cache of its own."""
     w = synth.make_workload("forkjoin-4096x1000-d16", B=instances)
-    layer = Layer.random()
-    caches = [DeviceCache(layer, pages=1 << 13) for _ in range(w.D)]
-    prompts = Prompts(w, layer.weight.shape[0], layer.weight.dtype)
-    run_stages(layer, caches[0], [Stage(0, prompts.rows(0), prompts.rows(8))], 1)  # libraries load at the first call
+    layers = [Layer.random(seed=m) for m in range(w.M)]
+    caches = [DeviceCache(layers[0], pages=1 << 13) for _ in range(w.D)]
+    prompts = Prompts(w, layers[0].weight.shape[0], layers[0].weight.dtype)
+    run_stages(layers[0], caches[0], [Stage(0, prompts.rows(0), prompts.rows(8))], 1)  # libraries load at the first call
     for number, wave in enumerate(plan_waves(w, waves)):
         stages = [[prompts.stage(flat) for flat, on in wave if on == d] for d in range(w.D)]
         took, found = [], 0
         for reuse in (False, True):
             torch.cuda.synchronize()
             t = time.perf_counter()
-            hits = [run_stages(layer, caches[d], stages[d], answer_tokens, reuse)[2] for d in range(w.D) if stages[d]]
+            hits = [run_stages(layers[m], caches[d], of, answer_tokens, reuse)[2]
+                    for d in range(w.D) for m, of in by_model(stages[d])]
             torch.cuda.synchronize()
             took.append((time.perf_counter() - t) * 1e3)
             found = sum(hits)

@@ -35,3 +35,17 @@ def test_positions_past_the_rotation_table_are_refused(prefix, own, answers):
         wave.run_stages(one, cache, [wave.Stage(1, rows(prefix), rows(own))], answers)
     assert len(cache.free) == 64
     wave.run_stages(one, cache, [wave.Stage(1, rows(prefix), rows(512 - prefix - answers))], answers)
+
+
+def test_models_do_not_share_keys():
+    """A prefix group that stages of two models start with: each model's keys and values serve its own stages alone."""
+    a, b = layer(seed=3), layer(seed=4)
+    cache = wave.DeviceCache(a, pages=64)
+    prefix, own = rows(48, 1), rows(20, 2)
+    first = wave.run_stages(a, cache, [wave.Stage(7, prefix, own, model=0)])
+    other = wave.run_stages(b, cache, [wave.Stage(7, prefix, own, model=1)])
+    assert first[2] == other[2] == 0
+    fresh = wave.run_stages(b, wave.DeviceCache(b, pages=64), [wave.Stage(7, prefix, own, model=1)])
+    assert torch.equal(other[0][0], fresh[0][0])
+    assert wave.run_stages(a, cache, [wave.Stage(7, prefix, own, model=0)])[2] == 48
+    assert wave.run_stages(b, cache, [wave.Stage(7, prefix, own, model=1)])[2] == 48
