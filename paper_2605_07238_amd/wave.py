@@ -63,7 +63,12 @@ class DeviceCache:
         self.free = list(range(pages - 1, -1, -1))
         self.groups = {}  # Stage.key of a prefix -> its full pages
 
-    def take(self, n: int):
+    def take(self, n: int, using=()):
+        """n free pages; the groups cached longest, but those in `using`, go where too few are free."""
+        for key in [k for k in self.groups if k not in using]:
+            if n <= len(self.free):
+                break
+            self.release(self.groups.pop(key))
         if n > len(self.free):
             raise RuntimeError("the cache has %d free pages, %d are needed" % (len(self.free), n))
         return [self.free.pop() for _ in range(n)]
@@ -129,6 +134,7 @@ def run_stages(layer: Layer, cache: DeviceCache, stages, answer_tokens: int = 0,
 def _run_stages(layer, cache, stages, answer_tokens, reuse, mine):
     P, hq, d = cache.page_size, layer.heads_q, layer.head_dim
     pages, keys, cached, outs = [], [], [], [None] * len(stages)
+    using = {s.key for s in stages}
     for s in stages:
         have = cache.groups.get(s.key, []) if reuse and s.group else []
         have = have[:s.prefix.shape[0] // P]
@@ -136,7 +142,7 @@ def _run_stages(layer, cache, stages, answer_tokens, reuse, mine):
         if total + answer_tokens > layer.table.shape[0]:
             raise ValueError("a stage of %d tokens with %d of an answer stands past the layer's %d positions" % (
                 total, answer_tokens, layer.table.shape[0]))
-        extra = cache.take(-(-(total + answer_tokens) // P) - len(have))
+        extra = cache.take(-(-(total + answer_tokens) // P) - len(have), using)
         mine.append(extra)
         pages.append(have + extra)
         keys.append(total)

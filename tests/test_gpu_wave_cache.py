@@ -49,3 +49,20 @@ def test_models_do_not_share_keys():
     assert torch.equal(other[0][0], fresh[0][0])
     assert wave.run_stages(a, cache, [wave.Stage(7, prefix, own, model=0)])[2] == 48
     assert wave.run_stages(b, cache, [wave.Stage(7, prefix, own, model=1)])[2] == 48
+
+
+def test_a_full_cache_lets_its_oldest_groups_go():
+    one = layer()
+    cache = wave.DeviceCache(one, pages=12)
+    stages = [wave.Stage(g, rows(48, g), rows(10, 50 + g)) for g in range(1, 9)]  # three full pages and one more
+    for s in stages:
+        assert wave.run_stages(one, cache, [s])[2] == 0
+    assert len(cache.groups) == 3 and len(cache.free) == 3
+    assert [wave.run_stages(one, cache, [s])[2] for s in (stages[7], stages[6], stages[5], stages[0])] == [48, 48, 48, 0]
+    # not those that the same call reads
+    out, _, found = wave.run_stages(one, cache, [stages[0], stages[7], stages[4]])
+    assert found == 96
+    fresh = wave.DeviceCache(one, pages=64)
+    for s, got in zip((stages[0], stages[7], stages[4]), out):
+        want = wave.run_stages(one, fresh, [s])[0][0]
+        assert torch.allclose(got.float(), want.float(), atol=0.02, rtol=0.02)
