@@ -4,8 +4,10 @@ the stages that the planner gave it.
 The planner (score, top-k, planning wave, commit; :mod:`.fate`) says which
 stages run on a device next and, through its prefix slots, which prompts start
 with a prefix whose keys and values the device still holds.  :class:`DeviceCache`
-is what such a slot stands for on the device: pages of a paged cache per prefix
-group.  :func:`run_stages` takes a wave's stages through one attention layer:
+is what such a slot stands for on the device: pages of a paged cache per workflow,
+model and prefix group.  :func:`carry_out` lets go of the groups that the plan's
+slots no longer name and gives each device its stages; :func:`run_stages` takes
+those of one model through one attention layer:
 
   stages whose prefix is cached   their own tokens are appended behind the
                                   shared pages and attend over them
@@ -17,8 +19,8 @@ group.  :func:`run_stages` takes a wave's stages through one attention layer:
                                   fate_attn_paged)
 
 ``python -m paper_2605_07238_amd.wave`` plans waves on a few fork-join
-workflows, carries out each device's share and prints per wave what cached
-prefixes saved.  Weights and tokens are random.
+workflows, carries out each device's share and prints per wave the time with
+cached prefixes and without.  Weights and tokens are random.
 """
 
 from __future__ import annotations
@@ -26,6 +28,7 @@ from __future__ import annotations
 import dataclasses
 import time
 
+import numpy as np
 import torch
 
 from . import fate, synth
@@ -63,6 +66,11 @@ class DeviceCache:
         self.free = list(range(pages - 1, -1, -1))
         self.groups = {}  # Stage.key of a prefix -> its full pages
 
+    def keep(self, instance: int, held):
+        """Lets go of a workflow's groups that are not in `held`, what its plan's slots on this device name."""
+        for key in [k for k in self.groups if k[0] == instance and k[2] not in held]:
+            self.release(self.groups.pop(key))
+
     def take(self, n: int, using=()):
         """n free pages; the groups cached longest, but those in `using`, go where too few are free."""
         for key in [k for k in self.groups if k not in using]:
@@ -79,17 +87,19 @@ class DeviceCache:
 
 @dataclasses.dataclass
 class Stage:
-    """A stage of a wave: its prefix group (0 = none), the tokens of the shared prefix, its own tokens, its model."""
+    """A stage of a wave: its prefix group (0 = none), the tokens of the shared prefix, its own tokens, its model, the
+    workflow that it is a stage of."""
 
     group: int
     prefix: torch.Tensor  # [P, hidden] token rows
     own: torch.Tensor     # [n, hidden], at least one
     model: int = 0
+    instance: int = 0
 
     @property
     def key(self):
-        """What the keys and values of the prefix depend on: the model that made them, too."""
-        return self.model, self.group
+        """What a device caches a prefix as: its keys and values are a model's, and each workflow's plan has slots of its own."""
+        return self.instance, self.model, self.group
 
 
 def _ints(values):
@@ -196,11 +206,13 @@ class Prompts:
             self.prefixes[group] = self.rows(int(self.w.prefix_tokens[flat]) if group else 0)
         lo, hi = self.own
         n = int(torch.randint(lo, hi + 1, (1,), generator=self.gen, device="cuda"))
-        return Stage(group, self.prefixes[group], self.rows(n), int(self.w.model[flat]))
+        instance = int(np.searchsorted(self.w.stage_off, flat, side="right")) - 1
+        return Stage(group, self.prefixes[group], self.rows(n), int(self.w.model[flat]), instance)
 
 
-def plan_waves(w, waves: int, k: int = 4):
-    """Waves of a plan, one after the other: lists of (flat stage id, device) of the single-device placements."""
+def follow_plan(w, waves: int, k: int = 4):
+    """Waves of a plan, one after the other: (flat stage id, device) of the single-device placements (a window's shards are
+    left out), and the prefix groups that the plan's slots hold on each device as the wave starts, [instances, devices, slots]."""
     packed = fate.fate_pack_dags(w)
     state = fate.fate_pack_state(packed, w, advance=True)
     params = fate.make_params(w)
@@ -212,16 +224,27 @@ def plan_waves(w, waves: int, k: int = 4):
         sel = fate.fate_plan_wave(state, idx, val)
         flat = fate.frontier_table(state)[0]
         chosen = sel[:F].cpu().tolist()
-        yield [(int(flat[f]), c) for f, c in enumerate(chosen) if 0 <= c < w.D]
+        yield [(int(flat[f]), c) for f, c in enumerate(chosen) if 0 <= c < w.D], fate.state_arrays(state)["prefix_cache"]
         fate.fate_commit_advance(packed, state, sel)
 
 
-def by_model(stages):
-    """The stages of each model: (model, its stages)."""
-    models = {}
-    for s in stages:
-        models.setdefault(s.model, []).append(s)
-    return sorted(models.items(), key=lambda x: x[0])
+def plan_waves(w, waves: int, k: int = 4):
+    """The placements of :func:`follow_plan`."""
+    for placed, _ in follow_plan(w, waves, k):
+        yield placed
+
+
+def carry_out(layers, caches, stages, devices, slots, answer_tokens: int = 0, reuse: bool = True):
+    """A wave's stages, each on its device: what the plan's slots no longer name leaves the device's cache, then each model's
+    stages go through its layer.  Returns how many prefix tokens were found cached."""
+    found = 0
+    for d, cache in enumerate(caches):
+        for instance, held in enumerate(slots[:, d].tolist()):
+            cache.keep(instance, held)
+        here = [s for s, on in zip(stages, devices) if on == d]
+        for model in sorted({s.model for s in here}):
+            found += run_stages(layers[model], cache, [s for s in here if s.model == model], answer_tokens, reuse)[2]
+    return found
 
 
 def main(instances: int = 4, waves: int = 12, answer_tokens: int = 4):
@@ -231,21 +254,18 @@ def main(instances: int = 4, waves: int = 12, answer_tokens: int = 4):
     caches = [DeviceCache(layers[0], pages=1 << 13) for _ in range(w.D)]
     prompts = Prompts(w, layers[0].weight.shape[0], layers[0].weight.dtype)
     run_stages(layers[0], caches[0], [Stage(0, prompts.rows(0), prompts.rows(8))], 1)  # libraries load at the first call
-    for number, wave in enumerate(plan_waves(w, waves)):
-        stages = [[prompts.stage(flat) for flat, on in wave if on == d] for d in range(w.D)]
-        took, found = [], 0
-        for reuse in (False, True):
+    for number, (placed, slots) in enumerate(follow_plan(w, waves)):
+        stages, devices = [prompts.stage(flat) for flat, _ in placed], [d for _, d in placed]
+        took, found = {}, 0
+        for reuse in (False, True) if number % 2 else (True, False):  # neither is always the first to meet the wave's shapes
             torch.cuda.synchronize()
             t = time.perf_counter()
-            hits = [run_stages(layers[m], caches[d], of, answer_tokens, reuse)[2]
-                    for d in range(w.D) for m, of in by_model(stages[d])]
+            found = max(found, carry_out(layers, caches, stages, devices, slots, answer_tokens, reuse))
             torch.cuda.synchronize()
-            took.append((time.perf_counter() - t) * 1e3)
-            found = sum(hits)
-        flat = [s for x in stages for s in x]
-        tokens = sum(s.prefix.shape[0] + s.own.shape[0] for s in flat)
+            took[reuse] = (time.perf_counter() - t) * 1e3
+        tokens = sum(s.prefix.shape[0] + s.own.shape[0] for s in stages)
         print("wave %d: %d stages on %d devices, %d prompt tokens, %d of them cached: %.2f ms, %.2f without the cached ones"
-              % (number, len(flat), sum(map(bool, stages)), tokens, found, took[1], took[0]), flush=True)
+              % (number, len(stages), len(set(devices)), tokens, found, took[True], took[False]), flush=True)
 
 
 if __name__ == "__main__":
