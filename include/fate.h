@@ -557,7 +557,7 @@ fate_status_t fate_place_baseline_device(const fate_dags_t *dags, const fate_sta
  *   fate_kv_append    stores new keys and values, rotated to their positions
  *   fate_attn_paged   new tokens (chunks, a few, one) over their sequences' pages
  *   fate_attn_prompt  whole prompts, packed, causal, without a cache
- * Forward only.  All arrays are device memory unless said otherwise; every
+ * Forward only: there is no backward pass.  All arrays are device memory unless said otherwise; every
  * call is enqueued on `stream`, never synchronises and can be captured.  The
  * host checks what it can see (sizes, types, strides, alignment); errors in
  * the device arrays (`off`, `kv_len`, `pages`) are found by the kernels, which
@@ -650,9 +650,9 @@ fate_status_t fate_attn_paged_ws_size(const fate_heads_t *heads, const fate_seqs
  * with the products of 16-bit operands summed in float32, the statistics in
  * float32 and the weights rounded to the operands' type for the second
  * product (in float16 by at most 2^-32 of the row's largest weight where that
- * exceeds the rounding itself).  A row that sees no key (p < 0) gets zeros and -infinity.  Keys and
- * values that a row does not see never reach it, whatever they hold (a page's
- * slots past the last key may hold anything).
+ * exceeds the rounding itself).  A row that sees no key (p < 0) gets zeros and
+ * -infinity.  Keys and values that a row does not see never reach it, whatever
+ * they hold (a page's slots past the last key may hold anything).
  *   max_new   an upper bound of the tokens per sequence (1 .. T), which picks
  *             the kernels; a larger sequence is still computed, slower
  *   scale     positive and finite

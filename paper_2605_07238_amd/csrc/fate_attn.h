@@ -40,7 +40,11 @@ struct AppendLaunch {
 int launch_append(const AppendLaunch &a, void *stream);
 
 // Tokens of an append's workgroup in large calls: its first wave finds them all
-// at once.  Four: 98.8 us for 18261 tokens (48 heads of 128); eight 112, sixteen 109.
+// at once.  Four: 82 us for 18261 tokens (48 heads of 128), 30.5 for 5579; two 80
+// and 32.5, eight 96 and 41, one 83 and 31.  One in calls of up to 1024, where
+// four leave compute units idle: 5.4 against 9.1 us for 64 tokens, 9.1 against
+// 12.2 for 1024 (for 2048 one would take 12.9 against four's 14.1, for 4096 20.6
+// against 24.4).
 constexpr int kAppendTokens = 4;
 inline int append_tokens(int64_t T) { return T <= 1024 ? 1 : kAppendTokens; }
 inline int64_t append_grid(int64_t T) { return (T + append_tokens(T) - 1) / append_tokens(T); }

@@ -90,7 +90,10 @@ PagedPlan plan_paged(const fate_heads_t *h, const fate_seqs_t *s, int64_t max_ne
     const int64_t G = h->heads_q / h->heads_kv, packed = (max_new > 1 ? max_new : 1) * G, few = h->head_dim <= 128 ? 32 : 16;
     PagedPlan p;
     p.rows = packed <= 16 ? 16 : packed <= few ? 32 : fate::kTileRows;
-    // what the chip runs at once: two workgroups a compute unit, one of head sizes over 128
+    // two workgroups a compute unit, one of head sizes over 128.  More shares cost more in joins and in the shares'
+    // starts than they bring in loads under way, also at head size 64 where four would fit: 768 and 1024 for a step
+    // of 64 answers over 128 to 8192 keys 61 and 61 against 57 us (at 128 113 and 111 against 108; at 256, for 256,
+    // 81 and 88 against 68), for two over 65536 and 131072 85 and 85 against 81, for 16 chunks 74 and 78 against 56
     const int target = h->head_dim <= 128 ? 512 : 256;
     p.pieces = target / h->heads_kv > 0 ? target / h->heads_kv : 1;
     p.tiles = tiles_of(s, G, p.rows);

@@ -2,20 +2,22 @@
 // an answer, some drafted tokens), and the joining of parts of the key axis.
 //
 // With few rows the call reads each key and value once and computes little:
-// memory bounds it.  k_attn_few: one workgroup of four waves per (sequence,
-// key head, 16 or 32 packed rows, part of the key axis); the parts are sized
-// from the lengths on the device so that the whole call makes about as many
-// pieces as the chip holds workgroups, whatever the mix of lengths.  A wave
-// takes every fourth block of 32 keys by itself: keys go from memory to
-// registers as the first product's operand (16-byte loads, 64 bytes of each of
-// 16 rows at a time), values through the wave's own LDS rows, because the
-// second product needs them transposed.  The products are transposed as in
+// memory bounds it.  k_attn_few: all row tiles of a key head (16 or 32 packed
+// rows of one sequence) lie on one axis of work, worked out from the lengths on
+// the device, and a workgroup of four waves walks an equal share of it: several
+// tiles, one, or parts at either end, which k_attn_join puts together.  There
+// are about as many shares as the chip runs workgroups, whatever the mix of
+// lengths.  In a tile, a wave takes every fourth block of 32 keys by itself:
+// keys go from memory to registers as the first product's operand (16-byte
+// loads, 64 bytes of each of 16 rows at a time), values through the wave's own
+// LDS rows, because the second product needs them transposed.  The products are transposed as in
 // the tile kernel (S^T = k q^T, O^T = v^T p^T), on 16 x 16 x 32 matrix
 // instructions: 16 packed rows are one column block.  The four waves'
 // statistics and outputs meet in LDS at the end.  A step of 64 answers over 128
-// to 8192 keys: 102 us and 6.7 for the join, 4.7 TB/s; two answers over 65536
-// and 131072: 143 and 8.3 us, 5.3 TB/s.  One block a wave at a time is enough:
-// two workgroups a compute unit hold 128 KB of loads under way.
+// to 8192 keys: 101 us and 6.4 for the join, 4.7 TB/s; two answers over 65536
+// and 131072: 144 and 8.3 us, 5.2 TB/s.  One block a wave at a time is enough:
+// two workgroups a compute unit hold 128 KB of loads under way (head size 128;
+// the shares' number: plan_paged).
 //
 // k_attn_join: the parts of a row tile, o = sum 2^(m_i - M) o_i / sum 2^(m_i - M) l_i.
 #include "fate_attn.h"

@@ -24,7 +24,7 @@
 // next tile's scores on the matrix cores beside the softmax of this one's in
 // the vector units.  With tiles that passed through registers, one ahead, and
 // each tile's scores in its own step: 2346 us for 16384 tokens against 2034.
-// Now 1971 us, 1116 TFLOP/s (a large library product reaches 1241): the matrix
+// Now 1978 us, 1112 TFLOP/s (a large library product reaches 1418): the matrix
 // cores are busy 58% of the cycles and the clock stands at 1.8 GHz for it.
 //
 // Key tiles go from the last to the first: the tiles on a row's causal edge

@@ -12,12 +12,14 @@
 // (token, head) pair: two chunks of eight that the rotation pairs (j and
 // j + rot / 2), or two neighbouring chunks.  The unit's place is worked out
 // once, and its elements belong to one thread, which lets queries be rotated
-// in place.  18261 tokens of 48 heads of 128: 86 us, 5250 GB/s (a copy of as
-// many bytes: 5400); with a division per unit and a token per wave, 154 us.
+// in place.  18261 tokens of 48 heads of 128, 451 MB: 82 us, 5480 GB/s, in calls
+// on the same few inputs, 97 on inputs and caches that were not near (a copy of
+// as many bytes: 84); with a division per unit and a token per wave, 154 us.
 //
-// A call that moves more than the last-level cache holds reads past it (86
-// against 99 us there; but 38.6 against 31.5 us for a third of the bytes, whose
-// rows the cache still has from the projection that wrote them).
+// A call that moves more than the last-level cache holds reads past it: 82
+// against 96 us there.  For a third of the bytes, 29 against 31 us on inputs in
+// turn, but 29 against 25 where the cache still has the rows from the projection
+// that wrote them.
 #include "fate_attn.h"
 
 namespace fate {
