@@ -674,6 +674,58 @@ fate_status_t fate_attn_prompt(const fate_heads_t *heads, const fate_seqs_t *seq
                                const fate_rows_t *k, const fate_rows_t *v, float scale, const fate_rows_t *out,
                                float *d_lse, int32_t *d_status, void *stream);
 
+/* Page tables of the cache, kept on the device: `pages` as in fate_seqs_t (its
+ * rows do not overlap), and a stack of the pages that no sequence has.
+ *   free[n_pages]  free[0 .. n_free - 1] are free pages, the next to be taken last
+ *   n_free         how many (device, one int32); a count outside 0 .. n_pages
+ *                  counts as none free, and no room
+ *   kv_len[B]      keys of each sequence in the cache: its first
+ *                  ceil(kv_len / page_size) entries of `pages` are its own, or
+ *                  shared with other sequences where all of a page is cached */
+typedef struct {
+    int32_t B, max_pages, page_size, n_pages;
+    int64_t pages_stride;
+    int32_t *pages, *free;
+    const int32_t *n_free, *kv_len;
+} fate_kv_tables_t;
+
+/* fate_kv_reserve: room for new_tokens[b] tokens behind each sequence's keys,
+ * and the arrays that the calls above then take.  Sequences are served in
+ * order: one is refused (FATE_ESIZE in d_status) when it needs pages and the
+ * sequences up to it ask for more than are free, or when the new tokens of the
+ * sequences up to it are more than T; it then gets nothing.  A sequence with a
+ * negative count, or that would pass max_pages * page_size keys, is in error
+ * (FATE_EINVAL) and asks for nothing; so is one whose own rows lie in a page
+ * outside 0 .. n_pages - 1 (its other rows are served).
+ *   off[B+1]        first row of each sequence in the call, off[B] rows in all
+ *   kv_len_out[B]   keys with the new ones; may be kv_len itself
+ *   n_free_out      pages left on the stack; may be n_free itself.  `free` keeps
+ *                   its entries
+ *   taken[B+1]      pages taken by the sequences before each, and by all
+ *   pages           entries of the pages taken are written, no others
+ *   slots[T]        page * page_size + place within the page of each row, or null
+ *   positions[T]    position of each row in its sequence, or null; both are -1
+ *                   from row off[B] on (slots also where a page is out of range)
+ * Outputs overlap nothing but as said.  B = 0 is a call without sequences.
+ * Errors: EINVAL (null pointers, negative sizes, page_size, alignment, strides
+ * that let rows overlap), ERANGE (page_size, max_pages * page_size past 2^30, B
+ * past 2^24, T at 2^31), EHIP. */
+fate_status_t fate_kv_reserve(const fate_kv_tables_t *tables, const int32_t *new_tokens, int64_t T, int32_t *off,
+                              int32_t *kv_len_out, int32_t *n_free_out, int32_t *taken, int64_t *slots,
+                              int32_t *positions, int32_t *d_status, void *stream);
+
+/* fate_kv_trim: each sequence is cut to its first keep[b] keys (those it has,
+ * if fewer); pages that hold none of these go back on the stack, sequence by
+ * sequence and in the order of its table.  0 ends a sequence; its shared
+ * prefix's length leaves that prefix's pages alone.
+ *   kv_len_out[B], n_free_out, given[B+1]  as above, pages given back
+ * A sequence with a negative length, with a page outside 0 .. n_pages - 1 to
+ * give, or whose pages the stack has no room for (a page given twice comes to
+ * that in the end: the call cannot see it) is in error and stays as it is.
+ * `pages` is only read.  Errors: as fate_kv_reserve. */
+fate_status_t fate_kv_trim(const fate_kv_tables_t *tables, const int32_t *keep, int32_t *kv_len_out,
+                           int32_t *n_free_out, int32_t *given, int32_t *d_status, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,263 @@
+// Page tables of the key-value cache on the device: pages for new tokens off
+// the stack of free ones, and back on it when a sequence is cut.
+//
+//   reserve  need_b = ceil((kv_b + new_b) / P) - ceil(kv_b / P); x_b, y_b = the
+//            sums of need and new up to b.  b is served if it needs no page or
+//            x_b <= n_free, and y_b <= T.  Both sums grow, so that of two
+//            sequences that need pages the earlier is served if the later is:
+//            the pages of those served lie on the stack without gaps.
+//   trim     the pages past ceil(min(keep, kv) / P) go on the stack, in order.
+//
+// Latency bounds both: an answer's step moves a few kilobytes.  One workgroup
+// adds the lengths up, 1024 sequences a step, and in small calls does the rest
+// too, in the same launch; in others a second launch spreads what is left over
+// the chip.  Nothing is kept between the launches but the call's results, so
+// that lengths and counts may be updated in place, which a grid that reads
+// them in every workgroup could not.
+#include "fate_attn.h"
+#include "fate_pages.h"
+
+namespace fate {
+namespace {
+
+constexpr int kThreads = 1024, kWaves = kThreads / 64;
+constexpr int kStaged = 4096;  // sequences whose offsets fit the search in LDS
+
+// Inclusive sums over the workgroup's threads; `before` holds kWaves entries.
+template <class I>
+__device__ __forceinline__ I block_scan(I x, I *before, I &total) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const I in_wave = wave_scan_add(x);
+    if (lane == 63) before[w] = in_wave;
+    __syncthreads();
+    I sum = 0;
+    total = 0;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+        if (i < w) sum += before[i];
+        total += before[i];
+    }
+    __syncthreads();
+    return sum + in_wave;
+}
+
+struct Scans {
+    int64_t a[kWaves], b[kWaves];
+};
+
+__device__ __forceinline__ int pages_for(int64_t keys, int shift) {
+    return (int)((keys + (1 << shift) - 1) >> shift);
+}
+
+// A count of free pages that no stack can hold counts as none.
+__device__ __forceinline__ int free_pages(const PagesLaunch &a) {
+    const int n = *a.n_free;
+    return n >= 0 && n <= a.n_pages ? n : 0;
+}
+
+// Lengths of all sequences: off, kv_out, taken, status and n_free_out.
+__device__ void reserve_lengths(const PagesLaunch &a, Scans &lds) {
+    const int tid = threadIdx.x, stack = *a.n_free, n_free = free_pages(a);
+    int64_t asked = 0, rows = 0, done = 0;  // before this step; done: rows and pages given, in the halves of a word
+    for (int64_t at = 0; at < a.B; at += kThreads) {
+        const int64_t b = at + tid;
+        int64_t fresh_tokens = 0, kv = 0;
+        bool good = false;
+        if (b < a.B) {
+            fresh_tokens = a.counts[b];
+            kv = a.kv_len[b];
+            good = fresh_tokens >= 0 && kv >= 0 && kv + fresh_tokens <= a.max_keys;
+            if (!good) fresh_tokens = 0;
+        }
+        const int need = good ? pages_for(kv + fresh_tokens, a.shift) - pages_for(kv, a.shift) : 0;
+        int64_t all_pages, all_rows, all_done;
+        const int64_t x = asked + block_scan((int64_t)need, lds.a, all_pages);
+        const int64_t y = rows + block_scan(fresh_tokens, lds.b, all_rows);
+        const bool fits = (need == 0 || x <= n_free) && y <= a.T;
+        const int64_t mine = fits ? fresh_tokens << 32 | need : 0;  // rows are at most T, pages at most n_free
+        const int64_t upto = done + block_scan(mine, lds.a, all_done);
+        if (b < a.B) {
+            a.off[b + 1] = (int)(upto >> 32);
+            a.moved[b + 1] = (int)upto;
+            a.kv_out[b] = (int)(fits ? kv + fresh_tokens : kv);
+            if (a.status && !(good && fits)) a.status[b] = good ? FATE_ESIZE : FATE_EINVAL;
+        }
+        asked += all_pages;
+        rows += all_rows;
+        done += all_done;
+    }
+    if (tid == 0) {
+        a.off[0] = a.moved[0] = 0;
+        *a.n_free_out = stack - (int)done;
+    }
+}
+
+// Rows [from, to): their positions, slots, and the pages that start with them.
+// `off` holds the offsets, in LDS where there are few.
+template <class Off>
+__device__ void reserve_rows(const PagesLaunch &a, const Off *off, int64_t from, int64_t to) {
+    const int stack = *a.n_free_out + a.moved[a.B];
+    const int64_t end = a.B ? off[a.B] : 0;
+    for (int64_t t = from + threadIdx.x; t < to; t += blockDim.x) {
+        int64_t slot = -1;
+        int pos = -1;
+        if (t < end) {
+            int lo = 0, hi = a.B - 1;  // the last sequence that starts at t or before, which has rows: its end is past t
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (off[mid + 1] <= t) lo = mid + 1;
+                else hi = mid;
+            }
+            const int start = off[lo], old = a.kv_out[lo] - (off[lo + 1] - start);
+            pos = old + (int)(t - start);
+            const int j = pos >> a.shift, have = pages_for(old, a.shift), in_page = pos & ((1 << a.shift) - 1);
+            int32_t *const entry = a.pages + lo * a.pages_stride + j;
+            int page;
+            if (j >= have) {
+                page = a.free[stack - 1 - a.moved[lo] - (j - have)];
+                if (in_page == 0) *entry = page;
+            } else {
+                page = *entry;
+            }
+            if ((uint32_t)page < (uint32_t)a.n_pages) slot = ((int64_t)page << a.shift) + in_page;
+            else if (a.status) a.status[lo] = FATE_EINVAL;
+        }
+        if (a.slots) a.slots[t] = slot;
+        if (a.positions) a.positions[t] = pos;
+    }
+}
+
+template <bool ROWS>
+__global__ __launch_bounds__(kThreads) void k_kv_reserve(PagesLaunch a) {
+    __shared__ Scans lds;
+    __shared__ int off[ROWS ? kStaged + 1 : 1];
+    reserve_lengths(a, lds);
+    if (ROWS) {
+        __syncthreads();
+        for (int i = threadIdx.x; i <= a.B; i += kThreads) off[i] = a.off[i];
+        __syncthreads();
+        reserve_rows(a, off, 0, a.T);
+    }
+}
+
+constexpr int kRowsPer = 1024;  // rows of a workgroup of the second launch
+
+template <bool STAGED>
+__global__ __launch_bounds__(256) void k_kv_rows(PagesLaunch a) {
+    __shared__ int off[STAGED ? kStaged + 1 : 1];
+    const int64_t from = (int64_t)blockIdx.x * kRowsPer, to = min(from + kRowsPer, a.T);
+    if (STAGED) {
+        for (int i = threadIdx.x; i <= a.B; i += 256) off[i] = a.off[i];
+        __syncthreads();
+        reserve_rows(a, off, from, to);
+    } else {
+        reserve_rows(a, a.off, from, to);
+    }
+}
+
+// Pages that each of the sequences b = first, first + step .. gives back, a
+// wave each: in moved[b + 1], -1 for a sequence in error.
+__device__ void trim_counts(const PagesLaunch &a, int first, int step) {
+    const int lane = threadIdx.x & 63;
+    for (int64_t b = first; b < a.B; b += step) {
+        const int kv = a.kv_len[b], keep = a.counts[b];
+        int gone = -1;
+        if (kv >= 0 && keep >= 0 && kv <= a.max_keys) {
+            const int left = pages_for(min(kv, keep), a.shift), have = pages_for(kv, a.shift);
+            bool bad = false;
+            for (int j = left + lane; j < have; j += 64)
+                bad = bad || (uint32_t)a.pages[b * a.pages_stride + j] >= (uint32_t)a.n_pages;
+            if (!__any(bad)) gone = have - left;
+        }
+        if (lane == 0) a.moved[b + 1] = gone;
+    }
+}
+
+__device__ void trim_lengths(const PagesLaunch &a, Scans &lds) {
+    const int tid = threadIdx.x, stack = *a.n_free;
+    const bool known = stack >= 0 && stack <= a.n_pages;
+    int64_t asked = 0, done = 0;
+    for (int64_t at = 0; at < a.B; at += kThreads) {
+        const int64_t b = at + tid;
+        const int gone = b < a.B ? a.moved[b + 1] : 0;
+        int64_t all, all_done;
+        const int64_t x = asked + block_scan((int64_t)max(gone, 0), lds.a, all);
+        const bool fits = gone == 0 || (gone > 0 && known && stack + x <= a.n_pages);
+        const int64_t upto = done + block_scan((int64_t)(fits ? gone : 0), lds.b, all_done);
+        if (b < a.B) {
+            a.moved[b + 1] = (int)upto;
+            const int kv = a.kv_len[b];
+            a.kv_out[b] = fits ? min(kv, a.counts[b]) : kv;
+            if (a.status && !fits) a.status[b] = FATE_EINVAL;
+        }
+        asked += all;
+        done += all_done;
+    }
+    if (tid == 0) {
+        a.moved[0] = 0;
+        *a.n_free_out = stack + (int)done;
+    }
+}
+
+__device__ void trim_pages(const PagesLaunch &a, int first, int step) {
+    const int lane = threadIdx.x & 63;
+    const int stack = *a.n_free_out - a.moved[a.B];
+    for (int64_t b = first; b < a.B; b += step) {
+        const int from = a.moved[b], n = a.moved[b + 1] - from;
+        if (n == 0) continue;
+        const int32_t *const entry = a.pages + b * a.pages_stride + pages_for(a.kv_out[b], a.shift);
+        for (int j = lane; j < n; j += 64) a.free[stack + from + j] = entry[j];
+    }
+}
+
+__global__ __launch_bounds__(kThreads) void k_kv_trim(PagesLaunch a) {
+    __shared__ Scans lds;
+    const int w = threadIdx.x >> 6;
+    trim_counts(a, w, kWaves);
+    __syncthreads();
+    trim_lengths(a, lds);
+    __syncthreads();
+    trim_pages(a, w, kWaves);
+}
+
+// The three steps of a large call.
+__global__ __launch_bounds__(256) void k_kv_trim_counts(PagesLaunch a) {
+    trim_counts(a, blockIdx.x * 4 + (threadIdx.x >> 6), gridDim.x * 4);
+}
+__global__ __launch_bounds__(kThreads) void k_kv_trim_lengths(PagesLaunch a) {
+    __shared__ Scans lds;
+    trim_lengths(a, lds);
+}
+__global__ __launch_bounds__(256) void k_kv_trim_pages(PagesLaunch a) {
+    trim_pages(a, blockIdx.x * 4 + (threadIdx.x >> 6), gridDim.x * 4);
+}
+
+}  // namespace
+
+int launch_reserve(const PagesLaunch &a, void *stream) {
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    if (a.B <= kStaged && a.T <= kReserveSmall) {
+        hipLaunchKernelGGL((k_kv_reserve<true>), dim3(1), dim3(kThreads), 0, s, a);
+        return (int)hipGetLastError();
+    }
+    hipLaunchKernelGGL((k_kv_reserve<false>), dim3(1), dim3(kThreads), 0, s, a);
+    const dim3 grid((unsigned)((a.T + kRowsPer - 1) / kRowsPer));
+    if (grid.x > 0 && a.B <= kStaged) hipLaunchKernelGGL((k_kv_rows<true>), grid, dim3(256), 0, s, a);
+    else if (grid.x > 0) hipLaunchKernelGGL((k_kv_rows<false>), grid, dim3(256), 0, s, a);
+    return (int)hipGetLastError();
+}
+
+int launch_trim(const PagesLaunch &a, void *stream) {
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    if (a.B <= kTrimSmall) {
+        hipLaunchKernelGGL(k_kv_trim, dim3(1), dim3(kThreads), 0, s, a);
+        return (int)hipGetLastError();
+    }
+    const unsigned groups = (unsigned)((a.B + 3) / 4 < 1024 ? (a.B + 3) / 4 : 1024);
+    hipLaunchKernelGGL(k_kv_trim_counts, dim3(groups), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(k_kv_trim_lengths, dim3(1), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL(k_kv_trim_pages, dim3(groups), dim3(256), 0, s, a);
+    return (int)hipGetLastError();
+}
+
+}  // namespace fate

@@ -16,7 +16,7 @@ import ctypes as C
 import functools
 import math
 import os
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import numpy as np
 
@@ -38,7 +38,7 @@ EXPORTS = ["fate_version", "fate_strerror", "fate_pack_dags_size", "fate_pack_da
            "fate_pack_dags_opt", "fate_layout_dags_opt", "fate_score_sweep", "fate_topk_sweep", "fate_plan_wave",
            "fate_simulate", "fate_place_baseline", "fate_sim_ws_size", "fate_simulate_device",
            "fate_place_baseline_device", "fate_kv_append", "fate_attn_paged_ws_size", "fate_attn_paged",
-           "fate_attn_prompt"]
+           "fate_attn_prompt", "fate_kv_reserve", "fate_kv_trim"]
 
 # Scoring variants and packing options (fate_params_t.flags, fate_pack_opts_t.levels).
 FATE_MEAN_PER_LEVEL, FATE_NO_WINDOWS = 1, 2
@@ -131,6 +131,12 @@ class Seqs(C.Structure):
                 ("off", C.c_void_p), ("kv_len", C.c_void_p), ("pages", C.c_void_p)]
 
 
+class KvTables(C.Structure):
+    _fields_ = [("B", C.c_int32), ("max_pages", C.c_int32), ("page_size", C.c_int32), ("n_pages", C.c_int32),
+                ("pages_stride", C.c_int64), ("pages", C.c_void_p), ("free", C.c_void_p), ("n_free", C.c_void_p),
+                ("kv_len", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -194,6 +200,9 @@ def load(path: Optional[str] = None):
                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
     lib.fate_attn_prompt.argtypes = [P(Heads), P(Seqs), P(Rows), P(Rows), P(Rows), C.c_float, P(Rows), C.c_void_p,
                                      C.c_void_p, C.c_void_p]
+    lib.fate_kv_reserve.argtypes = [P(KvTables), C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                    C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+    lib.fate_kv_trim.argtypes = [P(KvTables), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
     for name in EXPORTS[2:]:
         getattr(lib, name).restype = st
     if path is None:
@@ -700,7 +709,7 @@ class _Torch:
     def __init__(self):
         import torch
         self.types = {torch.bfloat16: FATE_BF16, torch.float16: FATE_F16}
-        self.int32, self.float32, self.uint8 = torch.int32, torch.float32, torch.uint8
+        self.int32, self.int64, self.float32, self.uint8 = torch.int32, torch.int64, torch.float32, torch.uint8
         self.empty, self.empty_like, self.Tensor = torch.empty, torch.empty_like, torch.Tensor
         self.device, self.stream = torch.cuda.device, torch.cuda.stream
         self.current_device = torch.cuda.current_device
@@ -731,8 +740,9 @@ def _there(device, stream, call, *args, **more):
         with _t.stream(stream):
             result = call(*args, **more)
         for x in args:
-            if isinstance(x, _t.Tensor):
-                x.record_stream(stream)
+            for y in x if isinstance(x, tuple) else (x,):
+                if isinstance(y, _t.Tensor):
+                    y.record_stream(stream)
         return result
 
 
@@ -960,6 +970,110 @@ def fate_attn_prompt(q, k, v, off, scale: Optional[float] = None, lse: bool = Fa
     if st != FATE_OK:
         raise FateError(st, "fate_attn_prompt")
     return out, sums
+
+
+class Reserved(NamedTuple):
+    """What :func:`fate_kv_reserve` returns, or writes to: off [B + 1], kv_len [B], n_free [1], taken [B + 1], slots [T]
+    int64, positions [T]; the others int32."""
+
+    off: object
+    kv_len: object
+    n_free: object
+    taken: object
+    slots: object
+    positions: object
+
+
+class Trimmed(NamedTuple):
+    """What :func:`fate_kv_trim` returns, or writes to: kv_len [B], n_free [1], given [B + 1], int32."""
+
+    kv_len: object
+    n_free: object
+    given: object
+
+
+def _ints_of(t, name, n, dtype, device):
+    """A contiguous tensor of n whole numbers."""
+    if t.dtype is not dtype or t.device != device or t.shape != (n,) or (n > 1 and t.stride(0) != 1):
+        raise ValueError("%s must be a contiguous %s tensor of %d elements on %s, got %s %s on %s" % (
+            name, dtype, n, device, t.dtype, list(t.shape), t.device))
+    return t.data_ptr()
+
+
+def _kv_tables(counts, name, kv_len, pages, free, n_free, page_size, device) -> KvTables:
+    int32 = _t.int32
+    if kv_len.dim() != 1 or pages.dim() != 2 or pages.shape[0] != kv_len.shape[0] or free.dim() != 1:
+        raise ValueError("kv_len must be [B], pages [B, max_pages] and free [n_pages], got %s, %s and %s" % (
+            list(kv_len.shape), list(pages.shape), list(free.shape)))
+    B, width = pages.shape
+    _ints_of(counts, name, B, int32, device)
+    row, one = pages.stride()
+    if pages.dtype is not int32 or pages.device != device or (one != 1 and width > 1):
+        raise ValueError("pages must be int32 on %s, each row contiguous" % device)
+    return KvTables(B, width, page_size, free.shape[0], row if B > 1 else width, pages.data_ptr(),
+                    _ints_of(free, "free", free.shape[0], int32, device), _ints_of(n_free, "n_free", 1, int32, device),
+                    _ints_of(kv_len, "kv_len", B, int32, device))
+
+
+def fate_kv_reserve(new, kv_len, pages, free, n_free, page_size: int, T: int, out: Optional[Reserved] = None, status=None,
+                    stream=None) -> Reserved:
+    """Room for new[b] tokens behind each sequence's keys: pages off the stack
+    free[:n_free], entered in ``pages``, and the arrays of the calls that follow.
+
+    new, kv_len [B], pages [B, max_pages], free [n_pages] and n_free [1] int32 on
+    the device; T, the rows of the call, is at least the sum of new.  Returns
+    :class:`Reserved`: off and kv_len (the new tokens among them) as
+    :func:`fate_kv_append` and the attention calls take them, what is left on
+    the stack, the pages taken before each sequence, and each row's slot
+    (page * page_size + place) and position, -1 behind the last row.  ``out``
+    names tensors to write to; its kv_len and n_free may be the call's own, its
+    slots and positions None.  ``status`` (int32 [B], cleared by the caller)
+    receives FATE_ESIZE for sequences that found too few pages or rows, which
+    get nothing, FATE_EINVAL for those in error."""
+    dev = pages.device
+    if not _here(dev, stream):
+        return _there(dev, stream, fate_kv_reserve, new, kv_len, pages, free, n_free, page_size, T, out, status)
+    int32, int64 = _t.int32, _t.int64
+    t = _kv_tables(new, "new", kv_len, pages, free, n_free, page_size, dev)
+    B = t.B
+    if out is None:
+        if T < 0:
+            raise ValueError("T must not be negative, got %d" % T)
+        n = _t.empty(3 * B + 3, dtype=int32, device=dev)
+        out = Reserved(n[:B + 1], n[B + 1:2 * B + 1], n[2 * B + 1:2 * B + 2], n[2 * B + 2:],
+                       _t.empty(T, dtype=int64, device=dev), _t.empty(T, dtype=int32, device=dev))
+    st = load().fate_kv_reserve(
+        t, new.data_ptr(), T, _ints_of(out.off, "out.off", B + 1, int32, dev), _ints_of(out.kv_len, "out.kv_len", B, int32, dev),
+        _ints_of(out.n_free, "out.n_free", 1, int32, dev), _ints_of(out.taken, "out.taken", B + 1, int32, dev),
+        None if out.slots is None else _ints_of(out.slots, "out.slots", T, int64, dev),
+        None if out.positions is None else _ints_of(out.positions, "out.positions", T, int32, dev),
+        _attn_status(status, B, dev), _t.raw_stream(dev.index))
+    if st != FATE_OK:
+        raise FateError(st, "fate_kv_reserve")
+    return out
+
+
+def fate_kv_trim(keep, kv_len, pages, free, n_free, page_size: int, out: Optional[Trimmed] = None, status=None,
+                 stream=None) -> Trimmed:
+    """Cut each sequence to its first keep[b] keys: pages that hold none of
+    these go back on the stack ``free``, which is written behind n_free;
+    ``pages`` is only read.  Arguments as for :func:`fate_kv_reserve`."""
+    dev = pages.device
+    if not _here(dev, stream):
+        return _there(dev, stream, fate_kv_trim, keep, kv_len, pages, free, n_free, page_size, out, status)
+    int32 = _t.int32
+    t = _kv_tables(keep, "keep", kv_len, pages, free, n_free, page_size, dev)
+    B = t.B
+    if out is None:
+        n = _t.empty(2 * B + 2, dtype=int32, device=dev)
+        out = Trimmed(n[:B], n[B:B + 1], n[B + 1:])
+    st = load().fate_kv_trim(t, keep.data_ptr(), _ints_of(out.kv_len, "out.kv_len", B, int32, dev),
+                             _ints_of(out.n_free, "out.n_free", 1, int32, dev),
+                             _ints_of(out.given, "out.given", B + 1, int32, dev), _attn_status(status, B, dev),
+                             _t.raw_stream(dev.index))
+    if st != FATE_OK:
+        raise FateError(st, "fate_kv_trim")
+    return out
 
 
 def rotation_table(positions: int, rot: int, base: float = 10000.0, device="cuda"):

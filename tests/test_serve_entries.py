@@ -1,0 +1,49 @@
+"""What the calls around a wave's attention refuse on the host, before anything reaches a GPU."""
+
+import pytest
+
+from paper_2605_07238_amd import fate
+
+A = 1 << 20  # an aligned address that is never read
+EINVAL, ERANGE = -1, -2
+
+
+def kv_tables(**x):
+    return fate.KvTables(**dict(dict(B=3, max_pages=4, page_size=16, n_pages=9, pages_stride=4, pages=A, free=A, n_free=A,
+                                     kv_len=A), **x))
+
+
+def reserve(t=None, new=A, T=7, off=A, kv=A, n=A, taken=A, slots=A, positions=A):
+    return fate.load().fate_kv_reserve(t or kv_tables(), new, T, off, kv, n, taken, slots, positions, None, None)
+
+
+def trim(t=None, keep=A, kv=A, n=A, given=A):
+    return fate.load().fate_kv_trim(t or kv_tables(), keep, kv, n, given, None, None)
+
+
+BAD_TABLES = [(dict(B=-1), EINVAL), (dict(max_pages=-1), EINVAL), (dict(n_pages=-1), EINVAL), (dict(pages_stride=-4), EINVAL),
+              (dict(page_size=0), EINVAL), (dict(page_size=-16), EINVAL), (dict(page_size=24), EINVAL),
+              (dict(page_size=2048), ERANGE), (dict(max_pages=1 << 27, pages_stride=1 << 27), ERANGE),
+              (dict(B=(1 << 24) + 1), ERANGE), (dict(pages_stride=3), EINVAL), (dict(pages=None), EINVAL),
+              (dict(pages=A + 2), EINVAL), (dict(free=None), EINVAL), (dict(n_free=None), EINVAL), (dict(n_free=A + 1), EINVAL),
+              (dict(kv_len=None), EINVAL)]
+
+
+@pytest.mark.parametrize("bad,status", BAD_TABLES, ids=str)
+def test_tables(bad, status):
+    for f in (reserve, trim):
+        assert f(t=kv_tables(**bad)) == status
+
+
+def test_reserve():
+    assert fate.load().fate_kv_reserve(None, A, 7, A, A, A, A, A, A, None, None) == EINVAL
+    assert reserve(T=-1) == EINVAL and reserve(T=1 << 31) == ERANGE and reserve(T=1 << 62) == ERANGE
+    for name in ("new", "off", "kv", "n", "taken"):
+        assert reserve(**{name: None}) == EINVAL and reserve(**{name: A + 2}) == EINVAL
+    assert reserve(slots=A + 4) == EINVAL and reserve(positions=A + 2) == EINVAL
+
+
+def test_trim():
+    assert fate.load().fate_kv_trim(None, A, A, A, A, None, None) == EINVAL
+    for name in ("keep", "kv", "n", "given"):
+        assert trim(**{name: None}) == EINVAL and trim(**{name: A + 2}) == EINVAL
