@@ -637,6 +637,31 @@ fate_status_t fate_kv_append(const fate_heads_t *heads, const fate_seqs_t *seqs,
                              int32_t rot, int32_t interleaved, const fate_kv_cache_t *cache,
                              const fate_rows_t *q_out, int32_t *d_status, void *stream);
 
+/* Rotation by several axes (time, height and width of an image's or a video's
+ * patches): pair j of a row turns by the token's position on axis pair_axis[j].
+ *   pair_axis[rot/2]  host memory, entries 0 .. n_axes - 1, n_axes 1 .. FATE_MAX_AXES:
+ *                     sections one behind the other, in turn, or any other way
+ *   positions         device memory: token t's position on axis x is
+ *                     positions[x * stride + t] */
+#define FATE_MAX_AXES 4
+typedef struct {
+    int32_t n_axes;
+    const uint8_t *pair_axis;
+    const int32_t *positions;
+    int64_t stride;
+} fate_axes_t;
+
+/* fate_kv_append_axes: fate_kv_append with table rows chosen by `axes` (a row's
+ * place in the cache is still its position in its sequence).  A position on
+ * any axis outside 0 .. table_rows - 1 is an error of its sequence; those of
+ * rows without a place are not looked at.
+ * Errors: as fate_kv_append, and EINVAL (rot 0, axes), ERANGE (n_axes). */
+fate_status_t fate_kv_append_axes(const fate_heads_t *heads, const fate_seqs_t *seqs, const fate_rows_t *q,
+                                  const fate_rows_t *k, const fate_rows_t *v, const float *table, int64_t table_rows,
+                                  int32_t rot, int32_t interleaved, const fate_axes_t *axes,
+                                  const fate_kv_cache_t *cache, const fate_rows_t *q_out, int32_t *d_status,
+                                  void *stream);
+
 /* fate_attn_paged_ws_size: device workspace bytes fate_attn_paged needs for
  * these heads, sequences (B, T, max_pages) and max_new.  Errors: EINVAL,
  * ERANGE. */

@@ -36,6 +36,11 @@ struct AppendLaunch {
     int64_t table_rows;
     int32_t hq, hkv, d, rot, interleaved, dtype;
     int32_t past_cache;  // the call moves more than the last-level cache holds
+    // rotation by several axes: each token's position on each, and the pairs' axes, two bits a pair
+    const int32_t *positions;
+    int64_t positions_stride;
+    int32_t n_axes;
+    uint32_t axis[FATE_MAX_HEAD_DIM / 2 / 16];
 };
 int launch_append(const AppendLaunch &a, void *stream);
 

@@ -123,14 +123,11 @@ fate_status_t fill(AttnLaunch &a, const fate_heads_t *h, const fate_rows_t *q, c
     return FATE_OK;
 }
 
-}  // namespace
-
-extern "C" {
-
-fate_status_t fate_kv_append(const fate_heads_t *heads, const fate_seqs_t *seqs, const fate_rows_t *q,
-                             const fate_rows_t *k, const fate_rows_t *v, const float *table, int64_t table_rows,
-                             int32_t rot, int32_t interleaved, const fate_kv_cache_t *cache,
-                             const fate_rows_t *q_out, int32_t *d_status, void *stream) {
+// `axes`: rotation by several axes, or null.
+fate_status_t append(const fate_heads_t *heads, const fate_seqs_t *seqs, const fate_rows_t *q, const fate_rows_t *k,
+                     const fate_rows_t *v, const float *table, int64_t table_rows, int32_t rot, int32_t interleaved,
+                     const fate_axes_t *axes, const fate_kv_cache_t *cache, const fate_rows_t *q_out, int32_t *d_status,
+                     void *stream) {
     fate_status_t st = check_heads(heads);
     if (st != FATE_OK || (st = check_sizes(heads, seqs)) != FATE_OK ||
         (st = check_cache(heads, seqs, cache)) != FATE_OK)
@@ -138,6 +135,12 @@ fate_status_t fate_kv_append(const fate_heads_t *heads, const fate_seqs_t *seqs,
     if (rot < 0 || rot > heads->head_dim || rot % 2 || table_rows < 0 || (interleaved != 0 && interleaved != 1))
         return FATE_EINVAL;
     if (rot && (!table || reinterpret_cast<uintptr_t>(table) % 4)) return FATE_EINVAL;
+    if (axes) {
+        if (rot < 2 || axes->n_axes < 1 || !axes->pair_axis || axes->stride < 0) return FATE_EINVAL;
+        if (axes->n_axes > FATE_MAX_AXES) return FATE_ERANGE;
+        for (int j = 0; j < rot / 2; ++j)
+            if (axes->pair_axis[j] >= axes->n_axes) return FATE_EINVAL;
+    }
     if (!q != !q_out) return FATE_EINVAL;
     if (seqs->T == 0 || seqs->B == 0) return FATE_OK;
     if (fate::append_grid(seqs->T) > kMaxGrid) return FATE_ERANGE;
@@ -145,6 +148,7 @@ fate_status_t fate_kv_append(const fate_heads_t *heads, const fate_seqs_t *seqs,
         return FATE_EINVAL;
     if (q && (!good_rows(q) || !good_out(q_out, heads))) return FATE_EINVAL;
     if (q && q->data == q_out->data && (q->token != q_out->token || q->head != q_out->head)) return FATE_EINVAL;
+    if (axes && (!axes->positions || reinterpret_cast<uintptr_t>(axes->positions) % 4)) return FATE_EINVAL;
     AppendLaunch a = {};
     set_seqs(a.s, seqs, cache);
     set_cache(a.c, cache);
@@ -165,9 +169,35 @@ fate_status_t fate_kv_append(const fate_heads_t *heads, const fate_seqs_t *seqs,
     a.rot = rot;
     a.interleaved = interleaved;
     a.dtype = heads->dtype;
+    if (axes) {
+        a.positions = axes->positions;
+        a.positions_stride = axes->stride;
+        a.n_axes = axes->n_axes;
+        for (int j = 0; j < rot / 2; ++j) a.axis[j / 16] |= (uint32_t)axes->pair_axis[j] << j % 16 * 2;
+    }
     const int64_t bytes = seqs->T * (2 * (int64_t)a.hq + 4 * (int64_t)a.hkv) * a.d * 2;
     a.past_cache = bytes > (int64_t(256) << 20);
     return fate::launch_append(a, stream) == 0 ? FATE_OK : FATE_EHIP;
+}
+
+}  // namespace
+
+extern "C" {
+
+fate_status_t fate_kv_append(const fate_heads_t *heads, const fate_seqs_t *seqs, const fate_rows_t *q,
+                             const fate_rows_t *k, const fate_rows_t *v, const float *table, int64_t table_rows,
+                             int32_t rot, int32_t interleaved, const fate_kv_cache_t *cache,
+                             const fate_rows_t *q_out, int32_t *d_status, void *stream) {
+    return append(heads, seqs, q, k, v, table, table_rows, rot, interleaved, nullptr, cache, q_out, d_status, stream);
+}
+
+fate_status_t fate_kv_append_axes(const fate_heads_t *heads, const fate_seqs_t *seqs, const fate_rows_t *q,
+                                  const fate_rows_t *k, const fate_rows_t *v, const float *table, int64_t table_rows,
+                                  int32_t rot, int32_t interleaved, const fate_axes_t *axes,
+                                  const fate_kv_cache_t *cache, const fate_rows_t *q_out, int32_t *d_status,
+                                  void *stream) {
+    if (!axes) return FATE_EINVAL;
+    return append(heads, seqs, q, k, v, table, table_rows, rot, interleaved, axes, cache, q_out, d_status, stream);
 }
 
 fate_status_t fate_attn_paged_ws_size(const fate_heads_t *heads, const fate_seqs_t *seqs,

@@ -30,15 +30,24 @@ struct Place {
     int pos;        // position; negative: no place
 };
 
+// With several axes: the token's position on each.
+struct Turns {
+    int on[FATE_MAX_AXES];
+};
+
 // VEC: chunks are 16-byte loads (rot / 2 a multiple of 8, or pairs
 // interleaved with rot a multiple of 8); otherwise element by element.
-// PAST: rows are read past the last-level cache.
-template <class T, bool VEC, bool PAST>
+// PAST: rows are read past the last-level cache.  AXES: a pair turns by its
+// axis's position instead of the token's own.  A unit whose pairs are all of
+// one axis reads its cosines and sines as one row's, as with one axis; pairs of
+// different axes read theirs one by one.
+template <class T, bool VEC, bool PAST, bool AXES>
 __global__ __launch_bounds__(256) void k_kv_append(AppendLaunch a, int per_wg, int units, int heads,
                                                    uint32_t heads_inv) {
     typedef typename T::el el;
     typedef typename T::x8 x8;
     __shared__ Place place[kAppendTokens];
+    __shared__ Turns turns[AXES ? kAppendTokens : 1];
     const int tid = threadIdx.x;
     const int64_t t0 = (int64_t)blockIdx.x * per_wg;
     const int toks = (int)min((int64_t)per_wg, a.s.T - t0);
@@ -69,7 +78,15 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendLaunch a, int per_wg, i
                 p.pos = -1;
                 if (pos >= 0) {
                     const int page = a.s.pages[b * a.s.pages_stride + (pos >> a.c.page_shift)];
-                    if (page < 0 || page >= a.c.n_pages || (a.rot && pos >= a.table_rows)) {
+                    bool turned = AXES || !a.rot || pos < a.table_rows;
+                    if (AXES) {
+                        for (int x = 0; x < a.n_axes; ++x) {
+                            const int on = a.positions[x * a.positions_stride + t0 + tid];
+                            turned = turned && on >= 0 && on < a.table_rows;
+                            turns[tid].on[x] = on;
+                        }
+                    }
+                    if (page < 0 || page >= a.c.n_pages || !turned) {
                         if (a.status) a.status[b] = FATE_EINVAL;
                     } else {
                         p.pos = (int)pos;
@@ -99,7 +116,14 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendLaunch a, int per_wg, i
         len1 = max(0, min(8, a.d - e1));
     }
     const bool rotated = pair || (a.interleaved && e0 < a.rot);
-    const int j0 = pair ? e0 : e0 / 2;  // the unit's first pair
+    const int j0 = pair ? e0 : e0 / 2;  // the unit's first pair: a multiple of 8
+    uint32_t axes = 0;                  // of its pairs
+    bool one_axis = true;
+    if (AXES && rotated) {
+        axes = a.axis[j0 / 16] >> (j0 % 16 * 2) & 0xffffu;
+        const uint32_t pairs = (1u << 2 * min(8, half - j0)) - 1;
+        one_axis = ((axes ^ (axes & 3u) * 0x5555u) & pairs) == 0;
+    }
 
     for (int x = hs; x < toks * heads; x += HS) {
         const int tk = heads == 1 ? x : (int)__umulhi((uint32_t)x, heads_inv), h = x - tk * heads;
@@ -128,9 +152,18 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendLaunch a, int per_wg, i
                 }
             }
             if (rotated && (is_q || is_k)) {
-                const float *row = a.table + (int64_t)p.pos * a.rot + j0;
+                const int pos = AXES ? turns[tk].on[axes & 3u] : p.pos;
+                const float *row = a.table + (int64_t)pos * a.rot + j0;
                 float cs[8] = {}, sn[8] = {};
-                if (VEC && j0 + 8 <= half) {
+                if (AXES && !one_axis) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (j0 + e < half) {
+                            const float *at = a.table + (int64_t)turns[tk].on[axes >> 2 * e & 3u] * a.rot + j0 + e;
+                            cs[e] = at[0];
+                            sn[e] = at[half];
+                        }
+                } else if (VEC && j0 + 8 <= half) {
                     __builtin_memcpy(cs, row, 32);
                     __builtin_memcpy(sn, row + half, 32);
                 } else {
@@ -190,9 +223,16 @@ int go(const AppendLaunch &a, hipStream_t s) {
     // multiplier of __umulhi for x / heads: ceil(2^32 / heads), exact while x * heads < 2^32 (x < kAppendTokens * heads)
     const uint32_t inv = heads > 1 ? (uint32_t)((0x100000000ull + heads - 1) / heads) : 0u;
     const dim3 g(grid), b(256);
-    if (vec && a.past_cache) hipLaunchKernelGGL((k_kv_append<T, true, true>), g, b, 0, s, a, per_wg, units, heads, inv);
-    else if (vec) hipLaunchKernelGGL((k_kv_append<T, true, false>), g, b, 0, s, a, per_wg, units, heads, inv);
-    else hipLaunchKernelGGL((k_kv_append<T, false, false>), g, b, 0, s, a, per_wg, units, heads, inv);
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, g, b, 0, s, a, per_wg, units, heads, inv); };
+    if (a.positions) {
+        if (vec && a.past_cache) launch(k_kv_append<T, true, true, true>);
+        else if (vec) launch(k_kv_append<T, true, false, true>);
+        else launch(k_kv_append<T, false, false, true>);
+    } else {
+        if (vec && a.past_cache) launch(k_kv_append<T, true, true, false>);
+        else if (vec) launch(k_kv_append<T, true, false, false>);
+        else launch(k_kv_append<T, false, false, false>);
+    }
     return (int)hipGetLastError();
 }
 

@@ -38,7 +38,7 @@ EXPORTS = ["fate_version", "fate_strerror", "fate_pack_dags_size", "fate_pack_da
            "fate_pack_dags_opt", "fate_layout_dags_opt", "fate_score_sweep", "fate_topk_sweep", "fate_plan_wave",
            "fate_simulate", "fate_place_baseline", "fate_sim_ws_size", "fate_simulate_device",
            "fate_place_baseline_device", "fate_kv_append", "fate_attn_paged_ws_size", "fate_attn_paged",
-           "fate_attn_prompt", "fate_kv_reserve", "fate_kv_trim"]
+           "fate_attn_prompt", "fate_kv_reserve", "fate_kv_trim", "fate_kv_append_axes"]
 
 # Scoring variants and packing options (fate_params_t.flags, fate_pack_opts_t.levels).
 FATE_MEAN_PER_LEVEL, FATE_NO_WINDOWS = 1, 2
@@ -131,6 +131,10 @@ class Seqs(C.Structure):
                 ("off", C.c_void_p), ("kv_len", C.c_void_p), ("pages", C.c_void_p)]
 
 
+class Axes(C.Structure):
+    _fields_ = [("n_axes", C.c_int32), ("pair_axis", C.c_void_p), ("positions", C.c_void_p), ("stride", C.c_int64)]
+
+
 class KvTables(C.Structure):
     _fields_ = [("B", C.c_int32), ("max_pages", C.c_int32), ("page_size", C.c_int32), ("n_pages", C.c_int32),
                 ("pages_stride", C.c_int64), ("pages", C.c_void_p), ("free", C.c_void_p), ("n_free", C.c_void_p),
@@ -200,6 +204,8 @@ def load(path: Optional[str] = None):
                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
     lib.fate_attn_prompt.argtypes = [P(Heads), P(Seqs), P(Rows), P(Rows), P(Rows), C.c_float, P(Rows), C.c_void_p,
                                      C.c_void_p, C.c_void_p]
+    lib.fate_kv_append_axes.argtypes = [P(Heads), P(Seqs), P(Rows), P(Rows), P(Rows), C.c_void_p, C.c_int64, C.c_int32,
+                                        C.c_int32, P(Axes), P(KvCache), P(Rows), C.c_void_p, C.c_void_p]
     lib.fate_kv_reserve.argtypes = [P(KvTables), C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
     lib.fate_kv_trim.argtypes = [P(KvTables), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
@@ -846,6 +852,12 @@ def fate_kv_append(q, k, v, k_cache, v_cache, off, kv_len, pages, table=None, in
                               (q is not None and q.requires_grad) or (table is not None and table.requires_grad) or
                               (q_out is not None and q_out.requires_grad)):
         raise _no_gradient()
+    return _append(q, k, v, k_cache, v_cache, off, kv_len, pages, table, None, interleaved, q_out, status)
+
+
+def _append(q, k, v, k_cache, v_cache, off, kv_len, pages, table, axes, interleaved, q_out, status):
+    """The call itself, on the current device and stream; axes: :class:`Axes` or None."""
+    dev, dtype = k.device, k.dtype
     shape = _three(k, "k")
     T, hkv, d = shape
     c = _attn_cache(k_cache, v_cache, hkv, d, dtype, dev)
@@ -868,11 +880,63 @@ def fate_kv_append(q, k, v, k_cache, v_cache, off, kv_len, pages, table=None, in
         ro = _rows(q_out, "q_out", shape, dtype, dev)
     elif q_out is not None:
         raise ValueError("q_out without q")
-    st = load().fate_kv_append(_attn_heads(dtype, shape, hkv), s, rq, rk, rv, turns, positions, rot,
-                               1 if interleaved else 0, c, ro, _attn_status(status, s.B, dev), _t.raw_stream(dev.index))
+    heads, state, stream = _attn_heads(dtype, shape, hkv), _attn_status(status, s.B, dev), _t.raw_stream(dev.index)
+    if axes is None:
+        st = load().fate_kv_append(heads, s, rq, rk, rv, turns, positions, rot, 1 if interleaved else 0, c, ro, state, stream)
+    else:
+        st = load().fate_kv_append_axes(heads, s, rq, rk, rv, turns, positions, rot, 1 if interleaved else 0, axes, c, ro,
+                                        state, stream)
     if st != FATE_OK:
-        raise FateError(st, "fate_kv_append")
+        raise FateError(st, "fate_kv_append" if axes is None else "fate_kv_append_axes")
     return q_out
+
+
+def fate_kv_append_axes(q, k, v, k_cache, v_cache, off, kv_len, pages, table, positions, axis, interleaved: bool = False,
+                        q_out=None, status=None, stream=None):
+    """:func:`fate_kv_append` for tokens with positions on several axes, as the
+    patches of images and videos have (time, height, width): pair j is rotated
+    by the table's row of the token's position on axis axis[j].
+
+    positions [axes, T] int32 on the device (each axis contiguous), up to four
+    axes; axis: a tuple of rot / 2 axis numbers (see :func:`rotation_axes`).  A
+    token's place in the cache follows from kv_len as before.  A position
+    outside the table is an error of its sequence."""
+    dev = k.device
+    if not _here(dev, stream):
+        return _there(dev, stream, fate_kv_append_axes, q, k, v, k_cache, v_cache, off, kv_len, pages, table, positions, axis,
+                      interleaved, q_out, status)
+    if _t.grad_enabled() and (k.requires_grad or v.requires_grad or k_cache.requires_grad or v_cache.requires_grad or
+                              (q is not None and q.requires_grad) or table.requires_grad or
+                              (q_out is not None and q_out.requires_grad)):
+        raise _no_gradient()
+    T = k.shape[0]
+    if positions.dtype is not _t.int32 or positions.device != dev or positions.dim() != 2 or positions.shape[1] != T:
+        raise ValueError("positions must be int32 [axes, %d] on %s, got %s %s on %s" % (
+            T, dev, positions.dtype, list(positions.shape), positions.device))
+    row, one = positions.stride()
+    if one != 1 and T > 1:
+        raise ValueError("each axis of positions must be contiguous")
+    if 2 * len(axis) != table.shape[-1]:
+        raise ValueError("axis must name one for each of the table's %d pairs, got %d" % (table.shape[-1] // 2, len(axis)))
+    of_pairs = _pair_axis(tuple(axis))
+    return _append(q, k, v, k_cache, v_cache, off, kv_len, pages, table,
+                   Axes(positions.shape[0], C.addressof(of_pairs), positions.data_ptr(), row), interleaved, q_out, status)
+
+
+@functools.lru_cache(maxsize=256)
+def _pair_axis(axis):
+    if not all(0 <= a < 256 for a in axis):
+        raise ValueError("axes are numbered from 0, got %s" % (axis,))
+    return (C.c_uint8 * max(1, len(axis)))(*axis)
+
+
+def rotation_axes(sections, cyclic: bool = False):
+    """Axes of the pairs for :func:`fate_kv_append_axes` from the number of
+    pairs that each axis has: one section behind the other, or, cyclic, one
+    pair of each in turn while it has any left."""
+    if not cyclic:
+        return tuple(a for a, n in enumerate(sections) for _ in range(n))
+    return tuple(a for i in range(max(sections, default=0)) for a, n in enumerate(sections) if i < n)
 
 
 def fate_attn_paged(q, k_cache, v_cache, off, kv_len, pages, max_new: Optional[int] = None, scale: Optional[float] = None,

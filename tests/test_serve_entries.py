@@ -1,8 +1,11 @@
 """What the calls around a wave's attention refuse on the host, before anything reaches a GPU."""
 
+import ctypes as C
+
 import pytest
 
 from paper_2605_07238_amd import fate
+from test_attn_entries import cache, heads, rows, seqs
 
 A = 1 << 20  # an aligned address that is never read
 EINVAL, ERANGE = -1, -2
@@ -47,3 +50,21 @@ def test_trim():
     assert fate.load().fate_kv_trim(None, A, A, A, A, None, None) == EINVAL
     for name in ("keep", "kv", "n", "given"):
         assert trim(**{name: None}) == EINVAL and trim(**{name: A + 2}) == EINVAL
+
+
+def test_axes():
+    names = (C.c_uint8 * 32)(*([0] * 10 + [1] * 10 + [2] * 12))
+    good = dict(n_axes=3, pair_axis=C.addressof(names), positions=A, stride=6)
+
+    def append(rot=64, k="", **x):
+        axes = fate.Axes(**dict(good, **x)) if x.get("n_axes", 1) is not None else None
+        return fate.load().fate_kv_append_axes(heads(), seqs(), rows(), rows() if k == "" else k, rows(), A, 9, rot, 0, axes, cache(),
+                                               rows(), None, None)
+
+    for bad, status in ((dict(n_axes=None), EINVAL), (dict(n_axes=0), EINVAL), (dict(n_axes=2), EINVAL), (dict(n_axes=5), ERANGE),
+                        (dict(pair_axis=None), EINVAL), (dict(positions=None), EINVAL), (dict(positions=A + 2), EINVAL),
+                        (dict(stride=-1), EINVAL), (dict(rot=0), EINVAL), (dict(rot=63), EINVAL), (dict(k=None), EINVAL)):
+        assert append(**bad) == status, bad
+    assert fate.rotation_axes((2, 1, 3)) == (0, 0, 1, 2, 2, 2)
+    assert fate.rotation_axes((2, 1, 3), cyclic=True) == (0, 1, 2, 0, 2, 2)
+    assert fate.rotation_axes(()) == fate.rotation_axes((), cyclic=True) == ()
