@@ -699,6 +699,43 @@ fate_status_t fate_attn_prompt(const fate_heads_t *heads, const fate_seqs_t *seq
                                const fate_rows_t *k, const fate_rows_t *v, float scale, const fate_rows_t *out,
                                float *d_lse, int32_t *d_status, void *stream);
 
+/* Shaped scores.  With s = scale q.k of the row at position p and the key at
+ * position j of its sequence:
+ *   cap     s becomes cap tanh(s / cap); 0 for none
+ *   slopes  [heads_q] float32 or null: s becomes s - slopes[head] |p - j| (after
+ *           the cap)
+ *   prefix  [B] or null: the first prefix[b] keys of sequence b (all it has, if
+ *           fewer) are seen by every row of it, also by rows that stand before
+ *           them; below 0 counts as 0
+ *   start   [T] or null: a row sees the keys from start[t] on (and the prefix's):
+ *           its document's first, or p - w + 1 for a window of w keys.  Within
+ *           a sequence start must not fall from a row to the next (max(start, 0)
+ *           counts); where it does, the sequence is in error
+ * A row thus sees key j when j < prefix, or start <= j <= p.  One that sees
+ * none (start past p and no prefix, or p < 0: it stands before the sequence,
+ * and the prefix is not for it) gets zeros and -infinity.  slopes, prefix and
+ * start are device memory. */
+typedef struct {
+    float cap;
+    const float *slopes;
+    const int32_t *prefix, *start;
+} fate_scores_t;
+
+/* fate_attn_paged_shaped, fate_attn_prompt_shaped: fate_attn_paged (its
+ * workspace, its size and all else alike) and fate_attn_prompt with the scores
+ * so shaped.  Keys that no row of a row tile sees are not read: the cost goes
+ * with what is seen.  A capped score is off by some 2^-22 of the cap.
+ * Errors: as those, and EINVAL (null scores, cap negative or not finite, or so
+ * far from scale that their quotient leaves float32, alignment). */
+fate_status_t fate_attn_paged_shaped(const fate_heads_t *heads, const fate_seqs_t *seqs, const fate_rows_t *q,
+                                     const fate_kv_cache_t *cache, int64_t max_new, float scale,
+                                     const fate_scores_t *scores, const fate_rows_t *out, float *d_lse,
+                                     int32_t *d_status, void *d_ws, size_t ws_bytes, void *stream);
+fate_status_t fate_attn_prompt_shaped(const fate_heads_t *heads, const fate_seqs_t *seqs, const fate_rows_t *q,
+                                      const fate_rows_t *k, const fate_rows_t *v, float scale,
+                                      const fate_scores_t *scores, const fate_rows_t *out, float *d_lse,
+                                      int32_t *d_status, void *stream);
+
 /* Page tables of the cache, kept on the device: `pages` as in fate_seqs_t (its
  * rows do not overlap), and a stack of the pages that no sequence has.
  *   free[n_pages]  free[0 .. n_free - 1] are free pages, the next to be taken last

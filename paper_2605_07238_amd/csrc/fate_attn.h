@@ -68,8 +68,14 @@ struct AttnLaunch {
     int32_t hq, hkv, G, d, dtype;
     int32_t pieces;   // paged calls: shares of the work axis (few rows), or parts aimed at (row tiles), per key head
     int32_t grid;     // workgroups per key head
+    // shaped scores (shaped = 1; otherwise causal ones, and none of these is read)
+    int32_t shaped, cap_wide;
+    float cap_log2, cap_in;  // cap log2(e) and 2 scale log2(e) / cap, or 0 for no cap
+    const float *slopes;     // [hq] or null
+    const int32_t *prefix, *start;  // [B], [T] or null
 };
 int launch_attn_tile(const AttnLaunch &a, bool paged, void *stream);
+int launch_attn_tile_shaped(const AttnLaunch &a, bool paged, void *stream);
 int launch_attn_few(const AttnLaunch &a, int rows, void *stream);
 int launch_attn_join(const AttnLaunch &a, int rows, int tiles, int groups, void *stream);
 
@@ -145,7 +151,7 @@ struct F16 {
 // Lowest finite value: the running maximum of rows that have seen no key yet.
 // Differences from it are finite or -infinity, never NaN.
 constexpr float kLowest = -3.402823466e38f;
-constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 
 // Nonzero if one of the pair's halves is an infinity or a NaN: the exponent
 // bits, plus their lowest bit, carry into the sign's place.
@@ -162,6 +168,23 @@ __device__ __forceinline__ uint32_t only_finite(uint32_t x) {
 }
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// cap tanh(s scale / cap) in log2 units, with cap_in = 2 scale log2(e) / cap and
+// cap in log2 units: cap - 2 cap / (1 + e^(2 s scale / cap)), which holds at
+// infinities too.  Its error is some 2^-23 of the cap, so that caps far over the
+// scores (over 100 in log2) take the odd series of tanh, to x^9, below 1/4 (the
+// next term is 2^-26 of it there).
+__device__ __forceinline__ float capped(float s, float cap_in, float cap) {
+    return __builtin_fmaf(-2.0f * cap, __builtin_amdgcn_rcpf(1.0f + exp2_fast(s * cap_in)), cap);
+}
+__device__ __forceinline__ float capped_wide(float s, float cap_in, float cap) {
+    const float x = s * (cap_in * (0.5f * kLn2)), y = x * x;
+    float f = __builtin_fmaf(y, 62.0f / 2835.0f, -17.0f / 315.0f);
+    f = __builtin_fmaf(y, f, 2.0f / 15.0f);
+    f = __builtin_fmaf(y, f, -1.0f / 3.0f);
+    f = __builtin_fmaf(x * y, f, x) * cap;
+    return __builtin_fabsf(x) < 0.25f ? f : capped(s, cap_in, cap);
+}
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ int64_t uniform64(int64_t x) {
@@ -215,15 +238,38 @@ __device__ __forceinline__ I wave_sum(I x) { return lane_of(wave_scan_add(x), 63
 // out of range (`report`: say so in the status).
 struct Lens {
     int lo, n, L;
+    int gap;  // shaped: keys between the prefix and the first row's first key, in whole key tiles, that no row sees
 };
+
+// The keys that a row sees: 0 .. pre - 1 and first .. end - 1.
+struct Seen {
+    int pre, first, end;
+    __device__ __forceinline__ bool has(int key) const { return key < pre || (key >= first && key < end); }
+};
+
+// Of rows of neighbouring tokens, whose first keys do not fall from one to the
+// next: keys below `most` and not in pre .. from - 1 are seen by some row; all
+// rows see keys below all_pre and all_from .. all_to - 1.
+struct Span {
+    int pre, from, most, all_pre, all_from, all_to;
+    __device__ __forceinline__ bool all(int key, int n) const {
+        return key + n <= all_pre || (key >= all_from && key + n <= all_to);
+    }
+};
+
+// Key blocks of N that a span's rows do not see, behind the blocks of the prefix.
+template <int N>
+__device__ __forceinline__ int blocks_unseen(int pre, int from, int most) {
+    return max(0, min(from, most) / N - (pre + N - 1) / N);
+}
 
 // Lane i: sequence at + i.  `reach`: the largest offset before the group, 0
 // for the first; on return, before the next one.  A sequence that starts below
 // an earlier offset is out of range: those that are not hold different rows,
 // in order, so that the tiles that the host counts from T and B are enough.
-template <bool PAGED, class A>
+template <bool PAGED, bool SHAPED = false, class A>
 __device__ __forceinline__ Lens read_lens(const A &a, int at, int lane, int &reach, bool report) {
-    Lens s = {0, 0, 0};
+    Lens s = {0, 0, 0, 0};
     const int b = at + lane;
     int hi = 0;
     if (b < a.s.B) {
@@ -240,6 +286,12 @@ __device__ __forceinline__ Lens read_lens(const A &a, int at, int lane, int &rea
     if (bad || b >= a.s.B) {
         s.lo = s.n = s.L = 0;
         if (report && a.status && b < a.s.B) a.status[b] = FATE_EINVAL;
+    }
+    if constexpr (SHAPED) {
+        if (a.start && s.n > 0) {
+            const int pre = a.prefix ? min(max(0, a.prefix[b]), s.L) : 0;
+            s.gap = blocks_unseen<kKeyTile>(pre, max(0, a.start[s.lo]), s.L) * kKeyTile;
+        }
     }
     return s;
 }
@@ -267,18 +319,18 @@ struct Group {
     int reach;
 };
 
-template <bool PAGED, class A>
+template <bool PAGED, bool SHAPED = false, class A>
 __device__ __forceinline__ Group first_group(const A &a, int lane, bool report) {
     Group g;
     g.reach = 0;
-    g.lens = read_lens<PAGED>(a, 0, lane, g.reach, report);
+    g.lens = read_lens<PAGED, SHAPED>(a, 0, lane, g.reach, report);
     return g;
 }
 
 // The group from sequence `at` on: `first`, or read; `reach` as in read_lens.
-template <bool PAGED, class A>
+template <bool PAGED, bool SHAPED = false, class A>
 __device__ __forceinline__ Lens group_at(const A &a, int at, int lane, const Group &first, int &reach) {
-    if (at > 0) return read_lens<PAGED>(a, at, lane, reach, false);
+    if (at > 0) return read_lens<PAGED, SHAPED>(a, at, lane, reach, false);
     reach = first.reach;
     return first.lens;
 }
@@ -292,6 +344,43 @@ struct Unit {
     int64_t start, cost;  // its place on the work axis (paged calls)
     bool ok;
 };
+
+// The keys that token `tok` of the unit's sequence sees.
+template <bool SHAPED, class A>
+__device__ __forceinline__ Seen seen_by(const A &a, const Unit &u, int tok, bool live) {
+    const int end = tok + (u.L - u.n + 1);
+    Seen s = {0, 0, live ? max(0, min(u.L, end)) : 0};
+    if constexpr (SHAPED) {
+        if (live && end > 0) {
+            if (a.prefix) s.pre = min(max(0, a.prefix[u.b]), u.L);
+            if (a.start) {
+                s.first = max(0, a.start[u.lo_row + (int64_t)tok]);
+                // (reported, not relied on: any order reads within the sequence's keys)
+                if (tok > 0 && a.start[u.lo_row + (int64_t)tok - 1] > s.first && a.status) a.status[u.b] = FATE_EINVAL;
+            }
+        }
+    }
+    return s;
+}
+
+// Of its tokens t0 to t1.
+template <class A>
+__device__ __forceinline__ Span span_of(const A &a, const Unit &u, int t0, int t1) {
+    const int end0 = t0 + (u.L - u.n + 1), end1 = t1 + (u.L - u.n + 1);
+    const int pre = a.prefix ? min(max(0, a.prefix[u.b]), u.L) : 0;
+    const int first0 = a.start ? max(0, a.start[u.lo_row + (int64_t)t0]) : 0;
+    const int first1 = a.start ? max(0, a.start[u.lo_row + (int64_t)t1]) : 0;
+    Span s;
+    s.pre = end1 > 0 ? pre : 0;
+    s.most = end1 > 0 ? max(min(u.L, end1), pre) : 0;
+    s.from = first0;
+    s.all_pre = end0 > 0 ? pre : 0;
+    s.all_from = first1 <= s.all_pre ? 0 : first1;
+    s.all_to = end0 <= 0 ? 0 : first1 <= s.all_pre ? max(min(u.L, end0), pre) : min(u.L, end0);
+    s.pre = uniform(s.pre), s.most = uniform(s.most), s.from = uniform(s.from);
+    s.all_pre = uniform(s.all_pre), s.all_from = uniform(s.all_from), s.all_to = uniform(s.all_to);
+    return s;
+}
 
 // ---- calls of few rows: an axis of work, equal shares -----------------------
 // The work axis of a paged call.  Its row tiles lie on it one after the other,
@@ -316,15 +405,15 @@ __device__ __forceinline__ int64_t axis_keys(int n, int L, int G) {
 }
 
 __device__ __forceinline__ int64_t seq_cost(const Lens &s, int G, int M) {
-    return tile_start(tiles_of(s.n * G, M), axis_keys(s.n, s.L, G), M);
+    return tile_start(tiles_of(s.n * G, M), axis_keys(s.n, s.L - s.gap, G), M);
 }
 
 // `first`: the first 64 sequences, which most calls end with.
-template <class A>
+template <bool SHAPED = false, class A>
 __device__ __forceinline__ Axis axis_of(const A &a, int M, const Group &first, int lane, bool report) {
     int64_t sum = seq_cost(first.lens, a.G, M);
     int reach = first.reach;
-    for (int at = 64; at < a.s.B; at += 64) sum += seq_cost(read_lens<true>(a, at, lane, reach, report), a.G, M);
+    for (int at = 64; at < a.s.B; at += 64) sum += seq_cost(read_lens<true, SHAPED>(a, at, lane, reach, report), a.G, M);
     Axis x;
     x.total = wave_sum(sum);
     const int64_t least_share = (int64_t)kFewLeast * kKeyTile * a.G;
@@ -341,7 +430,7 @@ struct Search {
 };
 
 // The row tile at place x < total of the axis.
-template <class A>
+template <bool SHAPED = false, class A>
 __device__ __forceinline__ Unit unit_at(const A &a, int M, const Group &first, int64_t x, int lane, Search &from) {
     Unit u;
     u.ok = false;
@@ -349,7 +438,7 @@ __device__ __forceinline__ Unit unit_at(const A &a, int M, const Group &first, i
     int reach = from.reach;
     for (int at = from.at; at < a.s.B; at += 64) {
         const int reach0 = reach;
-        const Lens s = group_at<true>(a, at, lane, first, reach);
+        const Lens s = group_at<true, SHAPED>(a, at, lane, first, reach);
         const int64_t mine = seq_cost(s, a.G, M);
         const int64_t end = before + wave_scan_add(mine);
         const uint64_t has = __ballot(x < end);
@@ -361,7 +450,7 @@ __device__ __forceinline__ Unit unit_at(const A &a, int M, const Group &first, i
             u.lo_row = lane_of(s.lo, src);
             u.L = lane_of(s.L, src);
             const int64_t base = lane_of(end - mine, src), y = x - base;
-            const int64_t GA = axis_keys(u.n, u.L, a.G);
+            const int64_t GA = axis_keys(u.n, u.L - (SHAPED ? lane_of(s.gap, src) : 0), a.G);
             const int tiles = tiles_of(u.n * a.G, M);
             int t = 0;
             if (tiles > 1) {
@@ -407,9 +496,10 @@ __device__ __forceinline__ int wave_max(int x) { return lane_of(wave_scan_max(x)
 // Sequences of a group of 64 by decreasing keys, to half an octave: what
 // belongs in this lane's place.  Few steps for the few classes that a batch
 // has (a full sort of 64 took 13 of 68 us of a call of 64 short prompts).
+template <bool SHAPED = false>
 __device__ __forceinline__ void sort_longest(int group, int lane, int &b, Lens &s) {
     constexpr int kTop = 0xff << 1;  // over every class of a 31-bit length
-    const int cls = (int)(__builtin_bit_cast(uint32_t, (float)max(s.L, 1)) >> 22);  // 254 to 314
+    const int cls = (int)(__builtin_bit_cast(uint32_t, (float)max(s.L - s.gap, 1)) >> 22);  // 254 to 314
     const bool in = lane < group;
     const int hi = wave_max(in ? cls : 0), lo = kTop - wave_max(in ? kTop - cls : 0);
     int rank = lane, before = 0;
@@ -421,6 +511,7 @@ __device__ __forceinline__ void sort_longest(int group, int lane, int &b, Lens &
     s.n = __builtin_amdgcn_ds_permute(rank << 2, s.n);
     s.L = __builtin_amdgcn_ds_permute(rank << 2, s.L);
     s.lo = __builtin_amdgcn_ds_permute(rank << 2, s.lo);
+    if (SHAPED) s.gap = __builtin_amdgcn_ds_permute(rank << 2, s.gap);
     b = __builtin_amdgcn_ds_permute(rank << 2, b);
 }
 
@@ -435,16 +526,16 @@ __device__ __forceinline__ int parts_of(int L, int chunk) {
 // fewer row tiles than parts it is raised by eighths, up to twice, until there
 // are no more than `pieces` parts (where the sequences fit the wave's lanes):
 // one part over what runs at once costs a whole round.
-template <class A>
+template <bool SHAPED = false, class A>
 __device__ __forceinline__ int chunk_of(const A &a, int M, const Group &first, int lane, bool report) {
-    const int nt = tiles_of(first.lens.n * a.G, M), kt = tiles_of(first.lens.L, kKeyTile);
+    const int nt = tiles_of(first.lens.n * a.G, M), kt = tiles_of(first.lens.L - first.lens.gap, kKeyTile);
     int64_t sum = (int64_t)nt * kt;
     int units = nt, reach = first.reach;
     for (int at = 64; at < a.s.B; at += 64) {
-        const Lens s = read_lens<true>(a, at, lane, reach, report);
+        const Lens s = read_lens<true, SHAPED>(a, at, lane, reach, report);
         const int t = tiles_of(s.n * a.G, M);
         units += t;
-        sum += (int64_t)t * tiles_of(s.L, kKeyTile);
+        sum += (int64_t)t * tiles_of(s.L - s.gap, kKeyTile);
     }
     const int64_t least = max((wave_sum(sum) + a.pieces - 1) / a.pieces, (int64_t)kTileLeast);
     int chunk = (int)min(least, (int64_t)0x7ffffffe);
@@ -460,15 +551,15 @@ __device__ __forceinline__ int chunk_of(const A &a, int M, const Group &first, i
 // The part with number `item`; JOIN: the row tile with number `item` among
 // those done in parts.  Row tiles of a sequence go from the last, which sees
 // the most keys, to the first.
-template <bool PAGED, bool JOIN, class A>
+template <bool PAGED, bool JOIN, bool SHAPED = false, class A>
 __device__ __forceinline__ Piece find_piece(const A &a, int M, const Group &first, int chunk, int item, int lane) {
     Piece p;
     p.u.ok = false;
     int items = 0, slots = 0, reach = 0;  // before this group of 64 sequences
     for (int at = 0; at < a.s.B; at += 64) {
         int b = at + lane;
-        Lens s = group_at<PAGED>(a, at, lane, first, reach);
-        int nt = tiles_of(s.n * a.G, M), sp = PAGED ? parts_of(s.L, chunk) : 1;
+        Lens s = group_at<PAGED, SHAPED>(a, at, lane, first, reach);
+        int nt = tiles_of(s.n * a.G, M), sp = PAGED ? parts_of(s.L - s.gap, chunk) : 1;
         int mine = JOIN ? (sp > 1 ? nt : 0) : nt * sp, my_slots = sp > 1 ? nt * sp : 0;
         const int group = min(64, a.s.B - at);
         if (at + 64 < a.s.B) {  // not in this group: its sums alone
@@ -480,9 +571,9 @@ __device__ __forceinline__ Piece find_piece(const A &a, int M, const Group &firs
             }
         }
         if (group > 1) {
-            sort_longest(group, lane, b, s);
+            sort_longest<SHAPED>(group, lane, b, s);
             nt = tiles_of(s.n * a.G, M);
-            sp = PAGED ? parts_of(s.L, chunk) : 1;
+            sp = PAGED ? parts_of(s.L - s.gap, chunk) : 1;
             mine = JOIN ? (sp > 1 ? nt : 0) : nt * sp;
             my_slots = sp > 1 ? nt * sp : 0;
         }

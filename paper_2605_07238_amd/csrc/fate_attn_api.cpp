@@ -180,6 +180,85 @@ fate_status_t append(const fate_heads_t *heads, const fate_seqs_t *seqs, const f
     return fate::launch_append(a, stream) == 0 ? FATE_OK : FATE_EHIP;
 }
 
+// Caps over 100 in log2 units: see capped_wide.
+constexpr float kWideCap = 100.0f;
+
+fate_status_t fill_scores(AttnLaunch &a, const fate_scores_t *s, float scale) {
+    if (!std::isfinite(s->cap) || s->cap < 0.0f) return FATE_EINVAL;
+    for (const void *p : {(const void *)s->slopes, (const void *)s->prefix, (const void *)s->start})
+        if (reinterpret_cast<uintptr_t>(p) % 4) return FATE_EINVAL;
+    a.shaped = 1;
+    if (s->cap > 0.0f) {
+        a.cap_log2 = (float)((double)s->cap * 1.4426950408889634);
+        a.cap_in = (float)(2.0 * (double)scale * 1.4426950408889634 / (double)s->cap);
+        if (!std::isnormal(a.cap_log2) || !std::isnormal(a.cap_in)) return FATE_EINVAL;
+        a.cap_wide = a.cap_log2 > kWideCap;
+    }
+    a.slopes = s->slopes;
+    a.prefix = s->prefix;
+    a.start = s->start;
+    return FATE_OK;
+}
+
+// `scores`: how the scores are shaped, or null for causal ones as they are.
+fate_status_t paged(const fate_heads_t *heads, const fate_seqs_t *seqs, const fate_rows_t *q,
+                    const fate_kv_cache_t *cache, int64_t max_new, float scale, const fate_scores_t *scores,
+                    const fate_rows_t *out, float *d_lse, int32_t *d_status, void *d_ws, size_t ws_bytes,
+                    void *stream) {
+    fate_status_t st = check_heads(heads);
+    if (st != FATE_OK || (st = check_sizes(heads, seqs)) != FATE_OK ||
+        (st = check_cache(heads, seqs, cache)) != FATE_OK)
+        return st;
+    if (max_new < 0 || max_new > seqs->T) return FATE_EINVAL;
+    if (seqs->T == 0 || seqs->B == 0) return FATE_OK;
+    if (cache->n_pages < 1 || !seqs->off || !seqs->kv_len || !seqs->pages) return FATE_EINVAL;
+    const PagedPlan p = plan_paged(heads, seqs, max_new);
+    if ((int64_t)p.grid * heads->heads_kv > kMaxGrid) return FATE_ERANGE;
+    AttnLaunch a = {};
+    if ((st = fill(a, heads, q, out, scale, d_lse, d_status)) != FATE_OK) return st;
+    if (scores && (st = fill_scores(a, scores, scale)) != FATE_OK) return st;
+    if (!d_ws || reinterpret_cast<uintptr_t>(d_ws) % 16) return FATE_EINVAL;
+    if (ws_bytes < ws_of(heads, p)) return FATE_ESIZE;
+    set_seqs(a.s, seqs, cache);
+    set_cache(a.c, cache);
+    a.part = static_cast<float *>(d_ws);
+    a.pieces = p.pieces;
+    const bool tile = p.rows == fate::kTileRows;
+    a.grid = p.grid;
+    const int rc = tile ? fate::launch_attn_tile(a, true, stream) : fate::launch_attn_few(a, p.rows, stream);
+    if (rc) return FATE_EHIP;
+    // row tiles done in parts: each has a part more than it has cuts, so fewer than there are shares; of those in
+    // order of length (each with over `chunk` key tiles of the sum) fewer than pieces, and no more than there are
+    const int tiles = !tile ? p.pieces - 1 : p.tiles < p.pieces ? p.tiles : p.pieces;
+    // (the tile kernel makes no part of fewer than kTileLeast key tiles)
+    if (tiles < 1 || (tile && a.s.max_keys <= (int64_t)fate::kTileLeast * fate::kKeyTile)) return FATE_OK;
+    // four rows a workgroup at a time, sixteen at most: as many workgroups as max_new tokens have rows for
+    const int64_t most = max_new * a.G < p.rows ? max_new * a.G : p.rows;
+    const int groups = most > 64 ? 8 : most > 4 ? (int)((most + 3) / 4) : 1;
+    return fate::launch_attn_join(a, p.rows, tiles, groups, stream) == 0 ? FATE_OK : FATE_EHIP;
+}
+
+fate_status_t prompt(const fate_heads_t *heads, const fate_seqs_t *seqs, const fate_rows_t *q, const fate_rows_t *k,
+                     const fate_rows_t *v, float scale, const fate_scores_t *scores, const fate_rows_t *out,
+                     float *d_lse, int32_t *d_status, void *stream) {
+    fate_status_t st = check_heads(heads);
+    if (st != FATE_OK || (st = check_sizes(heads, seqs)) != FATE_OK) return st;
+    if (seqs->T == 0 || seqs->B == 0) return FATE_OK;
+    const int64_t G = heads->heads_q / heads->heads_kv;
+    const int grid = tiles_of(seqs, G, fate::kTileRows);
+    if ((int64_t)grid * heads->heads_kv > kMaxGrid) return FATE_ERANGE;
+    if (!seqs->off || !good_rows(k) || !good_rows(v)) return FATE_EINVAL;
+    if (k->token >= kMaxToken || v->token >= kMaxToken) return FATE_ERANGE;
+    AttnLaunch a = {};
+    if ((st = fill(a, heads, q, out, scale, d_lse, d_status)) != FATE_OK) return st;
+    if (scores && (st = fill_scores(a, scores, scale)) != FATE_OK) return st;
+    set_seqs(a.s, seqs, nullptr);
+    a.k = rows(k);
+    a.v = rows(v);
+    a.grid = grid;
+    return fate::launch_attn_tile(a, false, stream) == 0 ? FATE_OK : FATE_EHIP;
+}
+
 }  // namespace
 
 extern "C" {
@@ -220,56 +299,29 @@ fate_status_t fate_attn_paged_ws_size(const fate_heads_t *heads, const fate_seqs
 fate_status_t fate_attn_paged(const fate_heads_t *heads, const fate_seqs_t *seqs, const fate_rows_t *q,
                               const fate_kv_cache_t *cache, int64_t max_new, float scale, const fate_rows_t *out,
                               float *d_lse, int32_t *d_status, void *d_ws, size_t ws_bytes, void *stream) {
-    fate_status_t st = check_heads(heads);
-    if (st != FATE_OK || (st = check_sizes(heads, seqs)) != FATE_OK ||
-        (st = check_cache(heads, seqs, cache)) != FATE_OK)
-        return st;
-    if (max_new < 0 || max_new > seqs->T) return FATE_EINVAL;
-    if (seqs->T == 0 || seqs->B == 0) return FATE_OK;
-    if (cache->n_pages < 1 || !seqs->off || !seqs->kv_len || !seqs->pages) return FATE_EINVAL;
-    const PagedPlan p = plan_paged(heads, seqs, max_new);
-    if ((int64_t)p.grid * heads->heads_kv > kMaxGrid) return FATE_ERANGE;
-    AttnLaunch a = {};
-    if ((st = fill(a, heads, q, out, scale, d_lse, d_status)) != FATE_OK) return st;
-    if (!d_ws || reinterpret_cast<uintptr_t>(d_ws) % 16) return FATE_EINVAL;
-    if (ws_bytes < ws_of(heads, p)) return FATE_ESIZE;
-    set_seqs(a.s, seqs, cache);
-    set_cache(a.c, cache);
-    a.part = static_cast<float *>(d_ws);
-    a.pieces = p.pieces;
-    const bool tile = p.rows == fate::kTileRows;
-    a.grid = p.grid;
-    const int rc = tile ? fate::launch_attn_tile(a, true, stream) : fate::launch_attn_few(a, p.rows, stream);
-    if (rc) return FATE_EHIP;
-    // row tiles done in parts: each has a part more than it has cuts, so fewer than there are shares; of those in
-    // order of length (each with over `chunk` key tiles of the sum) fewer than pieces, and no more than there are
-    const int tiles = !tile ? p.pieces - 1 : p.tiles < p.pieces ? p.tiles : p.pieces;
-    // (the tile kernel makes no part of fewer than kTileLeast key tiles)
-    if (tiles < 1 || (tile && a.s.max_keys <= (int64_t)fate::kTileLeast * fate::kKeyTile)) return FATE_OK;
-    // four rows a workgroup at a time, sixteen at most: as many workgroups as max_new tokens have rows for
-    const int64_t most = max_new * a.G < p.rows ? max_new * a.G : p.rows;
-    const int groups = most > 64 ? 8 : most > 4 ? (int)((most + 3) / 4) : 1;
-    return fate::launch_attn_join(a, p.rows, tiles, groups, stream) == 0 ? FATE_OK : FATE_EHIP;
+    return paged(heads, seqs, q, cache, max_new, scale, nullptr, out, d_lse, d_status, d_ws, ws_bytes, stream);
 }
 
 fate_status_t fate_attn_prompt(const fate_heads_t *heads, const fate_seqs_t *seqs, const fate_rows_t *q,
                                const fate_rows_t *k, const fate_rows_t *v, float scale, const fate_rows_t *out,
                                float *d_lse, int32_t *d_status, void *stream) {
-    fate_status_t st = check_heads(heads);
-    if (st != FATE_OK || (st = check_sizes(heads, seqs)) != FATE_OK) return st;
-    if (seqs->T == 0 || seqs->B == 0) return FATE_OK;
-    const int64_t G = heads->heads_q / heads->heads_kv;
-    const int grid = tiles_of(seqs, G, fate::kTileRows);
-    if ((int64_t)grid * heads->heads_kv > kMaxGrid) return FATE_ERANGE;
-    if (!seqs->off || !good_rows(k) || !good_rows(v)) return FATE_EINVAL;
-    if (k->token >= kMaxToken || v->token >= kMaxToken) return FATE_ERANGE;
-    AttnLaunch a = {};
-    if ((st = fill(a, heads, q, out, scale, d_lse, d_status)) != FATE_OK) return st;
-    set_seqs(a.s, seqs, nullptr);
-    a.k = rows(k);
-    a.v = rows(v);
-    a.grid = grid;
-    return fate::launch_attn_tile(a, false, stream) == 0 ? FATE_OK : FATE_EHIP;
+    return prompt(heads, seqs, q, k, v, scale, nullptr, out, d_lse, d_status, stream);
+}
+
+fate_status_t fate_attn_paged_shaped(const fate_heads_t *heads, const fate_seqs_t *seqs, const fate_rows_t *q,
+                                     const fate_kv_cache_t *cache, int64_t max_new, float scale,
+                                     const fate_scores_t *scores, const fate_rows_t *out, float *d_lse,
+                                     int32_t *d_status, void *d_ws, size_t ws_bytes, void *stream) {
+    if (!scores) return FATE_EINVAL;
+    return paged(heads, seqs, q, cache, max_new, scale, scores, out, d_lse, d_status, d_ws, ws_bytes, stream);
+}
+
+fate_status_t fate_attn_prompt_shaped(const fate_heads_t *heads, const fate_seqs_t *seqs, const fate_rows_t *q,
+                                      const fate_rows_t *k, const fate_rows_t *v, float scale,
+                                      const fate_scores_t *scores, const fate_rows_t *out, float *d_lse,
+                                      int32_t *d_status, void *stream) {
+    if (!scores) return FATE_EINVAL;
+    return prompt(heads, seqs, q, k, v, scale, scores, out, d_lse, d_status, stream);
 }
 
 }  // extern "C"

@@ -25,7 +25,7 @@
 namespace fate {
 namespace {
 
-template <class T, int D, int RT>
+template <class T, int D, int RT, bool SHAPED>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_few(AttnLaunch) {
     typedef typename T::el el;
     typedef typename T::x4 x4;
@@ -44,8 +44,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_few(AttnLaunch) 
         const Args &a = launch_args();
         const bool report = blockIdx.x == 0 && threadIdx.x < 64;
         hk = blockIdx.x % a.hkv, piece = blockIdx.x / a.hkv;
-        lens = first_group<true>(a, threadIdx.x & 63, report);
-        const Axis axis = axis_of(a, M, lens, threadIdx.x & 63, report);
+        lens = first_group<true, SHAPED>(a, threadIdx.x & 63, report);
+        const Axis axis = axis_of<SHAPED>(a, M, lens, threadIdx.x & 63, report);
         from = piece * axis.share;
         to = min(from + axis.share, axis.total);
     }
@@ -53,14 +53,21 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_few(AttnLaunch) 
     for (int64_t x = from; x < to;) {  // the row tiles of this share
         const Args &a = launch_args();
         const int tid = fresh(threadIdx.x), lane = tid & 63, w = uniform(tid >> 6);
-        const Unit p = unit_at(a, M, lens, x, lane, search);
+        const Unit p = unit_at<SHAPED>(a, M, lens, x, lane, search);
         if (!p.ok) return;
         x = p.start + p.cost;
 
         const int rows = p.n * a.G, row0 = p.tile * M;
         const int first = p.L - p.n + 1;
         const int last_row = min(row0 + M, rows) - 1;
-        const int most = min(p.L, max(0, last_row / a.G + first));
+        Span span = {};
+        if (SHAPED) span = span_of(a, p, row0 / a.G, last_row / a.G);
+        // Blocks of 32 keys that hold a key some row sees, numbered through; keys up to `most` likewise, `skip` of them
+        // left out behind the prefix's blocks.
+        const int pre_end = SHAPED ? (span.pre + 31) / 32 * 32 : 0;
+        const int skip = SHAPED ? blocks_unseen<32>(span.pre, span.from, span.most) * 32 : 0;
+        auto key_of = [&](int key) { return SHAPED && key >= pre_end ? key + skip : key; };
+        const int most = SHAPED ? span.most - skip : min(p.L, max(0, last_row / a.G + first));
         const int least = max(0, min(p.L, row0 / a.G + first));
         const int blocks = (most + 31) / 32;
         const bool part = p.start < from || p.start + p.cost > to;
@@ -69,13 +76,19 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_few(AttnLaunch) 
 
         const int c = lane & 15, g = lane >> 4;
         x8 q[RT][KS];
-        int ends[RT];
+        int ends[RT], pos[RT];
+        Seen seen[RT];
+        float slope[RT];
+        const float unit = SHAPED && (a.slopes || a.cap_log2 != 0.0f) ? 1.0f : a.scale_log2;  // of a score, in log2
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             const int row = row0 + rt * 16 + c;
             const bool live = row < rows;
             const int tok = live ? row / a.G : 0;
-            ends[rt] = live ? max(0, min(p.L, tok + first)) : 0;
+            seen[rt] = seen_by<SHAPED>(a, p, tok, live);
+            ends[rt] = seen[rt].end;
+            pos[rt] = tok + first - 1;
+            slope[rt] = SHAPED && a.slopes && live ? a.slopes[hk * a.G + row - tok * a.G] * kLog2e : 0.0f;
             const el *src = (const el *)a.q.data + (p.lo_row + (int64_t)tok) * a.q.token +
                             (int64_t)(hk * a.G + row - tok * a.G) * a.q.head + g * 8;
 #pragma unroll
@@ -103,7 +116,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_few(AttnLaunch) 
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const int key = kb + 16 * i + c;
-                pg[i] = key < k_hi ? table[key >> a.c.page_shift] : 0;
+                pg[i] = key < k_hi ? table[key_of(key) >> a.c.page_shift] : 0;
             }
         };
         find_pages(k_lo + 32 * w);
@@ -118,7 +131,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_few(AttnLaunch) 
                     in = false;
                     if (a.status) a.status[p.b] = FATE_EINVAL;
                 }
-                const int64_t at = pg[i] * a.c.page + (int64_t)hk * a.c.head + (key & mask) * a.c.token + g * 8;
+                const int64_t at = pg[i] * a.c.page + (int64_t)hk * a.c.head + (key_of(key) & mask) * a.c.token + g * 8;
 #pragma unroll
                 for (int s = 0; s < KS; ++s) {
                     const bool ld = in && s * 32 + g * 8 < a.d;
@@ -131,7 +144,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_few(AttnLaunch) 
                 }
             }
             find_pages(kb + 128);
-            const bool edge = kb + 32 > least;  // uniform
+            const int real = key_of(kb);
+            const bool edge = SHAPED ? !span.all(real, 32) : kb + 32 > least;  // uniform
             if (edge) {
                 uint32_t bad = 0;
 #pragma unroll
@@ -166,7 +180,39 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_few(AttnLaunch) 
                     for (int s = 0; s < KS; ++s) s2[i] = T::mfma16(__builtin_bit_cast(x8, rk[i][s]), q[rt][s], s2[i]);
                 }
                 // s2[i][j]: key 16 i + 4 g + j of the block, packed row c
-                if (edge || kb + 32 > k_hi) {
+                if (SHAPED) {
+                    if (a.cap_wide) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) s2[i][j] = capped_wide(s2[i][j], a.cap_in, a.cap_log2);
+                    } else if (a.cap_log2 != 0.0f) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) s2[i][j] = capped(s2[i][j], a.cap_in, a.cap_log2);
+                    } else if (a.slopes) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) s2[i] *= a.scale_log2;
+                    }
+                    if (a.slopes) {
+                        const float from = (float)(real + 4 * g - pos[rt]);
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                s2[i][j] = __builtin_fmaf(-slope[rt], __builtin_fabsf(from + (float)(16 * i + j)), s2[i][j]);
+                    }
+                    if (edge || kb + 32 > k_hi) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const int at = 4 * g + 16 * i + j;
+                                if (kb + at >= k_hi || !seen[rt].has(real + at)) s2[i][j] = -INFINITY;
+                            }
+                    }
+                } else if (edge || kb + 32 > k_hi) {
                     const int left = min(ends[rt], k_hi) - kb - 4 * g;
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
@@ -178,7 +224,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_few(AttnLaunch) 
                                   fmaxf(fmaxf(s2[1][0], s2[1][1]), fmaxf(s2[1][2], s2[1][3])));
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
-                top = fmaxf(top * a.scale_log2, kLowest);
+                top = fmaxf(top * unit, kLowest);
                 if (__any(top > m[rt] + (kLag + T::kLift))) {
                     const float next = fmaxf(m[rt], top - T::kLift), f = exp2_fast(m[rt] - next);
                     m[rt] = next;
@@ -190,7 +236,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_few(AttnLaunch) 
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const float x = exp2_fast(__builtin_fmaf(s2[i][j], a.scale_log2, -m[rt]));
+                        const float x = exp2_fast(__builtin_fmaf(s2[i][j], unit, -m[rt]));
                         l[rt] += x;
                         pr[rt][4 * i + j] = (el)x;
                     }
@@ -210,7 +256,9 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_few(AttnLaunch) 
 
         if (odd) {  // uniform in the wave
             for (int kb = k_lo + 32 * w; kb < k_hi; kb += 128)
-                for (int key = max(kb, least / 32 * 32); key < min(kb + 32, k_hi); ++key) {
+                for (int at = SHAPED ? kb : max(kb, least / 32 * 32); at < min(kb + 32, k_hi); ++at) {
+                    const int key = key_of(at);
+                    if (SHAPED && span.all(key_of(kb), 32)) break;
                     const int page = table[key >> a.c.page_shift];
                     if ((uint32_t)page >= (uint32_t)a.c.n_pages) continue;
                     const el *src = (const el *)a.c.v + page * a.c.page + (int64_t)hk * a.c.head + (key & mask) * a.c.token;
@@ -224,7 +272,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_few(AttnLaunch) 
                         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
                             for (int e = 0; e < 4; ++e)
-                                o[rt][dt][e] += key < ends[rt] && !__builtin_isfinite((float)x[e]) ? (float)x[e] : 0.0f;
+                                o[rt][dt][e] += (SHAPED ? seen[rt].has(key) : key < ends[rt]) && !__builtin_isfinite((float)x[e]) ? (float)x[e] : 0.0f;
                     }
                 }
         }
@@ -294,24 +342,24 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_few(AttnLaunch) 
 // every `groups`-th four after them): its lanes are sixteen chunks of eight
 // dimensions times four parts at a time, so that a row's parts are read side
 // by side and the chain of reads stays short however many parts there are.
-template <class T, bool TILE>
+template <class T, bool TILE, bool SHAPED>
 __global__ __launch_bounds__(256) void k_attn_join(AttnLaunch a, int M, int items, int groups) {
     typedef typename T::el el;
     typedef typename T::x8 x8;
     const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
     const int hk = blockIdx.x % a.hkv;
-    const Group lens = first_group<true>(a, lane, false);
+    const Group lens = first_group<true, SHAPED>(a, lane, false);
     Axis axis = {0, 0};
     int chunk = 0;
-    if (TILE) chunk = chunk_of(a, M, lens, lane, false);
-    else axis = axis_of(a, M, lens, lane, false);
+    if (TILE) chunk = chunk_of<SHAPED>(a, M, lens, lane, false);
+    else axis = axis_of<SHAPED>(a, M, lens, lane, false);
     for (int at = blockIdx.x / a.hkv; at < items * groups; at += gridDim.x / a.hkv) {
         const int item = at / groups, group = at - item * groups;
         // part i lies in slot first_slot (i = 0), next_slot + step * i (others)
         Unit p;
         int splits, first_slot, next_slot, step;
         if (TILE) {
-            const Piece piece = find_piece<true, true>(a, M, lens, chunk, item, lane);
+            const Piece piece = find_piece<true, true, SHAPED>(a, M, lens, chunk, item, lane);
             p = piece.u;
             if (!p.ok) return;
             splits = piece.splits;
@@ -321,7 +369,7 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnLaunch a, int M, int item
             Search search = {0, 0, 0};
             const int64_t cut = (item + 1) * axis.share;
             if (cut >= axis.total) return;
-            p = unit_at(a, M, lens, cut, lane, search);
+            p = unit_at<SHAPED>(a, M, lens, cut, lane, search);
             if (!p.ok || p.start >= cut || p.start < cut - axis.share) return;  // this row tile's first cut alone
             splits = uniform((int)((p.start + p.cost - 1) / axis.share)) - item + 1;
             first_slot = 2 * item + (p.start > cut - axis.share);  // behind the share's first where the tile begins within
@@ -379,38 +427,45 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnLaunch a, int M, int item
     }
 }
 
-template <class T, int D>
+template <class T, int D, bool SHAPED>
 int go(const AttnLaunch &a, int rows, hipStream_t s) {
     const dim3 grid((unsigned)a.grid * (unsigned)a.hkv);
-    if (rows == 16) hipLaunchKernelGGL((k_attn_few<T, D, 1>), grid, dim3(256), 0, s, a);
-    else if constexpr (D <= 128) hipLaunchKernelGGL((k_attn_few<T, D, 2>), grid, dim3(256), 0, s, a);
+    if (rows == 16) hipLaunchKernelGGL((k_attn_few<T, D, 1, SHAPED>), grid, dim3(256), 0, s, a);
+    else if constexpr (D <= 128) hipLaunchKernelGGL((k_attn_few<T, D, 2, SHAPED>), grid, dim3(256), 0, s, a);
     else return (int)hipErrorInvalidValue;
     return (int)hipGetLastError();
 }
 
-template <class T>
+template <class T, bool SHAPED>
 int go(const AttnLaunch &a, int rows, hipStream_t s) {
-    return a.d <= 64 ? go<T, 64>(a, rows, s) : a.d <= 128 ? go<T, 128>(a, rows, s) : go<T, 256>(a, rows, s);
+    return a.d <= 64 ? go<T, 64, SHAPED>(a, rows, s) : a.d <= 128 ? go<T, 128, SHAPED>(a, rows, s)
+                                                                  : go<T, 256, SHAPED>(a, rows, s);
+}
+
+template <class T, bool SHAPED>
+int join(const AttnLaunch &a, int rows, int tiles, int groups, hipStream_t s) {
+    // row tiles: at most about 1024 workgroups, each of which goes on a grid's length further; most calls cut few
+    const bool tile = rows == kTileRows;
+    const int most = 1024 / a.hkv > 0 ? 1024 / a.hkv : 1, all = tiles * groups;
+    const dim3 grid((unsigned)(tile && all > most ? most : all) * (unsigned)a.hkv);
+    if (tile) hipLaunchKernelGGL((k_attn_join<T, true, SHAPED>), grid, dim3(256), 0, s, a, rows, tiles, groups);
+    else hipLaunchKernelGGL((k_attn_join<T, false, SHAPED>), grid, dim3(256), 0, s, a, rows, tiles, groups);
+    return (int)hipGetLastError();
 }
 
 }  // namespace
 
 int launch_attn_few(const AttnLaunch &a, int rows, void *stream) {
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    return a.dtype == FATE_BF16 ? go<BF16>(a, rows, s) : go<F16>(a, rows, s);
+    if (a.dtype == FATE_BF16) return a.shaped ? go<BF16, true>(a, rows, s) : go<BF16, false>(a, rows, s);
+    return a.shaped ? go<F16, true>(a, rows, s) : go<F16, false>(a, rows, s);
 }
 
 int launch_attn_join(const AttnLaunch &a, int rows, int tiles, int groups, void *stream) {
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    // row tiles: at most about 1024 workgroups, each of which goes on a grid's length further; most calls cut few
-    const bool bf = a.dtype == FATE_BF16, tile = rows == kTileRows;
-    const int most = 1024 / a.hkv > 0 ? 1024 / a.hkv : 1, all = tiles * groups;
-    const dim3 grid((unsigned)(tile && all > most ? most : all) * (unsigned)a.hkv);
-    if (bf && tile) hipLaunchKernelGGL((k_attn_join<BF16, true>), grid, dim3(256), 0, s, a, rows, tiles, groups);
-    else if (bf) hipLaunchKernelGGL((k_attn_join<BF16, false>), grid, dim3(256), 0, s, a, rows, tiles, groups);
-    else if (tile) hipLaunchKernelGGL((k_attn_join<F16, true>), grid, dim3(256), 0, s, a, rows, tiles, groups);
-    else hipLaunchKernelGGL((k_attn_join<F16, false>), grid, dim3(256), 0, s, a, rows, tiles, groups);
-    return (int)hipGetLastError();
+    if (a.dtype == FATE_BF16)
+        return a.shaped ? join<BF16, true>(a, rows, tiles, groups, s) : join<BF16, false>(a, rows, tiles, groups, s);
+    return a.shaped ? join<F16, true>(a, rows, tiles, groups, s) : join<F16, false>(a, rows, tiles, groups, s);
 }
 
 }  // namespace fate

@@ -69,7 +69,7 @@ __device__ __forceinline__ float both_halves_max(float x) {
 // load, smaller pages.
 enum Source { kRows, kPages, kSmallPages };
 
-template <class T, int D, Source FROM>
+template <class T, int D, Source FROM, bool SHAPED>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch) {
     const Args &a = launch_args();  // read where they lie: copied, they go to scratch and what uses them after them
     typedef typename T::el el;
@@ -85,13 +85,13 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
     const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
     const int hk = blockIdx.x % a.hkv, item = blockIdx.x / a.hkv;
     const bool report = blockIdx.x == 0 && tid < 64;
-    const Group lens = first_group<PAGED>(a, lane, report);
+    const Group lens = first_group<PAGED, SHAPED>(a, lane, report);
     if (!PAGED && report) {
         int reach = lens.reach;
-        for (int at = 64; at < a.s.B; at += 64) read_lens<false>(a, at, lane, reach, true);
+        for (int at = 64; at < a.s.B; at += 64) read_lens<false, SHAPED>(a, at, lane, reach, true);
     }
-    const int chunk = PAGED ? chunk_of(a, kTileRows, lens, lane, report) : 0x7fffffff;
-    const Piece piece = find_piece<PAGED, false>(a, kTileRows, lens, chunk, item, lane);
+    const int chunk = PAGED ? chunk_of<SHAPED>(a, kTileRows, lens, lane, report) : 0x7fffffff;
+    const Piece piece = find_piece<PAGED, false, SHAPED>(a, kTileRows, lens, chunk, item, lane);
     const Unit &p = piece.u;
     if (!p.ok) return;
 
@@ -99,8 +99,15 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
     const int rows = p.n * a.G, row0 = p.tile * kTileRows;
     const int first = p.L - p.n + 1;
     const int wg_last = min(row0 + kTileRows, rows) - 1;
-    const int wg_most = min(p.L, max(0, wg_last / a.G + first));  // most keys a row of the workgroup sees
-    int t_lo = 0, t_hi = (wg_most + BK - 1) / BK;
+    Span wg = {};
+    if (SHAPED) wg = span_of(a, p, row0 / a.G, wg_last / a.G);
+    // most keys a row of the workgroup sees
+    const int wg_most = SHAPED ? wg.most : min(p.L, max(0, wg_last / a.G + first));
+    // Tiles that hold a key some row sees, numbered through; `skip` lie between those of the prefix and the others.
+    const int pre_tiles = SHAPED ? (wg.pre + BK - 1) / BK : 0;
+    const int skip = SHAPED ? blocks_unseen<BK>(wg.pre, wg.from, wg.most) : 0;
+    auto key_of = [&](int t) { return (SHAPED && t >= pre_tiles ? t + skip : t) * BK; };
+    int t_lo = 0, t_hi = (wg_most + BK - 1) / BK - skip;
     if (PAGED && piece.splits > 1) {
         t_lo = piece.split * chunk;
         t_hi = min(t_hi, t_lo + chunk);
@@ -111,9 +118,14 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
     const bool live = row < rows;
     const int tok = live ? row / a.G : 0;
     const int qh = hk * a.G + (row - tok * a.G);
-    const int ends = live ? max(0, min(p.L, tok + first)) : 0;  // keys this lane's row sees
-    const int w_most = wrow0 < rows ? min(p.L, max(0, (min(wrow0 + 32, rows) - 1) / a.G + first)) : 0;
+    const Seen seen = seen_by<SHAPED>(a, p, tok, live);  // keys this lane's row sees
+    const int ends = seen.end;
+    Span wave = {};
+    if (SHAPED && wrow0 < rows) wave = span_of(a, p, wrow0 / a.G, (min(wrow0 + 32, rows) - 1) / a.G);
+    const int w_most = SHAPED ? wave.most : wrow0 < rows ? min(p.L, max(0, (min(wrow0 + 32, rows) - 1) / a.G + first)) : 0;
     const int w_least = wrow0 < rows ? max(0, min(p.L, wrow0 / a.G + first)) : 0;
+    const float slope = SHAPED && a.slopes && live ? a.slopes[qh] * kLog2e : 0.0f;
+    const float unit = SHAPED && (a.slopes || a.cap_log2 != 0.0f) ? 1.0f : a.scale_log2;  // of a score, in log2
 
     // queries: the first product's second operand, column = row of the tile
     x8 q[D / 16];
@@ -161,7 +173,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
     auto pages_of = [&](int t) {
         int id = 0;
         if (FROM == kPages && lane < NI && t >= t_lo) {
-            const int key = t * BK + w * 16 + lane * RI;
+            const int key = key_of(t) + w * 16 + lane * RI;
             if (key < wg_most) {
                 id = a.s.pages[p.b * a.s.pages_stride + (key >> a.c.page_shift)];
                 if ((uint32_t)id >= (uint32_t)a.c.n_pages) {
@@ -174,7 +186,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
     };
     auto load_rows = [&](bool keys, int t, int ids, uint32_t dst) __attribute__((always_inline)) {
         dst += w * 16 * D * 2;
-        const int key0 = t * BK + w * 16;
+        const int key0 = key_of(t) + w * 16;
         const int64_t tok = keys ? tok_k : tok_v;
         const char *base = keys ? base_k : base_v;
 #pragma unroll
@@ -194,7 +206,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
             for (int x = 0; x < 2; ++x)
 #pragma unroll
                 for (int i = 0; i < NI; ++i) {
-                    const int t = x ? tk : tv, key = max(0, min(t * BK + w * 16 + i * RI + lr, wg_most - 1));
+                    const int t = x ? tk : tv, key = max(0, min(key_of(t) + w * 16 + i * RI + lr, wg_most - 1));
                     id[x][i] = a.s.pages[p.b * a.s.pages_stride + (key >> a.c.page_shift)];
                 }
         }
@@ -204,7 +216,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
             if (t < t_lo) continue;
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
-                const int key = min(t * BK + w * 16 + i * RI + lr, wg_most - 1), c = x ? chunk_k(i) : chunk_v(i);
+                const int key = min(key_of(t) + w * 16 + i * RI + lr, wg_most - 1), c = x ? chunk_k(i) : chunk_v(i);
                 const char *src = (x ? base_k : base_v) + c * 16;
                 bool in = c * 8 < a.d;
                 if (PAGED) {
@@ -252,6 +264,34 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
         }
     };
 
+    // Scores as the call shapes them, in log2: capped, then less slope times distance.
+    auto shape = [&](f32x16 (&s)[2], int key) __attribute__((always_inline)) {
+        if (a.cap_wide) {
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) s[kt][j] = capped_wide(s[kt][j], a.cap_in, a.cap_log2);
+        } else if (a.cap_log2 != 0.0f) {
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) s[kt][j] = capped(s[kt][j], a.cap_in, a.cap_log2);
+        } else if (a.slopes) {
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) s[kt][j] *= a.scale_log2;
+        }
+        if (a.slopes) {
+            const float from = (float)(key + 4 * half - (tok + first - 1));
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    s[kt][j] = __builtin_fmaf(-slope, __builtin_fabsf(from + (float)(kt * 32 + 8 * (j / 4) + j % 4)), s[kt][j]);
+        }
+    };
+
     // Tile t is in buffer B: its scores are in `cur` when its turn comes, and
     // the next tile's are worked out beside its softmax.
     auto step = [&](auto which, int t, f32x16 (&cur)[2], f32x16 (&nxt)[2]) {
@@ -259,7 +299,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
         load_tiles(false, t - 1, ids1, lds0 + (2 + (B ^ 1)) * kTile, t - 2, ids2, lds0 + B * kTile);
         ids1 = ids2;
         ids2 = pages_of(t - 3);
-        if ((t + 1) * BK > wg_least) {  // uniform: on the edge of some row
+        const int key = key_of(t);
+        if (SHAPED ? !wg.all(key, BK) : key + BK > wg_least) {  // uniform: on the edge of some row
             bool any = false;
 #pragma unroll
             for (int j = 0; j < BK * CH / 256; ++j) {
@@ -267,7 +308,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
                 u32x4 *at = (u32x4 *)(smem + (2 + B) * kTile + c * 16);
                 u32x4 x = *at;
                 if (not_finite<T>(x[0]) | not_finite<T>(x[1]) | not_finite<T>(x[2]) | not_finite<T>(x[3])) {
-                    any = any || t * BK + c / CH < wg_most;
+                    any = any || key + c / CH < wg_most;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) x[e] = only_finite<T>(x[e]);
                     *at = x;
@@ -276,11 +317,21 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
             if (any) odd = 1;
             __syncthreads();
         }
-        if (t * BK < w_most) {  // uniform in the wave
+        if (key < w_most) {  // uniform in the wave
             // cur[kt][j]: key kt * 32 + 8 (j / 4) + 4 half + j % 4 of the tile, row lane % 32
-            if ((t + 1) * BK > w_least) {
+            if (SHAPED) shape(cur, key);
+            if (SHAPED && !wave.all(key, BK)) {
+                asm volatile("");
+                const int at = key + 4 * half;
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        if (!seen.has(at + kt * 32 + 8 * (j / 4) + j % 4)) cur[kt][j] = -INFINITY;
+            }
+            if (!SHAPED && key + BK > w_least) {
                 asm volatile("");  // a branch, not selects in every tile
-                const int left = ends - t * BK - 4 * half;
+                const int left = ends - key - 4 * half;
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
@@ -292,7 +343,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
             for (int j = 1; j < 16; ++j) top = fmaxf(top, cur[0][j]);
 #pragma unroll
             for (int j = 0; j < 16; ++j) top = fmaxf(top, cur[1][j]);
-            top = fmaxf(both_halves_max(top) * a.scale_log2, kLowest);
+            top = fmaxf(both_halves_max(top) * unit, kLowest);
             if (__any(top > m + (kLag + T::kLift))) {
                 const float next = fmaxf(m, top - T::kLift), f = exp2_fast(m - next);
                 m = next;
@@ -308,7 +359,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float x = exp2_fast(__builtin_fmaf(cur[i / 2][8 * (i % 2) + e], a.scale_log2, -m));
+                    const float x = exp2_fast(__builtin_fmaf(cur[i / 2][8 * (i % 2) + e], unit, -m));
                     l += x;
                     pr[i][e] = (el)x;
                 }
@@ -338,7 +389,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
                 __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
                 __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
             }
-        } else if (t - 1 >= t_lo && (t - 1) * BK < w_most) {
+        } else if (t - 1 >= t_lo && key_of(t - 1) < w_most) {
             scores(nxt, (B ^ 1) * kTile);
         }
         dma_wait();
@@ -369,7 +420,11 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
     }
 
     if (odd) {  // values that the tiles left out, for the rows that see them (any weight makes them what they are)
-        for (int key = max(t_lo, wg_least / BK) * BK; key < min(ends, t_hi * BK); ++key) {
+        // (shaped: all of the part's tiles are looked through, in order)
+        const int odd_lo = SHAPED ? t_lo * BK : max(t_lo, wg_least / BK) * BK;
+        for (int at = odd_lo; at < (SHAPED ? t_hi * BK : min(ends, t_hi * BK)); ++at) {
+            const int key = SHAPED ? key_of(at / BK) + at % BK : at;
+            if (SHAPED && (wg.all(key_of(at / BK), BK) || !seen.has(key))) continue;
             const el *src;
             if (PAGED) {
                 const int page = a.s.pages[p.b * a.s.pages_stride + (key >> a.c.page_shift)];
@@ -439,12 +494,18 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
     }
 }
 
+#ifdef FATE_ATTN_SHAPED
+constexpr bool kShaped = true;
+#else
+constexpr bool kShaped = false;
+#endif
+
 template <class T, Source FROM>
 int go(const AttnLaunch &a, hipStream_t s) {
     const dim3 grid((unsigned)a.grid * (unsigned)a.hkv);
-    if (a.d <= 64) hipLaunchKernelGGL((k_attn_tile<T, 64, FROM>), grid, dim3(256), 0, s, a);
-    else if (a.d <= 128) hipLaunchKernelGGL((k_attn_tile<T, 128, FROM>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((k_attn_tile<T, 256, FROM>), grid, dim3(256), 0, s, a);
+    if (a.d <= 64) hipLaunchKernelGGL((k_attn_tile<T, 64, FROM, kShaped>), grid, dim3(256), 0, s, a);
+    else if (a.d <= 128) hipLaunchKernelGGL((k_attn_tile<T, 128, FROM, kShaped>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((k_attn_tile<T, 256, FROM, kShaped>), grid, dim3(256), 0, s, a);
     return (int)hipGetLastError();
 }
 
@@ -457,7 +518,12 @@ int go(const AttnLaunch &a, bool paged, hipStream_t s) {
 
 }  // namespace
 
+#ifdef FATE_ATTN_SHAPED
+int launch_attn_tile_shaped(const AttnLaunch &a, bool paged, void *stream) {
+#else
 int launch_attn_tile(const AttnLaunch &a, bool paged, void *stream) {
+    if (a.shaped) return launch_attn_tile_shaped(a, paged, stream);
+#endif
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     return a.dtype == FATE_BF16 ? go<BF16>(a, paged, s) : go<F16>(a, paged, s);
 }

@@ -38,7 +38,8 @@ EXPORTS = ["fate_version", "fate_strerror", "fate_pack_dags_size", "fate_pack_da
            "fate_pack_dags_opt", "fate_layout_dags_opt", "fate_score_sweep", "fate_topk_sweep", "fate_plan_wave",
            "fate_simulate", "fate_place_baseline", "fate_sim_ws_size", "fate_simulate_device",
            "fate_place_baseline_device", "fate_kv_append", "fate_attn_paged_ws_size", "fate_attn_paged",
-           "fate_attn_prompt", "fate_kv_reserve", "fate_kv_trim", "fate_kv_append_axes"]
+           "fate_attn_prompt", "fate_kv_reserve", "fate_kv_trim", "fate_kv_append_axes",
+           "fate_attn_paged_shaped", "fate_attn_prompt_shaped"]
 
 # Scoring variants and packing options (fate_params_t.flags, fate_pack_opts_t.levels).
 FATE_MEAN_PER_LEVEL, FATE_NO_WINDOWS = 1, 2
@@ -135,6 +136,10 @@ class Axes(C.Structure):
     _fields_ = [("n_axes", C.c_int32), ("pair_axis", C.c_void_p), ("positions", C.c_void_p), ("stride", C.c_int64)]
 
 
+class Scores(C.Structure):
+    _fields_ = [("cap", C.c_float), ("slopes", C.c_void_p), ("prefix", C.c_void_p), ("start", C.c_void_p)]
+
+
 class KvTables(C.Structure):
     _fields_ = [("B", C.c_int32), ("max_pages", C.c_int32), ("page_size", C.c_int32), ("n_pages", C.c_int32),
                 ("pages_stride", C.c_int64), ("pages", C.c_void_p), ("free", C.c_void_p), ("n_free", C.c_void_p),
@@ -206,6 +211,10 @@ def load(path: Optional[str] = None):
                                      C.c_void_p, C.c_void_p]
     lib.fate_kv_append_axes.argtypes = [P(Heads), P(Seqs), P(Rows), P(Rows), P(Rows), C.c_void_p, C.c_int64, C.c_int32,
                                         C.c_int32, P(Axes), P(KvCache), P(Rows), C.c_void_p, C.c_void_p]
+    lib.fate_attn_paged_shaped.argtypes = [P(Heads), P(Seqs), P(Rows), P(KvCache), C.c_int64, C.c_float, P(Scores), P(Rows),
+                                           C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.fate_attn_prompt_shaped.argtypes = [P(Heads), P(Seqs), P(Rows), P(Rows), P(Rows), C.c_float, P(Scores), P(Rows),
+                                            C.c_void_p, C.c_void_p, C.c_void_p]
     lib.fate_kv_reserve.argtypes = [P(KvTables), C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
     lib.fate_kv_trim.argtypes = [P(KvTables), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
@@ -956,6 +965,12 @@ def fate_attn_paged(q, k_cache, v_cache, off, kv_len, pages, max_new: Optional[i
     if _t.grad_enabled() and (q.requires_grad or k_cache.requires_grad or v_cache.requires_grad or
                               (out is not None and out.requires_grad)):
         raise _no_gradient()
+    return _paged(q, k_cache, v_cache, off, kv_len, pages, max_new, scale, None, lse, out, status, ws)
+
+
+def _paged(q, k_cache, v_cache, off, kv_len, pages, max_new, scale, shaping, lse, out, status, ws):
+    """The call itself, on the current device and stream; shaping: cap, slopes, prefix and start, or None."""
+    dev, dtype = q.device, q.dtype
     shape = _three(q, "q")
     T, hq, d = shape
     hkv = k_cache.shape[1] if k_cache.dim() == 4 else 0
@@ -972,12 +987,47 @@ def fate_attn_paged(q, k_cache, v_cache, off, kv_len, pages, max_new: Optional[i
         ws = _t.empty(_ws_bytes(h.dtype, hq, hkv, d, most), dtype=_t.uint8, device=dev)
     elif ws.device != dev or not ws.is_contiguous():
         raise ValueError("ws must be contiguous, on %s" % dev)
-    st = load().fate_attn_paged(h, s, rq, c, most, 1.0 / math.sqrt(d or 1) if scale is None else scale, ro,
-                                sums.data_ptr() if lse else None, _attn_status(status, s.B, dev), ws.data_ptr(),
-                                ws.nbytes, _t.raw_stream(dev.index))
+    scale = 1.0 / math.sqrt(d or 1) if scale is None else scale
+    rest = (ro, sums.data_ptr() if lse else None, _attn_status(status, s.B, dev), ws.data_ptr(), ws.nbytes,
+            _t.raw_stream(dev.index))
+    if shaping is None:
+        st = load().fate_attn_paged(h, s, rq, c, most, scale, *rest)
+    else:
+        st = load().fate_attn_paged_shaped(h, s, rq, c, most, scale, _scores(*shaping, hq, s.B, T, dev), *rest)
     if st != FATE_OK:
-        raise FateError(st, "fate_attn_paged")
+        raise FateError(st, "fate_attn_paged" if shaping is None else "fate_attn_paged_shaped")
     return out, sums
+
+
+def _scores(cap, slopes, prefix, start, heads, B, T, device) -> Scores:
+    def of(t, name, n, dtype):
+        if t is None:
+            return None
+        if t.dtype is not dtype or t.device != device or t.shape != (n,) or (n > 1 and t.stride(0) != 1):
+            raise ValueError("%s must be a contiguous %s tensor of %d elements on %s, got %s %s on %s" % (
+                name, dtype, n, device, t.dtype, list(t.shape), t.device))
+        return t.data_ptr()
+
+    return Scores(cap, of(slopes, "slopes", heads, _t.float32), of(prefix, "prefix", B, _t.int32), of(start, "start", T, _t.int32))
+
+
+def fate_attn_paged_shaped(q, k_cache, v_cache, off, kv_len, pages, max_new: Optional[int] = None,
+                           scale: Optional[float] = None, cap: float = 0.0, slopes=None, prefix=None, start=None,
+                           lse: bool = False, out=None, status=None, ws=None, stream=None):
+    """:func:`fate_attn_paged` with shaped scores.  With s = scale q.k of the
+    row at position p and the key at position j: s becomes cap tanh(s / cap)
+    where cap is not 0, less slopes[head] |p - j| (float32 [heads_q]); the row
+    sees j < prefix[b] (int32 [B]: a prefix that every row of the sequence sees)
+    and start[t] <= j <= p (int32 [T], not falling within a sequence: the first
+    key of the row's document, or p - w + 1 for a window of w keys)."""
+    dev = q.device
+    if not _here(dev, stream):
+        return _there(dev, stream, fate_attn_paged_shaped, q, k_cache, v_cache, off, kv_len, pages, max_new, scale, cap, slopes,
+                      prefix, start, lse, out, status, ws)
+    if _t.grad_enabled() and (q.requires_grad or k_cache.requires_grad or v_cache.requires_grad or
+                              (slopes is not None and slopes.requires_grad) or (out is not None and out.requires_grad)):
+        raise _no_gradient()
+    return _paged(q, k_cache, v_cache, off, kv_len, pages, max_new, scale, (cap, slopes, prefix, start), lse, out, status, ws)
 
 
 @functools.lru_cache(maxsize=1024)
@@ -1016,6 +1066,12 @@ def fate_attn_prompt(q, k, v, off, scale: Optional[float] = None, lse: bool = Fa
     if _t.grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad or
                               (out is not None and out.requires_grad)):
         raise _no_gradient()
+    return _prompt(q, k, v, off, scale, None, lse, out, status)
+
+
+def _prompt(q, k, v, off, scale, shaping, lse, out, status):
+    """The call itself, on the current device and stream; shaping as for :func:`_paged`."""
+    dev, dtype = q.device, q.dtype
     shape, kv_shape = _three(q, "q"), _three(k, "k")
     T, hq, d = shape
     if kv_shape[0] != T or kv_shape[2] != d:
@@ -1028,12 +1084,28 @@ def fate_attn_prompt(q, k, v, off, scale: Optional[float] = None, lse: bool = Fa
         out = _t.empty_like(q)
     ro = _rows(out, "out", shape, dtype, dev)
     sums = _t.empty((T, hq), dtype=_t.float32, device=dev) if lse else None
-    st = load().fate_attn_prompt(h, s, rq, rk, rv, 1.0 / math.sqrt(d or 1) if scale is None else scale, ro,
-                                 sums.data_ptr() if lse else None, _attn_status(status, s.B, dev),
-                                 _t.raw_stream(dev.index))
+    scale = 1.0 / math.sqrt(d or 1) if scale is None else scale
+    rest = (ro, sums.data_ptr() if lse else None, _attn_status(status, s.B, dev), _t.raw_stream(dev.index))
+    if shaping is None:
+        st = load().fate_attn_prompt(h, s, rq, rk, rv, scale, *rest)
+    else:
+        st = load().fate_attn_prompt_shaped(h, s, rq, rk, rv, scale, _scores(*shaping, hq, s.B, T, dev), *rest)
     if st != FATE_OK:
-        raise FateError(st, "fate_attn_prompt")
+        raise FateError(st, "fate_attn_prompt" if shaping is None else "fate_attn_prompt_shaped")
     return out, sums
+
+
+def fate_attn_prompt_shaped(q, k, v, off, scale: Optional[float] = None, cap: float = 0.0, slopes=None, prefix=None,
+                            start=None, lse: bool = False, out=None, status=None, stream=None):
+    """:func:`fate_attn_prompt` with scores shaped as in
+    :func:`fate_attn_paged_shaped`."""
+    dev = q.device
+    if not _here(dev, stream):
+        return _there(dev, stream, fate_attn_prompt_shaped, q, k, v, off, scale, cap, slopes, prefix, start, lse, out, status)
+    if _t.grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad or
+                              (slopes is not None and slopes.requires_grad) or (out is not None and out.requires_grad)):
+        raise _no_gradient()
+    return _prompt(q, k, v, off, scale, (cap, slopes, prefix, start), lse, out, status)
 
 
 class Reserved(NamedTuple):

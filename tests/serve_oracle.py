@@ -59,3 +59,46 @@ def trim(keep, kv, pages, free, n_free, P):
             status[b] = EINVAL
         given.append(total)
     return np.array(kv, np.int64).reshape(-1), np.array([n_free + total]), np.array(given), free, np.array(status, np.int64)
+
+
+def attend_shaped(q, keys, values, pos, prefix, first, scale, cap=0.0, slopes=None):
+    """One sequence: q [n, hq, d] at positions pos, keys and values [L, hkv, d], float64.  Returns out, lse, the bounds of the
+    kernel's error of both before the roundings to the operands' type, and sum p |v|."""
+    n, hq, d = q.shape
+    L, hkv = keys.shape[:2]
+    j = np.arange(L)
+    seen = ((j < prefix) | ((j >= first[:, None]) & (j <= pos[:, None]))) & (pos[:, None] >= 0)
+    some = seen.any(1)
+    out, lse = np.zeros((n, hq, d)), np.full((n, hq), -np.inf)
+    tol, tol_lse, weighted = np.zeros((n, hq, d)), np.zeros((n, hq)), np.zeros((n, hq, d))
+    for h in range(hq):
+        if not some.any():
+            break
+        k, v = keys[:, h // (hq // hkv)], values[:, h // (hq // hkv)]
+        k, v = (np.where(seen.any(0)[:, None], x, 0.0) for x in (k, v))  # what no row sees may be anything
+        s = scale * (q[:, h] @ k.T)
+        # a float32 sum of d products, and the scale
+        e = scale * (d + 2) * 2.0 ** -24 * (np.abs(q[:, h]) @ np.abs(k.T)) + 2.0 ** -23 * np.abs(s)
+        if cap:
+            # argument, exp2, sum and reciprocal are each off by 2^-23 or less of theirs: three steps of 2^-22 of the cap;
+            # caps over 100 / log2(e) by the series where the quotient is below 1/4, some roundings of the score itself
+            series = (np.abs(s) < 0.25 * cap) & (cap * 1.4426950408889634 > 100)
+            s = cap * np.tanh(s / cap)
+            e = e + np.where(series, 2.0 ** -21 * np.abs(s), 3 * 2.0 ** -22 * cap)
+        if slopes is not None:
+            far = slopes[h] * np.abs(pos[:, None] - j)
+            s = s - far
+            e = e + 2.0 ** -22 * np.abs(far) + 2.0 ** -24 * np.abs(s)
+        s = np.where(seen, s, -np.inf)[some]
+        top = s.max(1, keepdims=True)
+        p = np.exp(s - top)
+        total = p.sum(1, keepdims=True)
+        lse[some, h] = (top + np.log(total))[:, 0]
+        p /= total
+        # the difference to the running maximum, exp2, the sum of the weights
+        e = e[some] + 2.0 ** -22 + 2.0 ** -23 * (np.where(seen[some], np.abs(s), 0) + np.abs(top)) + (L + 64) * 2.0 ** -24
+        out[some, h], weighted[some, h] = p @ v, p @ np.abs(v)
+        mean = (p * e).sum(1, keepdims=True)
+        tol[some, h] = 2 * ((p * e) @ np.abs(v) + mean * weighted[some, h]) + 2.0 ** -25 * (seen[some] @ np.abs(v)) + 1e-30
+        tol_lse[some, h] = 2 * mean[:, 0] + 2.0 ** -22 * (1 + np.abs(lse[some, h]))
+    return out, lse, tol, tol_lse, weighted

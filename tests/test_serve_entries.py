@@ -68,3 +68,20 @@ def test_axes():
     assert fate.rotation_axes((2, 1, 3)) == (0, 0, 1, 2, 2, 2)
     assert fate.rotation_axes((2, 1, 3), cyclic=True) == (0, 1, 2, 0, 2, 2)
     assert fate.rotation_axes(()) == fate.rotation_axes((), cyclic=True) == ()
+
+
+def test_shaped_scores():
+    f = fate.load()
+
+    def paged(scores, **x):
+        return f.fate_attn_paged_shaped(heads(), seqs(), rows(), cache(), 2, 0.1, scores, rows(**x), None, None, A, 1 << 40, None)
+
+    def prompt(scores, **x):
+        return f.fate_attn_prompt_shaped(heads(), seqs(), rows(), rows(), rows(), 0.1, scores, rows(**x), None, None, None)
+
+    for call in (paged, prompt):
+        assert call(None) == EINVAL
+        assert call(fate.Scores(), data=A + 8) == EINVAL  # as the plain calls check
+        for bad in (dict(cap=-1.0), dict(cap=float("nan")), dict(cap=float("inf")), dict(cap=1e-44), dict(cap=3e38), dict(slopes=A + 2),
+                    dict(prefix=A + 1), dict(start=A + 3)):
+            assert call(fate.Scores(**bad)) == EINVAL, bad
