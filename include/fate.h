@@ -566,8 +566,9 @@ fate_status_t fate_place_baseline_device(const fate_dags_t *dags, const fate_sta
  * written there, so clear it first) and leave that sequence's results
  * unspecified. */
 
-/* Element types of queries, keys, values and outputs. */
-enum { FATE_BF16 = 0, FATE_F16 = 1 };
+/* Element types: of queries, keys, values and outputs the first two, of logits
+ * all. */
+enum { FATE_BF16 = 0, FATE_F16 = 1, FATE_F32 = 2 };
 
 #define FATE_MAX_HEAD_DIM 256
 #define FATE_MAX_HEADS 256
@@ -787,6 +788,56 @@ fate_status_t fate_kv_reserve(const fate_kv_tables_t *tables, const int32_t *new
  * `pages` is only read.  Errors: as fate_kv_reserve. */
 fate_status_t fate_kv_trim(const fate_kv_tables_t *tables, const int32_t *keep, int32_t *kv_len_out,
                            int32_t *n_free_out, int32_t *given, int32_t *d_status, void *stream);
+
+/* Sampling: one token of each row of logits.
+ *   logits       element i of row r is logits[r * stride + i], i < vocab; any
+ *                alignment of the type's own size; stride in elements, 0 for
+ *                rows that are all the same
+ *   u            [rows] float32, random numbers in [0, 1)
+ *   temperature  [rows] or null: at least 0, finite; 0 takes the largest logit
+ *   top_k        [rows] or null: how many tokens are kept, 0 for all
+ *   top_p        [rows] or null: in (0, 1], 1 for no cut
+ *   min_p        [rows] or null: in [0, 1], 0 for no cut
+ * Where an array is null every row has the value `..._all`.  Device memory. */
+typedef struct {
+    int32_t dtype, rows, vocab;
+    int64_t stride;
+    const void *logits;
+    const float *u;
+    const float *temperature;
+    const int32_t *top_k;
+    const float *top_p, *min_p;
+    float temperature_all;
+    int32_t top_k_all;
+    float top_p_all, min_p_all;
+} fate_sampling_t;
+
+/* fate_sample_ws_size: device workspace bytes of fate_sample, from the counts
+ * alone.  Errors: EINVAL, ERANGE. */
+fate_status_t fate_sample_ws_size(const fate_sampling_t *sampling, size_t *bytes);
+
+/* fate_sample: with w_i = exp((l_i - max l) / temperature) and the row's tokens
+ * by falling logit, equal ones by rising index:
+ *   top_k  the first top_k are kept
+ *   top_p  of these, those before which less than top_p of their sum lies (the
+ *          first always is)
+ *   min_p  of these, those with w_i >= min_p
+ *   d_token[r]    the lowest i for which the kept w_j, j <= i, sum to more than
+ *                 u times the sum of all kept
+ *   d_logprob[r]  log(w_i / sum of all kept), float32, or null; 0 at
+ *                 temperature 0
+ * Weights and sums are in 64 bits, in an order of their own for each size: two
+ * calls give the same token.  A logit of -infinity or NaN is never taken; where
+ * all are, the token is -1 and its logprob -infinity.  If the largest is
+ * +infinity the tokens at it share the row.  A row whose settings or random
+ * number are out of range gets these too, and FATE_EINVAL in d_status[r] ([rows]
+ * or null; nothing else is written there).
+ *   d_ws   fate_sample_ws_size bytes, aligned to 16, contents irrelevant; calls
+ *          that may overlap in time need one each
+ * Errors: EINVAL (null pointers, types, alignment, a value for all out of
+ * range), ERANGE (rows at 2^22, vocab past 2^30), ESIZE (workspace), EHIP. */
+fate_status_t fate_sample(const fate_sampling_t *sampling, int32_t *d_token, float *d_logprob, int32_t *d_status,
+                          void *d_ws, size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -1,9 +1,11 @@
-// C entries of the calls around the attention of a planned wave: page tables.
+// C entries of the calls around the attention of a planned wave: page tables, sampling.
 // Checks of what the host can see, launches.  Nothing here allocates or throws.
+#include <cmath>
 #include <cstdint>
 
 #include "fate.h"
 #include "fate_pages.h"
+#include "fate_sample.h"
 
 namespace {
 
@@ -35,6 +37,20 @@ PagesLaunch launch_of(const fate_kv_tables_t *t) {
     a.n_pages = t->n_pages;
     a.shift = __builtin_ctz((unsigned)t->page_size);
     return a;
+}
+
+// A launch takes fewer than 2^32 threads, and a row has a workgroup of 1024; places in a row are 32-bit.
+constexpr int32_t kMaxRows = (1 << 22) - 1, kMaxVocab = 1 << 30;
+
+fate_status_t check_sampling(const fate_sampling_t *s) {
+    if (!s || s->rows < 0 || s->vocab < 1 || s->stride < 0) return FATE_EINVAL;
+    if (s->dtype != FATE_BF16 && s->dtype != FATE_F16 && s->dtype != FATE_F32) return FATE_EINVAL;
+    if (s->rows > kMaxRows || s->vocab > kMaxVocab) return FATE_ERANGE;
+    if (!s->temperature && !(std::isfinite(s->temperature_all) && s->temperature_all >= 0.0f)) return FATE_EINVAL;
+    if (!s->top_k && s->top_k_all < 0) return FATE_EINVAL;
+    if (!s->top_p && !(s->top_p_all > 0.0f && s->top_p_all <= 1.0f)) return FATE_EINVAL;
+    if (!s->min_p && !(s->min_p_all >= 0.0f && s->min_p_all <= 1.0f)) return FATE_EINVAL;
+    return FATE_OK;
 }
 
 }  // namespace
@@ -77,6 +93,47 @@ fate_status_t fate_kv_trim(const fate_kv_tables_t *tables, const int32_t *keep, 
     a.moved = given;
     a.status = d_status;
     return fate::launch_trim(a, stream) == 0 ? FATE_OK : FATE_EHIP;
+}
+
+fate_status_t fate_sample_ws_size(const fate_sampling_t *s, size_t *bytes) {
+    const fate_status_t st = check_sampling(s);
+    if (st != FATE_OK) return st;
+    if (!bytes) return FATE_EINVAL;
+    *bytes = 0;
+    return FATE_OK;
+}
+
+fate_status_t fate_sample(const fate_sampling_t *s, int32_t *d_token, float *d_logprob, int32_t *d_status, void *d_ws,
+                          size_t ws_bytes, void *stream) {
+    size_t need = 0;
+    const fate_status_t st = fate_sample_ws_size(s, &need);
+    if (st != FATE_OK) return st;
+    if (s->rows == 0) return FATE_OK;
+    if (!aligned(s->logits, s->dtype == FATE_F32 ? 4 : 2) || !aligned(s->u, 4) || !aligned(d_token, 4)) return FATE_EINVAL;
+    for (const void *p : {(const void *)s->temperature, (const void *)s->top_k, (const void *)s->top_p,
+                          (const void *)s->min_p, (const void *)d_logprob, (const void *)d_status})
+        if (p && !aligned(p, 4)) return FATE_EINVAL;
+    if (need && !aligned(d_ws, 16)) return FATE_EINVAL;
+    if (ws_bytes < need) return FATE_ESIZE;
+    fate::SampleLaunch a = {};
+    a.logits = static_cast<const char *>(s->logits);
+    a.u = s->u;
+    a.temperature = s->temperature;
+    a.top_k = s->top_k;
+    a.top_p = s->top_p;
+    a.min_p = s->min_p;
+    a.token = d_token;
+    a.logprob = d_logprob;
+    a.status = d_status;
+    a.stride = s->stride;
+    a.rows = s->rows;
+    a.vocab = s->vocab;
+    a.dtype = s->dtype;
+    a.temperature_all = s->temperature_all;
+    a.top_k_all = s->top_k_all;
+    a.top_p_all = s->top_p_all;
+    a.min_p_all = s->min_p_all;
+    return fate::launch_sample(a, stream) == 0 ? FATE_OK : FATE_EHIP;
 }
 
 }  // extern "C"

@@ -39,14 +39,14 @@ EXPORTS = ["fate_version", "fate_strerror", "fate_pack_dags_size", "fate_pack_da
            "fate_simulate", "fate_place_baseline", "fate_sim_ws_size", "fate_simulate_device",
            "fate_place_baseline_device", "fate_kv_append", "fate_attn_paged_ws_size", "fate_attn_paged",
            "fate_attn_prompt", "fate_kv_reserve", "fate_kv_trim", "fate_kv_append_axes",
-           "fate_attn_paged_shaped", "fate_attn_prompt_shaped"]
+           "fate_attn_paged_shaped", "fate_attn_prompt_shaped", "fate_sample_ws_size", "fate_sample"]
 
 # Scoring variants and packing options (fate_params_t.flags, fate_pack_opts_t.levels).
 FATE_MEAN_PER_LEVEL, FATE_NO_WINDOWS = 1, 2
 FATE_LEVELS_HOP, FATE_LEVELS_TOPO = 0, 1
 FATE_MAX_SWEEP = 16
 FATE_PLACE_ROUND_ROBIN, FATE_PLACE_HEFT = 0, 1
-FATE_BF16, FATE_F16 = 0, 1
+FATE_BF16, FATE_F16, FATE_F32 = 0, 1, 2
 FATE_NOALLOC_WS_BYTES = 32 << 20  # workspace the library holds per GPU for fate_commit_advance_noalloc
 
 
@@ -146,6 +146,13 @@ class KvTables(C.Structure):
                 ("kv_len", C.c_void_p)]
 
 
+class Sampling(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("rows", C.c_int32), ("vocab", C.c_int32), ("stride", C.c_int64),
+                ("logits", C.c_void_p), ("u", C.c_void_p), ("temperature", C.c_void_p), ("top_k", C.c_void_p),
+                ("top_p", C.c_void_p), ("min_p", C.c_void_p), ("temperature_all", C.c_float), ("top_k_all", C.c_int32),
+                ("top_p_all", C.c_float), ("min_p_all", C.c_float)]
+
+
 _lib = None
 
 
@@ -218,6 +225,8 @@ def load(path: Optional[str] = None):
     lib.fate_kv_reserve.argtypes = [P(KvTables), C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
     lib.fate_kv_trim.argtypes = [P(KvTables), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+    lib.fate_sample_ws_size.argtypes = [P(Sampling), P(C.c_size_t)]
+    lib.fate_sample.argtypes = [P(Sampling), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
     for name in EXPORTS[2:]:
         getattr(lib, name).restype = st
     if path is None:
@@ -724,6 +733,7 @@ class _Torch:
     def __init__(self):
         import torch
         self.types = {torch.bfloat16: FATE_BF16, torch.float16: FATE_F16}
+        self.logit_types = {torch.bfloat16: FATE_BF16, torch.float16: FATE_F16, torch.float32: FATE_F32}
         self.int32, self.int64, self.float32, self.uint8 = torch.int32, torch.int64, torch.float32, torch.uint8
         self.empty, self.empty_like, self.Tensor = torch.empty, torch.empty_like, torch.Tensor
         self.device, self.stream = torch.cuda.device, torch.cuda.stream
@@ -1128,8 +1138,8 @@ class Trimmed(NamedTuple):
     given: object
 
 
-def _ints_of(t, name, n, dtype, device):
-    """A contiguous tensor of n whole numbers."""
+def _array(t, name, n, dtype, device):
+    """A contiguous tensor of n numbers."""
     if t.dtype is not dtype or t.device != device or t.shape != (n,) or (n > 1 and t.stride(0) != 1):
         raise ValueError("%s must be a contiguous %s tensor of %d elements on %s, got %s %s on %s" % (
             name, dtype, n, device, t.dtype, list(t.shape), t.device))
@@ -1142,13 +1152,13 @@ def _kv_tables(counts, name, kv_len, pages, free, n_free, page_size, device) -> 
         raise ValueError("kv_len must be [B], pages [B, max_pages] and free [n_pages], got %s, %s and %s" % (
             list(kv_len.shape), list(pages.shape), list(free.shape)))
     B, width = pages.shape
-    _ints_of(counts, name, B, int32, device)
+    _array(counts, name, B, int32, device)
     row, one = pages.stride()
     if pages.dtype is not int32 or pages.device != device or (one != 1 and width > 1):
         raise ValueError("pages must be int32 on %s, each row contiguous" % device)
     return KvTables(B, width, page_size, free.shape[0], row if B > 1 else width, pages.data_ptr(),
-                    _ints_of(free, "free", free.shape[0], int32, device), _ints_of(n_free, "n_free", 1, int32, device),
-                    _ints_of(kv_len, "kv_len", B, int32, device))
+                    _array(free, "free", free.shape[0], int32, device), _array(n_free, "n_free", 1, int32, device),
+                    _array(kv_len, "kv_len", B, int32, device))
 
 
 def fate_kv_reserve(new, kv_len, pages, free, n_free, page_size: int, T: int, out: Optional[Reserved] = None, status=None,
@@ -1179,10 +1189,10 @@ def fate_kv_reserve(new, kv_len, pages, free, n_free, page_size: int, T: int, ou
         out = Reserved(n[:B + 1], n[B + 1:2 * B + 1], n[2 * B + 1:2 * B + 2], n[2 * B + 2:],
                        _t.empty(T, dtype=int64, device=dev), _t.empty(T, dtype=int32, device=dev))
     st = load().fate_kv_reserve(
-        t, new.data_ptr(), T, _ints_of(out.off, "out.off", B + 1, int32, dev), _ints_of(out.kv_len, "out.kv_len", B, int32, dev),
-        _ints_of(out.n_free, "out.n_free", 1, int32, dev), _ints_of(out.taken, "out.taken", B + 1, int32, dev),
-        None if out.slots is None else _ints_of(out.slots, "out.slots", T, int64, dev),
-        None if out.positions is None else _ints_of(out.positions, "out.positions", T, int32, dev),
+        t, new.data_ptr(), T, _array(out.off, "out.off", B + 1, int32, dev), _array(out.kv_len, "out.kv_len", B, int32, dev),
+        _array(out.n_free, "out.n_free", 1, int32, dev), _array(out.taken, "out.taken", B + 1, int32, dev),
+        None if out.slots is None else _array(out.slots, "out.slots", T, int64, dev),
+        None if out.positions is None else _array(out.positions, "out.positions", T, int32, dev),
         _attn_status(status, B, dev), _t.raw_stream(dev.index))
     if st != FATE_OK:
         raise FateError(st, "fate_kv_reserve")
@@ -1203,13 +1213,88 @@ def fate_kv_trim(keep, kv_len, pages, free, n_free, page_size: int, out: Optiona
     if out is None:
         n = _t.empty(2 * B + 2, dtype=int32, device=dev)
         out = Trimmed(n[:B], n[B:B + 1], n[B + 1:])
-    st = load().fate_kv_trim(t, keep.data_ptr(), _ints_of(out.kv_len, "out.kv_len", B, int32, dev),
-                             _ints_of(out.n_free, "out.n_free", 1, int32, dev),
-                             _ints_of(out.given, "out.given", B + 1, int32, dev), _attn_status(status, B, dev),
+    st = load().fate_kv_trim(t, keep.data_ptr(), _array(out.kv_len, "out.kv_len", B, int32, dev),
+                             _array(out.n_free, "out.n_free", 1, int32, dev),
+                             _array(out.given, "out.given", B + 1, int32, dev), _attn_status(status, B, dev),
                              _t.raw_stream(dev.index))
     if st != FATE_OK:
         raise FateError(st, "fate_kv_trim")
     return out
+
+
+def fate_sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, logprob: bool = False, out=None, status=None,
+                ws=None, stream=None):
+    """One token of each row of logits [rows, vocab] (bfloat16, float16 or
+    float32, each row contiguous) from random numbers u [rows] in [0, 1).
+
+    temperature, top_k, top_p and min_p are numbers, or tensors [rows] (top_k
+    int32, the others float32): temperature 0 takes the largest logit (the lowest
+    index of equal ones), top_k 0, top_p 1 and min_p 0 cut nothing.  Of the tokens
+    by falling logit the first top_k are kept, of these those before which less
+    than top_p of their sum lies, of these those whose weight is at least min_p
+    times the largest.  The token is the lowest index at which the kept weights
+    sum to more than u of their whole.  Returns (token, logprob): int32 [rows], and
+    the logarithm of the token's share of what is kept, float32, if asked for,
+    else None.  Rows with nothing to take get -1.  ``out`` and ``ws`` (uint8, as
+    large as :func:`fate_sample_ws_size` says) are made if not given; ``status``
+    (int32 [rows], cleared by the caller) receives FATE_EINVAL for rows whose
+    settings or u are out of range.  There is no gradient."""
+    dev = logits.device
+    if not _here(dev, stream):
+        return _there(dev, stream, fate_sample, logits, u, temperature, top_k, top_p, min_p, logprob, out, status, ws)
+    if _t.grad_enabled() and logits.requires_grad:
+        raise ValueError("sampling has no gradient: pass detached logits or call it under torch.no_grad()")
+    s = _sampling(logits, dev)
+    R = s.rows
+    f32, i32 = _t.float32, _t.int32
+    s.u = _array(u, "u", R, f32, dev)
+    for name, value, dtype in (("temperature", temperature, f32), ("top_k", top_k, i32), ("top_p", top_p, f32), ("min_p", min_p, f32)):
+        if isinstance(value, _t.Tensor):
+            setattr(s, name, _array(value, name, R, dtype, dev))
+        else:
+            setattr(s, name + "_all", value)
+    if out is None:
+        out = _t.empty(R, dtype=i32, device=dev)
+    shares = _t.empty(R, dtype=f32, device=dev) if logprob else None
+    need = _sample_ws(s.dtype, R, s.vocab)
+    if ws is None:
+        ws = _t.empty(need, dtype=_t.uint8, device=dev) if need else None
+    elif ws.device != dev or not ws.is_contiguous():
+        raise ValueError("ws must be contiguous, on %s" % dev)
+    st = load().fate_sample(s, _array(out, "out", R, i32, dev), shares.data_ptr() if logprob else None,
+                            _attn_status(status, R, dev), None if ws is None else ws.data_ptr(), 0 if ws is None else ws.nbytes,
+                            _t.raw_stream(dev.index))
+    if st != FATE_OK:
+        raise FateError(st, "fate_sample")
+    return out, shares
+
+
+def _sampling(logits, dev) -> Sampling:
+    kind = _t.logit_types.get(logits.dtype)
+    if kind is None or logits.dim() != 2:
+        raise ValueError("logits must be bfloat16, float16 or float32 [rows, vocab], got %s %s" % (logits.dtype, list(logits.shape)))
+    R, V = logits.shape
+    row, one = logits.stride()
+    if one != 1 and V > 1:
+        raise ValueError("each row of logits must be contiguous")
+    return Sampling(kind, R, V, row if R > 1 else V, logits.data_ptr(), temperature_all=1.0, top_p_all=1.0)
+
+
+@functools.lru_cache(maxsize=1024)
+def _sample_ws(dtype: int, rows: int, vocab: int) -> int:
+    """The library's workspace size, which depends on these alone."""
+    nbytes = C.c_size_t(0)
+    st = load().fate_sample_ws_size(Sampling(dtype, rows, vocab, temperature_all=1.0, top_p_all=1.0), nbytes)
+    if st != FATE_OK:
+        raise FateError(st, "fate_sample_ws_size")
+    return nbytes.value
+
+
+def fate_sample_ws_size(logits) -> int:
+    """Workspace bytes of :func:`fate_sample` for logits of this type and shape."""
+    _here(logits.device, None)
+    s = _sampling(logits, logits.device)
+    return _sample_ws(s.dtype, s.rows, s.vocab)
 
 
 def rotation_table(positions: int, rot: int, base: float = 10000.0, device="cuda"):

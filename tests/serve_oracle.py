@@ -102,3 +102,29 @@ def attend_shaped(q, keys, values, pos, prefix, first, scale, cap=0.0, slopes=No
         tol[some, h] = 2 * ((p * e) @ np.abs(v) + mean * weighted[some, h]) + 2.0 ** -25 * (seen[some] @ np.abs(v)) + 1e-30
         tol_lse[some, h] = 2 * mean[:, 0] + 2.0 ** -22 * (1 + np.abs(lse[some, h]))
     return out, lse, tol, tol_lse, weighted
+
+
+def sample(row, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, u=0.0):
+    """The token of one row and the logarithm of its share; sums in extended precision."""
+    logits = np.where(np.isnan(row), -np.inf, np.asarray(row, np.float64))
+    top = logits.max()
+    if top == -np.inf:
+        return -1, -np.inf
+    if temperature == 0:
+        return int(np.argmax(logits)), 0.0
+    with np.errstate(invalid="ignore"):
+        w = np.where(logits == top, 0.0, (logits - top) / np.float64(temperature))
+    w = np.exp(w.astype(np.longdouble))
+    order = np.argsort(-logits, kind="stable")
+    order = order[logits[order] > -np.inf]
+    if top_k:
+        order = order[:top_k]
+    ranked = w[order]
+    keep = ranked >= min_p
+    if top_p < 1:
+        keep &= ranked.cumsum() - ranked < np.longdouble(top_p) * ranked.sum()
+    keep[0] = True
+    kept = np.sort(order[keep])
+    upto = w[kept].cumsum()
+    token = int(kept[min(np.searchsorted(upto, np.longdouble(u) * upto[-1], side="right"), len(kept) - 1)])
+    return token, float(np.log(w[token] / upto[-1]))

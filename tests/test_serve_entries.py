@@ -1,6 +1,8 @@
 """What the calls around a wave's attention refuse on the host, before anything reaches a GPU."""
 
 import ctypes as C
+import os
+import subprocess
 
 import pytest
 
@@ -85,3 +87,48 @@ def test_shaped_scores():
         for bad in (dict(cap=-1.0), dict(cap=float("nan")), dict(cap=float("inf")), dict(cap=1e-44), dict(cap=3e38), dict(slopes=A + 2),
                     dict(prefix=A + 1), dict(start=A + 3)):
             assert call(fate.Scores(**bad)) == EINVAL, bad
+
+
+def sampling(**x):
+    return fate.Sampling(**dict(dict(dtype=2, rows=3, vocab=100, stride=100, logits=A, u=A, temperature_all=1.0, top_p_all=1.0), **x))
+
+
+def test_sampling():
+    f, n = fate.load(), C.c_size_t(7)
+
+    def call(s, token=A, logprob=A, status=A, ws=A, ws_bytes=1 << 40):
+        return f.fate_sample(s, token, logprob, status, ws, ws_bytes, None)
+
+    nan, inf = float("nan"), float("inf")
+    for bad, status in ((dict(dtype=3), EINVAL), (dict(dtype=-1), EINVAL), (dict(rows=-1), EINVAL), (dict(vocab=0), EINVAL),
+                        (dict(stride=-1), EINVAL), (dict(rows=1 << 22), ERANGE), (dict(vocab=(1 << 30) + 1), ERANGE),
+                        (dict(temperature_all=-1.0), EINVAL), (dict(temperature_all=nan), EINVAL), (dict(temperature_all=inf), EINVAL),
+                        (dict(top_k_all=-1), EINVAL), (dict(top_p_all=0.0), EINVAL), (dict(top_p_all=1.5), EINVAL),
+                        (dict(top_p_all=nan), EINVAL), (dict(min_p_all=-0.5), EINVAL), (dict(min_p_all=1.5), EINVAL)):
+        assert call(sampling(**bad)) == status, bad
+        assert f.fate_sample_ws_size(sampling(**bad), n) == status and n.value == 7
+    for bad in (dict(logits=None), dict(logits=A + 2), dict(logits=A + 1, dtype=0), dict(u=None), dict(u=A + 2), dict(temperature=A + 1),
+                dict(top_k=A + 2), dict(top_p=A + 3), dict(min_p=A + 2)):
+        assert call(sampling(**bad)) == EINVAL, bad
+    assert call(None) == EINVAL and f.fate_sample_ws_size(None, n) == EINVAL and f.fate_sample_ws_size(sampling(), None) == EINVAL
+    assert call(sampling(), token=None) == call(sampling(), token=A + 2) == call(sampling(), logprob=A + 2) == EINVAL
+    assert call(sampling(), status=A + 2) == EINVAL
+    assert call(sampling(rows=0, logits=None)) == 0
+
+
+STRUCTS = [("fate_kv_tables_t", fate.KvTables), ("fate_axes_t", fate.Axes), ("fate_scores_t", fate.Scores), ("fate_sampling_t", fate.Sampling)]
+
+
+def test_structs_as_the_header_has_them(tmp_path):
+    lines, want = [], []
+    for name, mirror in STRUCTS:
+        lines.append('printf("%%zu\\n", sizeof(%s));' % name)
+        want.append(C.sizeof(mirror))
+        for field, _ in mirror._fields_:
+            lines.append('printf("%%zu\\n", offsetof(%s, %s));' % (name, field))
+            want.append(getattr(mirror, field).offset)
+    (tmp_path / "a.c").write_text('#include <stddef.h>\n#include <stdio.h>\n#include "fate.h"\nint main(void) {\n%s\nreturn 0; }\n' % "\n".join(lines))
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    subprocess.run(["gcc", "-std=c11", "-I", os.path.join(root, "include"), str(tmp_path / "a.c"), "-o", str(tmp_path / "a")], check=True)
+    out = subprocess.run([str(tmp_path / "a")], check=True, capture_output=True, text=True).stdout
+    assert [int(x) for x in out.split()] == want
