@@ -5,22 +5,25 @@
 //   top_p of their sum lies; of these those with w_i >= min_p.  The token is the
 //   lowest i with sum of w_j over the kept j <= i greater than u W, W the sum of
 //   all kept.  What is kept is a stretch of that order from its start, so one
-//   place in it, a key and an index, says which tokens are kept.
+//   place in it, a logit and an index, says which tokens are kept.
 //
 // Everything that a token hangs on is computed in 64 bits: between two
 // neighbours of 100000 tokens lies 1e-5 of W, and a sum that is off by 2^-24
 // would pick another one in every hundredth row.  Sums have a fixed order, and
 // where atomics add they add whole numbers: two calls give the same token.
 //
-// k_sample: one workgroup per row.  It reads the row once for its largest
-// logit.  Where few tokens can be kept (few tokens at all, a small top_k, a min_p
-// without top_p) a second reading gathers them into LDS, where they are
-// ranked, cut, put back in order and summed.  The bound for top_k is the k-th
-// largest of the threads' own largest logits: at least k tokens reach it, and
-// hardly more do.  Where the gathered do not fit, and for top_p over all tokens,
-// the place of the cut is found by its digits (11, 11 and 10 bits of the key),
-// each by a histogram, of counts or of weights as whole numbers; then two
-// readings find the token, of which the second is of a sixteenth of the row.
+// k_sample: one workgroup per row.  It reads the row for its largest logit and,
+// for top_p, once more for the sum of all weights.  Where few tokens can be kept
+// the next reading gathers them into LDS in the order of their indices, where
+// the place of the cut is found by ranking those in question against each other,
+// and the token by sums up to each.  What can be kept is known from bins of the
+// logits: of the threads' largest ones for top_k (at least k tokens reach the k-th
+// of these, and hardly more do), of all that matter, by weights as whole numbers,
+// for top_p.  Where the gathered do not fit, the place of the cut is found by its
+// digits (11, 11 and 10 bits of the key), each by a histogram, of counts or of
+// weights; then two readings find the token, of which the second is of a
+// sixteenth of the row.  Instructions bind it, of a weight some 22; code that is
+// run once costs what its fetching costs, so that loops are kept short.
 #include <hip/hip_runtime.h>
 
 #include "fate_sample.h"
@@ -32,20 +35,33 @@ typedef unsigned long long u64;
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
-constexpr int kList = 4096;   // tokens that are ranked in LDS
-constexpr int kSmallK = 1024; // largest top_k that the threads' largest logits bound
+constexpr int kOwn = 512;      // tokens that a wave gathers in LDS, at most
+constexpr int kMany = kWaves * kOwn + 1;  // more than the list holds
+constexpr int kRanked = 512;   // of these, most that are ranked
+constexpr int kSmallK = 1024;  // largest top_k that the threads' largest logits bound
 constexpr int kBins = 2048;
 
 struct Lds {
-    u64 list[kList];
+    double table[256];
+    u64 list[kWaves * kOwn];
     u64 hist[kBins];
-    u64 whole[kWaves];
+    struct {
+        u64 entry;
+        double weight;
+    } ranked[kRanked + 8];
+    u64 whole[kWaves], least[kWaves];
     double real[kWaves];
-    uint32_t word[kWaves];
-    int count, found, sub;
+    float ends[2][8];  // the values of the row's first and last piece
     u64 above, in_bin;
-    double rest, weight;
+    double share;
+    int found, counts[kWaves];
 };
+
+// The workgroup's, of the kernel and of what it calls.
+__device__ __forceinline__ Lds &lds() {
+    __shared__ Lds s;
+    return s;
+}
 
 // Keys: whole numbers in the order of the logits.  0 is no token: NaN, -infinity
 // and places outside the row.
@@ -57,6 +73,10 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 __device__ __forceinline__ float value_of(uint32_t key) {
     return __builtin_bit_cast(float, key & 0x80000000u ? key & 0x7fffffffu : ~key);
 }
+// A token of the list: key and index, larger ones earlier in the order.
+__device__ __forceinline__ u64 entry_of(uint32_t key, int index) { return (u64)key << 32 | (uint32_t)~index; }
+__device__ __forceinline__ float logit_of(u64 entry) { return value_of((uint32_t)(entry >> 32)); }
+__device__ __forceinline__ int index_of(u64 entry) { return (int)~(uint32_t)entry; }
 
 struct F32 {
     static constexpr int kPer = 4;
@@ -88,79 +108,103 @@ struct H16 {
 };
 
 // A row in pieces of 16 aligned bytes, numbered from that of its first element;
-// the first and last may reach over its ends, and are read element by element.
+// the first and the last may reach over its ends.
 template <class T>
 struct Row {
     const char *data;
     int V, lead, pieces;  // lead: places of the first piece before the row
+    int whole0, whole1;   // the first and the last piece within the row; none if the last is before the first
 
     __device__ __forceinline__ Row(const SampleLaunch &a, int row) {
         data = a.logits + (int64_t)row * a.stride * T::kBytes;
         V = a.vocab;
         lead = (int)((uintptr_t)data % 16) / T::kBytes;
         pieces = (int)(((int64_t)V + lead + T::kPer - 1) / T::kPer);
+        whole0 = lead ? 1 : 0;
+        whole1 = (int)(((int64_t)V + lead) / T::kPer) - 1;
     }
-    // Index of the piece's first element, and its keys.
-    __device__ __forceinline__ int keys(int piece, uint32_t (&k)[T::kPer]) const {
-        const int i0 = piece * T::kPer - lead;
-        if (i0 >= 0 && i0 + T::kPer <= V) {
-            const u32x4 x = *(const u32x4 *)(data + (int64_t)i0 * T::kBytes);
-#pragma unroll
-            for (int e = 0; e < T::kPer; ++e) k[e] = key_of(T::get(x, e));
-        } else {
-#pragma unroll
-            for (int e = 0; e < T::kPer; ++e) {
-                const int i = i0 + e;
-                k[e] = i >= 0 && i < V ? key_of(T::at(data, i)) : 0;
-            }
+    // (a barrier before the first `each`)
+    __device__ __forceinline__ void read_ends() const {
+        const int tid = threadIdx.x;
+        if (tid < 16) {
+            const int i = index(tid < 8 ? 0 : pieces - 1) + (tid & 7);
+            lds().ends[tid >> 3][tid & 7] = i >= 0 && i < V && (tid & 7) < T::kPer ? T::at(data, i) : __builtin_nanf("");
         }
-        return i0;
+    }
+    __device__ __forceinline__ int index(int piece) const { return piece * T::kPer - lead; }
+    __device__ __forceinline__ u32x4 load(int piece) const {
+        return *(const u32x4 *)(data + (int64_t)index(piece) * T::kBytes);
     }
 };
 
-// f(key, index) for the tokens of pieces from + lane, from + lane + step ..
+// f(values, index of the first) for pieces from, from + step .., in this order;
+// what lies outside the row is NaN, which compares as nothing.  Pieces within
+// the row go four (of 16-bit logits two) at a time, their loads together and
+// without checks of each.  All lanes of a wave call f as often, those without a
+// piece on NaN.
 template <class T, class F>
 __device__ __forceinline__ void each(const Row<T> &row, int from, int to, int step, F f) {
-    for (int p = from; p < to; p += step) {
-        uint32_t k[T::kPer];
-        const int i0 = row.keys(p, k);
+    constexpr int kAhead = 16 / T::kPer;
+    const int last = min(to - 1, row.whole1);
+    for (int p = from; __any(p < to);) {
+        if (__all(p >= row.whole0 && p + (kAhead - 1) * step <= last)) {
+            u32x4 x[kAhead];
 #pragma unroll
-        for (int e = 0; e < T::kPer; ++e)
-            if (k[e]) f(k[e], i0 + e);
+            for (int u = 0; u < kAhead; ++u) x[u] = row.load(p + u * step);
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                float v[T::kPer];
+#pragma unroll
+                for (int e = 0; e < T::kPer; ++e) v[e] = T::get(x[u], e);
+                f(v, row.index(p + u * step));
+            }
+            p += kAhead * step;
+        } else {
+            float v[T::kPer];
+#pragma unroll
+            for (int e = 0; e < T::kPer; ++e) v[e] = __builtin_nanf("");
+            if (p < to && (p < row.whole0 || p > row.whole1)) {
+#pragma unroll
+                for (int e = 0; e < T::kPer; ++e) v[e] = lds().ends[p > 0][e];
+            } else if (p < to) {
+                const u32x4 x = row.load(p);
+#pragma unroll
+                for (int e = 0; e < T::kPer; ++e) v[e] = T::get(x, e);
+            }
+            f(v, row.index(p));
+            p += step;
+        }
     }
 }
 
-// e^z for z <= 0 to some 2^-52: z = n ln 2 + x with |x| <= ln 2 / 2, and the
-// series of e^x to x^13 / 13! (the next term is 2^-57 of it).
-__device__ __forceinline__ double exp_of(double z) {
-    z = fmax(z, -800.0);  // 0 from -745 on
-    const double n = __builtin_rint(z * 1.4426950408889634074);
-    const double x = __builtin_fma(n, -0.69314718055994530942, z);
-    double f = 1.0 / 6227020800.0;
-    f = __builtin_fma(f, x, 1.0 / 479001600.0);
-    f = __builtin_fma(f, x, 1.0 / 39916800.0);
-    f = __builtin_fma(f, x, 1.0 / 3628800.0);
-    f = __builtin_fma(f, x, 1.0 / 362880.0);
-    f = __builtin_fma(f, x, 1.0 / 40320.0);
-    f = __builtin_fma(f, x, 1.0 / 5040.0);
-    f = __builtin_fma(f, x, 1.0 / 720.0);
-    f = __builtin_fma(f, x, 1.0 / 120.0);
-    f = __builtin_fma(f, x, 1.0 / 24.0);
-    f = __builtin_fma(f, x, 1.0 / 6.0);
-    f = __builtin_fma(f, x, 0.5);
-    f = __builtin_fma(f, x, 1.0);
-    f = __builtin_fma(f, x, 1.0);
-    return __builtin_ldexp(f, (int)n);
-}
-
-// Weight of a key below the largest one.
+// Weight of a logit, e^z with z = (l - max) / temperature <= 0; 0 of NaN and -infinity.
+// With y = z 256 / ln 2 = 256 n + j + x, |x| <= 1/2, it is 2^n 2^(j / 256) and
+// the series of e^(x ln 2 / 256) to its fourth power (the next term is 2^-54):
+// half the steps of a series without the table, 2^(j / 256) by j in LDS.
+constexpr int kTable = 256;
 struct Weight {
-    uint32_t top;
-    double max, per;  // 1 / temperature
-    __device__ __forceinline__ double operator()(uint32_t key) const {
-        return key == top ? 1.0 : exp_of(((double)value_of(key) - max) * per);
+    double max, per;  // per = 256 / (ln 2 temperature)
+    __device__ __forceinline__ double operator()(float v) const {
+        constexpr double c = 0.69314718055994530942 / kTable;
+        const double y = fmax(((double)v - max) * per, -4e5);  // 0 from there on
+        const double n = __builtin_rint(y), x = y - n;
+        double f = __builtin_fma(x, c * c * c * c / 24.0, c * c * c / 6.0);
+        f = __builtin_fma(f, x, c * c / 2.0);
+        f = __builtin_fma(f, x, c);
+        f = __builtin_fma(f, x, 1.0);
+        const int i = (int)n;
+        return __builtin_ldexp(f * lds().table[i & (kTable - 1)], i >> 8);
     }
+    __device__ __forceinline__ double of_key(uint32_t key) const { return (*this)(value_of(key)); }
 };
+
+// The kept tokens: those over a place in the order.
+struct Place {
+    float value;
+    int index;
+    __device__ __forceinline__ bool keeps(float v, int i) const { return (v > value) | ((v == value) & (i <= index)); }
+};
+constexpr int kAll = 0x7fffffff;
 
 // The least whole number that is p * n or more, p in (0, 1], 1 <= n < 2^63.
 __device__ __forceinline__ u64 share_of(float p, u64 n) {
@@ -171,29 +215,48 @@ __device__ __forceinline__ u64 share_of(float p, u64 n) {
     return (u64)((x + (((unsigned __int128)1 << shift) - 1)) >> shift);
 }
 
-// The kept tokens: those over a place in the order.
-struct Place {
-    uint32_t key;
-    int index;
-    __device__ __forceinline__ bool keeps(uint32_t k, int i) const { return k > key || (k == key && i <= index); }
-};
-constexpr int kAll = 0x7fffffff;
-
-__device__ __forceinline__ double wave_add(double x) {
-#pragma unroll
-    for (int i = 1; i < 64; i <<= 1) x += __shfl_xor(x, i);
-    return x;
+// Another lane's value, by a move within rows of 16 lanes or from one to the
+// next (0 where there is none), and lane i's value, the same in all lanes.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int moved32(int x) {
+    return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, false);
+}
+template <int CTRL, int ROWS, class I>
+__device__ __forceinline__ I moved(I x) {
+    static_assert(sizeof(I) == 8, "eight bytes");
+    const u64 y = __builtin_bit_cast(u64, x);
+    return __builtin_bit_cast(I, (u64)(uint32_t)moved32<CTRL, ROWS>((int)(y >> 32)) << 32 |
+                                     (uint32_t)moved32<CTRL, ROWS>((int)y));
+}
+template <class I>
+__device__ __forceinline__ I of_lane(I x, int i) {
+    const u64 y = __builtin_bit_cast(u64, x);
+    return __builtin_bit_cast(I, (u64)(uint32_t)__builtin_amdgcn_readlane((int)(y >> 32), i) << 32 |
+                                     (uint32_t)__builtin_amdgcn_readlane((int)y, i));
 }
 template <class I>
 __device__ __forceinline__ I wave_upto(I x) {  // sums up to and with this lane
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int i = 1; i < 64; i <<= 1) {
-        const I y = __shfl_up(x, i);
-        if (lane >= i) x += y;
-    }
+    x += moved<0x111, 0xF>(x);
+    x += moved<0x112, 0xF>(x);
+    x += moved<0x114, 0xF>(x);
+    x += moved<0x118, 0xF>(x);
+    x += moved<0x142, 0xA>(x);
+    x += moved<0x143, 0xC>(x);
     return x;
 }
+template <class I>
+__device__ __forceinline__ I wave_add(I x) { return of_lane(wave_upto(x), 63); }
+__device__ __forceinline__ u64 larger(u64 x, u64 y) { return x > y ? x : y; }
+__device__ __forceinline__ u64 wave_max(u64 x) {
+    x = larger(x, moved<0x111, 0xF>(x));
+    x = larger(x, moved<0x112, 0xF>(x));
+    x = larger(x, moved<0x114, 0xF>(x));
+    x = larger(x, moved<0x118, 0xF>(x));
+    x = larger(x, moved<0x142, 0xA>(x));
+    x = larger(x, moved<0x143, 0xC>(x));
+    return of_lane(x, 63);
+}
+
 // Sums up to and with this thread, and of all.
 template <class I>
 __device__ __forceinline__ I block_upto(I x, I (&part)[kWaves], I &total) {
@@ -212,97 +275,76 @@ __device__ __forceinline__ I block_upto(I x, I (&part)[kWaves], I &total) {
 }
 
 __device__ __forceinline__ u64 block_max(u64 x, Lds &s) {
-#pragma unroll
-    for (int i = 1; i < 64; i <<= 1) {
-        const u64 y = __shfl_xor(x, i);
-        x = y > x ? y : x;
-    }
+    x = wave_max(x);
     if ((threadIdx.x & 63) == 0) s.whole[threadIdx.x >> 6] = x;
     __syncthreads();
-    for (int i = 0; i < kWaves; ++i) x = s.whole[i] > x ? s.whole[i] : x;
+    x = 0;
+    for (int i = 0; i < kWaves; ++i) x = larger(x, s.whole[i]);
     __syncthreads();
     return x;
 }
 
-// The list's first n entries (n at most kList) by falling value, pair by pair
-// in a bitonic network: up to 64 in one wave's registers, more in LDS.
-__device__ void sort_list(Lds &s, int n) {
-    const int tid = threadIdx.x;
-    if (n <= 64) {
-        if (tid < 64) {
-            u64 x = tid < n ? s.list[tid] : 0;
-#pragma unroll
-            for (int size = 2; size <= 64; size <<= 1)
-#pragma unroll
-                for (int d = size >> 1; d > 0; d >>= 1) {
-                    const u64 y = __shfl_xor(x, d);
-                    const bool larger = ((tid & size) == 0) == ((tid & d) == 0);  // this lane keeps the larger one
-                    x = (y > x) == larger ? y : x;
-                }
-            if (tid < n) s.list[tid] = x;
-        }
-        __syncthreads();
-        return;
+// Bins of logits from `top` down to `bottom`, which falls into the last.
+struct Bins {
+    float top, per;
+    __device__ __forceinline__ Bins(float t, float bottom) : top(t), per((kBins - 1) / (t - bottom)) {}
+    __device__ __forceinline__ bool good() const { return per > 0.0f && per < INFINITY; }
+    __device__ __forceinline__ int of(float v) const {
+        return (int)fminf(__fmul_rn(__fsub_rn(top, v), per), kBins - 1);
     }
-    int all = 128;
-    while (all < n) all <<= 1;
-    for (int i = n + tid; i < all; i += kThreads) s.list[i] = 0;
-    __syncthreads();
-    for (int size = 2; size <= all; size <<= 1)
-        for (int d = size >> 1; d > 0; d >>= 1) {
-            for (int x = tid; x < all / 2; x += kThreads) {
-                const int i = 2 * x - (x & (d - 1)), j = i + d;
-                const u64 a = s.list[i], b = s.list[j];
-                if ((a < b) == ((i & size) == 0)) {
-                    s.list[i] = b;
-                    s.list[j] = a;
-                }
-            }
-            __syncthreads();
-        }
+    // a logit below all of the bin's
+    __device__ __forceinline__ float under(int bin) const {
+        const float edge = top - (float)(bin + 1) / per;
+        return edge - 1e-6f * (__builtin_fabsf(top) + __builtin_fabsf(edge));
+    }
+};
+
+__device__ __forceinline__ void clear_bins(Lds &s) {
+    for (int i = threadIdx.x; i < kBins; i += kThreads) s.hist[i] = 0;
 }
 
-// The k-th largest of the threads' words (1 <= k <= kThreads), by digits of eight bits.
-__device__ uint32_t kth_word(Lds &s, uint32_t mine, int k) {
+// The bin in which the sums of s.hist reach `target`, or -1.
+__device__ __forceinline__ int bin_at(Lds &s, u64 target) {
     const int tid = threadIdx.x;
-    uint32_t prefix = 0;
-    int left = k;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        if (tid < 256) s.hist[tid] = 0;
-        __syncthreads();
-        if (shift == 24 || mine >> (shift + 8) == prefix) atomicAdd(&s.hist[mine >> shift & 255u], 1ull);
-        __syncthreads();
-        u64 total;
-        const u64 has = tid < 256 ? s.hist[255 - tid] : 0;
-        const u64 upto = block_upto(has, s.whole, total);
-        if (has && upto >= (u64)left && upto - has < (u64)left) {
-            s.found = 255 - tid;
-            s.above = upto - has;
-        }
-        __syncthreads();
-        prefix = prefix << 8 | (uint32_t)s.found;
-        left -= (int)s.above;
-        __syncthreads();
-    }
-    return prefix;
+    if (tid == 0) s.found = -1;
+    const u64 hi = s.hist[2 * tid], lo = s.hist[2 * tid + 1];
+    u64 all;
+    const u64 upto = block_upto(hi + lo, s.whole, all), before = upto - hi - lo;
+    if (before < target && upto >= target) s.found = 2 * tid + (before + hi >= target ? 0 : 1);
+    __syncthreads();
+    const int bin = s.found;
+    __syncthreads();
+    return bin;
+}
+
+// A row's pieces are the waves' by sixteenths, of so many pieces each.
+template <class T>
+__device__ __forceinline__ int sixteenth(const Row<T> &row) {
+    return (row.pieces + kWaves - 1) / kWaves;
 }
 
 // Of the tokens that `kept` keeps, each of `size(key)`: the key at which the
 // sizes of the tokens with this key or a larger one reach aim(sum of all); how
 // many of this key that takes, and how many there are.
 template <class T, class Size, class Aim>
-__device__ uint32_t key_at(Lds &s, const Row<T> &row, const Place &kept, Size size, Aim aim, u64 &need, u64 &have) {
+__device__ __forceinline__ uint32_t key_at(Lds &s, const Row<T> &row, const Place &kept, Size size, Aim aim, u64 &need,
+                                           u64 &have) {
     const int tid = threadIdx.x;
     uint32_t prefix = 0;
     u64 above = 0, in_bin = 0, target = 0;
+#pragma nounroll
     for (int level = 0; level < 3; ++level) {
         const int shift = level == 0 ? 21 : level == 1 ? 10 : 0, bits = level == 2 ? 10 : 11;
         for (int i = tid; i < kBins; i += kThreads) s.hist[i] = 0;
         __syncthreads();
-        each(row, tid, row.pieces, kThreads, [&](uint32_t k, int i) {
-            if ((level == 0 || k >> (shift + bits) == prefix) && kept.keeps(k, i)) {
-                const u64 x = size(k);
-                if (x) atomicAdd(&s.hist[k >> shift & (uint32_t)((1 << bits) - 1)], x);
+        each(row, tid, row.pieces, kThreads, [&](const float (&v)[T::kPer], int i0) {
+#pragma unroll
+            for (int e = 0; e < T::kPer; ++e) {
+                const uint32_t k = key_of(v[e]);
+                if (k && (level == 0 || k >> (shift + bits) == prefix) && kept.keeps(v[e], i0 + e)) {
+                    const u64 x = size(k);
+                    if (x) atomicAdd(&s.hist[k >> shift & (uint32_t)((1 << bits) - 1)], x);
+                }
             }
         });
         __syncthreads();
@@ -329,20 +371,27 @@ __device__ uint32_t key_at(Lds &s, const Row<T> &row, const Place &kept, Size si
     return prefix;
 }
 
-// The lowest index at which the sums of size(key, index) exceed target(sum of
-// all), or the last of some size if rounding leaves none.
+// The lowest index at which the sums of size(logit, index) exceed target(sum of
+// all), or the last of some size if rounding leaves none.  `known`: s.real has
+// the sums of the sixteenths.
 template <class T, class Size, class Target>
-__device__ int index_at(Lds &s, const Row<T> &row, Size size, Target target, double &total) {
+__device__ __forceinline__ int index_at(Lds &s, const Row<T> &row, bool known, Size size, Target target, double &total) {
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     int from = 0, to = row.pieces;
     double t = 0.0;
+#pragma nounroll
     for (int level = 0; level < 2; ++level) {  // a sixteenth of the row, a sixteenth of that
-        const int n = (to - from + kWaves - 1) / kWaves;
-        double sum = 0.0;
-        each(row, from + w * n + lane, min(to, from + (w + 1) * n), 64, [&](uint32_t k, int i) { sum += size(k, i); });
-        sum = wave_add(sum);
-        if (lane == 0) s.real[w] = sum;
-        __syncthreads();
+        const int n = level == 0 ? sixteenth(row) : (to - from + kWaves - 1) / kWaves;
+        if (level > 0 || !known) {
+            double sum = 0.0;
+            each(row, from + w * n + lane, min(to, from + (w + 1) * n), 64, [&](const float (&v)[T::kPer], int i0) {
+#pragma unroll
+                for (int e = 0; e < T::kPer; ++e) sum += size(v[e], i0 + e);
+            });
+            sum = wave_add(sum);
+            if (lane == 0) s.real[w] = sum;
+            __syncthreads();
+        }
         if (level == 0) {
             total = 0.0;
             for (int i = 0; i < kWaves; ++i) total += s.real[i];
@@ -364,23 +413,27 @@ __device__ int index_at(Lds &s, const Row<T> &row, Size size, Target target, dou
         __syncthreads();
     }
     if (w == 0) {
-        const int n = (to - from + 63) / 64;
+        const int n = (to - from + 63) / 64, mine = from + lane * n, end = min(to, mine + n);
         double sum = 0.0;
-        const int mine = from + lane * n, end = min(to, mine + n);
-        each(row, mine, end, 1, [&](uint32_t k, int i) { sum += size(k, i); });
+        each(row, mine, end, 1, [&](const float (&v)[T::kPer], int i0) {
+#pragma unroll
+            for (int e = 0; e < T::kPer; ++e) sum += size(v[e], i0 + e);
+        });
         const double upto = wave_upto(sum);
         const u64 past = __ballot(sum > 0.0 && upto > t), some = __ballot(sum > 0.0);
         const int who = past ? __ffsll(past) - 1 : some ? 63 - __clzll(some) : 0;
         if (lane == who) {
             double at = upto - sum;
-            int index = -1;
+            int index = 0;
             bool done = false;
-            each(row, mine, end, 1, [&](uint32_t k, int i) {
-                const double x = size(k, i);
-                if (!done && x > 0.0) {
-                    index = i;
-                    at += x;
-                    done = at > t;
+            each(row, mine, end, 1, [&](const float (&v)[T::kPer], int i0) {
+                for (int e = 0; e < T::kPer; ++e) {
+                    const double x = size(v[e], i0 + e);
+                    if (!done && x > 0.0) {
+                        index = i0 + e;
+                        at += x;
+                        done = at > t;
+                    }
                 }
             });
             s.found = index;
@@ -396,187 +449,481 @@ struct Settings {
     double temperature, top_p, min_p, u;
     int top_k;  // 0: all
 };
+struct Answer {
+    int token;
+    double share;
+};
 
-// The list's n tokens, which are all that may be kept and all that count for
-// top_p: ranked, cut, put in order of their indices and summed.
-__device__ void from_list(Lds &s, const Settings &set, const Weight &weight, int n, int &token, double &share) {
-    constexpr int kPer = kList / kThreads;
+// The tokens that want(logit) takes, to the list; returns how many, or kMany if
+// they do not fit.  Each wave counts its own places, and they are moved together
+// behind it; a wave whose places run out stops.  In order of the indices each wave
+// goes through a sixteenth of the row, otherwise all through the same stretches:
+// 25 against 15 us for 64 rows of 131072.
+template <class T, class Want>
+__device__ __forceinline__ int gather(const Row<T> &row, bool in_order, Want want) {
+    Lds &s = lds();
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n16 = sixteenth(row);
+    u64 *const own = s.list + w * kOwn;
+    int count = 0;  // the same in all lanes
+    each(row, in_order ? w * n16 + lane : tid, in_order ? min(row.pieces, (w + 1) * n16) : row.pieces, in_order ? 64 : kThreads,
+         [&](const float (&v)[T::kPer], int i0) {
+        bool mine[T::kPer], any = false;
+#pragma unroll
+        for (int e = 0; e < T::kPer; ++e) any |= mine[e] = want(v[e]);
+        if (__any(any) && count <= kOwn) {
+            int at = count;  // places of lower lanes' tokens
+#pragma unroll
+            for (int e = 0; e < T::kPer; ++e) {
+                const u64 who = __ballot(mine[e]);
+                at += __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+                count += __popcll(who);
+            }
+#pragma unroll
+            for (int e = 0; e < T::kPer; ++e)
+                if (mine[e]) {
+                    if (at < kOwn) own[at] = entry_of(key_of(v[e]), i0 + e);
+                    ++at;
+                }
+        }
+    });
+    if (lane == 0) s.counts[w] = count;
+    __syncthreads();
+    int n = 0, before = 0;
+    bool fits = true;
+    for (int i = 0; i < kWaves; ++i) {
+        before += i < w ? s.counts[i] : 0;
+        n += s.counts[i];
+        fits = fits && s.counts[i] <= kOwn;
+    }
+    u64 x[kOwn / 64];
+#pragma unroll
+    for (int i = 0; i < kOwn / 64; ++i) x[i] = i * 64 + lane < count ? own[i * 64 + lane] : 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kOwn / 64; ++i)
+        if (fits && i * 64 + lane < count) s.list[before + i * 64 + lane] = x[i];
+    __syncthreads();
+    return fits ? n : kMany;
+}
+
+// The token among the list's n <= kRanked, in any order, which hold all that may
+// be kept: each is ranked, by the order of the cuts and by its index, against all.
+// top_p is of `whole`, or, if that is 0, of what top_k leaves.
+__device__ __noinline__ Answer from_short(Settings set, Weight weight, int n, double whole) {
+    Lds &s = lds();
     const int tid = threadIdx.x;
-    sort_list(s, n);  // by falling key, then rising index
-    const int most = set.top_k ? min(set.top_k, n) : n;
-    double w[kPer], sum = 0.0, total;
+    const u64 x = tid < n ? s.list[tid] : 0;
+    const double w = tid < n ? weight(logit_of(x)) : 0.0;
+    if (tid < n + 8 && tid < kRanked + 8) s.ranked[tid].entry = x, s.ranked[tid].weight = w;
+    __syncthreads();
+    int rank = 0, place = 0;
+    double before = 0.0, sum, total;
+    if (tid < n)
+        for (int i = 0; i < n; i += 8) {  // (past n lie zeros, whose indices are the largest)
+            u64 y[8];
+            double z[8];
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-        const int j = tid * kPer + e;
-        w[e] = j < most ? weight((uint32_t)(s.list[j] >> 32)) : 0.0;
-        sum += w[e];
-    }
-    double before = block_upto(sum, s.real, total) - sum;
-    if (tid == 0) s.count = 0;
-    __syncthreads();
-    int kept = 0;
+            for (int e = 0; e < 8; ++e) y[e] = s.ranked[i + e].entry, z[e] = s.ranked[i + e].weight;
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-        const int j = tid * kPer + e;
-        if (j < most && (j == 0 || ((set.top_p >= 1.0 || before < set.top_p * total) && w[e] >= set.min_p))) ++kept;
-        before += w[e];
-    }
-    if (kept) atomicAdd(&s.count, kept);
+            for (int e = 0; e < 8; ++e) {
+                rank += y[e] > x;
+                place += (uint32_t)y[e] > (uint32_t)x;
+                before += y[e] > x ? z[e] : 0.0;
+            }
+        }
+    const bool of_k = tid < n && (!set.top_k || rank < set.top_k);
+    block_upto(of_k ? w : 0.0, s.real, sum);  // (its barriers: the entries have been read)
+    const double aim = set.top_p * (whole > 0.0 ? whole : sum);
+    const bool kept = of_k && (set.top_p >= 1.0 || before < aim || rank == 0) && w >= set.min_p;
+    if (tid < n) s.ranked[place].entry = x, s.ranked[place].weight = kept ? w : 0.0;
     __syncthreads();
-    const int keep = s.count;
+    // by rising index, sums up to each
+    const double mine = tid < n ? s.ranked[tid].weight : 0.0, upto = block_upto(mine, s.real, total);
+    if (tid == 0) s.found = n - 1;
     __syncthreads();
-    // by rising index, with the key
-    for (int j = tid; j < keep; j += kThreads) {
+    if (mine > 0.0 && upto > set.u * total) atomicMin(&s.found, tid);
+    __syncthreads();
+    return {index_of(s.ranked[s.found].entry), s.ranked[s.found].weight / total};
+}
+
+// Of the list's n tokens from `floor` up (as entries), the last that is kept:
+// those of a bin before `cut` are, those in it are ranked, and the first `most`
+// of all are kept, or, where that is 0, those before which less than `aim` of the
+// weights lies.  0 if too many are to be ranked, or the cut is not in the bin,
+// where the rounding of the bins' sums has put it.
+__device__ __noinline__ u64 last_of_list(Weight weight, int n, Bins bins, int cut, u64 floor, int most, double aim) {
+    Lds &s = lds();
+    const int tid = threadIdx.x, per = (n + kThreads - 1) / kThreads, lo = tid * per, hi = min(n, lo + per);
+    u64 mine = 0, all;  // tokens to be ranked, and kept for sure, in the halves
+    double over = 0.0, above;
+    for (int j = lo; j < hi; ++j) {
         const u64 x = s.list[j];
-        s.list[j] = x << 32 | x >> 32;  // index complemented: falling is rising
+        const int b = x >= floor ? bins.of(logit_of(x)) : kBins;
+        mine += b == cut ? 1 : b < cut ? 1ull << 32 : 0;
+        over += b < cut ? weight(logit_of(x)) : 0.0;
     }
-    sort_list(s, keep);
-    sum = 0.0;
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-        const int j = tid * kPer + e;
-        w[e] = j < keep ? weight((uint32_t)s.list[j]) : 0.0;
-        sum += w[e];
+    int at = (int)(uint32_t)(block_upto(mine, s.whole, all) - mine);
+    const int m = (int)(uint32_t)all, sure = (int)(all >> 32);
+    block_upto(over, s.real, above);
+    if (m > kRanked) return 0;
+    for (int j = lo; j < hi; ++j) {
+        const u64 x = s.list[j];
+        if (x >= floor && bins.of(logit_of(x)) == cut) {
+            s.ranked[at].entry = x;
+            s.ranked[at].weight = weight(logit_of(x));
+            ++at;
+        }
     }
-    const double upto = block_upto(sum, s.real, total);
-    double at = upto - sum;
-    const double t = set.u * total;
-    if (tid == 0) s.found = keep - 1;
+    if (tid < 8) s.ranked[m + tid].entry = 0;
     __syncthreads();
+    int rank = 0;
+    double before = above, sum;
+    const u64 x = tid < m ? s.ranked[tid].entry : 0;
+    if (tid < m) {
+        for (int i = 0; i < m; i += 8) {
+            u64 y[8];
+            double z[8];
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-        const int j = tid * kPer + e;
-        at += w[e];
-        if (j < keep && w[e] > 0.0 && at > t) {
-            atomicMin(&s.found, j);
-            break;
+            for (int e = 0; e < 8; ++e) y[e] = s.ranked[i + e].entry, z[e] = s.ranked[i + e].weight;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                rank += y[e] > x;
+                before += y[e] > x ? z[e] : 0.0;
+            }
+        }
+    }
+    block_upto(tid < m ? s.ranked[tid].weight : 0.0, s.real, sum);
+    const bool kept = tid < m && (most ? sure + rank < most : before < aim || sure + rank == 0);
+    u64 n_kept;
+    block_upto((u64)kept, s.whole, n_kept);
+    if (n_kept == 0 || (!most && (int)n_kept == m && above + sum < aim)) return 0;
+    return ~block_max(kept ? ~x : 0, s);
+}
+
+// The token among those of the list's n that are kept, from `last` up; the list
+// is in order of the indices.
+__device__ __noinline__ Answer from_list(Settings set, Weight weight, int n, u64 last) {
+    Lds &s = lds();
+    const int tid = threadIdx.x, per = (n + kThreads - 1) / kThreads, lo = tid * per, hi = min(n, lo + per);
+    double part = 0.0, total;
+    for (int j = lo; j < hi; ++j) {
+        const double x = s.list[j] >= last ? weight(logit_of(s.list[j])) : 0.0;
+        part += x >= set.min_p ? x : 0.0;
+    }
+    const double upto = block_upto(part, s.real, total), t = set.u * total;
+    if (tid == 0) s.found = kThreads;
+    __syncthreads();
+    if (part > 0.0 && upto > t) atomicMin(&s.found, tid);
+    __syncthreads();
+    if (tid == s.found) {
+        double sofar = upto - part;
+        bool done = false;
+        for (int j = lo; j < hi && !done; ++j) {
+            const double x = s.list[j] >= last ? weight(logit_of(s.list[j])) : 0.0;
+            if (x > 0.0 && x >= set.min_p) {
+                sofar += x;
+                done = sofar > t;
+                s.counts[0] = index_of(s.list[j]);
+                s.share = x / total;
+            }
         }
     }
     __syncthreads();
-    const u64 x = s.list[s.found];
-    token = (int)~(uint32_t)(x >> 32);
-    share = weight((uint32_t)x) / total;
+    return {s.counts[0], s.share};
+}
+
+// The last that top_p keeps of the list's n tokens from `floor` up, which are all
+// that count for it; 0 as above.
+__device__ __noinline__ u64 nucleus_of_list(double top_p, Weight weight, int n, Bins bins, u64 floor) {
+    Lds &s = lds();
+    clear_bins(s);
+    __syncthreads();
+    double sum = 0.0, whole;
+    constexpr double magic = 256.0;  // + w: w as a whole number of 2^-44 in the last places
+    for (int j = threadIdx.x; j < n; j += kThreads) {
+        const u64 x = s.list[j];
+        if (x < floor) continue;
+        const double w = weight(logit_of(x));
+        sum += w;
+        atomicAdd(&s.hist[bins.of(logit_of(x))], __builtin_bit_cast(u64, w + magic) - __builtin_bit_cast(u64, magic));
+    }
+    block_upto(sum, s.real, whole);
+    const int cut = bin_at(s, (u64)__builtin_ldexp(top_p * whole, 44));
+    return cut < 0 ? 0 : last_of_list(weight, n, bins, cut, floor, 0, top_p * whole);
+}
+
+// The place of top_k's and top_p's cuts by its digits.
+template <class T>
+__device__ __noinline__ Place by_digits(Row<T> row, Settings set, Weight weight, float top_p) {
+    Lds &s = lds();
+    const int tid = threadIdx.x;
+    Place kept = {-INFINITY, kAll};
+#pragma nounroll
+    for (int by_weight = 0; by_weight < 2; ++by_weight) {
+        if (by_weight ? !(set.top_p < 1.0) : !(set.top_k > 0 && set.top_k < row.V)) continue;
+        // weights as whole numbers, 2^61 to 2^62 for all together: each is off by less than 2^-61 of the sum, equal
+        // ones alike
+        int unit = 0;
+        if (by_weight) {
+            double sum = 0.0, total;
+            each(row, tid, row.pieces, kThreads, [&](const float (&v)[T::kPer], int i0) {
+#pragma unroll
+                for (int e = 0; e < T::kPer; ++e) sum += weight(kept.keeps(v[e], i0 + e) ? v[e] : __builtin_nanf(""));
+            });
+            block_upto(sum, s.real, total);
+            unit = 61 - (int)((__builtin_bit_cast(u64, total) >> 52) - 1023);
+        }
+        const u64 k = (u64)set.top_k;
+        u64 need, have;
+        const uint32_t key = key_at(s, row, kept, [&](uint32_t x) {
+            return by_weight ? (u64)(__builtin_ldexp(weight.of_key(x), unit) + 0.5) : 1ull;
+        }, [&](u64 all) { return by_weight ? share_of(top_p, all) : k < all ? k : all; }, need, have);
+        // the first `need` of the key's `have` tokens are kept
+        const float value = value_of(key);
+        int index = kept.value == value ? kept.index : kAll;
+        if (need < have) {
+            double all;
+            const Place was = kept;
+            index = index_at(s, row, false, [&](float v, int i) { return ((v == value) & was.keeps(v, i)) ? 1.0 : 0.0; },
+                             [&](double) { return (double)need - 1.0; }, all);
+        }
+        kept = {value, index};
+    }
+    return kept;
+}
+
+// The token among those kept.  `known`: s.real has the sums of the sixteenths.
+template <class T>
+__device__ __noinline__ Answer token_at(Row<T> row, Settings set, Weight weight, Place kept, bool known) {
+    Lds &s = lds();
+    double total;
+    const int token = index_at(s, row, known, [&](float v, int i) {
+        const double x = weight(kept.keeps(v, i) ? v : __builtin_nanf(""));
+        return x < set.min_p ? 0.0 : x;
+    }, [&](double all) { return set.u * all; }, total);
+    return {token, weight(T::at(row.data, token)) / total};
+}
+
+// The tokens at +infinity share the row, and nothing else counts.
+template <class T>
+__device__ __noinline__ Answer token_at_infinity(Row<T> row, Settings set, float top_p) {
+    double n = 0.0, all;
+    const int token = index_at(lds(), row, false, [&](float v, int) { return v == INFINITY ? 1.0 : 0.0; }, [&](double x) {
+        n = set.top_k && set.top_k < x ? set.top_k : x;
+        if (top_p < 1.0f) n = (double)share_of(top_p, (u64)n);
+        return floor(set.u * n);
+    }, all);
+    return {token, 1.0 / n};
+}
+
+// The place of top_p's cut over all of a row, and the sums of what is kept of
+// each sixteenth in s.real: the tokens that it keeps do not fit the list, those of
+// the bin of the cut do.  `whole` is the sum of all weights.
+template <class T>
+__device__ __noinline__ bool cut_in_bin(Row<T> row, Settings set, Weight weight, Bins bins, float bottom, int cut,
+                                        double whole, Place &kept) {
+    Lds &s = lds();
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n16 = sixteenth(row);
+    double over = 0.0, part = 0.0, above;  // weights over the bin; of these, those that min_p leaves
+    const int n = gather(row, true, [&](float v) {
+        const int bin = v >= bottom ? bins.of(v) : kBins;
+        const double x = weight(bin < cut ? v : __builtin_nanf(""));
+        over += x;
+        part += x >= set.min_p ? x : 0.0;
+        return bin == cut;
+    });
+    if (n > kRanked) return false;
+    block_upto(over, s.real, above);
+    const u64 x = (int)threadIdx.x < n ? s.list[threadIdx.x] : 0;
+    if (x) s.ranked[threadIdx.x].weight = weight(logit_of(x));
+    __syncthreads();
+    double before = above, in_bin = 0.0;
+    for (int i = 0; i < n; ++i) {
+        const double z = s.ranked[i].weight;
+        in_bin += z;
+        before += s.list[i] > x ? z : 0.0;
+    }
+    // the last that is kept: before those after it lies enough
+    const bool keeps = x && before < set.top_p * whole;
+    u64 n_kept;
+    block_upto((u64)keeps, s.whole, n_kept);
+    const u64 first_out = block_max(x && !keeps ? x : 0, s), last = ~block_max(keeps ? ~x : 0, s);
+    // (the bins' rounding may put the cut into a neighbour, which is left to the digits)
+    if (n_kept == 0 || ((int)n_kept == n && above + in_bin < set.top_p * whole) || first_out > last) return false;
+    kept = {logit_of(last), index_of(last)};
+    for (int j = lane; j < n; j += 64) {
+        const u64 y = s.list[j];
+        if (y >= last && (index_of(y) + row.lead) / T::kPer / n16 == w) {
+            const double z = weight(logit_of(y));
+            part += z >= set.min_p ? z : 0.0;
+        }
+    }
+    part = wave_add(part);
+    __syncthreads();
+    if (lane == 0) s.real[w] = part;
+    __syncthreads();
+    return true;
 }
 
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_sample(SampleLaunch a) {
-    __shared__ Lds s;
+    Lds &s = lds();
     const int tid = threadIdx.x, r = blockIdx.x;
     Settings set;
     const float temperature = a.temperature ? a.temperature[r] : a.temperature_all;
     const float top_p = a.top_p ? a.top_p[r] : a.top_p_all, min_p = a.min_p ? a.min_p[r] : a.min_p_all, u = a.u[r];
     set.temperature = temperature, set.top_p = top_p, set.min_p = min_p, set.u = u;
     set.top_k = a.top_k ? a.top_k[r] : a.top_k_all;
-    auto answer = [&](int token, double logprob) {
+    auto answer = [&](int token, double share) {
         if (tid == 0) {
             a.token[r] = token;
-            if (a.logprob) a.logprob[r] = (float)logprob;
+            if (a.logprob) a.logprob[r] = (float)log(share);
         }
     };
     if (!(temperature >= 0.0f && temperature < INFINITY && set.top_k >= 0 && top_p > 0.0f && top_p <= 1.0f &&
           min_p >= 0.0f && min_p <= 1.0f && u >= 0.0f && u < 1.0f)) {
         if (tid == 0 && a.status) a.status[r] = FATE_EINVAL;
-        answer(-1, -INFINITY);
+        answer(-1, 0.0);
         return;
     }
     const Row<T> row(a, r);
+    row.read_ends();
+    if (tid < kTable) s.table[tid] = exp2(tid * (1.0 / kTable));
+    clear_bins(s);
+    __syncthreads();
 
     // the largest logit, of equal ones the lowest index
-    uint32_t mine = 0;
-    int mine_at = 0;
-    each(row, tid, row.pieces, kThreads, [&](uint32_t k, int i) {
-        if (k > mine) {
-            mine = k;
-            mine_at = i;
-        }
+    float best = -INFINITY;
+    int best_at = 0;
+    each(row, tid, row.pieces, kThreads, [&](const float (&v)[T::kPer], int i0) {
+#pragma unroll
+        for (int e = 0; e < T::kPer; ++e)
+            if (v[e] > best) {
+                best = v[e];
+                best_at = i0 + e;
+            }
     });
-    const u64 best = block_max((u64)mine << 32 | (mine ? (uint32_t)~mine_at : 0u), s);
-    Weight weight;
-    weight.top = (uint32_t)(best >> 32);
-    if (weight.top == 0) {  // nothing to choose from
-        answer(-1, -INFINITY);
+    const uint32_t mine = key_of(best);
+    const u64 first = wave_max(mine ? entry_of(mine, best_at) : 0), low = wave_max(mine ? ~(u64)mine : 0);
+    if ((tid & 63) == 0) s.whole[tid >> 6] = first, s.least[tid >> 6] = low;
+    __syncthreads();
+    u64 top_entry = 0, low_key = 0;
+    for (int i = 0; i < kWaves; ++i) top_entry = larger(top_entry, s.whole[i]), low_key = larger(low_key, s.least[i]);
+    __syncthreads();
+    if (top_entry == 0) {  // nothing to choose from
+        answer(-1, 0.0);
         return;
     }
     if (temperature == 0.0f || set.top_k == 1) {
-        answer((int)~(uint32_t)best, 0.0);
+        answer(index_of(top_entry), 1.0);
         return;
     }
-    weight.max = value_of(weight.top);
-    weight.per = 1.0 / set.temperature;
+    const float top = logit_of(top_entry);
+    Weight weight;
+    weight.max = top;
+    weight.per = 369.32993046757463 / set.temperature;
+    if (__builtin_isinf(top)) {
+        const Answer x = token_at_infinity(row, set, top_p);
+        answer(x.token, x.share);
+        return;
+    }
 
-    int token;
-    double share;
-    const bool small_k = set.top_k > 0 && set.top_k <= kSmallK, least = set.top_p >= 1.0 && set.min_p > 0.0;
-    if (row.V <= kList || small_k || least) {
-        uint32_t bound = 1;
-        if (row.V > kList) {
-            if (small_k) bound = max(bound, kth_word(s, mine, set.top_k));
-            if (least) {  // a little below the logit of weight min_p; weights decide
-                const double x = weight.max + set.temperature * log(set.min_p);
-                bound = max(bound, key_of((float)(x - 1e-6 * (fabs(x) + fabs(weight.max)))));
-            }
+    // The bins of what may be kept, and that of the cut where it is known.
+    constexpr float kLowest = -3.402823466e38f;
+    const bool cuts_k = set.top_k > 0 && set.top_k < row.V, small_k = cuts_k && set.top_k <= kSmallK;
+    const bool nucleus = set.top_p < 1.0 && !cuts_k;
+    float bottom = kLowest;
+    if (set.min_p > 0.0 && (nucleus || set.top_p >= 1.0)) {  // a little below the logit of weight min_p; weights decide
+        const double x = weight.max + set.temperature * log(set.min_p);
+        bottom = fmaxf(bottom, (float)(x - 1e-6 * (fabs(x) + fabs(weight.max))));
+    }
+    int cut = -1, about = 0;  // about: how many tokens are to be listed, if that is known
+    double whole = 0.0;
+    if (small_k) {
+        const Bins of_threads(top, value_of(~(uint32_t)low_key));
+        if (of_threads.good()) {
+            if (mine) atomicAdd(&s.hist[of_threads.of(best)], 1ull);
+            __syncthreads();
+            const int bin = bin_at(s, (u64)set.top_k);
+            if (bin >= 0) bottom = fmaxf(bottom, of_threads.under(bin));
         }
-        if (tid == 0) s.count = 0;
-        __syncthreads();
-        each(row, tid, row.pieces, kThreads, [&](uint32_t k, int i) {
-            if (k >= bound) {
-                const int at = atomicAdd(&s.count, 1);
-                if (at < kList) s.list[at] = (u64)k << 32 | (uint32_t)~i;
+    }
+    Bins bins(top, bottom);
+    if (nucleus) {
+        // Tokens of weight (1 - top_p) S / V or less sum to (1 - top_p) S at most and are cut, and the threads' largest
+        // logits give a bound of S from below: the tokens over that weight are summed by bins while S is.
+        double low_sum;
+        block_upto(mine ? weight(best) : 0.0, s.real, low_sum);
+        const double x = weight.max + set.temperature * log((1.0 - set.top_p) * low_sum / row.V);
+        bottom = fmaxf(bottom, (float)(x - 1e-6 * (fabs(x) + fabs(weight.max))));
+        bins = Bins(top, bottom);
+        const bool good = bins.good();
+        // w + 2^(52 - bits) has w as a whole number of 2^-bits in its last places; a sum of V of them stays under 2^63
+        const int bits = min(52, 30 + __builtin_clz((uint32_t)row.V));
+        const double magic = __builtin_ldexp(1.0, 52 - bits);
+        double sum = 0.0;
+        each(row, tid, row.pieces, kThreads, [&](const float (&v)[T::kPer], int) {
+#pragma unroll
+            for (int e = 0; e < T::kPer; ++e) {
+                const double y = weight(v[e]);
+                sum += y;
+                if (good & (v[e] >= bottom))
+                    atomicAdd(&s.hist[bins.of(v[e])], __builtin_bit_cast(u64, y + magic) - __builtin_bit_cast(u64, magic));
             }
         });
-        __syncthreads();
-        const int n = s.count;
-        __syncthreads();
-        if (n <= kList) {
-            from_list(s, set, weight, n, token, share);
-            answer(token, log(share));
+        block_upto(sum, s.real, whole);
+        if (good) cut = bin_at(s, (u64)__builtin_ldexp(set.top_p * whole, bits));
+        if (cut >= 0) {  // how many they may be: a bin's sum by the weight in its middle
+            double n = 0.0, all;
+            for (int b = 2 * tid; b < 2 * tid + 2 && b <= cut; ++b)
+                if (s.hist[b]) n += __builtin_ldexp((double)s.hist[b], -bits) / weight(top - ((float)b + 0.5f) / bins.per);
+            block_upto(n, s.real, all);
+            about = (int)fmin(all, (double)kMany);
+        }
+        if (good && cut < 0 && set.min_p > 0.0) cut = kBins;  // min_p cuts before top_p does
+    }
+    Place kept = {-INFINITY, kAll};
+    bool listed = row.V <= kRanked || small_k || cut >= 0, known = false;
+    if (!set.top_k && set.top_p >= 1.0 && set.min_p > 0.0) {  // all that is gathered is kept
+        cut = kBins;
+        listed = true;
+    }
+    if (listed) {
+        auto want = [&](float v) { return (v >= bottom) & (cut < 0 || bins.of(v) <= cut); };
+        int n = about <= kRanked ? gather(row, false, want) : about < kMany ? kRanked + 1 : kMany;
+        if (n <= kRanked) {
+            const Answer x = from_short(set, weight, n, whole);
+            answer(x.token, x.share);
             return;
         }
-    }
-
-    Place kept = {0, kAll};
-    auto cut = [&](uint32_t key, u64 need, u64 have) {  // the first `need` of the key's `have` tokens are kept
-        int index = kAll;
-        if (need < have) {
-            double all;
-            const Place was = kept;
-            index = index_at(s, row, [&](uint32_t k, int i) { return k == key && was.keeps(k, i) ? 1.0 : 0.0; },
-                             [&](double) { return (double)need - 1.0; }, all);
-        } else if (kept.key == key) {
-            index = kept.index;
+        if (small_k && bins.good()) {  // many reach the bound: the bin of the k-th of all
+            clear_bins(s);
+            __syncthreads();
+            each(row, tid, row.pieces, kThreads, [&](const float (&v)[T::kPer], int) {
+#pragma unroll
+                for (int e = 0; e < T::kPer; ++e)
+                    if (v[e] >= bottom) atomicAdd(&s.hist[bins.of(v[e])], 1ull);
+            });
+            __syncthreads();
+            cut = bin_at(s, (u64)set.top_k);
         }
-        kept = {key, index};
-    };
-    if (set.top_k > 0 && set.top_k < row.V) {
-        u64 need, have;
-        const u64 k = (u64)set.top_k;
-        const uint32_t key = key_at(s, row, kept, [](uint32_t) { return 1ull; },
-                                    [&](u64 all) { return k < all ? k : all; }, need, have);
-        cut(key, need, have);
+        if ((n < kMany || small_k) && cut >= 0 && bins.good()) {
+            n = gather(row, true, want);
+            u64 last = n < kMany;
+            if (last && cut < kBins)
+                last = last_of_list(weight, n, bins, cut, 1, small_k ? set.top_k : 0, set.top_p * whole);
+            if (last && small_k && set.top_p < 1.0) last = nucleus_of_list(set.top_p, weight, n, bins, last);
+            if (last) {
+                const Answer x = from_list(set, weight, n, last);
+                answer(x.token, x.share);
+                return;
+            }
+        }
     }
-    if (set.top_p < 1.0) {
-        double sum = 0.0;
-        each(row, tid, row.pieces, kThreads, [&](uint32_t k, int i) {
-            if (kept.keeps(k, i)) sum += weight(k);
-        });
-        double total;
-        block_upto(sum, s.real, total);
-        // weights as whole numbers, 2^61 to 2^62 for all together: each is off by less than 2^-61 of the sum, equal
-        // ones alike
-        const int unit = 61 - (int)((__builtin_bit_cast(u64, total) >> 52) - 1023);
-        u64 need, have;
-        const uint32_t key = key_at(s, row, kept, [&](uint32_t k) { return (u64)(__builtin_ldexp(weight(k), unit) + 0.5); },
-                                    [&](u64 all) { return share_of(top_p, all); }, need, have);
-        cut(key, need, have);
-    }
-    double total;
-    token = index_at(s, row, [&](uint32_t k, int i) {
-        if (!kept.keeps(k, i)) return 0.0;
-        const double w = weight(k);
-        return w >= set.min_p ? w : 0.0;
-    }, [&](double all) { return set.u * all; }, total);
-    if (a.logprob) share = weight(key_of(T::at(row.data, max(token, 0)))) / total;
-    answer(token, a.logprob ? log(share) : 0.0);
+    if (nucleus && cut >= 0 && cut < kBins) known = cut_in_bin(row, set, weight, bins, bottom, cut, whole, kept);
+    if (!known && (cuts_k || set.top_p < 1.0)) kept = by_digits(row, set, weight, top_p);
+    const Answer x = token_at(row, set, weight, kept, known);
+    answer(x.token, x.share);
 }
 
 }  // namespace
