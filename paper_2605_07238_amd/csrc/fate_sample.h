@@ -1,6 +1,7 @@
 // Launch arguments of the sampling kernel.
 #pragma once
 
+#include <stddef.h>
 #include <stdint.h>
 
 #include "fate.h"
@@ -17,7 +18,16 @@ struct SampleLaunch {
     int32_t rows, vocab, dtype;
     int32_t top_k_all;
     float temperature_all, top_p_all, min_p_all;
+    // calls of few rows, by slices of each: of each slice the largest entry, the complement of the threads' least key,
+    // the sums by bins or by waves, those over the cut by waves and in all, what is listed, the threads' largest logits;
+    // of each row the sum of all and the bin of the cut
+    int32_t slices;
+    unsigned long long *tops, *lows, *hist, *lists;
+    double *parts, *kept, *over, *wholes;
+    float *best;
+    int32_t *counts, *cuts;
 };
-int launch_sample(const SampleLaunch &a, void *stream);
+size_t sample_ws(int64_t rows, int64_t vocab);  // bytes
+int launch_sample(const SampleLaunch &a, void *ws, void *stream);
 
 }  // namespace fate

@@ -371,16 +371,24 @@ __device__ __forceinline__ uint32_t key_at(Lds &s, const Row<T> &row, const Plac
     return prefix;
 }
 
+// A stretch of a row's pieces, and where in its sums a token is sought.
+struct Part {
+    int from, to;
+    double t;
+};
+
 // The lowest index at which the sums of size(logit, index) exceed target(sum of
 // all), or the last of some size if rounding leaves none.  `known`: s.real has
-// the sums of the sixteenths.
+// the sums of the sixteenths; `part`: of these or other parts of the row, the one
+// that it lies in, found already.
 template <class T, class Size, class Target>
-__device__ __forceinline__ int index_at(Lds &s, const Row<T> &row, bool known, Size size, Target target, double &total) {
+__device__ __forceinline__ int index_at(Lds &s, const Row<T> &row, bool known, const Part *part, Size size, Target target,
+                                        double &total) {
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    int from = 0, to = row.pieces;
-    double t = 0.0;
+    int from = part ? part->from : 0, to = part ? part->to : row.pieces;
+    double t = part ? part->t : 0.0;
 #pragma nounroll
-    for (int level = 0; level < 2; ++level) {  // a sixteenth of the row, a sixteenth of that
+    for (int level = part ? 1 : 0; level < 2; ++level) {  // a sixteenth of the row, a sixteenth of that
         const int n = level == 0 ? sixteenth(row) : (to - from + kWaves - 1) / kWaves;
         if (level > 0 || !known) {
             double sum = 0.0;
@@ -398,17 +406,17 @@ __device__ __forceinline__ int index_at(Lds &s, const Row<T> &row, bool known, S
             t = target(total);
         }
         double upto = 0.0, rest = t;
-        int part = 0;
+        int at = 0;
         for (int i = 0; i < kWaves; ++i) {
             if (s.real[i] > 0.0) {
-                part = i;
+                at = i;
                 rest = t - upto;
             }
             upto += s.real[i];
             if (upto > t) break;
         }
         t = rest;
-        from += part * n;
+        from += at * n;
         to = min(to, from + n);
         __syncthreads();
     }
@@ -455,17 +463,17 @@ struct Answer {
 };
 
 // The tokens that want(logit) takes, to the list; returns how many, or kMany if
-// they do not fit.  Each wave counts its own places, and they are moved together
-// behind it; a wave whose places run out stops.  In order of the indices each wave
-// goes through a sixteenth of the row, otherwise all through the same stretches:
-// 25 against 15 us for 64 rows of 131072.
+// they do not fit: of the pieces from .. to.  Each wave counts its own places, and
+// they are moved together behind it; a wave whose places run out stops.  In order
+// of the indices each wave goes through n16 pieces of its own, otherwise all go
+// through the same stretches, which for a whole row of 131072 takes 6 us less.
 template <class T, class Want>
-__device__ __forceinline__ int gather(const Row<T> &row, bool in_order, Want want) {
+__device__ __forceinline__ int gather(const Row<T> &row, int from, int to, int n16, bool in_order, Want want) {
     Lds &s = lds();
-    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n16 = sixteenth(row);
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     u64 *const own = s.list + w * kOwn;
     int count = 0;  // the same in all lanes
-    each(row, in_order ? w * n16 + lane : tid, in_order ? min(row.pieces, (w + 1) * n16) : row.pieces, in_order ? 64 : kThreads,
+    each(row, from + (in_order ? w * n16 + lane : tid), in_order ? min(to, from + (w + 1) * n16) : to, in_order ? 64 : kThreads,
          [&](const float (&v)[T::kPer], int i0) {
         bool mine[T::kPer], any = false;
 #pragma unroll
@@ -632,24 +640,41 @@ __device__ __noinline__ Answer from_list(Settings set, Weight weight, int n, u64
     return {s.counts[0], s.share};
 }
 
-// The last that top_p keeps of the list's n tokens from `floor` up, which are all
-// that count for it; 0 as above.
-__device__ __noinline__ u64 nucleus_of_list(double top_p, Weight weight, int n, Bins bins, u64 floor) {
+// The last that top_k, and then top_p, keep of the list's n tokens, which hold
+// all that they may keep; 0 as above.  Bins of the list's own logits tell where.
+__device__ __noinline__ u64 last_of_k(Settings set, Weight weight, int n, Bins bins) {
     Lds &s = lds();
-    clear_bins(s);
-    __syncthreads();
-    double sum = 0.0, whole;
     constexpr double magic = 256.0;  // + w: w as a whole number of 2^-44 in the last places
-    for (int j = threadIdx.x; j < n; j += kThreads) {
-        const u64 x = s.list[j];
-        if (x < floor) continue;
-        const double w = weight(logit_of(x));
-        sum += w;
-        atomicAdd(&s.hist[bins.of(logit_of(x))], __builtin_bit_cast(u64, w + magic) - __builtin_bit_cast(u64, magic));
+    u64 last = 1;
+    double whole = 0.0;
+#pragma nounroll
+    for (int by_weight = 0; by_weight < (set.top_p < 1.0 ? 2 : 1); ++by_weight) {
+        clear_bins(s);
+        __syncthreads();
+        double sum = 0.0;
+        for (int j = threadIdx.x; j < n; j += kThreads) {
+            const u64 x = s.list[j];
+            if (x < last) continue;
+            const double w = weight(logit_of(x));
+            sum += w;
+            atomicAdd(&s.hist[bins.of(logit_of(x))],
+                      by_weight ? __builtin_bit_cast(u64, w + magic) - __builtin_bit_cast(u64, magic) : 1ull);
+        }
+        block_upto(sum, s.real, whole);
+        const int cut = bin_at(s, by_weight ? (u64)__builtin_ldexp(set.top_p * whole, 44) : (u64)set.top_k);
+        if (cut < 0) return 0;
+        last = last_of_list(weight, n, bins, cut, last, by_weight ? 0 : set.top_k, set.top_p * whole);
+        if (last == 0) return 0;
     }
-    block_upto(sum, s.real, whole);
-    const int cut = bin_at(s, (u64)__builtin_ldexp(top_p * whole, 44));
-    return cut < 0 ? 0 : last_of_list(weight, n, bins, cut, floor, 0, top_p * whole);
+    return last;
+}
+
+// The token of the list's n, in order of their indices, and all that top_k may
+// keep; false where their number or their ties are too many.
+__device__ __forceinline__ bool from_list_of_k(const Settings &set, const Weight &weight, int n, const Bins &bins, Answer &x) {
+    const u64 last = last_of_k(set, weight, n, bins);
+    if (last) x = from_list(set, weight, n, last);
+    return last != 0;
 }
 
 // The place of top_k's and top_p's cuts by its digits.
@@ -684,7 +709,7 @@ __device__ __noinline__ Place by_digits(Row<T> row, Settings set, Weight weight,
         if (need < have) {
             double all;
             const Place was = kept;
-            index = index_at(s, row, false, [&](float v, int i) { return ((v == value) & was.keeps(v, i)) ? 1.0 : 0.0; },
+            index = index_at(s, row, false, nullptr, [&](float v, int i) { return ((v == value) & was.keeps(v, i)) ? 1.0 : 0.0; },
                              [&](double) { return (double)need - 1.0; }, all);
         }
         kept = {value, index};
@@ -692,12 +717,12 @@ __device__ __noinline__ Place by_digits(Row<T> row, Settings set, Weight weight,
     return kept;
 }
 
-// The token among those kept.  `known`: s.real has the sums of the sixteenths.
+// The token among those kept.  `known`, `part` (within `total`): as above.
 template <class T>
-__device__ __noinline__ Answer token_at(Row<T> row, Settings set, Weight weight, Place kept, bool known) {
+__device__ __noinline__ Answer token_at(Row<T> row, Settings set, Weight weight, Place kept, bool known, bool parted,
+                                        Part part, double total) {
     Lds &s = lds();
-    double total;
-    const int token = index_at(s, row, known, [&](float v, int i) {
+    const int token = index_at(s, row, known, parted ? &part : nullptr, [&](float v, int i) {
         const double x = weight(kept.keeps(v, i) ? v : __builtin_nanf(""));
         return x < set.min_p ? 0.0 : x;
     }, [&](double all) { return set.u * all; }, total);
@@ -708,7 +733,7 @@ __device__ __noinline__ Answer token_at(Row<T> row, Settings set, Weight weight,
 template <class T>
 __device__ __noinline__ Answer token_at_infinity(Row<T> row, Settings set, float top_p) {
     double n = 0.0, all;
-    const int token = index_at(lds(), row, false, [&](float v, int) { return v == INFINITY ? 1.0 : 0.0; }, [&](double x) {
+    const int token = index_at(lds(), row, false, nullptr, [&](float v, int) { return v == INFINITY ? 1.0 : 0.0; }, [&](double x) {
         n = set.top_k && set.top_k < x ? set.top_k : x;
         if (top_p < 1.0f) n = (double)share_of(top_p, (u64)n);
         return floor(set.u * n);
@@ -716,72 +741,407 @@ __device__ __noinline__ Answer token_at_infinity(Row<T> row, Settings set, float
     return {token, 1.0 / n};
 }
 
-// The place of top_p's cut over all of a row, and the sums of what is kept of
-// each sixteenth in s.real: the tokens that it keeps do not fit the list, those of
-// the bin of the cut do.  `whole` is the sum of all weights.
+// Weights of the pieces of this wave's part of from .. to, `n16` pieces a wave,
+// that lie over the bin `cut`: `over`, and of these, those that min_p leaves; the
+// tokens of the bin to the list, in order of their indices.
 template <class T>
-__device__ __noinline__ bool cut_in_bin(Row<T> row, Settings set, Weight weight, Bins bins, float bottom, int cut,
-                                        double whole, Place &kept) {
-    Lds &s = lds();
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n16 = sixteenth(row);
-    double over = 0.0, part = 0.0, above;  // weights over the bin; of these, those that min_p leaves
-    const int n = gather(row, true, [&](float v) {
-        const int bin = v >= bottom ? bins.of(v) : kBins;
+__device__ __forceinline__ int sums_over_bin(const Row<T> &row, int from, int to, int n16, const Settings &set,
+                                             const Weight &weight, const Bins &bins, float bottom, int cut, double &over,
+                                             double &part) {
+    over = part = 0.0;
+    return gather(row, from, to, n16, true, [&](float v) {
+        const int bin = v >= bottom ? bins.of(v) : kBins + 1;
         const double x = weight(bin < cut ? v : __builtin_nanf(""));
         over += x;
         part += x >= set.min_p ? x : 0.0;
         return bin == cut;
     });
-    if (n > kRanked) return false;
-    block_upto(over, s.real, above);
-    const u64 x = (int)threadIdx.x < n ? s.list[threadIdx.x] : 0;
-    if (x) s.ranked[threadIdx.x].weight = weight(logit_of(x));
+}
+
+// The last that top_p keeps of the list's n tokens, those of the bin of the cut,
+// with `above` before them and `whole` in all; 0 if they are too many, or the cut
+// is not in the bin, where the rounding of the bins' sums has put it.
+__device__ __noinline__ u64 last_in_bin(Settings set, Weight weight, int n, double above, double whole) {
+    Lds &s = lds();
+    const int tid = threadIdx.x;
+    if (n > kRanked) return 0;
+    const u64 x = tid < n ? s.list[tid] : 0;
+    const double w = x ? weight(logit_of(x)) : 0.0;
+    if (tid < kRanked + 8) s.ranked[tid].entry = x, s.ranked[tid].weight = w;
     __syncthreads();
-    double before = above, in_bin = 0.0;
-    for (int i = 0; i < n; ++i) {
-        const double z = s.ranked[i].weight;
-        in_bin += z;
-        before += s.list[i] > x ? z : 0.0;
-    }
-    // the last that is kept: before those after it lies enough
-    const bool keeps = x && before < set.top_p * whole;
-    u64 n_kept;
-    block_upto((u64)keeps, s.whole, n_kept);
-    const u64 first_out = block_max(x && !keeps ? x : 0, s), last = ~block_max(keeps ? ~x : 0, s);
-    // (the bins' rounding may put the cut into a neighbour, which is left to the digits)
-    if (n_kept == 0 || ((int)n_kept == n && above + in_bin < set.top_p * whole) || first_out > last) return false;
-    kept = {logit_of(last), index_of(last)};
-    for (int j = lane; j < n; j += 64) {
+    double before = above, in_bin;
+    if (tid < n)
+        for (int i = 0; i < n; i += 8) {
+            u64 y[8];
+            double z[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = s.ranked[i + e].entry, z[e] = s.ranked[i + e].weight;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) before += y[e] > x ? z[e] : 0.0;
+        }
+    block_upto(w, s.real, in_bin);
+    // kept while less than top_p lies before; a maximum, so that it is a stretch from the start whatever rounding does
+    const double aim = set.top_p * whole;
+    const bool keeps = x && before < aim;
+    const u64 last = ~block_max(keeps ? ~x : 0, s), none = ~0ull;
+    if (last == none || (above + in_bin < aim && last == ~block_max(x ? ~x : 0, s))) return 0;
+    return last;
+}
+
+// The place of top_p's cut over all of a row, and the sums of what is kept of
+// each sixteenth in s.real, where what it keeps does not fit the list; false as
+// above.
+template <class T>
+__device__ __noinline__ bool cut_in_bin(Row<T> row, Settings set, Weight weight, Bins bins, float bottom, int cut,
+                                        double whole, Place &kept) {
+    Lds &s = lds();
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n16 = sixteenth(row);
+    double over, part, above;
+    const int n = sums_over_bin(row, 0, row.pieces, n16, set, weight, bins, bottom, cut, over, part);
+    block_upto(over, s.real, above);
+    const u64 last = cut == kBins ? 1 : last_in_bin(set, weight, n, above, whole);
+    if (last == 0) return false;
+    if (cut < kBins) kept = {logit_of(last), index_of(last)};
+    for (int j = lane; j < n; j += 64) {  // of the bin's tokens, those kept count for their sixteenths
         const u64 y = s.list[j];
-        if (y >= last && (index_of(y) + row.lead) / T::kPer / n16 == w) {
+        const int first = row.index(w * n16), end = row.index((w + 1) * n16);
+        if (y >= last && index_of(y) >= first && index_of(y) < end) {
             const double z = weight(logit_of(y));
             part += z >= set.min_p ? z : 0.0;
         }
     }
     part = wave_add(part);
-    __syncthreads();
     if (lane == 0) s.real[w] = part;
     __syncthreads();
     return true;
 }
 
+// What a call asks of a row.
+__device__ __forceinline__ Settings settings_of(const SampleLaunch &a, int r) {
+    Settings set;
+    set.temperature = a.temperature ? a.temperature[r] : a.temperature_all;
+    set.top_p = a.top_p ? a.top_p[r] : a.top_p_all;
+    set.min_p = a.min_p ? a.min_p[r] : a.min_p_all;
+    set.u = a.u[r];
+    set.top_k = a.top_k ? a.top_k[r] : a.top_k_all;
+    return set;
+}
+__device__ __forceinline__ bool good(const Settings &x) {
+    return x.temperature >= 0.0 && x.temperature < INFINITY && x.top_k >= 0 && x.top_p > 0.0 && x.top_p <= 1.0 &&
+           x.min_p >= 0.0 && x.min_p <= 1.0 && x.u >= 0.0 && x.u < 1.0;
+}
+// top_p over all of a row of V tokens; no cuts at all.
+__device__ __forceinline__ bool by_nucleus(const Settings &x, int V) { return x.top_p < 1.0 && !(x.top_k > 0 && x.top_k < V); }
+__device__ __forceinline__ bool uncut(const Settings &x, int V) {
+    return x.top_p >= 1.0 && !(x.top_k > 0 && x.top_k < V) && x.min_p == 0.0;
+}
+
+__device__ __forceinline__ Weight weight_of(const Settings &set, float top) {
+    return {top, 369.32993046757463 / set.temperature};
+}
+
+// A little below the logit of weight w; weights decide.
+__device__ __forceinline__ float logit_below(const Settings &set, float top, double w) {
+    const double x = (double)top + set.temperature * log(w);
+    return fmaxf((float)(x - 1e-6 * (fabs(x) + fabs((double)top))), -3.402823466e38f);
+}
+
+// A thread's largest logits of each of a row's slices; -infinity past them.
+constexpr int kSlices = 8;
+template <int N>
+struct Mine {
+    float best[N];
+};
+
+// The lowest logit that top_p over all of a row may keep: tokens of weight
+// (1 - top_p) S / V or less sum to (1 - top_p) S at most and are cut, and the
+// threads' largest logits give a bound of S from below.
+template <int N>
+__device__ __forceinline__ float nucleus_bottom(Lds &s, const Settings &set, const Weight &weight, float top, int V,
+                                                const Mine<N> &mine) {
+    double low = 0.0, all;
+#pragma nounroll
+    for (int i = 0; i < N; ++i) {  // (0 of -infinity)
+        float best = mine.best[0];
+#pragma unroll
+        for (int j = 1; j < N; ++j) best = i == j ? mine.best[j] : best;
+        low += weight(best);
+    }
+    block_upto(low, s.real, all);
+    return logit_below(set, top, fmax((1.0 - set.top_p) * all / V, set.min_p));
+}
+
+// Weights of the pieces from .. to: their sum, by thread, and those at `bottom` and
+// over it in the bins, as whole numbers of 2^-bits: w + 2^(52 - bits) has them in
+// its last places, and a sum of V of them stays under 2^63.
+__device__ __forceinline__ int bits_of(int V) { return min(52, 30 + __builtin_clz((uint32_t)V)); }
 template <class T>
+__device__ __forceinline__ double sum_by_bins(Lds &s, const Row<T> &row, int from, int to, const Weight &weight,
+                                              const Bins &bins, float bottom) {
+    const bool good = bins.good();
+    const double magic = __builtin_ldexp(1.0, 52 - bits_of(row.V));
+    double sum = 0.0;
+    each(row, from + (int)threadIdx.x, to, kThreads, [&](const float (&v)[T::kPer], int) {
+#pragma unroll
+        for (int e = 0; e < T::kPer; ++e) {
+            const double y = weight(v[e]);
+            sum += y;
+            if (good & (v[e] >= bottom))
+                atomicAdd(&s.hist[bins.of(v[e])], __builtin_bit_cast(u64, y + magic) - __builtin_bit_cast(u64, magic));
+        }
+    });
+    return sum;
+}
+
+// The largest logit of pieces from .. to and, of equal ones, the lowest index:
+// this thread's.
+template <class T>
+__device__ __forceinline__ u64 best_of(const Row<T> &row, int from, int to, float &best) {
+    int at = 0;
+    best = -INFINITY;
+    each(row, from + (int)threadIdx.x, to, kThreads, [&](const float (&v)[T::kPer], int i0) {
+#pragma unroll
+        for (int e = 0; e < T::kPer; ++e)
+            if (v[e] > best) {
+                best = v[e];
+                at = i0 + e;
+            }
+    });
+    return key_of(best) ? entry_of(key_of(best), at) : 0;
+}
+
+// The largest entry of the workgroup, and the complement of its least key.
+__device__ __forceinline__ void block_range(Lds &s, u64 mine, u64 &top, u64 &low) {
+    const int w = threadIdx.x >> 6;
+    const u64 first = wave_max(mine), least = wave_max(mine ? ~(mine >> 32) : 0);
+    if ((threadIdx.x & 63) == 0) s.whole[w] = first, s.least[w] = least;
+    __syncthreads();
+    top = low = 0;
+    for (int i = 0; i < kWaves; ++i) top = larger(top, s.whole[i]), low = larger(low, s.least[i]);
+    __syncthreads();
+}
+
+// Calls of few rows: each row's readings by `slices` workgroups, so that the chip
+// is filled, in a launch each; k_sample then takes what they found.  64 rows of
+// 131072 with top_p 0.9: 117 us by one workgroup a row, 67 so.
+template <class T>
+__device__ __forceinline__ int slice_of(const Row<T> &row, int slices) { return (row.pieces + slices - 1) / slices; }
+
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_sample_tops(SampleLaunch a) {
+    Lds &s = lds();
+    const int r = blockIdx.x / a.slices, g = blockIdx.x - r * a.slices;
+    const Row<T> row(a, r);
+    row.read_ends();
+    __syncthreads();
+    const int n = slice_of(row, a.slices);
+    float best;
+    u64 top, low;
+    const u64 mine = best_of(row, g * n, min(row.pieces, (g + 1) * n), best);
+    block_range(s, mine, top, low);
+    a.best[(int64_t)blockIdx.x * kThreads + threadIdx.x] = best;
+    if (threadIdx.x == 0) a.tops[blockIdx.x] = top, a.lows[blockIdx.x] = low;
+}
+
+// What the slices have found, all of it asked for at once: a round trip to what
+// another chiplet has written takes a microsecond.
+__device__ __forceinline__ void tops_of(const SampleLaunch &a, int r, u64 &top, u64 &low, Mine<kSlices> &mine) {
+    const int lane = threadIdx.x & 63;
+    const bool has = lane < a.slices;
+    const u64 its_top = has ? a.tops[r * a.slices + lane] : 0, its_low = has ? a.lows[r * a.slices + lane] : 0;
+    const float *const best = a.best + (int64_t)r * a.slices * kThreads + threadIdx.x;
+#pragma unroll
+    for (int g = 0; g < kSlices; ++g) mine.best[g] = g < a.slices ? best[g * kThreads] : -INFINITY;
+    top = wave_max(its_top);
+    low = wave_max(its_low);
+}
+
+// Sums of the rows that need all weights: by bins for top_p, of each wave's part
+// without cuts.
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_sample_sums(SampleLaunch a) {
+    Lds &s = lds();
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, r = blockIdx.x / a.slices, g = blockIdx.x - r * a.slices;
+    const Settings set = settings_of(a, r);
+    u64 first, low;
+    Mine<kSlices> mine;
+    tops_of(a, r, first, low, mine);
+    const bool nucleus = by_nucleus(set, a.vocab);
+    if (!good(set) || set.temperature == 0.0 || set.top_k == 1 || first == 0 || !(nucleus || uncut(set, a.vocab))) return;
+    const float top = logit_of(first);
+    if (__builtin_isinf(top)) return;
+    const Row<T> row(a, r);
+    row.read_ends();
+    if (tid < kTable) s.table[tid] = exp2(tid * (1.0 / kTable));
+    clear_bins(s);
+    __syncthreads();
+    const Weight weight = weight_of(set, top);
+    const int n = slice_of(row, a.slices), from = g * n, to = min(row.pieces, from + n);
+    if (nucleus) {
+        const float bottom = nucleus_bottom(s, set, weight, top, row.V, mine);
+        double whole;
+        block_upto(sum_by_bins(s, row, from, to, weight, Bins(top, bottom), bottom), s.real, whole);
+        if (tid == 0) a.parts[(int64_t)blockIdx.x * kWaves] = whole;
+        for (int i = tid; i < kBins; i += kThreads) a.hist[(int64_t)blockIdx.x * kBins + i] = s.hist[i];
+    } else {
+        const int n16 = (n + kWaves - 1) / kWaves;
+        double sum = 0.0;
+        each(row, from + w * n16 + lane, min(to, from + (w + 1) * n16), 64, [&](const float (&v)[T::kPer], int) {
+#pragma unroll
+            for (int e = 0; e < T::kPer; ++e) sum += weight(v[e]);
+        });
+        sum = wave_add(sum);
+        if (lane == 0) a.parts[(int64_t)blockIdx.x * kWaves + w] = sum;
+    }
+}
+
+// The lowest logit that may be kept by rows whose tokens are listed: small top_k,
+// or min_p alone.  At least top_k tokens reach the top_k-th largest of the threads'
+// largest logits.
+template <int N>
+__device__ __forceinline__ float list_bottom(Lds &s, const Settings &set, float top, u64 low, bool small_k, const Mine<N> &mine) {
+    float bottom = -3.402823466e38f;
+    if (set.min_p > 0.0 && set.top_p >= 1.0) bottom = logit_below(set, top, set.min_p);
+    if (small_k) {
+        const Bins of_threads(top, value_of(~(uint32_t)low));
+        if (of_threads.good()) {
+            for (float best : mine.best)
+                if (best > -INFINITY) atomicAdd(&s.hist[of_threads.of(best)], 1ull);
+            __syncthreads();
+            const int bin = bin_at(s, (u64)set.top_k);
+            if (bin >= 0) bottom = fmaxf(bottom, of_threads.under(bin));
+        }
+    }
+    return bottom;
+}
+__device__ __forceinline__ bool has_small_k(const Settings &x, int V) { return x.top_k > 0 && x.top_k < V && x.top_k <= kSmallK; }
+// What is gathered over its bottom is kept, as far as min_p leaves it.
+__device__ __forceinline__ bool only_min_p(const Settings &x, int V) {
+    return x.top_p >= 1.0 && x.min_p > 0.0 && !(x.top_k > 0 && x.top_k < V);
+}
+
+// The bin of top_p's cut, from the sums of the slices; -1 if none, kBins if min_p
+// cuts before it.  `whole`: the sum of all weights.
+__device__ __forceinline__ int cut_of_slices(Lds &s, const SampleLaunch &a, int r, const Settings &set, const Bins &bins,
+                                             double &whole) {
+    const int tid = threadIdx.x;
+    u64 bin[kSlices][2];
+    double its[kSlices];
+    const int64_t at = (int64_t)r * a.slices;
+#pragma unroll
+    for (int g = 0; g < kSlices; ++g) {
+        its[g] = g < a.slices ? a.parts[(at + g) * kWaves] : 0.0;
+        bin[g][0] = g < a.slices ? a.hist[(at + g) * kBins + tid] : 0;
+        bin[g][1] = g < a.slices ? a.hist[(at + g) * kBins + kThreads + tid] : 0;
+    }
+    u64 sum0 = 0, sum1 = 0;
+    whole = 0.0;
+#pragma unroll
+    for (int g = 0; g < kSlices; ++g) whole += its[g], sum0 += bin[g][0], sum1 += bin[g][1];
+    s.hist[tid] = sum0, s.hist[kThreads + tid] = sum1;
+    __syncthreads();
+    int cut = -1;
+    if (bins.good()) cut = bin_at(s, (u64)__builtin_ldexp(set.top_p * whole, bits_of(a.vocab)));
+    return bins.good() && cut < 0 && set.min_p > 0.0 ? kBins : cut;
+}
+
+// Each slice's tokens that may be kept, or, for top_p over all, those of the bin of
+// the cut, and the sums over it of each wave's part.
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_sample_lists(SampleLaunch a) {
+    Lds &s = lds();
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, r = blockIdx.x / a.slices, g = blockIdx.x - r * a.slices;
+    const Settings set = settings_of(a, r);
+    u64 first, low;
+    Mine<kSlices> mine;
+    tops_of(a, r, first, low, mine);
+    const bool nucleus = by_nucleus(set, a.vocab), small_k = has_small_k(set, a.vocab);
+    if (!good(set) || set.temperature == 0.0 || set.top_k == 1 || first == 0) return;
+    if (!nucleus && !small_k && !only_min_p(set, a.vocab)) return;
+    const float top = logit_of(first);
+    if (__builtin_isinf(top)) return;
+    const Row<T> row(a, r);
+    row.read_ends();
+    if (tid < kTable) s.table[tid] = exp2(tid * (1.0 / kTable));
+    clear_bins(s);
+    __syncthreads();
+    const Weight weight = weight_of(set, top);
+    const int n = slice_of(row, a.slices), from = g * n, to = min(row.pieces, from + n), n16 = (n + kWaves - 1) / kWaves;
+    int count;
+    if (nucleus) {
+        const float bottom = nucleus_bottom(s, set, weight, top, row.V, mine);
+        const Bins bins(top, bottom);
+        double whole, over = 0.0, part = 0.0, all;
+        const int cut = cut_of_slices(s, a, r, set, bins, whole);
+        if (g == 0 && tid == 0) a.cuts[r] = cut, a.wholes[r] = whole;
+        if (cut < 0) return;
+        count = sums_over_bin(row, from, to, n16, set, weight, bins, bottom, cut, over, part);
+        block_upto(over, s.real, all);
+        part = wave_add(part);
+        if (lane == 0) a.kept[(int64_t)blockIdx.x * kWaves + w] = part;
+        if (tid == 0) a.over[blockIdx.x] = all;
+    } else {
+        const float bottom = list_bottom(s, set, top, low, small_k, mine);
+        count = gather(row, from, to, n16, true, [&](float v) { return v >= bottom; });
+    }
+    if (tid == 0) a.counts[blockIdx.x] = count;
+    if (count < kMany)
+        for (int i = tid; i < count; i += kThreads) a.lists[(int64_t)blockIdx.x * (kMany - 1) + i] = s.list[i];
+}
+
+// The least entry of the list's n.
+__device__ __forceinline__ u64 block_bottom(Lds &s, int n) {
+    u64 x = 0;
+    for (int i = threadIdx.x; i < n; i += kThreads) x = larger(x, ~s.list[i]);
+    return ~block_max(x, s);
+}
+
+// The slices' lists, one behind the other; returns how many tokens they are, kMany
+// if they do not fit.
+__device__ __forceinline__ int lists_of(Lds &s, const SampleLaunch &a, int r) {
+    const int lane = threadIdx.x & 63;
+    const int its = lane < a.slices ? a.counts[r * a.slices + lane] : 0;
+    int n = 0;
+    for (int g = 0; g < a.slices; ++g) {
+        const int count = __builtin_amdgcn_readlane(its, g);
+        if (n + count >= kMany) return kMany;
+        const u64 *const list = a.lists + (int64_t)(r * a.slices + g) * (kMany - 1);
+        for (int i = threadIdx.x; i < count; i += kThreads) s.list[n + i] = list[i];
+        n += count;
+    }
+    __syncthreads();
+    return n;
+}
+
+// The part of the row in which the sums of `sum` (this thread's part of the
+// slices' waves) pass u of their whole.
+template <class T>
+__device__ __forceinline__ Part part_of(Lds &s, const Row<T> &row, int slices, double sum, double u, double &whole) {
+    const int tid = threadIdx.x, n = slice_of(row, slices), n16 = (n + kWaves - 1) / kWaves;
+    const double upto = block_upto(sum, s.real, whole), t = u * whole;
+    if (tid == 0) s.found = kThreads;
+    __syncthreads();
+    if (sum > 0.0 && upto > t) atomicMin(&s.found, tid);
+    __syncthreads();
+    if (tid == s.found) s.share = t - (upto - sum);
+    __syncthreads();
+    const int g = s.found / kWaves, from = g * n + s.found % kWaves * n16;
+    return {from, min(min(row.pieces, (g + 1) * n), from + n16), s.share};
+}
+
+// SLICED: the launches above have gone before.
+template <class T, bool SLICED>
 __global__ __launch_bounds__(kThreads) void k_sample(SampleLaunch a) {
     Lds &s = lds();
     const int tid = threadIdx.x, r = blockIdx.x;
-    Settings set;
-    const float temperature = a.temperature ? a.temperature[r] : a.temperature_all;
-    const float top_p = a.top_p ? a.top_p[r] : a.top_p_all, min_p = a.min_p ? a.min_p[r] : a.min_p_all, u = a.u[r];
-    set.temperature = temperature, set.top_p = top_p, set.min_p = min_p, set.u = u;
-    set.top_k = a.top_k ? a.top_k[r] : a.top_k_all;
+    const Settings set = settings_of(a, r);
     auto answer = [&](int token, double share) {
         if (tid == 0) {
             a.token[r] = token;
             if (a.logprob) a.logprob[r] = (float)log(share);
         }
     };
-    if (!(temperature >= 0.0f && temperature < INFINITY && set.top_k >= 0 && top_p > 0.0f && top_p <= 1.0f &&
-          min_p >= 0.0f && min_p <= 1.0f && u >= 0.0f && u < 1.0f)) {
+    if (!good(set)) {
         if (tid == 0 && a.status) a.status[r] = FATE_EINVAL;
         answer(-1, 0.0);
         return;
@@ -792,148 +1152,170 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleLaunch a) {
     clear_bins(s);
     __syncthreads();
 
-    // the largest logit, of equal ones the lowest index
-    float best = -INFINITY;
-    int best_at = 0;
-    each(row, tid, row.pieces, kThreads, [&](const float (&v)[T::kPer], int i0) {
-#pragma unroll
-        for (int e = 0; e < T::kPer; ++e)
-            if (v[e] > best) {
-                best = v[e];
-                best_at = i0 + e;
-            }
-    });
-    const uint32_t mine = key_of(best);
-    const u64 first = wave_max(mine ? entry_of(mine, best_at) : 0), low = wave_max(mine ? ~(u64)mine : 0);
-    if ((tid & 63) == 0) s.whole[tid >> 6] = first, s.least[tid >> 6] = low;
-    __syncthreads();
-    u64 top_entry = 0, low_key = 0;
-    for (int i = 0; i < kWaves; ++i) top_entry = larger(top_entry, s.whole[i]), low_key = larger(low_key, s.least[i]);
-    __syncthreads();
-    if (top_entry == 0) {  // nothing to choose from
+    u64 first, low;
+    Mine<SLICED ? kSlices : 1> mine;
+    if constexpr (SLICED) tops_of(a, r, first, low, mine);
+    else block_range(s, best_of(row, 0, row.pieces, mine.best[0]), first, low);
+    if (first == 0) {  // nothing to choose from
         answer(-1, 0.0);
         return;
     }
-    if (temperature == 0.0f || set.top_k == 1) {
-        answer(index_of(top_entry), 1.0);
+    if (set.temperature == 0.0 || set.top_k == 1) {
+        answer(index_of(first), 1.0);
         return;
     }
-    const float top = logit_of(top_entry);
-    Weight weight;
-    weight.max = top;
-    weight.per = 369.32993046757463 / set.temperature;
+    const float top = logit_of(first);
+    const Weight weight = weight_of(set, top);
     if (__builtin_isinf(top)) {
-        const Answer x = token_at_infinity(row, set, top_p);
+        const Answer x = token_at_infinity(row, set, (float)set.top_p);
         answer(x.token, x.share);
         return;
     }
 
-    // The bins of what may be kept, and that of the cut where it is known.
-    constexpr float kLowest = -3.402823466e38f;
-    const bool cuts_k = set.top_k > 0 && set.top_k < row.V, small_k = cuts_k && set.top_k <= kSmallK;
-    const bool nucleus = set.top_p < 1.0 && !cuts_k;
-    float bottom = kLowest;
-    if (set.min_p > 0.0 && (nucleus || set.top_p >= 1.0)) {  // a little below the logit of weight min_p; weights decide
-        const double x = weight.max + set.temperature * log(set.min_p);
-        bottom = fmaxf(bottom, (float)(x - 1e-6 * (fabs(x) + fabs(weight.max))));
-    }
-    int cut = -1, about = 0;  // about: how many tokens are to be listed, if that is known
-    double whole = 0.0;
-    if (small_k) {
-        const Bins of_threads(top, value_of(~(uint32_t)low_key));
-        if (of_threads.good()) {
-            if (mine) atomicAdd(&s.hist[of_threads.of(best)], 1ull);
-            __syncthreads();
-            const int bin = bin_at(s, (u64)set.top_k);
-            if (bin >= 0) bottom = fmaxf(bottom, of_threads.under(bin));
-        }
-    }
-    Bins bins(top, bottom);
-    if (nucleus) {
-        // Tokens of weight (1 - top_p) S / V or less sum to (1 - top_p) S at most and are cut, and the threads' largest
-        // logits give a bound of S from below: the tokens over that weight are summed by bins while S is.
-        double low_sum;
-        block_upto(mine ? weight(best) : 0.0, s.real, low_sum);
-        const double x = weight.max + set.temperature * log((1.0 - set.top_p) * low_sum / row.V);
-        bottom = fmaxf(bottom, (float)(x - 1e-6 * (fabs(x) + fabs(weight.max))));
-        bins = Bins(top, bottom);
-        const bool good = bins.good();
-        // w + 2^(52 - bits) has w as a whole number of 2^-bits in its last places; a sum of V of them stays under 2^63
-        const int bits = min(52, 30 + __builtin_clz((uint32_t)row.V));
-        const double magic = __builtin_ldexp(1.0, 52 - bits);
-        double sum = 0.0;
-        each(row, tid, row.pieces, kThreads, [&](const float (&v)[T::kPer], int) {
-#pragma unroll
-            for (int e = 0; e < T::kPer; ++e) {
-                const double y = weight(v[e]);
-                sum += y;
-                if (good & (v[e] >= bottom))
-                    atomicAdd(&s.hist[bins.of(v[e])], __builtin_bit_cast(u64, y + magic) - __builtin_bit_cast(u64, magic));
-            }
-        });
-        block_upto(sum, s.real, whole);
-        if (good) cut = bin_at(s, (u64)__builtin_ldexp(set.top_p * whole, bits));
-        if (cut >= 0) {  // how many they may be: a bin's sum by the weight in its middle
-            double n = 0.0, all;
-            for (int b = 2 * tid; b < 2 * tid + 2 && b <= cut; ++b)
-                if (s.hist[b]) n += __builtin_ldexp((double)s.hist[b], -bits) / weight(top - ((float)b + 0.5f) / bins.per);
-            block_upto(n, s.real, all);
-            about = (int)fmin(all, (double)kMany);
-        }
-        if (good && cut < 0 && set.min_p > 0.0) cut = kBins;  // min_p cuts before top_p does
-    }
+    const bool cuts_k = set.top_k > 0 && set.top_k < row.V, small_k = has_small_k(set, row.V);
+    const bool nucleus = by_nucleus(set, row.V);
     Place kept = {-INFINITY, kAll};
-    bool listed = row.V <= kRanked || small_k || cut >= 0, known = false;
-    if (!set.top_k && set.top_p >= 1.0 && set.min_p > 0.0) {  // all that is gathered is kept
-        cut = kBins;
-        listed = true;
-    }
-    if (listed) {
-        auto want = [&](float v) { return (v >= bottom) & (cut < 0 || bins.of(v) <= cut); };
-        int n = about <= kRanked ? gather(row, false, want) : about < kMany ? kRanked + 1 : kMany;
+    bool known = false;        // s.real has the sums of the sixteenths
+    Part part = {0, 0, 0.0};   // or the part that the token lies in is known
+    double whole = 0.0;
+    Answer x;
+    if (nucleus) {
+        if constexpr (SLICED) {
+            const int lane = tid & 63, cut = a.cuts[r];
+            whole = a.wholes[r];
+            if (cut >= 0) {
+                const double over = lane < a.slices ? a.over[r * a.slices + lane] : 0.0;
+                double sum = tid < a.slices * kWaves ? a.kept[(int64_t)r * a.slices * kWaves + tid] : 0.0;
+                const int n = lists_of(s, a, r);
+                const double above = wave_add(over);
+                const u64 last = cut == kBins ? 1 : n < kMany ? last_in_bin(set, weight, n, above, whole) : 0;
+                if (last) {
+                    if (cut < kBins) kept = {logit_of(last), index_of(last)};
+                    // of the bin's tokens, those kept count for their parts
+                    if (tid < n) {
+                        const int its = slice_of(row, a.slices), n16 = (its + kWaves - 1) / kWaves;
+                        const u64 y = s.list[tid];
+                        const int piece = (index_of(y) + row.lead) / T::kPer, g = piece / its;
+                        const double z = y >= last ? weight(logit_of(y)) : 0.0;
+                        s.ranked[tid].entry = g * kWaves + (piece - g * its) / n16;
+                        s.ranked[tid].weight = z >= set.min_p ? z : 0.0;
+                    }
+                    __syncthreads();
+                    if (tid < a.slices * kWaves)
+                        for (int j = 0; j < n; ++j) sum += s.ranked[j].entry == (u64)tid ? s.ranked[j].weight : 0.0;
+                    part = part_of(s, row, a.slices, sum, set.u, whole);
+                }
+            }
+        } else {
+            const float bottom = nucleus_bottom(s, set, weight, top, row.V, mine);
+            const Bins bins(top, bottom);
+            block_upto(sum_by_bins(s, row, 0, row.pieces, weight, bins, bottom), s.real, whole);
+            const int bits = bits_of(row.V);
+            int cut = bins.good() ? bin_at(s, (u64)__builtin_ldexp(set.top_p * whole, bits)) : -1;
+            if (bins.good() && cut < 0 && set.min_p > 0.0) cut = kBins;  // min_p cuts before top_p does
+            if (cut >= 0) {  // how many it keeps, about: a bin's sum by the weight in its middle
+                double n = 0.0, all;
+                for (int b = 2 * tid; b < 2 * tid + 2 && b <= cut; ++b)
+                    if (s.hist[b]) n += __builtin_ldexp((double)s.hist[b], -bits) / weight(top - ((float)b + 0.5f) / bins.per);
+                block_upto(n, s.real, all);
+                if (all <= kRanked) {
+                    const int listed = gather(row, 0, row.pieces, sixteenth(row), false, [&](float v) {
+                        return (v >= bottom) & (bins.of(v) <= cut);
+                    });
+                    if (listed <= kRanked) {
+                        x = from_short(set, weight, listed, whole);
+                        answer(x.token, x.share);
+                        return;
+                    }
+                }
+                known = cut_in_bin(row, set, weight, bins, bottom, cut, whole, kept);
+            }
+        }
+    } else if (small_k || only_min_p(set, row.V)) {
+        int n = 0;
+        float bottom = -3.402823466e38f;
+        if constexpr (SLICED) {
+            n = lists_of(s, a, r);
+            if (n < kMany && n > 0) bottom = logit_of(block_bottom(s, n));
+        } else {
+            bottom = list_bottom(s, set, top, low, small_k, mine);
+            n = gather(row, 0, row.pieces, sixteenth(row), false, [&](float v) { return v >= bottom; });
+        }
         if (n <= kRanked) {
-            const Answer x = from_short(set, weight, n, whole);
+            x = from_short(set, weight, n, 0.0);
             answer(x.token, x.share);
             return;
         }
-        if (small_k && bins.good()) {  // many reach the bound: the bin of the k-th of all
-            clear_bins(s);
-            __syncthreads();
-            each(row, tid, row.pieces, kThreads, [&](const float (&v)[T::kPer], int) {
-#pragma unroll
-                for (int e = 0; e < T::kPer; ++e)
-                    if (v[e] >= bottom) atomicAdd(&s.hist[bins.of(v[e])], 1ull);
-            });
-            __syncthreads();
-            cut = bin_at(s, (u64)set.top_k);
+        if (!SLICED && n < kMany) n = gather(row, 0, row.pieces, sixteenth(row), true, [&](float v) { return v >= bottom; });
+        const Bins bins(top, bottom);
+        if (n < kMany && (small_k ? bins.good() && from_list_of_k(set, weight, n, bins, x) : (x = from_list(set, weight, n, 1), true))) {
+            answer(x.token, x.share);
+            return;
         }
-        if ((n < kMany || small_k) && cut >= 0 && bins.good()) {
-            n = gather(row, true, want);
-            u64 last = n < kMany;
-            if (last && cut < kBins)
-                last = last_of_list(weight, n, bins, cut, 1, small_k ? set.top_k : 0, set.top_p * whole);
-            if (last && small_k && set.top_p < 1.0) last = nucleus_of_list(set.top_p, weight, n, bins, last);
-            if (last) {
-                const Answer x = from_list(set, weight, n, last);
-                answer(x.token, x.share);
-                return;
-            }
-        }
+    } else if (SLICED && uncut(set, row.V)) {
+        part = part_of(s, row, a.slices, tid < a.slices * kWaves ? a.parts[(int64_t)r * a.slices * kWaves + tid] : 0.0, set.u, whole);
     }
-    if (nucleus && cut >= 0 && cut < kBins) known = cut_in_bin(row, set, weight, bins, bottom, cut, whole, kept);
-    if (!known && (cuts_k || set.top_p < 1.0)) kept = by_digits(row, set, weight, top_p);
-    const Answer x = token_at(row, set, weight, kept, known);
+    const bool parted = part.to > 0;
+    if (!known && !parted && (cuts_k || set.top_p < 1.0)) kept = by_digits(row, set, weight, (float)set.top_p);
+    x = token_at(row, set, weight, kept, known, parted, part, whole);
     answer(x.token, x.share);
 }
 
 }  // namespace
 
-int launch_sample(const SampleLaunch &a, void *stream) {
+// Workgroups of a row's slices: calls of up to 128 rows by as many as the chip
+// runs at once, of 32768 logits each at least.  The three launches more cost some
+// 10 us: for 64 rows of 32768 top-p 0.9 46 us by one workgroup a row and 59 by four,
+// for one of 50001 38 and 48, and top-k 50 18 and 24.
+int sample_slices(int64_t rows, int64_t vocab) {
+    const int64_t fill = rows > 0 ? 256 / rows : 1, most = vocab / 32768;
+    const int64_t n = fill < most ? fill : most;
+    return n < 2 ? 1 : n > kSlices ? kSlices : (int)n;
+}
+
+size_t sample_ws(int64_t rows, int64_t vocab) {
+    const int n = sample_slices(rows, vocab);
+    if (n == 1) return 0;
+    return (size_t)rows * n * ((2 + kMany - 1 + kBins) * sizeof(u64) + (2 * kWaves + 1) * sizeof(double) +
+                               kThreads * sizeof(float) + sizeof(int32_t)) +
+           (size_t)rows * (sizeof(double) + sizeof(int32_t));
+}
+
+namespace {
+
+template <class T>
+void go(SampleLaunch a, void *ws, hipStream_t s) {
+    const dim3 block(kThreads);
+    a.slices = sample_slices(a.rows, a.vocab);
+    if (a.slices == 1) {
+        hipLaunchKernelGGL((k_sample<T, false>), dim3((unsigned)a.rows), block, 0, s, a);
+        return;
+    }
+    const int64_t n = (int64_t)a.rows * a.slices;
+    a.tops = static_cast<unsigned long long *>(ws);
+    a.lows = a.tops + n;
+    a.hist = a.lows + n;
+    a.parts = reinterpret_cast<double *>(a.hist + n * kBins);
+    a.kept = a.parts + n * kWaves;
+    a.over = a.kept + n * kWaves;
+    a.wholes = a.over + n;
+    a.lists = reinterpret_cast<unsigned long long *>(a.wholes + a.rows);
+    a.best = reinterpret_cast<float *>(a.lists + n * (kMany - 1));
+    a.counts = reinterpret_cast<int32_t *>(a.best + n * kThreads);
+    a.cuts = a.counts + n;
+    hipLaunchKernelGGL((k_sample_tops<T>), dim3((unsigned)n), block, 0, s, a);
+    hipLaunchKernelGGL((k_sample_sums<T>), dim3((unsigned)n), block, 0, s, a);
+    hipLaunchKernelGGL((k_sample_lists<T>), dim3((unsigned)n), block, 0, s, a);
+    hipLaunchKernelGGL((k_sample<T, true>), dim3((unsigned)a.rows), block, 0, s, a);
+}
+
+}  // namespace
+
+int launch_sample(const SampleLaunch &a, void *ws, void *stream) {
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    const dim3 grid((unsigned)a.rows), block(kThreads);
-    if (a.dtype == FATE_BF16) hipLaunchKernelGGL((k_sample<B16>), grid, block, 0, s, a);
-    else if (a.dtype == FATE_F16) hipLaunchKernelGGL((k_sample<H16>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((k_sample<F32>), grid, block, 0, s, a);
+    if (a.dtype == FATE_BF16) go<B16>(a, ws, s);
+    else if (a.dtype == FATE_F16) go<H16>(a, ws, s);
+    else go<F32>(a, ws, s);
     return (int)hipGetLastError();
 }
 

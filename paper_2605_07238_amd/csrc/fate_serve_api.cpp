@@ -99,7 +99,7 @@ fate_status_t fate_sample_ws_size(const fate_sampling_t *s, size_t *bytes) {
     const fate_status_t st = check_sampling(s);
     if (st != FATE_OK) return st;
     if (!bytes) return FATE_EINVAL;
-    *bytes = 0;
+    *bytes = fate::sample_ws(s->rows, s->vocab);
     return FATE_OK;
 }
 
@@ -133,7 +133,7 @@ fate_status_t fate_sample(const fate_sampling_t *s, int32_t *d_token, float *d_l
     a.top_k_all = s->top_k_all;
     a.top_p_all = s->top_p_all;
     a.min_p_all = s->min_p_all;
-    return fate::launch_sample(a, stream) == 0 ? FATE_OK : FATE_EHIP;
+    return fate::launch_sample(a, d_ws, stream) == 0 ? FATE_OK : FATE_EHIP;
 }
 
 }  // extern "C"
