@@ -21,7 +21,30 @@ namespace fate {
 namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
-constexpr int kStaged = 4096;  // sequences whose offsets fit the search in LDS
+constexpr int kStaged = 2048;  // sequences that fit LDS
+
+struct Scans {
+    int64_t a[kWaves], b[kWaves];
+};
+
+// Inclusive sums over the workgroup's threads, of two values in the same steps.
+__device__ __forceinline__ void block_scan2(int64_t &x, int64_t &y, Scans &s, int64_t &all_x, int64_t &all_y) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    x = wave_scan_add(x);
+    y = wave_scan_add(y);
+    if (lane == 63) s.a[w] = x, s.b[w] = y;
+    __syncthreads();
+    int64_t before_x = 0, before_y = 0;
+    all_x = all_y = 0;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+        if (i < w) before_x += s.a[i], before_y += s.b[i];
+        all_x += s.a[i], all_y += s.b[i];
+    }
+    x += before_x;
+    y += before_y;
+    __syncthreads();
+}
 
 // Inclusive sums over the workgroup's threads; `before` holds kWaves entries.
 template <class I>
@@ -41,8 +64,10 @@ __device__ __forceinline__ I block_scan(I x, I *before, I &total) {
     return sum + in_wave;
 }
 
-struct Scans {
-    int64_t a[kWaves], b[kWaves];
+// Of each sequence, where rows are placed: its first row, its keys before the
+// call, and the pages taken before it.
+struct Staged {
+    int off[kStaged + 1], old[kStaged], taken[kStaged];
 };
 
 __device__ __forceinline__ int pages_for(int64_t keys, int shift) {
@@ -55,8 +80,9 @@ __device__ __forceinline__ int free_pages(const PagesLaunch &a) {
     return n >= 0 && n <= a.n_pages ? n : 0;
 }
 
-// Lengths of all sequences: off, kv_out, taken, status and n_free_out.
-__device__ void reserve_lengths(const PagesLaunch &a, Scans &lds) {
+// Lengths of all sequences: off, kv_out, taken, status and n_free_out; in LDS too
+// if `staged` is given.  Returns the rows of the call.
+__device__ __forceinline__ int reserve_lengths(const PagesLaunch &a, Scans &lds, Staged *staged) {
     const int tid = threadIdx.x, stack = *a.n_free, n_free = free_pages(a);
     int64_t asked = 0, rows = 0, done = 0;  // before this step; done: rows and pages given, in the halves of a word
     for (int64_t at = 0; at < a.B; at += kThreads) {
@@ -71,12 +97,17 @@ __device__ void reserve_lengths(const PagesLaunch &a, Scans &lds) {
         }
         const int need = good ? pages_for(kv + fresh_tokens, a.shift) - pages_for(kv, a.shift) : 0;
         int64_t all_pages, all_rows, all_done;
-        const int64_t x = asked + block_scan((int64_t)need, lds.a, all_pages);
-        const int64_t y = rows + block_scan(fresh_tokens, lds.b, all_rows);
-        const bool fits = (need == 0 || x <= n_free) && y <= a.T;
+        int64_t x = need, y = fresh_tokens;
+        block_scan2(x, y, lds, all_pages, all_rows);
+        const bool fits = (need == 0 || asked + x <= n_free) && rows + y <= a.T;
         const int64_t mine = fits ? fresh_tokens << 32 | need : 0;  // rows are at most T, pages at most n_free
         const int64_t upto = done + block_scan(mine, lds.a, all_done);
         if (b < a.B) {
+            if (staged) {
+                staged->off[b + 1] = (int)(upto >> 32);
+                staged->old[b] = (int)kv;
+                staged->taken[b] = (int)upto - (fits ? need : 0);
+            }
             a.off[b + 1] = (int)(upto >> 32);
             a.moved[b + 1] = (int)upto;
             a.kv_out[b] = (int)(fits ? kv + fresh_tokens : kv);
@@ -87,17 +118,18 @@ __device__ void reserve_lengths(const PagesLaunch &a, Scans &lds) {
         done += all_done;
     }
     if (tid == 0) {
+        if (staged) staged->off[0] = 0;
         a.off[0] = a.moved[0] = 0;
         *a.n_free_out = stack - (int)done;
     }
+    return (int)(done >> 32);
 }
 
-// Rows [from, to): their positions, slots, and the pages that start with them.
-// `off` holds the offsets, in LDS where there are few.
-template <class Off>
-__device__ void reserve_rows(const PagesLaunch &a, const Off *off, int64_t from, int64_t to) {
-    const int stack = *a.n_free_out + a.moved[a.B];
-    const int64_t end = a.B ? off[a.B] : 0;
+// Rows [from, to): their positions, slots, and the pages that start with them;
+// `end` rows are in the call, and `stack` pages were free before it.
+template <class Old, class Taken>
+__device__ __forceinline__ void reserve_rows(const PagesLaunch &a, const int *off, Old old_of, Taken taken_of, int stack,
+                                             int64_t end, int64_t from, int64_t to) {
     for (int64_t t = from + threadIdx.x; t < to; t += blockDim.x) {
         int64_t slot = -1;
         int pos = -1;
@@ -108,13 +140,13 @@ __device__ void reserve_rows(const PagesLaunch &a, const Off *off, int64_t from,
                 if (off[mid + 1] <= t) lo = mid + 1;
                 else hi = mid;
             }
-            const int start = off[lo], old = a.kv_out[lo] - (off[lo + 1] - start);
+            const int start = off[lo], old = old_of(lo);
             pos = old + (int)(t - start);
             const int j = pos >> a.shift, have = pages_for(old, a.shift), in_page = pos & ((1 << a.shift) - 1);
             int32_t *const entry = a.pages + lo * a.pages_stride + j;
             int page;
             if (j >= have) {
-                page = a.free[stack - 1 - a.moved[lo] - (j - have)];
+                page = a.free[stack - 1 - taken_of(lo) - (j - have)];
                 if (in_page == 0) *entry = page;
             } else {
                 page = *entry;
@@ -127,32 +159,37 @@ __device__ void reserve_rows(const PagesLaunch &a, const Off *off, int64_t from,
     }
 }
 
-template <bool ROWS>
 __global__ __launch_bounds__(kThreads) void k_kv_reserve(PagesLaunch a) {
     __shared__ Scans lds;
-    __shared__ int off[ROWS ? kStaged + 1 : 1];
-    reserve_lengths(a, lds);
-    if (ROWS) {
-        __syncthreads();
-        for (int i = threadIdx.x; i <= a.B; i += kThreads) off[i] = a.off[i];
-        __syncthreads();
-        reserve_rows(a, off, 0, a.T);
-    }
+    reserve_lengths(a, lds, nullptr);
+}
+
+// Small calls: with the rows, from LDS.  (Read back from memory, what the scan
+// has written costs two round trips more: 8.0 against 7.0 us for 64 sequences.)
+__global__ __launch_bounds__(kThreads) void k_kv_reserve_small(PagesLaunch a) {
+    __shared__ Scans lds;
+    __shared__ Staged s;
+    const int stack = *a.n_free;
+    const int end = reserve_lengths(a, lds, &s);
+    __syncthreads();
+    reserve_rows(a, s.off, [&](int b) { return s.old[b]; }, [&](int b) { return s.taken[b]; }, stack, end, 0, a.T);
 }
 
 constexpr int kRowsPer = 1024;  // rows of a workgroup of the second launch
 
 template <bool STAGED>
 __global__ __launch_bounds__(256) void k_kv_rows(PagesLaunch a) {
-    __shared__ int off[STAGED ? kStaged + 1 : 1];
+    __shared__ int in_lds[STAGED ? kStaged + 1 : 1];
     const int64_t from = (int64_t)blockIdx.x * kRowsPer, to = min(from + kRowsPer, a.T);
+    const int *off = a.off;
+    const int end = a.B ? a.off[a.B] : 0, stack = *a.n_free_out + a.moved[a.B];
     if (STAGED) {
-        for (int i = threadIdx.x; i <= a.B; i += 256) off[i] = a.off[i];
+        for (int i = threadIdx.x; i <= a.B; i += 256) in_lds[i] = a.off[i];
         __syncthreads();
-        reserve_rows(a, off, from, to);
-    } else {
-        reserve_rows(a, a.off, from, to);
+        off = in_lds;
     }
+    reserve_rows(a, off, [&](int b) { return a.kv_out[b] - (off[b + 1] - off[b]); }, [&](int b) { return a.moved[b]; }, stack,
+                 end, from, to);
 }
 
 // Pages that each of the sequences b = first, first + step .. gives back, a
@@ -237,10 +274,10 @@ __global__ __launch_bounds__(256) void k_kv_trim_pages(PagesLaunch a) {
 int launch_reserve(const PagesLaunch &a, void *stream) {
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     if (a.B <= kStaged && a.T <= kReserveSmall) {
-        hipLaunchKernelGGL((k_kv_reserve<true>), dim3(1), dim3(kThreads), 0, s, a);
+        hipLaunchKernelGGL(k_kv_reserve_small, dim3(1), dim3(kThreads), 0, s, a);
         return (int)hipGetLastError();
     }
-    hipLaunchKernelGGL((k_kv_reserve<false>), dim3(1), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL(k_kv_reserve, dim3(1), dim3(kThreads), 0, s, a);
     const dim3 grid((unsigned)((a.T + kRowsPer - 1) / kRowsPer));
     if (grid.x > 0 && a.B <= kStaged) hipLaunchKernelGGL((k_kv_rows<true>), grid, dim3(256), 0, s, a);
     else if (grid.x > 0) hipLaunchKernelGGL((k_kv_rows<false>), grid, dim3(256), 0, s, a);

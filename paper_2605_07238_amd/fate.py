@@ -1185,15 +1185,17 @@ def fate_kv_reserve(new, kv_len, pages, free, n_free, page_size: int, T: int, ou
     if out is None:
         if T < 0:
             raise ValueError("T must not be negative, got %d" % T)
-        n = _t.empty(3 * B + 3, dtype=int32, device=dev)
-        out = Reserved(n[:B + 1], n[B + 1:2 * B + 1], n[2 * B + 1:2 * B + 2], n[2 * B + 2:],
-                       _t.empty(T, dtype=int64, device=dev), _t.empty(T, dtype=int32, device=dev))
-    st = load().fate_kv_reserve(
-        t, new.data_ptr(), T, _array(out.off, "out.off", B + 1, int32, dev), _array(out.kv_len, "out.kv_len", B, int32, dev),
-        _array(out.n_free, "out.n_free", 1, int32, dev), _array(out.taken, "out.taken", B + 1, int32, dev),
-        None if out.slots is None else _array(out.slots, "out.slots", T, int64, dev),
-        None if out.positions is None else _array(out.positions, "out.positions", T, int32, dev),
-        _attn_status(status, B, dev), _t.raw_stream(dev.index))
+        n, slots = _t.empty(3 * B + 3 + T, dtype=int32, device=dev), _t.empty(T, dtype=int64, device=dev)
+        off, kv, left, taken, positions = n.split((B + 1, B, 1, B + 1, T))
+        out = Reserved(off, kv, left, taken, slots, positions)
+        at = n.data_ptr()
+        where = (at, at + 4 * B + 4, at + 8 * B + 4, at + 8 * B + 8, slots.data_ptr(), at + 12 * B + 12)
+    else:
+        where = (_array(out.off, "out.off", B + 1, int32, dev), _array(out.kv_len, "out.kv_len", B, int32, dev),
+                 _array(out.n_free, "out.n_free", 1, int32, dev), _array(out.taken, "out.taken", B + 1, int32, dev),
+                 None if out.slots is None else _array(out.slots, "out.slots", T, int64, dev),
+                 None if out.positions is None else _array(out.positions, "out.positions", T, int32, dev))
+    st = load().fate_kv_reserve(t, new.data_ptr(), T, *where, _attn_status(status, B, dev), _t.raw_stream(dev.index))
     if st != FATE_OK:
         raise FateError(st, "fate_kv_reserve")
     return out
@@ -1212,11 +1214,12 @@ def fate_kv_trim(keep, kv_len, pages, free, n_free, page_size: int, out: Optiona
     B = t.B
     if out is None:
         n = _t.empty(2 * B + 2, dtype=int32, device=dev)
-        out = Trimmed(n[:B], n[B:B + 1], n[B + 1:])
-    st = load().fate_kv_trim(t, keep.data_ptr(), _array(out.kv_len, "out.kv_len", B, int32, dev),
-                             _array(out.n_free, "out.n_free", 1, int32, dev),
-                             _array(out.given, "out.given", B + 1, int32, dev), _attn_status(status, B, dev),
-                             _t.raw_stream(dev.index))
+        out, at = Trimmed(*n.split((B, 1, B + 1))), n.data_ptr()
+        where = (at, at + 4 * B, at + 4 * B + 4)
+    else:
+        where = (_array(out.kv_len, "out.kv_len", B, int32, dev), _array(out.n_free, "out.n_free", 1, int32, dev),
+                 _array(out.given, "out.given", B + 1, int32, dev))
+    st = load().fate_kv_trim(t, keep.data_ptr(), *where, _attn_status(status, B, dev), _t.raw_stream(dev.index))
     if st != FATE_OK:
         raise FateError(st, "fate_kv_trim")
     return out
