@@ -23,7 +23,9 @@
 // digits (11, 11 and 10 bits of the key), each by a histogram, of counts or of
 // weights; then two readings find the token, of which the second is of a
 // sixteenth of the row.  Instructions bind it, of a weight some 22; code that is
-// run once costs what its fetching costs, so that loops are kept short.
+// run once costs what its fetching costs, so that loops are kept short.  Rows of
+// 16-bit logits can go by their values instead (by_values): 512 rows of 131072 in
+// bfloat16 with top_p 0.9, inputs in turn, 91 us where weights of each token took 218.
 #include <hip/hip_runtime.h>
 
 #include "fate_sample.h"
@@ -41,14 +43,36 @@ constexpr int kRanked = 512;   // of these, most that are ranked
 constexpr int kSmallK = 1024;  // largest top_k that the threads' largest logits bound
 constexpr int kBins = 2048;
 
+struct Ranked {
+    u64 entry;
+    double weight;
+};
+
+// Rows of 16-bit logits by their values (see by_values): how many tokens have each
+// of the 65536, two counts to a word, and then the weights of the kept ones; of the
+// stretches of 64 values that occur, the value that starts them, their tokens, and
+// the sum of their weights.
+constexpr int kValues = 65536, kStretch = 64, kStretches = kValues / kStretch;
+constexpr int kWeights = 16384;
+struct Values {
+    union {
+        uint32_t counts[kValues / 2];
+        double weights[kWeights];
+    };
+    double sum[kStretches];
+    int num[kStretches], first[kStretches];
+};
+
 struct Lds {
     double table[256];
-    u64 list[kWaves * kOwn];
-    u64 hist[kBins];
-    struct {
-        u64 entry;
-        double weight;
-    } ranked[kRanked + 8];
+    union {
+        struct {
+            u64 list[kWaves * kOwn];
+            u64 hist[kBins];
+            Ranked ranked[kRanked + 8];
+        };
+        Values values;
+    };
     u64 whole[kWaves], least[kWaves];
     double real[kWaves];
     float ends[2][8];  // the values of the row's first and last piece
@@ -85,7 +109,7 @@ struct F32 {
         return __builtin_bit_cast(float, w);
     }
     static __device__ __forceinline__ float at(const char *p, int64_t i) { return ((const float *)p)[i]; }
-    static constexpr int kBytes = 4;
+    static constexpr int kBytes = 4, kValuesFrom = 0;
 };
 struct B16 {
     static constexpr int kPer = 8;
@@ -97,6 +121,9 @@ struct B16 {
         return __builtin_bit_cast(float, (uint32_t)((const uint16_t *)p)[i] << 16);
     }
     static constexpr int kBytes = 2;
+    static constexpr int kInfinity = 0x7f80, kValuesFrom = 8192;
+    static __device__ __forceinline__ float of_bits(int b) { return __builtin_bit_cast(float, (uint32_t)b << 16); }
+    static __device__ __forceinline__ uint32_t bits(float v) { return __builtin_bit_cast(uint32_t, v) >> 16; }
 };
 struct H16 {
     static constexpr int kPer = 8;
@@ -105,6 +132,9 @@ struct H16 {
     }
     static __device__ __forceinline__ float at(const char *p, int64_t i) { return (float)((const _Float16 *)p)[i]; }
     static constexpr int kBytes = 2;
+    static constexpr int kInfinity = 0x7c00, kValuesFrom = 16384;
+    static __device__ __forceinline__ float of_bits(int b) { return (float)__builtin_bit_cast(_Float16, (uint16_t)b); }
+    static __device__ __forceinline__ uint32_t bits(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
 };
 
 // A row in pieces of 16 aligned bytes, numbered from that of its first element;
@@ -257,29 +287,25 @@ __device__ __forceinline__ u64 wave_max(u64 x) {
     return of_lane(x, 63);
 }
 
-// Sums up to and with this thread, and of all.
+// Sums up to and with this thread, and of all.  (The waves' sums go through lanes:
+// added one after the other by every wave they took 2 us.)
 template <class I>
 __device__ __forceinline__ I block_upto(I x, I (&part)[kWaves], I &total) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     x = wave_upto(x);
     if (lane == 63) part[w] = x;
     __syncthreads();
-    I before = 0;
-    total = 0;
-    for (int i = 0; i < kWaves; ++i) {
-        if (i < w) before += part[i];
-        total += part[i];
-    }
+    const I upto = wave_upto(lane < kWaves ? part[lane] : I(0));
     __syncthreads();
-    return before + x;
+    total = of_lane(upto, kWaves - 1);
+    return w ? of_lane(upto, w - 1) + x : x;
 }
 
 __device__ __forceinline__ u64 block_max(u64 x, Lds &s) {
     x = wave_max(x);
     if ((threadIdx.x & 63) == 0) s.whole[threadIdx.x >> 6] = x;
     __syncthreads();
-    x = 0;
-    for (int i = 0; i < kWaves; ++i) x = larger(x, s.whole[i]);
+    x = wave_max((threadIdx.x & 63) < kWaves ? s.whole[threadIdx.x & 63] : 0);
     __syncthreads();
     return x;
 }
@@ -836,6 +862,22 @@ __device__ __forceinline__ bool uncut(const Settings &x, int V) {
     return x.top_p >= 1.0 && !(x.top_k > 0 && x.top_k < V) && x.min_p == 0.0;
 }
 
+// Rows that go by their values: 16-bit logits whose nucleus, or many largest, are
+// asked for.  512 rows of 131072 in bfloat16 take 74 us so for any cut, otherwise
+// 210 for top-p 0.9 and 73 to 147 for top-k 200 to 1000, but 57 for 50; 64 rows of
+// 8192 15 for top-p, otherwise 23, and of 4096 15 either way; in float16, of which
+// more values occur, of 16384 26 against 39, and of 8192 24 against 23.  Past 2^19
+// the slices of a row's other way win: 100 against 105 us for one of 524288.
+template <class T>
+__device__ __host__ __forceinline__ bool by_values_pays(double temperature, int top_k, double top_p, int V) {
+    if (T::kBytes > 2 || V < T::kValuesFrom || V > 1 << 19 || !(temperature > 0.0)) return false;
+    return top_k > 0 && top_k < V ? top_k > 256 : top_p < 1.0;
+}
+template <class T>
+__device__ __forceinline__ bool goes_by_values(const Settings &x, int V) {
+    return by_values_pays<T>(x.temperature, x.top_k, x.top_p, V);
+}
+
 __device__ __forceinline__ Weight weight_of(const Settings &set, float top) {
     return {top, 369.32993046757463 / set.temperature};
 }
@@ -912,12 +954,12 @@ __device__ __forceinline__ u64 best_of(const Row<T> &row, int from, int to, floa
 
 // The largest entry of the workgroup, and the complement of its least key.
 __device__ __forceinline__ void block_range(Lds &s, u64 mine, u64 &top, u64 &low) {
-    const int w = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const u64 first = wave_max(mine), least = wave_max(mine ? ~(mine >> 32) : 0);
-    if ((threadIdx.x & 63) == 0) s.whole[w] = first, s.least[w] = least;
+    if (lane == 0) s.whole[w] = first, s.least[w] = least;
     __syncthreads();
-    top = low = 0;
-    for (int i = 0; i < kWaves; ++i) top = larger(top, s.whole[i]), low = larger(low, s.least[i]);
+    top = wave_max(lane < kWaves ? s.whole[lane] : 0);
+    low = wave_max(lane < kWaves ? s.least[lane] : 0);
     __syncthreads();
 }
 
@@ -931,6 +973,7 @@ template <class T>
 __global__ __launch_bounds__(kThreads) void k_sample_tops(SampleLaunch a) {
     Lds &s = lds();
     const int r = blockIdx.x / a.slices, g = blockIdx.x - r * a.slices;
+    if (T::kBytes == 2 && goes_by_values<T>(settings_of(a, r), a.vocab)) return;
     const Row<T> row(a, r);
     row.read_ends();
     __syncthreads();
@@ -963,6 +1006,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_sums(SampleLaunch a) {
     Lds &s = lds();
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, r = blockIdx.x / a.slices, g = blockIdx.x - r * a.slices;
     const Settings set = settings_of(a, r);
+    if (T::kBytes == 2 && goes_by_values<T>(set, a.vocab)) return;
     u64 first, low;
     Mine<kSlices> mine;
     tops_of(a, r, first, low, mine);
@@ -1052,6 +1096,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_lists(SampleLaunch a) {
     Lds &s = lds();
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, r = blockIdx.x / a.slices, g = blockIdx.x - r * a.slices;
     const Settings set = settings_of(a, r);
+    if (T::kBytes == 2 && goes_by_values<T>(set, a.vocab)) return;
     u64 first, low;
     Mine<kSlices> mine;
     tops_of(a, r, first, low, mine);
@@ -1129,6 +1174,269 @@ __device__ __forceinline__ Part part_of(Lds &s, const Row<T> &row, int slices, d
     return {from, min(min(row.pieces, (g + 1) * n), from + n16), s.share};
 }
 
+// 16-bit logits are few values, and what is kept is a stretch of these: of its
+// last value the first `need` tokens.  One reading counts each value's tokens, the
+// cuts are found among the values, and a second reading adds up weights from a
+// table.  Values by falling order: 0 is the bits 0x7fff, 32767 is 0, and from there
+// on they are the bits themselves.
+__device__ __forceinline__ int turned(int x) { return x < 0x8000 ? 0x7fff - x : x; }  // bits to order, and back
+template <class T>
+__device__ __forceinline__ int order_of(float v) { return turned((int)T::bits(v + 0.0f)); }  // -0 is 0
+
+struct Kept {
+    int upto, need;  // the values before `upto`, and so many tokens of it
+};
+
+// The first of n stretches with which the sums of size(stretch) reach the target,
+// n - 1 if none; `before`: the sum of those before it.  (One wave's work.)
+template <class I, class Size>
+__device__ __forceinline__ int stretch_at(int n, I target, Size size, I &before) {
+    const int lane = threadIdx.x & 63;
+    I sum = 0;
+    for (int base = 0;; base += 64) {
+        const int i = base + lane;
+        const I upto = sum + wave_upto(i < n ? size(i) : I(0));
+        const u64 reach = __ballot(i < n && upto >= target);
+        if (reach || base + 64 >= n) {
+            const int at = reach ? __builtin_amdgcn_readfirstlane(__ffsll(reach) - 1) : n - 1 - base;
+            before = at ? of_lane(upto, at - 1) : sum;
+            return base + at;
+        }
+        sum = of_lane(upto, 63);
+    }
+}
+
+// This lane's value of a stretch: its place in the order, its tokens, its weight.
+template <class T>
+__device__ __forceinline__ int value_in(const Values &s, const Weight &weight, int stretch, int &count, double &w) {
+    const int order = s.first[stretch] + (int)(threadIdx.x & 63);
+    count = ((const uint16_t *)s.counts)[turned(order)];
+    w = count ? weight(T::of_bits(turned(order))) : 0.0;
+    return order;
+}
+
+// What the settings keep of a row with n stretches.
+template <class T>
+__device__ __forceinline__ Kept cuts_of(const Values &s, const Settings &set, const Weight &weight, int V, int n) {
+    int count, last = n - 1;
+    double w, before, whole;
+    int order = value_in<T>(s, weight, last, count, w);
+    const int end = 63 - __clzll(__ballot(count > 0));  // (a stretch has a token)
+    Kept kept = {__builtin_amdgcn_readlane(order, end) + 1, 0};
+    if (set.top_k > 0 && set.top_k < V) {
+        u64 tokens;
+        const int at = stretch_at<u64>(n, (u64)set.top_k, [&](int i) { return (u64)s.num[i]; }, tokens);
+        order = value_in<T>(s, weight, at, count, w);
+        const u64 upto = tokens + wave_upto((u64)count), reach = __ballot(upto >= (u64)set.top_k);
+        if (reach) {
+            const int i = __builtin_amdgcn_readfirstlane(__ffsll(reach) - 1);
+            last = at;
+            kept = {__builtin_amdgcn_readlane(order, i),
+                    (int)((u64)set.top_k - of_lane(upto, i)) + __builtin_amdgcn_readlane(count, i)};
+        }
+    }
+    // of the last stretch, what is kept so far
+    order = value_in<T>(s, weight, last, count, w);
+    const double rest = wave_add((order < kept.upto ? count : order == kept.upto ? kept.need : 0) * w);
+    auto sum = [&](int i) { return i == last ? rest : s.sum[i]; };
+    if (set.top_p < 1.0) {
+        stretch_at<double>(last + 1, INFINITY, sum, whole);
+        const double aim = set.top_p * (whole + rest);
+        const int at = stretch_at<double>(last + 1, aim, sum, before);
+        order = value_in<T>(s, weight, at, count, w);
+        count = order < kept.upto ? count : order == kept.upto ? kept.need : 0;
+        before += wave_upto(count * w) - count * w;
+        const u64 some = __ballot(count > 0), less = __ballot(count > 0 && before < aim);
+        const int i = __builtin_amdgcn_readfirstlane(less ? 63 - __clzll(less) : __ffsll(some) - 1);
+        const double need = __builtin_ceil((aim - before) / w);  // tokens of the value before which less than top_p lies
+        kept = {__builtin_amdgcn_readlane(order, i),
+                __builtin_amdgcn_readlane(need >= count ? count : need > 1.0 ? (int)need : 1, i)};
+    }
+    if (set.min_p > 0.0)
+        for (int i = 0; i < n && s.first[i] <= kept.upto; ++i) {
+            order = value_in<T>(s, weight, i, count, w);
+            const u64 less = __ballot(count > 0 && w < set.min_p);
+            if (less) {
+                order = __builtin_amdgcn_readlane(order, __builtin_amdgcn_readfirstlane(__ffsll(less) - 1));
+                if (order <= kept.upto) kept = {order, 0};
+                break;
+            }
+        }
+    return kept;
+}
+
+// Weights of the values first .. upto - 1, and 0 behind them; of more than fit,
+// all but `gap` from `hole` on, next to zero, which are worked out where they occur.
+template <class T>
+struct Table {
+    Weight weight;
+    int first, upto, hole, gap;
+    __device__ __forceinline__ Table(const Weight &w, int f, int u) : weight(w), first(f), upto(u) {
+        gap = max(0, upto - first - (kWeights - 1));
+        hole = min(max(0x8000 - gap / 2, first), upto - gap);
+    }
+    __device__ __forceinline__ void fill(Values &s) const {
+        const int n = upto - first - gap;
+        for (int i = threadIdx.x; i <= n; i += kThreads) {
+            const int order = first + i + (first + i < hole ? 0 : gap);
+            s.weights[i] = i < n ? weight(T::of_bits(turned(order))) : 0.0;
+        }
+    }
+    // (NaN comes before `first` or behind `upto`, -infinity behind it or at it, where nothing is kept then)
+    template <bool GAP>
+    __device__ __forceinline__ double of(const Values &s, int order, float v) const {
+        const uint32_t i = min((uint32_t)(order - first), (uint32_t)(upto - first));
+        if (!GAP) return s.weights[i];
+        if (order >= hole && order < hole + gap) return weight(v);
+        return s.weights[order < hole && order >= first ? i : i - gap];
+    }
+};
+
+// Of some tokens, the sum of the weights of values that are kept, and how many have
+// the last of them.
+struct Sums {
+    double sum;
+    int ties;
+};
+template <bool GAP, class T>
+__device__ __forceinline__ Sums sums_of(const Values &s, const Row<T> &row, const Table<T> &table, int from, int to, int step) {
+    Sums x = {0.0, 0};
+    each(row, from, to, step, [&](const float (&v)[T::kPer], int) {
+#pragma unroll
+        for (int e = 0; e < T::kPer; ++e) {
+            const int order = order_of<T>(v[e]);
+            x.sum += table.template of<GAP>(s, order, v[e]);
+            x.ties += order == table.upto;
+        }
+    });
+    return x;
+}
+
+// The token, from the table and `need` ties: a sixteenth of the row, a sixteenth of
+// that, and there a lane's pieces.
+template <bool GAP, class T>
+__device__ __forceinline__ void token_by_table(Lds &all_of, const Row<T> &row, const Table<T> &table, double tie, int need, double u) {
+    const Values &s = all_of.values;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int from = 0, to = row.pieces, left = need;  // left: ties that are still to be kept
+    double t = 0.0, total = 0.0;
+#pragma nounroll
+    for (int level = 0; level < 2; ++level) {
+        const int per = (to - from + kWaves - 1) / kWaves;
+        const Sums x = sums_of<GAP>(s, row, table, from + wave * per + lane, min(to, from + (wave + 1) * per), 64);
+        const double its = wave_add(x.sum);
+        const u64 ties = wave_add((u64)x.ties);
+        if (lane == 0) all_of.real[wave] = its, all_of.counts[wave] = (int)ties;
+        __syncthreads();
+        const int mine = lane < kWaves ? all_of.counts[lane] : 0;
+        const int my_left = max(0, left - (int)(wave_upto((u64)mine) - (u64)mine));
+        const double sum = lane < kWaves ? all_of.real[lane] + min(my_left, mine) * tie : 0.0, upto = wave_upto(sum);
+        if (level == 0) {
+            total = of_lane(upto, 63);
+            t = u * total;
+        }
+        const u64 past = __ballot(sum > 0.0 && upto > t), some = __ballot(sum > 0.0);
+        const int part = __builtin_amdgcn_readfirstlane(past ? __ffsll(past) - 1 : some ? 63 - __clzll(some) : 0);
+        t -= of_lane(upto - sum, part);
+        left = __builtin_amdgcn_readlane(my_left, part);
+        from += part * per;
+        to = min(to, from + per);
+        __syncthreads();
+    }
+    if (wave == 0) {
+        const int its = (to - from + 63) / 64, mine = from + lane * its, end = min(to, mine + its);
+        const Sums x = sums_of<GAP>(s, row, table, mine, end, 1);
+        const int my_left = max(0, left - (int)(wave_upto((u64)x.ties) - (u64)x.ties));
+        const double sum = x.sum + min(my_left, x.ties) * tie, upto = wave_upto(sum);
+        const u64 past = __ballot(sum > 0.0 && upto > t), some = __ballot(sum > 0.0);
+        const int who = past ? __ffsll(past) - 1 : some ? 63 - __clzll(some) : 0;
+        if (lane == who) {
+            double at = upto - sum, share = 0.0;
+            int index = 0, ties = 0;
+            bool done = false;
+            each(row, mine, end, 1, [&](const float (&v)[T::kPer], int i0) {
+                for (int e = 0; e < T::kPer; ++e) {
+                    const int order = order_of<T>(v[e]);
+                    const bool tied = order == table.upto && ties < my_left;
+                    const double w = tied ? tie : table.template of<GAP>(s, order, v[e]);
+                    ties += tied;
+                    if (!done && w > 0.0) {
+                        index = i0 + e;
+                        share = w;
+                        at += w;
+                        done = at > t;
+                    }
+                }
+            });
+            all_of.found = index;
+            all_of.share = share / total;
+        }
+    }
+    __syncthreads();
+}
+
+// The token and its share, by values; false where a count does not fit 16 bits, or
+// infinities or no tokens are there.
+template <class T>
+__device__ __noinline__ bool by_values(Row<T> row, Settings set, Answer &answer) {
+    Lds &all_of = lds();
+    Values &s = all_of.values;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    for (int i = tid; i < kValues / 8; i += kThreads) ((u32x4 *)s.counts)[i] = u32x4{0, 0, 0, 0};
+    if (tid == 0) all_of.found = 0;
+    __syncthreads();
+    int tokens = 0;
+    each(row, tid, row.pieces, kThreads, [&](const float (&v)[T::kPer], int) {
+#pragma unroll
+        for (int e = 0; e < T::kPer; ++e)
+            if (v[e] > -INFINITY) {
+                const uint32_t bits = T::bits(v[e] + 0.0f);  // -0 is 0
+                atomicAdd(&s.counts[bits >> 1], bits & 1 ? 0x10000u : 1u);
+                ++tokens;
+            }
+    });
+    tokens = (int)wave_add((u64)tokens);
+    if (lane == 0) atomicAdd(&all_of.found, tokens);
+    __syncthreads();
+    // a thread's stretch: its tokens.  (A count that has passed 65535 makes the sum of all less than it should be.)
+    const int start = (tid < kStretches / 2 ? kStretches / 2 - 1 - tid : tid) * (kStretch / 8);
+    int count = 0;
+    for (int i = 0; i < kStretch / 8; ++i) {
+        const u32x4 x = ((const u32x4 *)s.counts)[start + (i + tid) % (kStretch / 8)];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) count += (int)(x[e] & 0xffff) + (int)(x[e] >> 16);
+    }
+    u64 found;
+    const int at = (int)(block_upto((u64)(count > 0) << 32 | (uint32_t)count, all_of.whole, found) >> 32);
+    const int n = (int)(found >> 32);
+    if (count > 0) s.num[at - 1] = count, s.first[at - 1] = tid * kStretch;
+    __syncthreads();
+    if (n == 0 || (int)(uint32_t)found != all_of.found || ((const uint16_t *)s.counts)[T::kInfinity] > 0) return false;
+    const int top = s.first[0] + __ffsll(__ballot(((const uint16_t *)s.counts)[turned(s.first[0] + lane)] > 0)) - 1;
+    const Weight weight = weight_of(set, T::of_bits(turned(top)));
+    for (int i = wave; i < n; i += kWaves) {
+        double w;
+        value_in<T>(s, weight, i, count, w);
+        const double sum = wave_add(count * w);
+        if (lane == 0) s.sum[i] = sum;
+    }
+    __syncthreads();
+    if (wave == 0) {
+        const Kept x = cuts_of<T>(s, set, weight, row.V, n);
+        if (lane == 0) all_of.counts[0] = x.upto, all_of.counts[1] = x.need;
+    }
+    __syncthreads();
+    const Kept kept = {all_of.counts[0], all_of.counts[1]};
+    const Table<T> table(weight, top, kept.upto);
+    table.fill(s);
+    const double tie = weight(T::of_bits(turned(kept.upto)));
+    __syncthreads();
+    if (table.gap) token_by_table<true>(all_of, row, table, tie, kept.need, set.u);
+    else token_by_table<false>(all_of, row, table, tie, kept.need, set.u);
+    answer = {all_of.found, all_of.share};
+    return true;
+}
+
 // SLICED: the launches above have gone before.
 template <class T, bool SLICED>
 __global__ __launch_bounds__(kThreads) void k_sample(SampleLaunch a) {
@@ -1152,10 +1460,25 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleLaunch a) {
     clear_bins(s);
     __syncthreads();
 
-    u64 first, low;
+    Answer x;
+    bool sliced = SLICED;  // not where by_values has not been the way after all
+    if constexpr (T::kBytes == 2)
+        if (goes_by_values<T>(set, row.V)) {
+            if (by_values(row, set, x)) {
+                answer(x.token, x.share);
+                return;
+            }
+            sliced = false;
+            __syncthreads();
+            clear_bins(s);
+            __syncthreads();
+        }
+
+    u64 first = 0, low = 0;
     Mine<SLICED ? kSlices : 1> mine;
-    if constexpr (SLICED) tops_of(a, r, first, low, mine);
-    else block_range(s, best_of(row, 0, row.pieces, mine.best[0]), first, low);
+    if constexpr (SLICED)
+        if (sliced) tops_of(a, r, first, low, mine);
+    if (!sliced) block_range(s, best_of(row, 0, row.pieces, mine.best[0]), first, low);
     if (first == 0) {  // nothing to choose from
         answer(-1, 0.0);
         return;
@@ -1178,11 +1501,10 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleLaunch a) {
     bool known = false;        // s.real has the sums of the sixteenths
     Part part = {0, 0, 0.0};   // or the part that the token lies in is known
     double whole = 0.0;
-    Answer x;
     if (nucleus) {
         if constexpr (SLICED) {
-            const int lane = tid & 63, cut = a.cuts[r];
-            whole = a.wholes[r];
+            const int lane = tid & 63, cut = sliced ? a.cuts[r] : -1;
+            if (sliced) whole = a.wholes[r];
             if (cut >= 0) {
                 const double over = lane < a.slices ? a.over[r * a.slices + lane] : 0.0;
                 double sum = tid < a.slices * kWaves ? a.kept[(int64_t)r * a.slices * kWaves + tid] : 0.0;
@@ -1235,7 +1557,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleLaunch a) {
         int n = 0;
         float bottom = -3.402823466e38f;
         if constexpr (SLICED) {
-            n = lists_of(s, a, r);
+            n = sliced ? lists_of(s, a, r) : kMany;
             if (n < kMany && n > 0) bottom = logit_of(block_bottom(s, n));
         } else {
             bottom = list_bottom(s, set, top, low, small_k, mine);
@@ -1286,7 +1608,9 @@ namespace {
 template <class T>
 void go(SampleLaunch a, void *ws, hipStream_t s) {
     const dim3 block(kThreads);
-    a.slices = sample_slices(a.rows, a.vocab);
+    const bool by_values = !a.temperature && !a.top_k && !a.top_p &&
+                           by_values_pays<T>(a.temperature_all, a.top_k_all, a.top_p_all, a.vocab);
+    a.slices = by_values ? 1 : sample_slices(a.rows, a.vocab);
     if (a.slices == 1) {
         hipLaunchKernelGGL((k_sample<T, false>), dim3((unsigned)a.rows), block, 0, s, a);
         return;

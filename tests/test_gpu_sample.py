@@ -134,6 +134,42 @@ def test_layouts():
     assert fate.fate_sample(torch.empty(0, 9, device="cuda"), torch.empty(0, device="cuda"))[0].shape == (0,)
 
 
+def few_values(kind, R, V, dtype, seed):
+    gen = torch.Generator().manual_seed(seed)
+    x = torch.randn(R, V, generator=gen)
+    if kind == "wide":  # more values than a table of weights holds, on both sides of zero
+        x = torch.sign(x) * torch.exp2(torch.rand(R, V, generator=gen) * (60 if dtype == BF else 20) - (50 if dtype == BF else 12))
+    elif kind == "zeros":
+        x = torch.where(x.abs() < 1.2, torch.copysign(torch.zeros(()), torch.randn(R, V, generator=gen)), x)
+    elif kind == "tiny":
+        x *= 1e-30 if dtype == BF else 1e-6
+    elif kind == "below zero":
+        x = x * 2 - 60
+    elif kind == "holes":
+        x[torch.rand(R, V, generator=gen) < 0.3] = -float("inf")
+        x[torch.rand(R, V, generator=gen) < 0.3] = float("nan")
+    elif kind == "infinite":
+        x[::2, ::max(1, V // 3)] = float("inf")
+        x[1, :] = -float("inf")
+    elif kind == "crowded":  # one value more often than 16 bits count
+        x[:, :V - V // 8] = 0.75
+    return x.to(dtype)
+
+
+@pytest.mark.parametrize("kind", ["plain", "wide", "zeros", "tiny", "below zero", "holes", "infinite", "crowded"])
+@pytest.mark.parametrize("V", [8192, 16384, 16391, 100003, 131072])
+@pytest.mark.parametrize("dtype", [BF, HF], ids=["bf16", "f16"])
+def test_few_values(dtype, V, kind):
+    """Cuts among the values of 16-bit logits, in calls of one setting and, of long rows too, of a setting for each row."""
+    seed = V + len(kind)
+    x, u = few_values(kind, 6, V, dtype, seed), [0.0, LAST] + uniform(4, seed)
+    for filters in (dict(top_p=0.9), dict(top_k=257), dict(top_k=V - 1, top_p=0.5), dict(top_k=V // 3, min_p=0.9), dict(top_p=0.97, min_p=0.02),
+                    dict(top_p=0.999, temperature=50.0), dict(top_p=0.5, temperature=1e-4), dict(top_p=1e-6), dict(top_k=V // 2, temperature=1e30)):
+        check(x, u, **filters)
+    check(x, u, temperature=[1.0, 0.5, 0.0, 3.0, 1.0, 9.0], top_k=[0, 3000, 5, 0, V - 5, 0], top_p=[0.9, 0.8, 0.7, 1.0, 1.0, 0.999],
+          min_p=[0.0, 0.0, 0.1, 0.0, 0.2, 0.0])
+
+
 def test_more_rows_than_the_chip_runs():
     R = 3001
     check(logits_of(R, 70, FF, 0), uniform(R, 0), top_p=0.9)
