@@ -69,7 +69,7 @@ struct Lds {
         struct {
             u64 list[kWaves * kOwn];
             u64 hist[kBins];
-            Ranked ranked[kRanked + 8];
+            Ranked ranked[kRanked];
         };
         Values values;
     };
@@ -404,7 +404,7 @@ struct Part {
 };
 
 // The lowest index at which the sums of size(logit, index) exceed target(sum of
-// all), or the last of some size if rounding leaves none.  `known`: s.real has
+// all), or the last of some size if rounding leaves none; its size in s.share.  `known`: s.real has
 // the sums of the sixteenths; `part`: of these or other parts of the row, the one
 // that it lies in, found already.
 template <class T, class Size, class Target>
@@ -426,51 +426,52 @@ __device__ __forceinline__ int index_at(Lds &s, const Row<T> &row, bool known, c
             if (lane == 0) s.real[w] = sum;
             __syncthreads();
         }
+        const double sum = lane < kWaves ? s.real[lane] : 0.0, upto = wave_upto(sum);
         if (level == 0) {
-            total = 0.0;
-            for (int i = 0; i < kWaves; ++i) total += s.real[i];
+            total = of_lane(upto, 63);
             t = target(total);
         }
-        double upto = 0.0, rest = t;
-        int at = 0;
-        for (int i = 0; i < kWaves; ++i) {
-            if (s.real[i] > 0.0) {
-                at = i;
-                rest = t - upto;
-            }
-            upto += s.real[i];
-            if (upto > t) break;
-        }
-        t = rest;
+        const u64 past = __ballot(sum > 0.0 && upto > t), some = __ballot(sum > 0.0);
+        const int at = __builtin_amdgcn_readfirstlane(past ? __ffsll(past) - 1 : some ? 63 - __clzll(some) : 0);
+        t -= of_lane(upto - sum, at);
         from += at * n;
         to = min(to, from + n);
         __syncthreads();
     }
     if (w == 0) {
         const int n = (to - from + 63) / 64, mine = from + lane * n, end = min(to, mine + n);
-        double sum = 0.0;
+        double sum = 0.0, x[T::kPer] = {};  // x: sizes of the lane's last piece, its only one where there are few
+        int x0 = 0;
         each(row, mine, end, 1, [&](const float (&v)[T::kPer], int i0) {
+            x0 = i0;
 #pragma unroll
-            for (int e = 0; e < T::kPer; ++e) sum += size(v[e], i0 + e);
+            for (int e = 0; e < T::kPer; ++e) sum += x[e] = size(v[e], i0 + e);
         });
         const double upto = wave_upto(sum);
         const u64 past = __ballot(sum > 0.0 && upto > t), some = __ballot(sum > 0.0);
         const int who = past ? __ffsll(past) - 1 : some ? 63 - __clzll(some) : 0;
         if (lane == who) {
-            double at = upto - sum;
+            double at = upto - sum, its = 0.0;
             int index = 0;
             bool done = false;
-            each(row, mine, end, 1, [&](const float (&v)[T::kPer], int i0) {
-                for (int e = 0; e < T::kPer; ++e) {
-                    const double x = size(v[e], i0 + e);
-                    if (!done && x > 0.0) {
-                        index = i0 + e;
-                        at += x;
-                        done = at > t;
-                    }
+            auto look = [&](double y, int i) __attribute__((always_inline)) {
+                if (!done && y > 0.0) {
+                    index = i;
+                    its = y;
+                    at += y;
+                    done = at > t;
                 }
-            });
+            };
+            if (n == 1) {
+#pragma unroll
+                for (int e = 0; e < T::kPer; ++e) look(x[e], x0 + e);
+            } else {
+                each(row, mine, end, 1, [&](const float (&v)[T::kPer], int i0) {
+                    for (int e = 0; e < T::kPer; ++e) look(size(v[e], i0 + e), i0 + e);
+                });
+            }
             s.found = index;
+            s.share = its;
         }
     }
     __syncthreads();
@@ -540,36 +541,57 @@ __device__ __forceinline__ int gather(const Row<T> &row, int from, int to, int n
     return fits ? n : kMany;
 }
 
+// Of this thread's one of the n <= kRanked entries of s.ranked: how many are
+// before it, the sum of their weights, and how many have lower indices.  Where n
+// is small several neighbouring threads share an entry, `owns` in the first.
+struct Rank {
+    int entry, rank, place;
+    bool owns;
+    double before;
+};
+template <int CTRL>
+__device__ __forceinline__ void add_moved(Rank &x) {
+    x.rank += moved32<CTRL, 0xF>(x.rank);
+    x.place += moved32<CTRL, 0xF>(x.place);
+    x.before += moved<CTRL, 0xF>(x.before);
+}
+__device__ __forceinline__ Rank rank_of(const Lds &s, int n) {
+    const int share = n > 256 ? 1 : n > 128 ? 2 : n > 64 ? 3 : 4;  // 2 to 16 threads
+    const int tid = threadIdx.x, part = tid & ((1 << share) - 1);
+    Rank x = {tid >> share, 0, 0, part == 0 && tid >> share < n, 0.0};
+    const u64 mine = x.entry < n ? s.ranked[x.entry].entry : 0;
+#pragma unroll 4
+    for (int i = part; i < n; i += 1 << share) {
+        const u64 y = s.ranked[i].entry;
+        const double z = s.ranked[i].weight;
+        x.rank += y > mine;
+        x.place += (uint32_t)y > (uint32_t)mine;
+        x.before += y > mine ? z : 0.0;
+    }
+    add_moved<0xB1>(x);  // neighbours, pairs of them, then the mirror images of quads and of eights
+    if (share > 1) add_moved<0x4E>(x);
+    if (share > 2) add_moved<0x141>(x);
+    if (share > 3) add_moved<0x140>(x);
+    return x;
+}
+
 // The token among the list's n <= kRanked, in any order, which hold all that may
 // be kept: each is ranked, by the order of the cuts and by its index, against all.
 // top_p is of `whole`, or, if that is 0, of what top_k leaves.
 __device__ __noinline__ Answer from_short(Settings set, Weight weight, int n, double whole) {
     Lds &s = lds();
     const int tid = threadIdx.x;
-    const u64 x = tid < n ? s.list[tid] : 0;
-    const double w = tid < n ? weight(logit_of(x)) : 0.0;
-    if (tid < n + 8 && tid < kRanked + 8) s.ranked[tid].entry = x, s.ranked[tid].weight = w;
+    if (tid < n) s.ranked[tid].entry = s.list[tid], s.ranked[tid].weight = weight(logit_of(s.list[tid]));
     __syncthreads();
-    int rank = 0, place = 0;
-    double before = 0.0, sum, total;
-    if (tid < n)
-        for (int i = 0; i < n; i += 8) {  // (past n lie zeros, whose indices are the largest)
-            u64 y[8];
-            double z[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = s.ranked[i + e].entry, z[e] = s.ranked[i + e].weight;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                rank += y[e] > x;
-                place += (uint32_t)y[e] > (uint32_t)x;
-                before += y[e] > x ? z[e] : 0.0;
-            }
-        }
-    const bool of_k = tid < n && (!set.top_k || rank < set.top_k);
+    const Rank at = rank_of(s, n);
+    const u64 x = at.owns ? s.ranked[at.entry].entry : 0;
+    const double w = at.owns ? s.ranked[at.entry].weight : 0.0;
+    double sum, total;
+    const bool of_k = at.owns && (!set.top_k || at.rank < set.top_k);
     block_upto(of_k ? w : 0.0, s.real, sum);  // (its barriers: the entries have been read)
     const double aim = set.top_p * (whole > 0.0 ? whole : sum);
-    const bool kept = of_k && (set.top_p >= 1.0 || before < aim || rank == 0) && w >= set.min_p;
-    if (tid < n) s.ranked[place].entry = x, s.ranked[place].weight = kept ? w : 0.0;
+    const bool kept = of_k && (set.top_p >= 1.0 || at.before < aim || at.rank == 0) && w >= set.min_p;
+    if (at.owns) s.ranked[at.place].entry = x, s.ranked[at.place].weight = kept ? w : 0.0;
     __syncthreads();
     // by rising index, sums up to each
     const double mine = tid < n ? s.ranked[tid].weight : 0.0, upto = block_upto(mine, s.real, total);
@@ -608,26 +630,13 @@ __device__ __noinline__ u64 last_of_list(Weight weight, int n, Bins bins, int cu
             ++at;
         }
     }
-    if (tid < 8) s.ranked[m + tid].entry = 0;
     __syncthreads();
-    int rank = 0;
-    double before = above, sum;
-    const u64 x = tid < m ? s.ranked[tid].entry : 0;
-    if (tid < m) {
-        for (int i = 0; i < m; i += 8) {
-            u64 y[8];
-            double z[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = s.ranked[i + e].entry, z[e] = s.ranked[i + e].weight;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                rank += y[e] > x;
-                before += y[e] > x ? z[e] : 0.0;
-            }
-        }
-    }
-    block_upto(tid < m ? s.ranked[tid].weight : 0.0, s.real, sum);
-    const bool kept = tid < m && (most ? sure + rank < most : before < aim || sure + rank == 0);
+    const Rank its = rank_of(s, m);
+    const u64 x = its.owns ? s.ranked[its.entry].entry : 0;
+    const double before = above + its.before;
+    double sum;
+    block_upto(its.owns ? s.ranked[its.entry].weight : 0.0, s.real, sum);
+    const bool kept = its.owns && (most ? sure + its.rank < most : before < aim || sure + its.rank == 0);
     u64 n_kept;
     block_upto((u64)kept, s.whole, n_kept);
     if (n_kept == 0 || (!most && (int)n_kept == m && above + sum < aim)) return 0;
@@ -752,7 +761,7 @@ __device__ __noinline__ Answer token_at(Row<T> row, Settings set, Weight weight,
         const double x = weight(kept.keeps(v, i) ? v : __builtin_nanf(""));
         return x < set.min_p ? 0.0 : x;
     }, [&](double all) { return set.u * all; }, total);
-    return {token, weight(T::at(row.data, token)) / total};
+    return {token, s.share / total};
 }
 
 // The tokens at +infinity share the row, and nothing else counts.
@@ -791,22 +800,13 @@ __device__ __noinline__ u64 last_in_bin(Settings set, Weight weight, int n, doub
     Lds &s = lds();
     const int tid = threadIdx.x;
     if (n > kRanked) return 0;
-    const u64 x = tid < n ? s.list[tid] : 0;
-    const double w = x ? weight(logit_of(x)) : 0.0;
-    if (tid < kRanked + 8) s.ranked[tid].entry = x, s.ranked[tid].weight = w;
+    if (tid < n) s.ranked[tid].entry = s.list[tid], s.ranked[tid].weight = weight(logit_of(s.list[tid]));
     __syncthreads();
-    double before = above, in_bin;
-    if (tid < n)
-        for (int i = 0; i < n; i += 8) {
-            u64 y[8];
-            double z[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = s.ranked[i + e].entry, z[e] = s.ranked[i + e].weight;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) before += y[e] > x ? z[e] : 0.0;
-        }
-    block_upto(w, s.real, in_bin);
-    // kept while less than top_p lies before; a maximum, so that it is a stretch from the start whatever rounding does
+    const Rank at = rank_of(s, n);
+    const u64 x = at.owns ? s.ranked[at.entry].entry : 0;
+    const double before = above + at.before;
+    double in_bin;
+    block_upto(at.owns ? s.ranked[at.entry].weight : 0.0, s.real, in_bin);
     const double aim = set.top_p * whole;
     const bool keeps = x && before < aim;
     const u64 last = ~block_max(keeps ? ~x : 0, s), none = ~0ull;
@@ -900,10 +900,10 @@ struct Mine {
 // threads' largest logits give a bound of S from below.
 template <int N>
 __device__ __forceinline__ float nucleus_bottom(Lds &s, const Settings &set, const Weight &weight, float top, int V,
-                                                const Mine<N> &mine) {
+                                                const Mine<N> &mine, int slices) {
     double low = 0.0, all;
 #pragma nounroll
-    for (int i = 0; i < N; ++i) {  // (0 of -infinity)
+    for (int i = 0; i < slices; ++i) {  // (0 of -infinity)
         float best = mine.best[0];
 #pragma unroll
         for (int j = 1; j < N; ++j) best = i == j ? mine.best[j] : best;
@@ -1022,7 +1022,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_sums(SampleLaunch a) {
     const Weight weight = weight_of(set, top);
     const int n = slice_of(row, a.slices), from = g * n, to = min(row.pieces, from + n);
     if (nucleus) {
-        const float bottom = nucleus_bottom(s, set, weight, top, row.V, mine);
+        const float bottom = nucleus_bottom(s, set, weight, top, row.V, mine, a.slices);
         double whole;
         block_upto(sum_by_bins(s, row, from, to, weight, Bins(top, bottom), bottom), s.real, whole);
         if (tid == 0) a.parts[(int64_t)blockIdx.x * kWaves] = whole;
@@ -1114,7 +1114,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_lists(SampleLaunch a) {
     const int n = slice_of(row, a.slices), from = g * n, to = min(row.pieces, from + n), n16 = (n + kWaves - 1) / kWaves;
     int count;
     if (nucleus) {
-        const float bottom = nucleus_bottom(s, set, weight, top, row.V, mine);
+        const float bottom = nucleus_bottom(s, set, weight, top, row.V, mine, a.slices);
         const Bins bins(top, bottom);
         double whole, over = 0.0, part = 0.0, all;
         const int cut = cut_of_slices(s, a, r, set, bins, whole);
@@ -1529,7 +1529,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleLaunch a) {
                 }
             }
         } else {
-            const float bottom = nucleus_bottom(s, set, weight, top, row.V, mine);
+            const float bottom = nucleus_bottom(s, set, weight, top, row.V, mine, a.slices);
             const Bins bins(top, bottom);
             block_upto(sum_by_bins(s, row, 0, row.pieces, weight, bins, bottom), s.real, whole);
             const int bits = bits_of(row.V);
