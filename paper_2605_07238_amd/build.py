@@ -11,6 +11,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -73,10 +74,16 @@ def build(verbose: bool = False) -> str:
     objdir = os.path.join(HERE, "_build")
     os.makedirs(objdir, exist_ok=True)
     tmp = LIB + ".tmp%d" % os.getpid()
-    for cmd in commands(tmp, objdir):
+    *compiles, link = commands(tmp, objdir)
+
+    def run(cmd):
         if verbose:
             print(" ".join(cmd), flush=True)
         subprocess.run(cmd, check=True)
+
+    with ThreadPoolExecutor(int(os.environ.get("MAX_JOBS", 0)) or min(8, os.cpu_count() or 1)) as pool:
+        list(pool.map(run, compiles))
+    run(link)
     os.replace(tmp, LIB)
     return LIB
 
