@@ -1556,19 +1556,20 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleLaunch a) {
     } else if (small_k || only_min_p(set, row.V)) {
         int n = 0;
         float bottom = -3.402823466e38f;
+        const bool in_order = SLICED || (small_k && set.top_k > kRanked);  // as many at least are listed, too many to be ranked
         if constexpr (SLICED) {
             n = sliced ? lists_of(s, a, r) : kMany;
             if (n < kMany && n > 0) bottom = logit_of(block_bottom(s, n));
         } else {
             bottom = list_bottom(s, set, top, low, small_k, mine);
-            n = gather(row, 0, row.pieces, sixteenth(row), false, [&](float v) { return v >= bottom; });
+            n = gather(row, 0, row.pieces, sixteenth(row), in_order, [&](float v) { return v >= bottom; });
         }
         if (n <= kRanked) {
             x = from_short(set, weight, n, 0.0);
             answer(x.token, x.share);
             return;
         }
-        if (!SLICED && n < kMany) n = gather(row, 0, row.pieces, sixteenth(row), true, [&](float v) { return v >= bottom; });
+        if (!in_order && n < kMany) n = gather(row, 0, row.pieces, sixteenth(row), true, [&](float v) { return v >= bottom; });
         const Bins bins(top, bottom);
         if (n < kMany && (small_k ? bins.good() && from_list_of_k(set, weight, n, bins, x) : (x = from_list(set, weight, n, 1), true))) {
             answer(x.token, x.share);
