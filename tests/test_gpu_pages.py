@@ -138,7 +138,7 @@ def trim(keep, kv, pages, free, n_free, P, in_place=False):
 
 
 @pytest.mark.parametrize("in_place", [False, True])
-@pytest.mark.parametrize("B,P,most", [(1, 16, 100), (64, 16, 4096), (65, 1, 300), (511, 8, 100), (513, 8, 100), (1025, 16, 90),
+@pytest.mark.parametrize("B,P,most", [(1, 16, 100), (64, 16, 4096), (65, 1, 300), (255, 8, 1500), (256, 4, 1100), (257, 4, 1100), (511, 8, 100), (513, 8, 100), (1025, 16, 90),
                                       (5000, 4, 60), (3, 16, 100000)], ids=str)
 def test_trim(B, P, most, in_place):
     rng = np.random.default_rng(B)
