@@ -965,7 +965,7 @@ __device__ __forceinline__ void block_range(Lds &s, u64 mine, u64 &top, u64 &low
 
 // Calls of few rows: each row's readings by `slices` workgroups, so that the chip
 // is filled, in a launch each; k_sample then takes what they found.  64 rows of
-// 131072 with top_p 0.9: 117 us by one workgroup a row, 67 so.
+// 131072 with top_p 0.9: 100 us by one workgroup a row, 63 so.
 template <class T>
 __device__ __forceinline__ int slice_of(const Row<T> &row, int slices) { return (row.pieces + slices - 1) / slices; }
 
@@ -1588,8 +1588,11 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleLaunch a) {
 
 // Workgroups of a row's slices: calls of up to 128 rows by as many as the chip
 // runs at once, of 32768 logits each at least.  The three launches more cost some
-// 10 us: for 64 rows of 32768 top-p 0.9 46 us by one workgroup a row and 59 by four,
-// for one of 50001 38 and 48, and top-k 50 18 and 24.
+// 10 us.  By one workgroup a row and by slices of 32768, us, 1 and 64 rows:
+//   131072  top-p 0.9 93 and 51, 100 and 63; no cut 41 and 23, 44 and 30; top-k 1000 42 and 32, 45 and 36; top-k 50 21 and 23,
+//           23 and 28; min-p 18 and 21, 21 and 26
+//   64 rows of 32768 by one and by two  top-p 0.9 42 and 43, no cut 17 and 22, top-k 50 14 and 24
+// Where the host knows that a call's rows list few tokens at once, it is one.
 int sample_slices(int64_t rows, int64_t vocab) {
     const int64_t fill = rows > 0 ? 256 / rows : 1, most = vocab / 32768;
     const int64_t n = fill < most ? fill : most;
@@ -1611,7 +1614,11 @@ void go(SampleLaunch a, void *ws, hipStream_t s) {
     const dim3 block(kThreads);
     const bool by_values = !a.temperature && !a.top_k && !a.top_p &&
                            by_values_pays<T>(a.temperature_all, a.top_k_all, a.top_p_all, a.vocab);
-    a.slices = by_values ? 1 : sample_slices(a.rows, a.vocab);
+    const bool largest = !a.temperature && a.temperature_all == 0.0f;
+    const bool small_k = !a.top_k && a.top_k_all > 0 && a.top_k_all <= 256;
+    const bool only_min_p = !a.top_k && !a.top_p && !a.min_p && a.top_k_all == 0 && a.top_p_all >= 1.0f && a.min_p_all > 0.0f;
+    const bool listed = a.vocab <= 1 << 17 && (largest || small_k || only_min_p);
+    a.slices = by_values || listed ? 1 : sample_slices(a.rows, a.vocab);
     if (a.slices == 1) {
         hipLaunchKernelGGL((k_sample<T, false>), dim3((unsigned)a.rows), block, 0, s, a);
         return;
