@@ -557,6 +557,12 @@ fate_status_t fate_place_baseline_device(const fate_dags_t *dags, const fate_sta
  *   fate_kv_append    stores new keys and values, rotated to their positions
  *   fate_attn_paged   new tokens (chunks, a few, one) over their sequences' pages
  *   fate_attn_prompt  whole prompts, packed, causal, without a cache
+ * and, around them, what keeps a step of answers on the device:
+ *   fate_kv_reserve, fate_kv_trim       pages for new tokens, and given up again
+ *   fate_kv_append_axes                 positions on several axes
+ *   fate_attn_paged_shaped, fate_attn_prompt_shaped  capped and biased scores,
+ *                                       documents, windows, prefixes
+ *   fate_sample                         a token from each row of logits
  * Forward only: there is no backward pass.  All arrays are device memory unless said otherwise; every
  * call is enqueued on `stream`, never synchronises and can be captured.  The
  * host checks what it can see (sizes, types, strides, alignment); errors in
@@ -725,7 +731,7 @@ typedef struct {
 /* fate_attn_paged_shaped, fate_attn_prompt_shaped: fate_attn_paged (its
  * workspace, its size and all else alike) and fate_attn_prompt with the scores
  * so shaped.  Keys that no row of a row tile sees are not read: the cost goes
- * with what is seen.  A capped score is off by some 2^-22 of the cap.
+ * with what is seen.  A capped score is off by some 2^-21 of the cap.
  * Errors: as those, and EINVAL (null scores, cap negative or not finite, or so
  * far from scale that their quotient leaves float32, alignment). */
 fate_status_t fate_attn_paged_shaped(const fate_heads_t *heads, const fate_seqs_t *seqs, const fate_rows_t *q,

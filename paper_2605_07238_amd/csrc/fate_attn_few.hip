@@ -19,6 +19,12 @@
 // two workgroups a compute unit hold 128 KB of loads under way (head size 128;
 // the shares' number: plan_paged).
 //
+// Shaped scores (SHAPED): a tile's blocks are those that hold a key some row
+// sees, numbered through, and shares are cut over these.  64 answers over 128 to
+// 16384 keys, each behind a window of 4096, 32 heads of 128 over 8, capped: 106
+// and 6.2 us for the join, 4.9 TB/s of the keys within the windows (114 with no
+// cap; 178 where all keys are seen).
+//
 // k_attn_join: the parts of a row tile, o = sum 2^(m_i - M) o_i / sum 2^(m_i - M) l_i.
 #include "fate_attn.h"
 

@@ -7,7 +7,12 @@ fallback: if the library is missing or a call fails, an exception is raised.
 
 Entry points mirror the C names: :func:`fate_pack_dags`,
 :func:`fate_pack_state`, :func:`fate_score_frontier`, :func:`fate_topk`, plus
-the host-only :func:`fate_layout_dags` / :func:`fate_layout_state`.
+the host-only :func:`fate_layout_dags` / :func:`fate_layout_state`.  The calls
+that a device makes for a plan's stages are :func:`fate_kv_reserve`,
+:func:`fate_kv_append` (:func:`fate_kv_append_axes`), :func:`fate_attn_paged` and
+:func:`fate_attn_prompt` (their scores shaped: :func:`fate_attn_paged_shaped`,
+:func:`fate_attn_prompt_shaped`), :func:`fate_sample` and :func:`fate_kv_trim`;
+a whole step of them can be captured in a graph.
 """
 
 from __future__ import annotations
