@@ -1570,6 +1570,8 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleLaunch a) {
             return;
         }
         if (!in_order && n < kMany) n = gather(row, 0, row.pieces, sixteenth(row), true, [&](float v) { return v >= bottom; });
+        // (of few threads' largest logits no bound follows: the bins go by the least that is listed)
+        if (!SLICED && n < kMany && small_k && bottom == -3.402823466e38f) bottom = logit_of(block_bottom(s, n));
         const Bins bins(top, bottom);
         if (n < kMany && (small_k ? bins.good() && from_list_of_k(set, weight, n, bins, x) : (x = from_list(set, weight, n, 1), true))) {
             answer(x.token, x.share);
