@@ -134,7 +134,10 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
     const int w_most = SHAPED ? wave.most : wrow0 < rows ? min(p.L, max(0, (min(wrow0 + 32, rows) - 1) / a.G + first)) : 0;
     const int w_least = wrow0 < rows ? max(0, min(p.L, wrow0 / a.G + first)) : 0;
     const float slope = SHAPED && a.slopes && live ? a.slopes[qh] * kLog2e : 0.0f;
-    const float unit = SHAPED && (a.slopes || a.cap_log2 != 0.0f) ? 1.0f : a.scale_log2;  // of a score, in log2
+    // a score in log2: unit times what `shape` leaves, and zero
+    const bool caps = SHAPED && a.cap_log2 != 0.0f && !a.cap_wide && !a.slopes;
+    const float unit = caps ? 2.0f * a.cap_log2 : SHAPED && (a.slopes || a.cap_log2 != 0.0f) ? 1.0f : a.scale_log2;
+    const float zero = caps ? a.cap_log2 : 0.0f;
 
     // queries: the first product's second operand, column = row of the tile
     x8 q[D / 16];
@@ -273,9 +276,15 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
         }
     };
 
-    // Scores as the call shapes them, in log2: capped, then less slope times distance.
+    // Scores as the call shapes them: capped, then less slope times distance.  Of a cap alone what is left is
+    // -1 / (1 + e^2x), cap tanh x = cap + 2 cap times that, which the weights' exponents take in.
     auto shape = [&](f32x16 (&s)[2], int key) __attribute__((always_inline)) {
-        if (a.cap_wide) {
+        if (caps) {
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) s[kt][j] = __builtin_amdgcn_rcpf(-1.0f - exp2_fast(s[kt][j] * a.cap_in));
+        } else if (a.cap_wide) {
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
@@ -352,7 +361,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
             for (int j = 1; j < 16; ++j) top = fmaxf(top, cur[0][j]);
 #pragma unroll
             for (int j = 0; j < 16; ++j) top = fmaxf(top, cur[1][j]);
-            top = fmaxf(both_halves_max(top) * unit, kLowest);
+            top = both_halves_max(top);
+            top = fmaxf(SHAPED ? __builtin_fmaf(top, unit, zero) : top * unit, kLowest);
             if (__any(top > m + (kLag + T::kLift))) {
                 const float next = fmaxf(m, top - T::kLift), f = exp2_fast(m - next);
                 m = next;
@@ -363,12 +373,13 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
                     for (int j = 0; j < 16; ++j) o[i][j] *= f;
             }
             scores(nxt, (B ^ 1) * kTile);  // past the last tile: of nothing, and not used
+            const float shift = SHAPED ? zero - m : -m;
             x8 pr[4];                      // weights of keys 16 i + 8 (e / 4) + 4 half + e % 4
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float x = exp2_fast(__builtin_fmaf(cur[i / 2][8 * (i % 2) + e], unit, -m));
+                    const float x = exp2_fast(__builtin_fmaf(cur[i / 2][8 * (i % 2) + e], unit, shift));
                     l += x;
                     pr[i][e] = (el)x;
                 }
