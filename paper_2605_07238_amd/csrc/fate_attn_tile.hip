@@ -35,12 +35,13 @@
 //
 // Shaped scores (SHAPED) walk over the tiles that some row sees only: those of the
 // prefix, then those from the workgroup's first key on.  18261 tokens in 16
-// prompts, 32 heads of 128 over 8, take 388 us with no shape, 470 with a cap, 401
+// prompts, 32 heads of 128 over 8, take 388 us with no shape, 458 with a cap, 401
 // with a bias by distance; one row of 16384 tokens in documents of 100 to 4000,
 // behind 200 keys that all see, 390 (326 without those), causally 2090.  A cap
-// costs 28 cycles of the vector units a score, which run beside the matrix cores
-// but little: a wave's step of 64 keys takes 3099 cycles, of which these work 1830
-// and the matrix cores 1027 (2467, 1115 and 1027 with no cap).
+// costs 24 cycles of the vector units a score, which run beside the matrix cores
+// but little: with 28, before its last step went into the weights' exponents, a
+// wave's step of 64 keys took 3099 cycles, of which these worked 1830 and the
+// matrix cores 1027 (2467, 1115 and 1027 with no cap).
 #include <type_traits>
 
 #include "fate_attn.h"
