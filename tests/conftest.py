@@ -1,3 +1,4 @@
+import gc
 import os
 import sys
 
@@ -13,3 +14,10 @@ for p in (ROOT, HERE):
 def pytest_configure(config):
     config.addinivalue_line("markers", "gpu: needs an MI355X (gfx950) and the built HIP library")
     config.addinivalue_line("markers", "slow: longer CPU test")
+
+
+def pytest_collection_finish(session):
+    """What the run has loaded lives as long as it: left out of collections, which took some 100 ms each, longer than tests
+    that look at a stream while it is busy keep it so."""
+    gc.collect()
+    gc.freeze()

@@ -11,13 +11,6 @@ pytestmark = pytest.mark.gpu
 BF, HF = torch.bfloat16, torch.float16
 
 
-@pytest.fixture(autouse=True, scope="module")
-def memory_goes_back():
-    """Cached memory in odd pieces makes a later allocation ask the driver, which waits for streams that a test keeps busy."""
-    yield
-    torch.cuda.empty_cache()
-
-
 def ints(x):
     return torch.as_tensor(np.ascontiguousarray(x), dtype=torch.int32).cuda()
 

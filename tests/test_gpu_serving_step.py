@@ -9,7 +9,7 @@ import torch
 import serve_oracle as so
 from paper_2605_07238_amd import fate
 from test_gpu_attention import compare
-from test_gpu_attention_shaped import cached, expected
+from test_gpu_shaped_attention import cached, expected
 
 pytestmark = pytest.mark.gpu
 HQ, HKV, D, P, WIDTH, N_PAGES, V, HIDDEN, WINDOW = 6, 2, 64, 16, 9, 40, 1031, 48, 37

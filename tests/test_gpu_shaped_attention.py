@@ -15,13 +15,6 @@ from test_gpu_attention import BF, HEADS, HF, LENGTHS, compare, make_paged
 pytestmark = pytest.mark.gpu
 
 
-@pytest.fixture(autouse=True, scope="module")
-def memory_goes_back():
-    """Cached memory in odd pieces makes a later allocation ask the driver, which waits for streams that a test keeps busy."""
-    yield
-    torch.cuda.empty_cache()
-
-
 def shaping(kind, new, kv, hq, rng):
     """Arguments of a call of these lengths."""
     more, first = {}, []
