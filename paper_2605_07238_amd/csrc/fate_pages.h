@@ -23,8 +23,9 @@ int launch_trim(const PagesLaunch &a, void *stream);
 // Calls of one workgroup and one launch: rows of a reserve, sequences of a trim.
 // A launch more costs the host 2 us; one workgroup needs 6.9 us for 512 rows and
 // 9.9 for 4096, of 64 sequences (8192 rows in two launches 10.3), and for trims of
-// 256 and 512 sequences 14 and 24 us, where three launches take 7.6 and the host 16.
+// 256, 512 and 1024 sequences 9, 14 and 26 us, where three launches take 7.5 to 8
+// and their host 15 (of one launch 10).
 constexpr int64_t kReserveSmall = 4096;
-constexpr int32_t kTrimSmall = 256;
+constexpr int32_t kTrimSmall = 512;
 
 }  // namespace fate

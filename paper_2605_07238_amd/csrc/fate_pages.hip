@@ -202,24 +202,26 @@ __device__ __forceinline__ Given given_by(const PagesLaunch &a, int64_t b) {
     if (kv < 0 || keep < 0 || kv > a.max_keys) return {0, -1};
     return {pages_for(min(kv, keep), a.shift), pages_for(kv, a.shift)};
 }
-// f(j, page j) for the pages, four of a lane's asked for at once.
-template <class F>
+// f(j, page j) for the pages, by LANES neighbouring threads, LOADS of each asked for at once.
+template <int LANES, int LOADS, class F>
 __device__ __forceinline__ void each_page(const PagesLaunch &a, int64_t b, Given x, F f) {
     const int32_t *const row = a.pages + b * a.pages_stride;
-    for (int j = x.left + (int)(threadIdx.x & 63); j < x.have; j += 256) {
-        int page[4];
+    for (int j = x.left + (int)(threadIdx.x & (LANES - 1)); j < x.have; j += LANES * LOADS) {
+        int page[LOADS];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) page[i] = j + 64 * i < x.have ? row[j + 64 * i] : 0;
+        for (int i = 0; i < LOADS; ++i) page[i] = j + LANES * i < x.have ? row[j + LANES * i] : 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (j + 64 * i < x.have) f(j + 64 * i, page[i]);
+        for (int i = 0; i < LOADS; ++i)
+            if (j + LANES * i < x.have) f(j + LANES * i, page[i]);
     }
 }
-// How many pages a sequence gives back, -1 if it is in error.
+// How many pages a sequence gives back, -1 if it is in error.  (All lanes of the wave come here.)
+template <int LANES, int LOADS>
 __device__ __forceinline__ int gone_of(const PagesLaunch &a, int64_t b, Given x) {
     bool bad = x.have < 0;
-    each_page(a, b, x, [&](int, int page) { bad = bad || (uint32_t)page >= (uint32_t)a.n_pages; });
-    return __any(bad) ? -1 : x.have - x.left;
+    each_page<LANES, LOADS>(a, b, x, [&](int, int page) { bad = bad || (uint32_t)page >= (uint32_t)a.n_pages; });
+    const uint64_t who = __ballot(bad) >> (threadIdx.x & 63 & -LANES);
+    return (LANES < 64 ? who & ((1ull << LANES % 64) - 1) : who) ? -1 : x.have - x.left;
 }
 
 // Of the sequences of a small call: what each gives back, and the sum up to it.
@@ -258,33 +260,36 @@ __device__ __forceinline__ void trim_lengths(const PagesLaunch &a, Scans &lds, G
     }
 }
 
-// A call of one workgroup, a wave a sequence.  The lengths are read once, by
-// threads, and pages four loads at a time: 200 sequences with up to 512 pages
-// took 14.4 us with a lane's loads one behind the other, 11.4 so.
+// A call of one workgroup, sixteen lanes a sequence.  The lengths are read once, by
+// threads, and pages eight loads at a time: 200 sequences with up to 512 pages
+// took 14.4 us by a wave each with a lane's loads one behind the other, 11.3 with
+// four at a time, 7.5 so.
 __global__ __launch_bounds__(kThreads) void k_kv_trim(PagesLaunch a) {
+    constexpr int kLanes = 16, kLoads = 8;
     __shared__ Scans lds;
     __shared__ Trimmed s;
-    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), stack = *a.n_free;
+    const int mine = threadIdx.x / kLanes, stack = *a.n_free;
     if ((int)threadIdx.x < a.B) s.given[threadIdx.x] = given_by(a, threadIdx.x);
     __syncthreads();
-    for (int b = w; b < a.B; b += kWaves) {
-        const int gone = gone_of(a, b, s.given[b]);
-        if ((threadIdx.x & 63) == 0) s.gone[b] = gone;
+    for (int at = 0; at < a.B; at += kThreads / kLanes) {
+        const int b = at + mine;
+        const int gone = gone_of<kLanes, kLoads>(a, b, b < a.B ? s.given[b] : Given{0, 0});
+        if (b < a.B && threadIdx.x % kLanes == 0) s.gone[b] = gone;
     }
     __syncthreads();
     trim_lengths(a, lds, [&](int64_t b) { return s.gone[b]; }, &s);
     __syncthreads();
-    for (int b = w; b < a.B; b += kWaves) {
+    for (int b = mine; b < a.B; b += kThreads / kLanes) {
         if (s.gone[b] <= 0) continue;
         int32_t *const to = a.free + stack + s.upto[b] - s.gone[b] - s.given[b].left;
-        each_page(a, b, s.given[b], [&](int j, int page) { to[j] = page; });
+        each_page<kLanes, kLoads>(a, b, s.given[b], [&](int j, int page) { to[j] = page; });
     }
 }
 
 // The three steps of a large call.
 __global__ __launch_bounds__(256) void k_kv_trim_counts(PagesLaunch a) {
     for (int64_t b = blockIdx.x * 4 + (threadIdx.x >> 6); b < a.B; b += gridDim.x * 4) {
-        const int gone = gone_of(a, b, given_by(a, b));
+        const int gone = gone_of<64, 4>(a, b, given_by(a, b));
         if ((threadIdx.x & 63) == 0) a.moved[b + 1] = gone;
     }
 }
@@ -297,7 +302,7 @@ __global__ __launch_bounds__(256) void k_kv_trim_pages(PagesLaunch a) {
     for (int64_t b = blockIdx.x * 4 + (threadIdx.x >> 6); b < a.B; b += gridDim.x * 4) {
         const int from = a.moved[b], n = a.moved[b + 1] - from, left = pages_for(a.kv_out[b], a.shift);
         int32_t *const to = a.free + stack + from - left;
-        if (n) each_page(a, b, {left, left + n}, [&](int j, int page) { to[j] = page; });
+        if (n) each_page<64, 4>(a, b, {left, left + n}, [&](int j, int page) { to[j] = page; });
     }
 }
 

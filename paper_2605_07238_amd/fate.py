@@ -1157,13 +1157,14 @@ def _kv_tables(counts, name, kv_len, pages, free, n_free, page_size, device) -> 
         raise ValueError("kv_len must be [B], pages [B, max_pages] and free [n_pages], got %s, %s and %s" % (
             list(kv_len.shape), list(pages.shape), list(free.shape)))
     B, width = pages.shape
-    _array(counts, name, B, int32, device)
     row, one = pages.stride()
     if pages.dtype is not int32 or pages.device != device or (one != 1 and width > 1):
         raise ValueError("pages must be int32 on %s, each row contiguous" % device)
-    return KvTables(B, width, page_size, free.shape[0], row if B > 1 else width, pages.data_ptr(),
-                    _array(free, "free", free.shape[0], int32, device), _array(n_free, "n_free", 1, int32, device),
-                    _array(kv_len, "kv_len", B, int32, device))
+    for t, its, n in ((counts, name, B), (kv_len, "kv_len", B), (free, "free", free.shape[0]), (n_free, "n_free", 1)):
+        if t.dtype is not int32 or t.device != device or t.shape != (n,) or not t.is_contiguous():
+            _array(t, its, n, int32, device)  # says what is wrong
+    return KvTables(B, width, page_size, free.shape[0], row if B > 1 else width, pages.data_ptr(), free.data_ptr(), n_free.data_ptr(),
+                    kv_len.data_ptr())
 
 
 def fate_kv_reserve(new, kv_len, pages, free, n_free, page_size: int, T: int, out: Optional[Reserved] = None, status=None,
@@ -1191,7 +1192,8 @@ def fate_kv_reserve(new, kv_len, pages, free, n_free, page_size: int, T: int, ou
         if T < 0:
             raise ValueError("T must not be negative, got %d" % T)
         n, slots = _t.empty(3 * B + 3 + T, dtype=int32, device=dev), _t.empty(T, dtype=int64, device=dev)
-        off, kv, left, taken, positions = n.split((B + 1, B, 1, B + 1, T))
+        # (whole numbers: no gradient has to follow the views)
+        off, kv, left, taken, positions = n.unsafe_split_with_sizes((B + 1, B, 1, B + 1, T))
         out = Reserved(off, kv, left, taken, slots, positions)
         at = n.data_ptr()
         where = (at, at + 4 * B + 4, at + 8 * B + 4, at + 8 * B + 8, slots.data_ptr(), at + 12 * B + 12)
@@ -1219,7 +1221,7 @@ def fate_kv_trim(keep, kv_len, pages, free, n_free, page_size: int, out: Optiona
     B = t.B
     if out is None:
         n = _t.empty(2 * B + 2, dtype=int32, device=dev)
-        out, at = Trimmed(*n.split((B, 1, B + 1))), n.data_ptr()
+        out, at = Trimmed(*n.unsafe_split_with_sizes((B, 1, B + 1))), n.data_ptr()
         where = (at, at + 4 * B, at + 4 * B + 4)
     else:
         where = (_array(out.kv_len, "out.kv_len", B, int32, dev), _array(out.n_free, "out.n_free", 1, int32, dev),

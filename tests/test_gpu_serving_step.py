@@ -79,7 +79,7 @@ class Serving:
         told("trim", before, (keep, cut))
 
 
-def checker(s, T):
+def checks(s, T):
     """Checks of one step's calls; the cache and tables as they stand when a call has been made."""
     kept = {}
     num = lambda x: x.cpu().numpy()  # noqa: E731
@@ -152,12 +152,12 @@ def prompts(s, check=None):
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=["bf16", "f16"])
 def test_every_call_of_a_run(dtype):
     s = Serving(dtype)
-    prompts(s, checker)
+    prompts(s, checks)
     rng = torch.Generator().manual_seed(2)
     for step in range(10):
         new, drop = plan(step)
         s.new.copy_(ints(new)), s.drop.copy_(ints(drop)), s.u.copy_(torch.rand(B, generator=rng))
-        s.step(B, check=checker(s, B))
+        s.step(B, check=checks(s, B))
         assert not s.status.any()
     held = int((-(-s.kv_len // P)).sum())
     assert int(s.n_free) + held == N_PAGES and s.kv_len[3] == 0
