@@ -24,11 +24,12 @@ SOURCES = [os.path.join(CSRC, "fate_host.cpp"), os.path.join(CSRC, "fate_kernels
            os.path.join(CSRC, "fate_attn_api.cpp"), os.path.join(CSRC, "fate_attn_tile.hip"),
            os.path.join(CSRC, "fate_attn_few.hip"), os.path.join(CSRC, "fate_kv.hip"),
            os.path.join(CSRC, "fate_serve_api.cpp"), os.path.join(CSRC, "fate_pages.hip"),
-           os.path.join(CSRC, "fate_attn_shaped.hip"), os.path.join(CSRC, "fate_sample.hip")]
+           os.path.join(CSRC, "fate_attn_masks.hip"), os.path.join(CSRC, "fate_attn_scores.hip"),
+           os.path.join(CSRC, "fate_sample.hip")]
 # The attention and sampling kernels take what the caller's tensors hold: NaN and
 # infinities keep their meaning there, so they are compiled without KERNEL_FLAGS.
-NAN_SOURCES = ("fate_attn_tile.hip", "fate_attn_few.hip", "fate_kv.hip", "fate_attn_shaped.hip", "fate_pages.hip",
-               "fate_sample.hip")
+NAN_SOURCES = ("fate_attn_tile.hip", "fate_attn_few.hip", "fate_kv.hip", "fate_attn_masks.hip",
+               "fate_attn_scores.hip", "fate_pages.hip", "fate_sample.hip")
 ARCH = os.environ.get("FATE_OFFLOAD_ARCH", "gfx950")
 
 

@@ -75,7 +75,8 @@ struct AttnLaunch {
     const int32_t *prefix, *start;  // [B], [T] or null
 };
 int launch_attn_tile(const AttnLaunch &a, bool paged, void *stream);
-int launch_attn_tile_shaped(const AttnLaunch &a, bool paged, void *stream);
+int launch_attn_tile_masks(const AttnLaunch &a, bool paged, void *stream);
+int launch_attn_tile_scores(const AttnLaunch &a, bool paged, void *stream);
 int launch_attn_few(const AttnLaunch &a, int rows, void *stream);
 int launch_attn_join(const AttnLaunch &a, int rows, int tiles, int groups, void *stream);
 

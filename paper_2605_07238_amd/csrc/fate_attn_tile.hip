@@ -37,7 +37,8 @@
 // prefix, then those from the workgroup's first key on.  18261 tokens in 16
 // prompts, 32 heads of 128 over 8, take 388 us with no shape, 458 with a cap, 401
 // with a bias by distance; one row of 16384 tokens in documents of 100 to 4000,
-// behind 200 keys that all see, 390 (326 without those), causally 2090.  A cap
+// behind 200 keys that all see, 385 (397 by the instances that shape scores too;
+// some 325 without the 200), causally 2090.  A cap
 // costs 24 cycles of the vector units a score, which run beside the matrix cores
 // but little: with 28, before its last step went into the weights' exponents, a
 // wave's step of 64 keys took 3099 cycles, of which these worked 1830 and the
@@ -79,8 +80,12 @@ __device__ __forceinline__ float both_halves_max(float x) {
 // load, smaller pages.
 enum Source { kRows, kPages, kSmallPages };
 
-template <class T, int D, Source FROM, bool SHAPED>
+// What a call shapes: nothing, which keys a row sees, or the scores too.
+enum Shape { kCausal, kMasks, kScores };
+
+template <class T, int D, Source FROM, Shape SHAPE>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch) {
+    constexpr bool SHAPED = SHAPE != kCausal, SCORES = SHAPE == kScores;
     const Args &a = launch_args();  // read where they lie: copied, they go to scratch and what uses them after them
     typedef typename T::el el;
     typedef typename T::x4 x4;
@@ -134,10 +139,10 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
     if (SHAPED && wrow0 < rows) wave = span_of(a, p, wrow0 / a.G, (min(wrow0 + 32, rows) - 1) / a.G);
     const int w_most = SHAPED ? wave.most : wrow0 < rows ? min(p.L, max(0, (min(wrow0 + 32, rows) - 1) / a.G + first)) : 0;
     const int w_least = wrow0 < rows ? max(0, min(p.L, wrow0 / a.G + first)) : 0;
-    const float slope = SHAPED && a.slopes && live ? a.slopes[qh] * kLog2e : 0.0f;
+    const float slope = SCORES && a.slopes && live ? a.slopes[qh] * kLog2e : 0.0f;
     // a score in log2: unit times what `shape` leaves, and zero
-    const bool caps = SHAPED && a.cap_log2 != 0.0f && !a.cap_wide && !a.slopes;
-    const float unit = caps ? 2.0f * a.cap_log2 : SHAPED && (a.slopes || a.cap_log2 != 0.0f) ? 1.0f : a.scale_log2;
+    const bool caps = SCORES && a.cap_log2 != 0.0f && !a.cap_wide && !a.slopes;
+    const float unit = caps ? 2.0f * a.cap_log2 : SCORES ? 1.0f : a.scale_log2;
     const float zero = caps ? a.cap_log2 : 0.0f;
 
     // queries: the first product's second operand, column = row of the tile
@@ -338,7 +343,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
         }
         if (key < w_most) {  // uniform in the wave
             // cur[kt][j]: key kt * 32 + 8 (j / 4) + 4 half + j % 4 of the tile, row lane % 32
-            if (SHAPED) shape(cur, key);
+            if (SCORES) shape(cur, key);
             if (SHAPED && !wave.all(key, BK)) {
                 asm volatile("");
                 const int at = key + 4 * half;
@@ -363,7 +368,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
 #pragma unroll
             for (int j = 0; j < 16; ++j) top = fmaxf(top, cur[1][j]);
             top = both_halves_max(top);
-            top = fmaxf(SHAPED ? __builtin_fmaf(top, unit, zero) : top * unit, kLowest);
+            top = fmaxf(SCORES ? __builtin_fmaf(top, unit, zero) : top * unit, kLowest);
             if (__any(top > m + (kLag + T::kLift))) {
                 const float next = fmaxf(m, top - T::kLift), f = exp2_fast(m - next);
                 m = next;
@@ -374,7 +379,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
                     for (int j = 0; j < 16; ++j) o[i][j] *= f;
             }
             scores(nxt, (B ^ 1) * kTile);  // past the last tile: of nothing, and not used
-            const float shift = SHAPED ? zero - m : -m;
+            const float shift = SCORES ? zero - m : -m;
             x8 pr[4];                      // weights of keys 16 i + 8 (e / 4) + 4 half + e % 4
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -515,18 +520,17 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_attn_tile(AttnLaunch)
     }
 }
 
-#ifdef FATE_ATTN_SHAPED
-constexpr bool kShaped = true;
-#else
-constexpr bool kShaped = false;
+#ifndef FATE_ATTN_SHAPE
+#define FATE_ATTN_SHAPE 0
 #endif
+constexpr Shape kShape = (Shape)FATE_ATTN_SHAPE;
 
 template <class T, Source FROM>
 int go(const AttnLaunch &a, hipStream_t s) {
     const dim3 grid((unsigned)a.grid * (unsigned)a.hkv);
-    if (a.d <= 64) hipLaunchKernelGGL((k_attn_tile<T, 64, FROM, kShaped>), grid, dim3(256), 0, s, a);
-    else if (a.d <= 128) hipLaunchKernelGGL((k_attn_tile<T, 128, FROM, kShaped>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((k_attn_tile<T, 256, FROM, kShaped>), grid, dim3(256), 0, s, a);
+    if (a.d <= 64) hipLaunchKernelGGL((k_attn_tile<T, 64, FROM, kShape>), grid, dim3(256), 0, s, a);
+    else if (a.d <= 128) hipLaunchKernelGGL((k_attn_tile<T, 128, FROM, kShape>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((k_attn_tile<T, 256, FROM, kShape>), grid, dim3(256), 0, s, a);
     return (int)hipGetLastError();
 }
 
@@ -539,11 +543,14 @@ int go(const AttnLaunch &a, bool paged, hipStream_t s) {
 
 }  // namespace
 
-#ifdef FATE_ATTN_SHAPED
-int launch_attn_tile_shaped(const AttnLaunch &a, bool paged, void *stream) {
+#if FATE_ATTN_SHAPE == 2
+int launch_attn_tile_scores(const AttnLaunch &a, bool paged, void *stream) {
+#elif FATE_ATTN_SHAPE == 1
+int launch_attn_tile_masks(const AttnLaunch &a, bool paged, void *stream) {
 #else
 int launch_attn_tile(const AttnLaunch &a, bool paged, void *stream) {
-    if (a.shaped) return launch_attn_tile_shaped(a, paged, stream);
+    if (a.shaped && (a.slopes || a.cap_log2 != 0.0f)) return launch_attn_tile_scores(a, paged, stream);
+    if (a.shaped) return launch_attn_tile_masks(a, paged, stream);
 #endif
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     return a.dtype == FATE_BF16 ? go<BF16>(a, paged, s) : go<F16>(a, paged, s);
