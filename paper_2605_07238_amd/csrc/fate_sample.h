@@ -20,11 +20,11 @@ struct SampleLaunch {
     float temperature_all, top_p_all, min_p_all;
     // calls of few rows, by slices of each: of each slice the largest entry, the complement of the threads' least key,
     // the sums by bins or by waves, those over the cut by waves and in all, what is listed, the threads' largest logits;
-    // of each row the sum of all and the bin of the cut
+    // of each row the sum of all, the bin of the cut and the lowest logit in question
     int32_t slices;
     unsigned long long *tops, *lows, *hist, *lists;
     double *parts, *kept, *over, *wholes;
-    float *best;
+    float *best, *bottoms;
     int32_t *counts, *cuts;
 };
 size_t sample_ws(int64_t rows, int64_t vocab);  // bytes

@@ -1023,6 +1023,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_sums(SampleLaunch a) {
     const int n = slice_of(row, a.slices), from = g * n, to = min(row.pieces, from + n);
     if (nucleus) {
         const float bottom = nucleus_bottom(s, set, weight, top, row.V, mine, a.slices);
+        if (g == 0 && tid == 0) a.bottoms[r] = bottom;
         double whole;
         block_upto(sum_by_bins(s, row, from, to, weight, Bins(top, bottom), bottom), s.real, whole);
         if (tid == 0) a.parts[(int64_t)blockIdx.x * kWaves] = whole;
@@ -1064,28 +1065,38 @@ __device__ __forceinline__ bool only_min_p(const Settings &x, int V) {
     return x.top_p >= 1.0 && x.min_p > 0.0 && !(x.top_k > 0 && x.top_k < V);
 }
 
-// The bin of top_p's cut, from the sums of the slices; -1 if none, kBins if min_p
-// cuts before it.  `whole`: the sum of all weights.
-__device__ __forceinline__ int cut_of_slices(Lds &s, const SampleLaunch &a, int r, const Settings &set, const Bins &bins,
-                                             double &whole) {
-    const int tid = threadIdx.x;
+// The slices' sums by bins, this thread's two, and of all.  (Asked for ahead of
+// what the launch does first.)
+struct SlicesSums {
     u64 bin[kSlices][2];
     double its[kSlices];
+};
+__device__ __forceinline__ SlicesSums sums_of_slices(const SampleLaunch &a, int r) {
+    SlicesSums x;
+    const int tid = threadIdx.x;
     const int64_t at = (int64_t)r * a.slices;
 #pragma unroll
     for (int g = 0; g < kSlices; ++g) {
-        its[g] = g < a.slices ? a.parts[(at + g) * kWaves] : 0.0;
-        bin[g][0] = g < a.slices ? a.hist[(at + g) * kBins + tid] : 0;
-        bin[g][1] = g < a.slices ? a.hist[(at + g) * kBins + kThreads + tid] : 0;
+        x.its[g] = g < a.slices ? a.parts[(at + g) * kWaves] : 0.0;
+        x.bin[g][0] = g < a.slices ? a.hist[(at + g) * kBins + tid] : 0;
+        x.bin[g][1] = g < a.slices ? a.hist[(at + g) * kBins + kThreads + tid] : 0;
     }
+    return x;
+}
+
+// The bin of top_p's cut, from these; -1 if none, kBins if min_p cuts before it.
+// `whole`: the sum of all weights.
+__device__ __forceinline__ int cut_of_slices(Lds &s, const SlicesSums &x, const Settings &set, int V, const Bins &bins,
+                                             double &whole) {
+    const int tid = threadIdx.x;
     u64 sum0 = 0, sum1 = 0;
     whole = 0.0;
 #pragma unroll
-    for (int g = 0; g < kSlices; ++g) whole += its[g], sum0 += bin[g][0], sum1 += bin[g][1];
+    for (int g = 0; g < kSlices; ++g) whole += x.its[g], sum0 += x.bin[g][0], sum1 += x.bin[g][1];
     s.hist[tid] = sum0, s.hist[kThreads + tid] = sum1;
     __syncthreads();
     int cut = -1;
-    if (bins.good()) cut = bin_at(s, (u64)__builtin_ldexp(set.top_p * whole, bits_of(a.vocab)));
+    if (bins.good()) cut = bin_at(s, (u64)__builtin_ldexp(set.top_p * whole, bits_of(V)));
     return bins.good() && cut < 0 && set.min_p > 0.0 ? kBins : cut;
 }
 
@@ -1097,6 +1108,12 @@ __global__ __launch_bounds__(kThreads) void k_sample_lists(SampleLaunch a) {
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, r = blockIdx.x / a.slices, g = blockIdx.x - r * a.slices;
     const Settings set = settings_of(a, r);
     if (T::kBytes == 2 && goes_by_values<T>(set, a.vocab)) return;
+    SlicesSums sums = {};
+    float bottom_of_row = 0.0f;
+    if (by_nucleus(set, a.vocab)) {
+        sums = sums_of_slices(a, r);
+        bottom_of_row = a.bottoms[r];
+    }
     u64 first, low;
     Mine<kSlices> mine;
     tops_of(a, r, first, low, mine);
@@ -1114,10 +1131,10 @@ __global__ __launch_bounds__(kThreads) void k_sample_lists(SampleLaunch a) {
     const int n = slice_of(row, a.slices), from = g * n, to = min(row.pieces, from + n), n16 = (n + kWaves - 1) / kWaves;
     int count;
     if (nucleus) {
-        const float bottom = nucleus_bottom(s, set, weight, top, row.V, mine, a.slices);
+        const float bottom = bottom_of_row;
         const Bins bins(top, bottom);
         double whole, over = 0.0, part = 0.0, all;
-        const int cut = cut_of_slices(s, a, r, set, bins, whole);
+        const int cut = cut_of_slices(s, sums, set, a.vocab, bins, whole);
         if (g == 0 && tid == 0) a.cuts[r] = cut, a.wholes[r] = whole;
         if (cut < 0) return;
         count = sums_over_bin(row, from, to, n16, set, weight, bins, bottom, cut, over, part);
@@ -1454,6 +1471,16 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleLaunch a) {
         answer(-1, 0.0);
         return;
     }
+    // (of the slices, asked for ahead of what comes first; used where they have left it)
+    int cut_of_row = -1;
+    double whole_of_row = 0.0, its_over = 0.0, its_kept = 0.0;
+    if constexpr (SLICED)
+        if (by_nucleus(set, a.vocab)) {
+            cut_of_row = a.cuts[r];
+            whole_of_row = a.wholes[r];
+            its_over = (tid & 63) < a.slices ? a.over[r * a.slices + (tid & 63)] : 0.0;
+            its_kept = tid < a.slices * kWaves ? a.kept[(int64_t)r * a.slices * kWaves + tid] : 0.0;
+        }
     const Row<T> row(a, r);
     row.read_ends();
     if (tid < kTable) s.table[tid] = exp2(tid * (1.0 / kTable));
@@ -1503,13 +1530,12 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleLaunch a) {
     double whole = 0.0;
     if (nucleus) {
         if constexpr (SLICED) {
-            const int lane = tid & 63, cut = sliced ? a.cuts[r] : -1;
-            if (sliced) whole = a.wholes[r];
+            const int cut = sliced ? cut_of_row : -1;
+            if (sliced) whole = whole_of_row;
             if (cut >= 0) {
-                const double over = lane < a.slices ? a.over[r * a.slices + lane] : 0.0;
-                double sum = tid < a.slices * kWaves ? a.kept[(int64_t)r * a.slices * kWaves + tid] : 0.0;
+                double sum = its_kept;
                 const int n = lists_of(s, a, r);
-                const double above = wave_add(over);
+                const double above = wave_add(its_over);
                 const u64 last = cut == kBins ? 1 : n < kMany ? last_in_bin(set, weight, n, above, whole) : 0;
                 if (last) {
                     if (cut < kBins) kept = {logit_of(last), index_of(last)};
@@ -1606,7 +1632,7 @@ size_t sample_ws(int64_t rows, int64_t vocab) {
     if (n == 1) return 0;
     return (size_t)rows * n * ((2 + kMany - 1 + kBins) * sizeof(u64) + (2 * kWaves + 1) * sizeof(double) +
                                kThreads * sizeof(float) + sizeof(int32_t)) +
-           (size_t)rows * (sizeof(double) + sizeof(int32_t));
+           (size_t)rows * (sizeof(double) + sizeof(int32_t) + sizeof(float));
 }
 
 namespace {
@@ -1637,6 +1663,7 @@ void go(SampleLaunch a, void *ws, hipStream_t s) {
     a.best = reinterpret_cast<float *>(a.lists + n * (kMany - 1));
     a.counts = reinterpret_cast<int32_t *>(a.best + n * kThreads);
     a.cuts = a.counts + n;
+    a.bottoms = reinterpret_cast<float *>(a.cuts + a.rows);
     hipLaunchKernelGGL((k_sample_tops<T>), dim3((unsigned)n), block, 0, s, a);
     hipLaunchKernelGGL((k_sample_sums<T>), dim3((unsigned)n), block, 0, s, a);
     hipLaunchKernelGGL((k_sample_lists<T>), dim3((unsigned)n), block, 0, s, a);
