@@ -897,20 +897,21 @@ struct Mine {
 
 // The lowest logit that top_p over all of a row may keep: tokens of weight
 // (1 - top_p) S / V or less sum to (1 - top_p) S at most and are cut, and the
-// threads' largest logits give a bound of S from below.
+// threads' largest logits give a bound of S from below (in 32 bits, less what
+// these may be off by).
 template <int N>
 __device__ __forceinline__ float nucleus_bottom(Lds &s, const Settings &set, const Weight &weight, float top, int V,
-                                                const Mine<N> &mine, int slices) {
-    double low = 0.0, all;
-#pragma nounroll
-    for (int i = 0; i < slices; ++i) {  // (0 of -infinity)
-        float best = mine.best[0];
+                                                const Mine<N> &mine) {
+    const float per = (float)(weight.per / kTable);
+    float low = 0.0f;
 #pragma unroll
-        for (int j = 1; j < N; ++j) best = i == j ? mine.best[j] : best;
-        low += weight(best);
+    for (int i = 0; i < N; ++i) {
+        const float z = mine.best[i] - top;
+        if (mine.best[i] > -INFINITY) low += z < 0.0f ? __builtin_amdgcn_exp2f(z * per) : 1.0f;
     }
-    block_upto(low, s.real, all);
-    return logit_below(set, top, fmax((1.0 - set.top_p) * all / V, set.min_p));
+    double all;
+    block_upto((double)low, s.real, all);
+    return logit_below(set, top, fmax((1.0 - set.top_p) * 0.999 * all / V, set.min_p));
 }
 
 // Weights of the pieces from .. to: their sum, by thread, and those at `bottom` and
@@ -1022,7 +1023,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_sums(SampleLaunch a) {
     const Weight weight = weight_of(set, top);
     const int n = slice_of(row, a.slices), from = g * n, to = min(row.pieces, from + n);
     if (nucleus) {
-        const float bottom = nucleus_bottom(s, set, weight, top, row.V, mine, a.slices);
+        const float bottom = nucleus_bottom(s, set, weight, top, row.V, mine);
         if (g == 0 && tid == 0) a.bottoms[r] = bottom;
         double whole;
         block_upto(sum_by_bins(s, row, from, to, weight, Bins(top, bottom), bottom), s.real, whole);
@@ -1555,7 +1556,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleLaunch a) {
                 }
             }
         } else {
-            const float bottom = nucleus_bottom(s, set, weight, top, row.V, mine, a.slices);
+            const float bottom = nucleus_bottom(s, set, weight, top, row.V, mine);
             const Bins bins(top, bottom);
             block_upto(sum_by_bins(s, row, 0, row.pieces, weight, bins, bottom), s.real, whole);
             const int bits = bits_of(row.V);
