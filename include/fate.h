@@ -832,8 +832,8 @@ fate_status_t fate_sample_ws_size(const fate_sampling_t *sampling, size_t *bytes
  *                 u times the sum of all kept
  *   d_logprob[r]  log(w_i / sum of all kept), float32, or null; 0 at
  *                 temperature 0
- * Weights and sums are in 64 bits, in an order of their own for each size: two
- * calls give the same token.  A logit of -infinity or NaN is never taken; where
+ * Weights and sums are in 64 bits, in an order of their own for each size and
+ * form of the settings: two calls give the same token.  A logit of -infinity or NaN is never taken; where
  * all are, the token is -1 and its logprob -infinity.  If the largest is
  * +infinity the tokens at it share the row.  A row whose settings or random
  * number are out of range gets these too, and FATE_EINVAL in d_status[r] ([rows]

@@ -966,7 +966,7 @@ __device__ __forceinline__ void block_range(Lds &s, u64 mine, u64 &top, u64 &low
 
 // Calls of few rows: each row's readings by `slices` workgroups, so that the chip
 // is filled, in a launch each; k_sample then takes what they found.  64 rows of
-// 131072 with top_p 0.9: 100 us by one workgroup a row, 63 so.
+// 131072 with top_p 0.9: 100 us by one workgroup a row, 59 so.
 template <class T>
 __device__ __forceinline__ int slice_of(const Row<T> &row, int slices) { return (row.pieces + slices - 1) / slices; }
 
@@ -1618,7 +1618,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleLaunch a) {
 // Workgroups of a row's slices: calls of up to 128 rows by as many as the chip
 // runs at once, of 32768 logits each at least.  The three launches more cost some
 // 10 us.  By one workgroup a row and by slices of 32768, us, 1 and 64 rows:
-//   131072  top-p 0.9 93 and 51, 100 and 63; no cut 41 and 23, 44 and 30; top-k 1000 42 and 32, 45 and 36; top-k 50 21 and 23,
+//   131072  top-p 0.9 93 and 51, 100 and 59; no cut 41 and 23, 44 and 30; top-k 1000 42 and 32, 45 and 36; top-k 50 21 and 23,
 //           23 and 28; min-p 18 and 21, 21 and 26
 //   64 rows of 32768 by one and by two  top-p 0.9 42 and 43, no cut 17 and 22, top-k 50 14 and 24
 // Where the host knows that a call's rows list few tokens at once, it is one.
