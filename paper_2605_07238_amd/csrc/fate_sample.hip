@@ -329,6 +329,13 @@ __device__ __forceinline__ void clear_bins(Lds &s) {
     for (int i = threadIdx.x; i < kBins; i += kThreads) s.hist[i] = 0;
 }
 
+// What top_p keeps of a sum, as a whole number of 2^-bits: 1 at least, since the first token always is kept, and no bin
+// reaches 0.
+__device__ __forceinline__ u64 aim_of(double top_p, double whole, int bits) {
+    const u64 aim = (u64)__builtin_ldexp(top_p * whole, bits);
+    return aim ? aim : 1;
+}
+
 // The bin in which the sums of s.hist reach `target`, or -1.
 __device__ __forceinline__ int bin_at(Lds &s, u64 target) {
     const int tid = threadIdx.x;
@@ -696,7 +703,7 @@ __device__ __noinline__ u64 last_of_k(Settings set, Weight weight, int n, Bins b
                       by_weight ? __builtin_bit_cast(u64, w + magic) - __builtin_bit_cast(u64, magic) : 1ull);
         }
         block_upto(sum, s.real, whole);
-        const int cut = bin_at(s, by_weight ? (u64)__builtin_ldexp(set.top_p * whole, 44) : (u64)set.top_k);
+        const int cut = bin_at(s, by_weight ? aim_of(set.top_p, whole, 44) : (u64)set.top_k);
         if (cut < 0) return 0;
         last = last_of_list(weight, n, bins, cut, last, by_weight ? 0 : set.top_k, set.top_p * whole);
         if (last == 0) return 0;
@@ -814,6 +821,11 @@ __device__ __noinline__ u64 last_in_bin(Settings set, Weight weight, int n, doub
     return last;
 }
 
+// Where the bins' sums do not reach top_p's cut (kBins), whether it lies behind all tokens in question, so that min_p
+// cuts before it: weights decide, `over` their sum, since sums of whole numbers fall short of the cut also by what
+// small weights lose in them.
+__device__ __forceinline__ bool min_p_cuts(const Settings &set, double over, double whole) { return over < set.top_p * whole; }
+
 // The place of top_p's cut over all of a row, and the sums of what is kept of
 // each sixteenth in s.real, where what it keeps does not fit the list; false as
 // above.
@@ -825,7 +837,7 @@ __device__ __noinline__ bool cut_in_bin(Row<T> row, Settings set, Weight weight,
     double over, part, above;
     const int n = sums_over_bin(row, 0, row.pieces, n16, set, weight, bins, bottom, cut, over, part);
     block_upto(over, s.real, above);
-    const u64 last = cut == kBins ? 1 : last_in_bin(set, weight, n, above, whole);
+    const u64 last = cut == kBins ? (u64)min_p_cuts(set, above, whole) : last_in_bin(set, weight, n, above, whole);
     if (last == 0) return false;
     if (cut < kBins) kept = {logit_of(last), index_of(last)};
     for (int j = lane; j < n; j += 64) {  // of the bin's tokens, those kept count for their sixteenths
@@ -1085,7 +1097,7 @@ __device__ __forceinline__ SlicesSums sums_of_slices(const SampleLaunch &a, int 
     return x;
 }
 
-// The bin of top_p's cut, from these; -1 if none, kBins if min_p cuts before it.
+// The bin of top_p's cut, from these; -1 if none, kBins if they do not reach it, as where min_p cuts before it.
 // `whole`: the sum of all weights.
 __device__ __forceinline__ int cut_of_slices(Lds &s, const SlicesSums &x, const Settings &set, int V, const Bins &bins,
                                              double &whole) {
@@ -1097,7 +1109,7 @@ __device__ __forceinline__ int cut_of_slices(Lds &s, const SlicesSums &x, const 
     s.hist[tid] = sum0, s.hist[kThreads + tid] = sum1;
     __syncthreads();
     int cut = -1;
-    if (bins.good()) cut = bin_at(s, (u64)__builtin_ldexp(set.top_p * whole, bits_of(V)));
+    if (bins.good()) cut = bin_at(s, aim_of(set.top_p, whole, bits_of(V)));
     return bins.good() && cut < 0 && set.min_p > 0.0 ? kBins : cut;
 }
 
@@ -1537,7 +1549,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleLaunch a) {
                 double sum = its_kept;
                 const int n = lists_of(s, a, r);
                 const double above = wave_add(its_over);
-                const u64 last = cut == kBins ? 1 : n < kMany ? last_in_bin(set, weight, n, above, whole) : 0;
+                const u64 last = cut == kBins ? (u64)min_p_cuts(set, above, whole) : n < kMany ? last_in_bin(set, weight, n, above, whole) : 0;
                 if (last) {
                     if (cut < kBins) kept = {logit_of(last), index_of(last)};
                     // of the bin's tokens, those kept count for their parts
@@ -1560,8 +1572,8 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleLaunch a) {
             const Bins bins(top, bottom);
             block_upto(sum_by_bins(s, row, 0, row.pieces, weight, bins, bottom), s.real, whole);
             const int bits = bits_of(row.V);
-            int cut = bins.good() ? bin_at(s, (u64)__builtin_ldexp(set.top_p * whole, bits)) : -1;
-            if (bins.good() && cut < 0 && set.min_p > 0.0) cut = kBins;  // min_p cuts before top_p does
+            int cut = bins.good() ? bin_at(s, aim_of(set.top_p, whole, bits)) : -1;
+            if (bins.good() && cut < 0 && set.min_p > 0.0) cut = kBins;  // min_p may cut before top_p does
             if (cut >= 0) {  // how many it keeps, about: a bin's sum by the weight in its middle
                 double n = 0.0, all;
                 for (int b = 2 * tid; b < 2 * tid + 2 && b <= cut; ++b)

@@ -237,3 +237,50 @@ def test_what_the_binding_refuses():
         fate.fate_sample(x.clone().requires_grad_(), u)
     with torch.no_grad():
         fate.fate_sample(x.clone().requires_grad_(), u)
+
+
+@pytest.mark.parametrize("R,V", [(3, 5003), (3, 131072), (130, 131072), (2, 1 << 20)], ids=str)
+@pytest.mark.parametrize("top_p", [1e-7, 1e-14, 1e-30, 1e-45])
+def test_top_p_below_what_bins_hold(top_p, R, V):
+    """A top_p of less than the units of the bins' sums keeps the largest logit alone (the next one has a weight of 1 before
+    it, the aim is below V times 1e-7), whatever min_p leaves: thousands of flat logits here."""
+    x = torch.rand(2, V, generator=torch.Generator().manual_seed(V))
+    x[0, V // 3] = x[0, V - 2] = x[1, 5] = 1.25
+    rows = x[torch.arange(R) % 2].cuda()
+    u = torch.linspace(0, LAST, R).cuda()
+    want = torch.tensor([V // 3, 5], dtype=torch.int32)[torch.arange(R) % 2]
+    for filters in (dict(min_p=0.01), dict(min_p=0.9), dict(), dict(top_k=1000, min_p=0.01), dict(top_k=V - 1, min_p=0.01)):
+        for temperature in (1.0, 1.5):
+            token, logprob = fate.fate_sample(rows, u, temperature, top_p=top_p, logprob=True, **filters)
+            assert torch.equal(token.cpu(), want) and not logprob.any(), (filters, temperature)
+    check(x, [0.3, LAST], top_p=top_p, min_p=0.01)
+
+
+def tail(V):
+    """One large logit, and V - 1 of weights that the bins of a row of 2^20 round to nothing."""
+    x = -29.25 + 0.1 * torch.rand(1, V, generator=torch.Generator().manual_seed(V))
+    x[0, V // 2] = 0.0
+    return x
+
+
+@pytest.mark.parametrize("R", [2, 129])
+def test_top_p_in_a_tail_that_bins_do_not_hold(R):
+    """The cut of top_p lies among tokens whose weights together are 2e-7 of the whole: sums of whole numbers do not reach it.
+    A smaller min_p must not stand in for it."""
+    V, us, settings = 1 << 20, [LAST, 1 - 2.0 ** -23, 0.5, 0.0], dict(top_p=LAST, min_p=float(np.float32(1e-30)))
+    x = tail(V)
+    row = x.double().numpy()[0]
+    w = np.exp(row.astype(np.longdouble))
+    order = np.argsort(-row, kind="stable")
+    before = w[order].cumsum() - w[order]
+    kept = before < np.longdouble(LAST) * w.sum()
+    assert V // 2 < kept.sum() < 0.9 * V
+    upto = np.where(np.isin(np.arange(V), order[kept]), w, 0).cumsum()
+    dx = x.cuda().expand(R, V)
+    for u in us:
+        # float64 sums and the cut may be off by some 2e-15, a hundredth of a token: u is not that near a border
+        t = np.longdouble(u) * upto[-1]
+        want, share = so.sample(row, u=u, **settings)
+        assert upto[want] - t > 2e-14 and t - (upto[want] - w[want]) > 2e-14 or u == 0
+        token, logprob = fate.fate_sample(dx, torch.full((R,), u, device="cuda"), logprob=True, **settings)
+        assert (token == want).all() and (logprob - share).abs().max() <= 2.0 ** -23 * abs(share) + 2.0 ** -38, u
