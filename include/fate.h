@@ -717,7 +717,8 @@ fate_status_t fate_attn_prompt(const fate_heads_t *heads, const fate_seqs_t *seq
  *   start   [T] or null: a row sees the keys from start[t] on (and the prefix's):
  *           its document's first, or p - w + 1 for a window of w keys.  Within
  *           a sequence start must not fall from a row to the next (max(start, 0)
- *           counts); where it does, the sequence is in error
+ *           counts), also among rows that stand before the sequence; where
+ *           it does, the sequence is in error
  * A row thus sees key j when j < prefix, or start <= j <= p.  One that sees
  * none (start past p and no prefix, or p < 0: it stands before the sequence,
  * and the prefix is not for it) gets zeros and -infinity.  slopes, prefix and

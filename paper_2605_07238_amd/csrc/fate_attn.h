@@ -352,11 +352,12 @@ __device__ __forceinline__ Seen seen_by(const A &a, const Unit &u, int tok, bool
     const int end = tok + (u.L - u.n + 1);
     Seen s = {0, 0, live ? max(0, min(u.L, end)) : 0};
     if constexpr (SHAPED) {
-        if (live && end > 0) {
-            if (a.prefix) s.pre = min(max(0, a.prefix[u.b]), u.L);
+        if (live) {
+            if (a.prefix && end > 0) s.pre = min(max(0, a.prefix[u.b]), u.L);
             if (a.start) {
                 s.first = max(0, a.start[u.lo_row + (int64_t)tok]);
-                // (reported, not relied on: any order reads within the sequence's keys)
+                // (reported, not relied on: any order reads within the sequence's keys; also of rows before the sequence,
+                // since the first key of a span is that of its first row, wherever this stands)
                 if (tok > 0 && a.start[u.lo_row + (int64_t)tok - 1] > s.first && a.status) a.status[u.b] = FATE_EINVAL;
             }
         }

@@ -277,3 +277,32 @@ def test_what_the_binding_refuses():
                 call(cap=cap)
         with pytest.raises(ValueError, match="gradient"):
             call(slopes=good["slopes"].clone().requires_grad_())
+
+
+@pytest.mark.parametrize("n", [3, 300])
+def test_first_keys_that_fall_before_a_sequence_are_reported(n):
+    """Rows that stand before their sequence (fewer keys than rows) see nothing, but where the first keys fall among them, or
+    from them to the first that sees a key, the sequence is in error like any other; rows without a fall are not."""
+    short = n - n // 3  # as many rows stand before the sequence
+    new, kv = [n] * 3, [n + 50, n - short, n + 9]
+    args = make_paged(new, kv, 8, 1, 64, BF, 16, seed=n)
+    good = np.tile(np.arange(n), 3)
+    for at in {1, short // 2, short - 1, short}:
+        start = good.copy()
+        start[n:n + at] = 1000
+        for most in (n, None):
+            status = torch.zeros(3, dtype=torch.int32, device="cuda")
+            out, lse = run_paged(args, dict(start=start), max_new=most, status=status)
+            assert status.tolist() == [0, -1, 0], (at, most)
+            want, lse2 = run_paged(args, dict(start=good), max_new=most, status=status.zero_())
+            assert not status.any()
+            keep = np.r_[0:n, 2 * n:3 * n]
+            assert torch.equal(out[keep], want[keep]) and torch.equal(lse[keep], lse2[keep])
+    # below 0 counts as 0 here too, and none of it is looked at across sequences
+    start = good.copy()
+    start[n:n + short] = np.arange(short)[::-1] - 2 * n
+    for most in (n, None):
+        status = torch.zeros(3, dtype=torch.int32, device="cuda")
+        compare(*run_paged(args, dict(start=start), max_new=most, status=status),
+                expected(args[0], cached(*args[1:3], kv, args[5]), args[3], dict(start=start), 1 / math.sqrt(64)))
+        assert not status.any()
