@@ -1262,6 +1262,8 @@ def fate_sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, logpr
         if isinstance(value, _t.Tensor):
             setattr(s, name, _array(value, name, R, dtype, dev))
         else:
+            if name == "top_k":  # the field would take a larger number by its low bits; no row has so many tokens
+                value = max(-1, min(value, 0x7fffffff))
             setattr(s, name + "_all", value)
     if out is None:
         out = _t.empty(R, dtype=i32, device=dev)

@@ -284,3 +284,15 @@ def test_top_p_in_a_tail_that_bins_do_not_hold(R):
         assert upto[want] - t > 2e-14 and t - (upto[want] - w[want]) > 2e-14 or u == 0
         token, logprob = fate.fate_sample(dx, torch.full((R,), u, device="cuda"), logprob=True, **settings)
         assert (token == want).all() and (logprob - share).abs().max() <= 2.0 ** -23 * abs(share) + 2.0 ** -38, u
+
+
+def test_top_k_past_32_bits_cuts_nothing():
+    x, u = logits_of(4, 300, FF, 1).cuda(), torch.tensor(uniform(4, 2)).cuda()
+    want = fate.fate_sample(x, u)[0]
+    for k in ((1 << 31) - 1, 1 << 31, (1 << 32) + 1, (1 << 63) - 1, 1 << 70):
+        assert torch.equal(fate.fate_sample(x, u, top_k=k)[0], want), k
+    for k in (-1, -(1 << 31) - 1, -(1 << 32) + 1, -(1 << 70)):
+        with pytest.raises(fate.FateError):
+            fate.fate_sample(x, u, top_k=k)
+    with pytest.raises(TypeError):
+        fate.fate_sample(x, u, top_k=2.0)
