@@ -1160,6 +1160,8 @@ def _kv_tables(counts, name, kv_len, pages, free, n_free, page_size, device) -> 
     row, one = pages.stride()
     if pages.dtype is not int32 or pages.device != device or (one != 1 and width > 1):
         raise ValueError("pages must be int32 on %s, each row contiguous" % device)
+    if not -(1 << 31) <= page_size < 1 << 31:  # (the field would take its low bits)
+        raise ValueError("page_size must be a 32-bit number, got %d" % page_size)
     for t, its, n in ((counts, name, B), (kv_len, "kv_len", B), (free, "free", free.shape[0]), (n_free, "n_free", 1)):
         if t.dtype is not int32 or t.device != device or t.shape != (n,) or not t.is_contiguous():
             _array(t, its, n, int32, device)  # says what is wrong
@@ -1188,9 +1190,9 @@ def fate_kv_reserve(new, kv_len, pages, free, n_free, page_size: int, T: int, ou
     int32, int64 = _t.int32, _t.int64
     t = _kv_tables(new, "new", kv_len, pages, free, n_free, page_size, dev)
     B = t.B
+    if not 0 <= T < 1 << 63:
+        raise ValueError("T must not be negative or past 64 bits, got %d" % T)
     if out is None:
-        if T < 0:
-            raise ValueError("T must not be negative, got %d" % T)
         n, slots = _t.empty(3 * B + 3 + T, dtype=int32, device=dev), _t.empty(T, dtype=int64, device=dev)
         # (whole numbers: no gradient has to follow the views)
         off, kv, left, taken, positions = n.unsafe_split_with_sizes((B + 1, B, 1, B + 1, T))

@@ -224,3 +224,18 @@ def test_what_the_binding_refuses():
     got = fate.fate_kv_reserve(**good, stream=side)
     side.synchronize()
     assert got.kv_len.tolist() == [4, 1]
+
+
+def test_numbers_past_their_types_are_refused():
+    """Not taken by their low bits."""
+    good = dict(kv_len=ints([3, 0]), pages=ints(np.full((2, 4), 0)), free=ints([1, 2, 3]), n_free=ints([3]), page_size=16)
+    for size in ((1 << 32) + 16, 16 - (1 << 32), 1 << 31, 1 << 70):
+        with pytest.raises(ValueError):
+            fate.fate_kv_reserve(ints([1, 1]), T=2, **dict(good, page_size=size))
+        with pytest.raises(ValueError):
+            fate.fate_kv_trim(ints([1, 0]), **dict(good, page_size=size))
+    out = fate.Reserved(ints([0] * 3), ints([0] * 2), ints([0]), ints([0] * 3), None, None)
+    for T in ((1 << 64) + 2, 2 - (1 << 64), -1):
+        with pytest.raises(ValueError):
+            fate.fate_kv_reserve(ints([1, 1]), T=T, out=out, **good)
+    assert fate.fate_kv_reserve(ints([1, 1]), T=2, out=out, **good).off.tolist() == [0, 1, 2]
