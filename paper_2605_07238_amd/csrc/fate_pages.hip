@@ -263,7 +263,7 @@ __device__ __forceinline__ void trim_lengths(const PagesLaunch &a, Scans &lds, G
 // A call of one workgroup, sixteen lanes a sequence.  The lengths are read once, by
 // threads, and pages eight loads at a time: 200 sequences with up to 512 pages
 // took 14.4 us by a wave each with a lane's loads one behind the other, 11.3 with
-// four at a time, 8.3 so.
+// four at a time, 8.2 so.
 __global__ __launch_bounds__(kThreads) void k_kv_trim(PagesLaunch a) {
     constexpr int kLanes = 16, kLoads = 8;
     __shared__ Scans lds;
